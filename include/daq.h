@@ -528,6 +528,116 @@ daq_status daq_clip_search(const daq_conv_desc* desc, const float* dY, float alp
                            int32_t* best_j, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Linear and activation layers in few bits: microscaled 4-bit products and 8-bit activation checkpoints
+ *
+ * What Algorithm 1 does for a convolution - narrow operands for the matrix cores, and of the forward pass
+ * only narrow copies kept for the backward pass - for the layers of a transformer block.  Matrices are
+ * row-major with a row stride `ld` in elements (ld >= columns), fp32 or bfloat16 (daq_dtype), and need the
+ * alignment of their elements only; packed buffers are 256-byte aligned.  Sizes of zero rows (no tokens)
+ * are legal: nothing is read, and what sums over them is zero.  Conventions as above: nothing is allocated
+ * or synchronised, arguments are checked before anything is launched.  Sizes: up to 2^31 - 1 rows or
+ * columns and 2^40 elements of a matrix, else DAQ_ERR_UNSUPPORTED; the same for launches of more workgroups
+ * than a grid holds.
+ *
+ * Both formats share a power-of-two scale 2^(byte - 127) among 32 neighbours, so that decoding is exact in
+ * bfloat16 and fp32 and products of decoded values need no rounding before their fp32 sums.  The byte is at
+ * least 1 (a block whose largest magnitude is below the smallest scale keeps that).  A block that holds a
+ * NaN or an infinity gets the byte 255 and decodes to NaN in all its places; every sum it enters is NaN.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { DAQ_FP32 = 0, DAQ_BF16 = 1 } daq_dtype;
+
+/* Microscaled 4-bit matrix: elements of 1 sign, 2 exponent and 1 mantissa bit (0, .5, 1, 1.5, 2, 3, 4, 6), blocks of 32
+ * along a row.  The buffer is in the register order of the matrix cores.  With r = row, b = column / 32:
+ *   codes   element (row, column) is nibble column % 2 (0: low) of byte
+ *           (((r/32)*steps + b/2)*2 + b%2)*512 + (r%32)*16 + (column%32)/2 ,        steps = 4 * groups
+ *   scales  byte off_scales + (((r/32)*groups + b/8)*2 + b%2)*128 + (r%32)*4 + (b/2)%4 ,  groups = ceil(columns / 256)
+ * Rows are padded to a multiple of 32, columns to a multiple of 256; padding is zero, scales included. */
+typedef struct {
+    int64_t bytes, off_scales;
+    int32_t row_blocks, groups;
+} daq_mx4_layout;
+daq_status daq_layout_mx4(int64_t rows, int64_t cols, daq_mx4_layout* out);
+
+/* Matrix saved in 8 bits: codes -127 .. 127 at byte (row*parts + part)*pitch + column, pitch = columns of a part rounded
+ * up to 32; scales at off_scales + (row*parts + part)*(pitch/32) + column/32.  Padding codes are zero. */
+typedef struct {
+    int64_t bytes, off_scales;
+    int64_t pitch;
+} daq_ckpt8_layout;
+daq_status daq_layout_ckpt8(int64_t rows, int64_t cols, int32_t parts, daq_ckpt8_layout* out);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_mx4_quantize -- src [rows][cols] to microscaled 4 bits.  Per block, with a = max |x|:
+ *   nearest     e = floor(log2 a) - 2; code = x / 2^e to the nearest element, ties to the even code, at most 6 (what lies
+ *               above 7 * 2^e loses up to a quarter of itself: the usual rule for operands of a forward pass);
+ *   stochastic  e = the smallest integer with a <= 6 * 2^e, so that nothing is cut off and the code is unbiased:
+ *               between its neighbours lo < hi,  hi iff  floor(2^16 * (|x|/2^e - lo) / (hi - lo)) > U.
+ *   Element (r, c) draws U, 16 bits, from h = fmix32((r*ceil(cols/2) + c/2) ^ key), key from the seed as in
+ *   daq_quantize_grad: h >> 16 for even c, h & 0xFFFF for odd c.  At most 2^31 elements in this mode.
+ * transpose != 0: the blocks lie along the columns of src and `dst` is the packed [cols][rows] matrix (its layout is that
+ * of daq_layout_mx4(cols, rows)); the draws stay those of (r, c).
+ *   dst   out  daq_layout_mx4 buffer, 256-byte aligned, written whole
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_mx4_quantize(const void* src, daq_dtype dtype, int64_t rows, int64_t cols, int64_t ld, int32_t transpose,
+                            daq_round mode, uint64_t seed, uint8_t* dst, void* stream);
+/* The values of a packed [rows][cols] matrix, exact in either type (but 2^128, which stochastic rounding can make of magnitudes
+ * above 1.5 * 2^127, is an infinity). */
+daq_status daq_mx4_dequantize(const uint8_t* src, int64_t rows, int64_t cols, void* dst, daq_dtype dtype, int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_mx4_matmul -- D[m][n] = sum over k of A[m][k] * B[n][k], both packed with K columns; products are exact, sums fp32,
+ * D rounded once to its type.
+ * daq_mx4_linear -- the same with A quantized in the call from X [M][K] (mode, seed as daq_mx4_quantize): a linear layer
+ * Y = X W^T with W packed once; with the transposed packing of W its data gradient dX = dY W.
+ *   workspace  of the bytes daq_mx4_matmul_workspace / daq_mx4_linear_workspace report; may be NULL where that is 0
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_mx4_matmul_workspace(int64_t M, int64_t N, int64_t K, size_t* bytes);
+daq_status daq_mx4_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, daq_dtype dtype,
+                          int64_t ldd, void* workspace, size_t workspace_bytes, void* stream);
+daq_status daq_mx4_linear_workspace(int64_t M, int64_t N, int64_t K, size_t* bytes);
+daq_status daq_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, daq_dtype x_dtype, int64_t ldx, daq_round mode,
+                          uint64_t seed, const uint8_t* W, void* Y, daq_dtype y_dtype, int64_t ldy, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_ckpt8_save / daq_ckpt8_restore -- src [rows][parts*cols] (the parts side by side) to 8 bits and back.  Per block
+ * e = floor(log2 a) - 6, code = x / 2^e to the nearest integer, ties to even, within -127 .. 127: an error of at most half
+ * a step of a/64 (a whole one for codes that would be 128).  Restored values are exact in either type.
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_ckpt8_save(const void* src, daq_dtype dtype, int64_t rows, int64_t cols, int32_t parts, int64_t ld,
+                          uint8_t* ckpt, void* stream);
+daq_status daq_ckpt8_restore(const uint8_t* ckpt, int64_t rows, int64_t cols, int32_t parts, void* dst, daq_dtype dtype,
+                             int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Activation layers that keep their input in 8 bits only.  f = SiLU, x / (1 + exp(-x)), or GELU, x * Phi(x).
+ *   plain (gated == 0)   y = f(h),                h [rows][cols]
+ *   gated                y = f(g) * u,            h = [g | u], [rows][2*cols]
+ * daq_ckpt8_act_forward writes y (the type of h) and saves h (parts = 1 or 2).
+ * daq_ckpt8_act_backward computes, from the saved h^ = g^, u^ and dy,
+ *   plain  dh = dy * f'(h^);    gated  dh = [dy * u^ * f'(g^) | dy * f(g^)],   in fp32, rounded once to the type of dy,
+ * and, where y_ckpt is not NULL, saves y recomputed from h^ in 8 bits (a daq_layout_ckpt8(rows, cols, 1) buffer): the input
+ * of the next linear layer for its weight gradient, so that the forward pass need not keep it.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { DAQ_ACT_SILU = 0, DAQ_ACT_GELU = 1 } daq_act;
+daq_status daq_ckpt8_act_forward(const void* h, daq_dtype dtype, int64_t rows, int64_t cols, int64_t ldh, daq_act act,
+                                 int32_t gated, void* y, int64_t ldy, uint8_t* ckpt, void* stream);
+daq_status daq_ckpt8_act_backward(const void* dy, daq_dtype dtype, int64_t rows, int64_t cols, int64_t lddy, const uint8_t* ckpt,
+                                  daq_act act, int32_t gated, void* dh, int64_t lddh, uint8_t* y_ckpt, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_ckpt8_weight_grad -- dW[n][k] = sum over m of dY[m][n] * X^[m][k], X^ the saved input [M][K] (parts = 1) of a linear
+ * layer: products on the bfloat16 matrix cores, where X^ is exact, and fp32 sums.  An fp32 dY enters as the sum of three
+ * bfloat16 values (its 24 bits).  accumulate != 0 adds to dW.
+ *   dW         i/o  fp32 [N][K], row stride ldw
+ *   workspace  of the bytes daq_ckpt8_weight_grad_workspace reports; may be NULL where that is 0
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_ckpt8_weight_grad_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, size_t* bytes);
+daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, const void* dY, daq_dtype dtype, int64_t lddy,
+                                 const uint8_t* x_ckpt, float* dW, int64_t ldw, int32_t accumulate, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Measurement aid (not part of the method).  Between daq_prof_begin() and daq_prof_end() every
  * kernel the library launches is bracketed by a HIP event pair on its stream.  daq_prof_end()
  * waits for those events and fills one row per distinct kernel name.  The list of pending event

@@ -23,6 +23,8 @@ SCHEME_DAQ, SCHEME_GQ, SCHEME_GVQ, SCHEME_MCS = range(4)
 CLASS_GAUSS, CLASS_INVT = 0, 1
 OP_QUANTIZE_GRAD, OP_CONV_FWD, OP_CONV_BWD_DATA, OP_CONV_BWD_FILTER, OP_CONV_BWD, OP_CLIP_SEARCH = range(6)
 LAYOUT_NHWC, LAYOUT_CNHW = 0, 1
+FP32, BF16 = 0, 1
+ACT_SILU, ACT_GELU = 0, 1
 SCHEDULE_AUTO, SCHEDULE_THREE_SWEEPS, SCHEDULE_EARLY_COPY, SCHEDULE_CHANNEL_RESIDENT = range(4)
 
 EXPORTS = [
@@ -30,6 +32,9 @@ EXPORTS = [
     "daq_layout_qw", "daq_workspace_bytes", "daq_quantize_grad", "daq_quantize_grad_scheme", "daq_quantize_grad_bf16", "daq_quantize_grad_ex", "daq_quantize_grad_split", "daq_quantize_grad_from_stats", "daq_quantize_grad_noalloc", "daq_conv_fwd_int8", "daq_conv_fwd_int8_ex", "daq_conv_bwd_data_int8",
     "daq_conv_bwd_filter_int8", "daq_conv_bwd_int8", "daq_conv_bwd_data_int8_bf16", "daq_conv_bwd_filter_int8_bf16", "daq_conv_bwd_data_int8_chan", "daq_clip_search", "daq_conv3d_out_d", "daq_conv3d_out_h", "daq_conv3d_out_w", "daq_conv3d_carriers", "daq_conv3d_qw_bytes",
     "daq_conv3d_workspace_bytes", "daq_quantize_grad3d", "daq_conv3d_fwd_int8", "daq_conv3d_bwd_data_int8", "daq_conv3d_bwd_filter_int8",
+    "daq_layout_mx4", "daq_layout_ckpt8", "daq_mx4_quantize", "daq_mx4_dequantize", "daq_mx4_matmul_workspace", "daq_mx4_matmul",
+    "daq_mx4_linear_workspace", "daq_mx4_linear", "daq_ckpt8_save", "daq_ckpt8_restore", "daq_ckpt8_act_forward", "daq_ckpt8_act_backward",
+    "daq_ckpt8_weight_grad_workspace", "daq_ckpt8_weight_grad",
     "daq_prof_begin", "daq_prof_end", "daq_status_string", "daq_ceiling_mfma_i8", "daq_ceiling_stream",
 ]
 
@@ -189,6 +194,14 @@ class QuantizeOpts(C.Structure):
     _fields_ = [("scheme", C.c_int32), ("schedule", C.c_int32), ("dy_bf16", C.c_int32), ("reserved", C.c_int32)]
 
 
+class Mx4Layout(C.Structure):
+    _fields_ = [("bytes", C.c_int64), ("off_scales", C.c_int64), ("row_blocks", C.c_int32), ("groups", C.c_int32)]
+
+
+class Ckpt8Layout(C.Structure):
+    _fields_ = [("bytes", C.c_int64), ("off_scales", C.c_int64), ("pitch", C.c_int64)]
+
+
 class ProfRow(C.Structure):
     _fields_ = [("name", C.c_char * 64), ("total_ms", C.c_double), ("launches", C.c_int32)]
 
@@ -242,6 +255,21 @@ def lib():
         L.daq_conv3d_fwd_int8.argtypes = [C.POINTER(Conv3dDesc)] + [vp] * 10 + [sz, vp]
         L.daq_conv3d_bwd_data_int8.argtypes = [C.POINTER(Conv3dDesc)] + [vp] * 7 + [sz, vp]
         L.daq_conv3d_bwd_filter_int8.argtypes = [C.POINTER(Conv3dDesc)] + [vp] * 7 + [sz, vp]
+        i64, i32, psz = C.c_int64, C.c_int32, C.POINTER(C.c_size_t)
+        L.daq_layout_mx4.argtypes = [i64, i64, C.POINTER(Mx4Layout)]
+        L.daq_layout_ckpt8.argtypes = [i64, i64, i32, C.POINTER(Ckpt8Layout)]
+        L.daq_mx4_quantize.argtypes = [vp, C.c_int, i64, i64, i64, i32, C.c_int, u64, vp, vp]
+        L.daq_mx4_dequantize.argtypes = [vp, i64, i64, vp, C.c_int, i64, vp]
+        L.daq_mx4_matmul_workspace.argtypes = [i64, i64, i64, psz]
+        L.daq_mx4_matmul.argtypes = [i64, i64, i64, vp, vp, vp, C.c_int, i64, vp, sz, vp]
+        L.daq_mx4_linear_workspace.argtypes = [i64, i64, i64, psz]
+        L.daq_mx4_linear.argtypes = [i64, i64, i64, vp, C.c_int, i64, C.c_int, u64, vp, vp, C.c_int, i64, vp, sz, vp]
+        L.daq_ckpt8_save.argtypes = [vp, C.c_int, i64, i64, i32, i64, vp, vp]
+        L.daq_ckpt8_restore.argtypes = [vp, i64, i64, i32, vp, C.c_int, i64, vp]
+        L.daq_ckpt8_act_forward.argtypes = [vp, C.c_int, i64, i64, i64, C.c_int, i32, vp, i64, vp, vp]
+        L.daq_ckpt8_act_backward.argtypes = [vp, C.c_int, i64, i64, i64, vp, C.c_int, i32, vp, i64, vp, vp]
+        L.daq_ckpt8_weight_grad_workspace.argtypes = [i64, i64, i64, C.c_int, psz]
+        L.daq_ckpt8_weight_grad.argtypes = [i64, i64, i64, vp, C.c_int, i64, vp, vp, i64, i32, vp, sz, vp]
         L.daq_prof_end.argtypes = [C.POINTER(ProfRow), C.c_int32, C.POINTER(C.c_int32)]
         L.daq_ceiling_mfma_i8.argtypes = [C.c_int32, C.c_int32, vp, C.POINTER(C.c_double), vp]
         L.daq_ceiling_stream.argtypes = [C.c_int32, vp, vp, sz, C.c_int32, vp, vp]
@@ -634,6 +662,187 @@ def conv3d_bwd_filter_int8(d: Conv3dDesc, qx_cnhw, s_x, vq, s_chan, acc: Optiona
                                           ws.numel(), _stream(stream))
     _check(rc, "daq_conv3d_bwd_filter_int8")
     return dW
+
+
+# ------------------------------------------------------------------------------------------------
+# linear and activation layers in few bits
+# ------------------------------------------------------------------------------------------------
+_DTYPES = {torch.float32: FP32, torch.bfloat16: BF16}
+
+
+@dataclass
+class Mx4:
+    """A [rows, cols] matrix in microscaled 4 bits (daq_layout_mx4)."""
+    buf: torch.Tensor       # u8
+    rows: int
+    cols: int
+
+
+@dataclass
+class Ckpt8:
+    """A [rows, parts * cols] matrix saved in 8 bits (daq_layout_ckpt8)."""
+    buf: torch.Tensor       # u8
+    rows: int
+    cols: int
+    parts: int = 1
+
+
+def layout_mx4(rows: int, cols: int) -> Mx4Layout:
+    L = Mx4Layout()
+    _check(lib().daq_layout_mx4(rows, cols, C.byref(L)), "daq_layout_mx4")
+    return L
+
+
+def layout_ckpt8(rows: int, cols: int, parts: int = 1) -> Ckpt8Layout:
+    L = Ckpt8Layout()
+    _check(lib().daq_layout_ckpt8(rows, cols, parts, C.byref(L)), "daq_layout_ckpt8")
+    return L
+
+
+def _matrix(t: torch.Tensor) -> bool:
+    """On the GPU, fp32 or bfloat16, two axes, elements of a row next to each other, rows that do not overlap."""
+    return t.is_cuda and t.dtype in _DTYPES and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def alloc_mx4(rows: int, cols: int, device="cuda") -> Mx4:
+    return Mx4(torch.empty(layout_mx4(rows, cols).bytes, dtype=torch.uint8, device=device), rows, cols)
+
+
+def alloc_ckpt8(rows: int, cols: int, parts: int = 1, device="cuda") -> Ckpt8:
+    return Ckpt8(torch.empty(layout_ckpt8(rows, cols, parts).bytes, dtype=torch.uint8, device=device), rows, cols, parts)
+
+
+def mx4_quantize(x: torch.Tensor, transpose: bool = False, mode=ROUND_NEAREST, seed=0, out: Optional[Mx4] = None, stream=None) -> Mx4:
+    """daq_mx4_quantize: ``x`` [rows, cols] with blocks along its rows, or (``transpose``) its transpose, with blocks along its columns."""
+    assert _matrix(x)
+    rows, cols = x.shape
+    shape = (cols, rows) if transpose else (rows, cols)
+    if out is None:
+        out = alloc_mx4(*shape, x.device)
+    assert (out.rows, out.cols) == shape
+    _check(lib().daq_mx4_quantize(_ptr(x), _DTYPES[x.dtype], rows, cols, _ld(x), int(transpose), mode, seed, _ptr(out.buf), _stream(stream)),
+           "daq_mx4_quantize")
+    return out
+
+
+def mx4_dequantize(q: Mx4, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_mx4_dequantize: the values that ``q`` holds, exact in either type."""
+    if out is None:
+        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.buf.device)
+    assert _matrix(out) and tuple(out.shape) == (q.rows, q.cols)
+    _check(lib().daq_mx4_dequantize(_ptr(q.buf), q.rows, q.cols, _ptr(out), _DTYPES[out.dtype], _ld(out), _stream(stream)), "daq_mx4_dequantize")
+    return out
+
+
+def mx4_matmul(a: Mx4, b: Mx4, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """daq_mx4_matmul: a b^T, [a.rows, b.rows]."""
+    assert a.cols == b.cols
+    if out is None:
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=b.buf.device)
+    assert _matrix(out) and tuple(out.shape) == (a.rows, b.rows)
+    if workspace is None:
+        workspace = _few_ws("daq_mx4_matmul_workspace", b.buf.device, a.rows, b.rows, a.cols)
+    _check(lib().daq_mx4_matmul(a.rows, b.rows, a.cols, _ptr(a.buf), _ptr(b.buf), _ptr(out), _DTYPES[out.dtype], _ld(out), _ptr(workspace),
+                                0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_matmul")
+    return out
+
+
+def mx4_linear(x: torch.Tensor, w: Mx4, mode=ROUND_NEAREST, seed=0, dtype=None, out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_mx4_linear: x w^T with ``x`` [M, w.cols] quantized in the call; the result is of ``dtype`` (that of ``x`` if not given)."""
+    assert _matrix(x) and x.shape[1] == w.cols
+    M = x.shape[0]
+    if out is None:
+        out = torch.empty((M, w.rows), dtype=dtype or x.dtype, device=x.device)
+    assert _matrix(out) and tuple(out.shape) == (M, w.rows)
+    if workspace is None:
+        workspace = _few_ws("daq_mx4_linear_workspace", x.device, M, w.rows, w.cols)
+    _check(lib().daq_mx4_linear(M, w.rows, w.cols, _ptr(x), _DTYPES[x.dtype], _ld(x), mode, seed, _ptr(w.buf), _ptr(out), _DTYPES[out.dtype],
+                                _ld(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_linear")
+    return out
+
+
+def _few_ws(fn_name: str, device, *sizes) -> Optional[torch.Tensor]:
+    """The workspace a call of these sizes needs, None where it needs none."""
+    n = C.c_size_t(0)
+    _check(getattr(lib(), fn_name)(*sizes, C.byref(n)), fn_name)
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+
+
+def ckpt8_save(x: torch.Tensor, parts: int = 1, out: Optional[Ckpt8] = None, stream=None) -> Ckpt8:
+    """daq_ckpt8_save: ``x`` [rows, parts * cols] in 8 bits."""
+    assert _matrix(x) and x.shape[1] % parts == 0
+    rows, cols = x.shape[0], x.shape[1] // parts
+    if out is None:
+        out = alloc_ckpt8(rows, cols, parts, x.device)
+    assert (out.rows, out.cols, out.parts) == (rows, cols, parts)
+    _check(lib().daq_ckpt8_save(_ptr(x), _DTYPES[x.dtype], rows, cols, parts, _ld(x), _ptr(out.buf), _stream(stream)), "daq_ckpt8_save")
+    return out
+
+
+def ckpt8_restore(c: Ckpt8, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_ckpt8_restore: the values that ``c`` holds, exact in either type."""
+    shape = (c.rows, c.parts * c.cols)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=c.buf.device)
+    assert _matrix(out) and tuple(out.shape) == shape
+    _check(lib().daq_ckpt8_restore(_ptr(c.buf), c.rows, c.cols, c.parts, _ptr(out), _DTYPES[out.dtype], _ld(out), _stream(stream)),
+           "daq_ckpt8_restore")
+    return out
+
+
+def ckpt8_act_forward(h: torch.Tensor, act: int, gated: bool = False, out: Optional[torch.Tensor] = None, ckpt: Optional[Ckpt8] = None,
+                      stream=None):
+    """daq_ckpt8_act_forward: (y, the checkpoint of ``h``).  ``h`` [rows, cols], or [rows, 2 * cols] = gate | up when ``gated``."""
+    assert _matrix(h) and (not gated or h.shape[1] % 2 == 0)
+    parts = 2 if gated else 1
+    rows, cols = h.shape[0], h.shape[1] // parts
+    if out is None:
+        out = torch.empty((rows, cols), dtype=h.dtype, device=h.device)
+    assert _matrix(out) and out.dtype == h.dtype and tuple(out.shape) == (rows, cols)
+    if ckpt is None:
+        ckpt = alloc_ckpt8(rows, cols, parts, h.device)
+    assert (ckpt.rows, ckpt.cols, ckpt.parts) == (rows, cols, parts)
+    _check(lib().daq_ckpt8_act_forward(_ptr(h), _DTYPES[h.dtype], rows, cols, _ld(h), act, int(gated), _ptr(out), _ld(out), _ptr(ckpt.buf),
+                                       _stream(stream)), "daq_ckpt8_act_forward")
+    return out, ckpt
+
+
+def ckpt8_act_backward(dy: torch.Tensor, ckpt: Ckpt8, act: int, out: Optional[torch.Tensor] = None, y_ckpt: Optional[Ckpt8] = None,
+                       stream=None) -> torch.Tensor:
+    """daq_ckpt8_act_backward: the gradient of the layer's input, of the type of ``dy``; ``y_ckpt`` receives the layer's output, recomputed, in
+    8 bits."""
+    assert _matrix(dy) and tuple(dy.shape) == (ckpt.rows, ckpt.cols)
+    shape = (ckpt.rows, ckpt.parts * ckpt.cols)
+    if out is None:
+        out = torch.empty(shape, dtype=dy.dtype, device=dy.device)
+    assert _matrix(out) and out.dtype == dy.dtype and tuple(out.shape) == shape
+    assert y_ckpt is None or (y_ckpt.rows, y_ckpt.cols, y_ckpt.parts) == (ckpt.rows, ckpt.cols, 1)
+    _check(lib().daq_ckpt8_act_backward(_ptr(dy), _DTYPES[dy.dtype], ckpt.rows, ckpt.cols, _ld(dy), _ptr(ckpt.buf), act, int(ckpt.parts == 2),
+                                        _ptr(out), _ld(out), None if y_ckpt is None else _ptr(y_ckpt.buf), _stream(stream)),
+           "daq_ckpt8_act_backward")
+    return out
+
+
+def ckpt8_weight_grad(dy: torch.Tensor, x: Ckpt8, out: Optional[torch.Tensor] = None, accumulate: bool = False,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_ckpt8_weight_grad: dy^T x^, fp32 [N, K]; ``accumulate`` adds it to ``out``."""
+    assert _matrix(dy) and x.parts == 1 and dy.shape[0] == x.rows
+    N = dy.shape[1]
+    assert out is not None or not accumulate
+    if out is None:
+        out = torch.empty((N, x.cols), dtype=torch.float32, device=dy.device)
+    assert _matrix(out) and out.dtype == torch.float32 and tuple(out.shape) == (N, x.cols)
+    if workspace is None:
+        workspace = _few_ws("daq_ckpt8_weight_grad_workspace", dy.device, x.rows, N, x.cols, _DTYPES[dy.dtype])
+    _check(lib().daq_ckpt8_weight_grad(x.rows, N, x.cols, _ptr(dy), _DTYPES[dy.dtype], _ld(dy), _ptr(x.buf), _ptr(out), _ld(out), int(accumulate),
+                                       _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_ckpt8_weight_grad")
+    return out
 
 
 # ------------------------------------------------------------------------------------------------

@@ -105,6 +105,21 @@ __device__ __forceinline__ void store_result4(float* base, int64_t off, float a,
     }
 }
 
+// ---- random words of stochastic rounding: the 32-bit finalizer of MurmurHash3 over a counter and a key ------------------
+__host__ __device__ __forceinline__ uint32_t fmix32_rest(uint32_t h) {   // fmix32 behind its first step
+    h *= 0x85EBCA6Bu;
+    h ^= h >> 13;
+    h *= 0xC2B2AE35u;
+    h ^= h >> 16;
+    return h;
+}
+__host__ __device__ __forceinline__ uint32_t fmix32(uint32_t h) { return fmix32_rest(h ^ (h >> 16)); }
+// key = fmix32(seed_lo ^ fmix32(seed_hi ^ 0x9E3779B9)); it travels in the kernels' 64-bit seed argument
+inline uint64_t round_keys(uint64_t seed) {
+    const uint32_t lo = (uint32_t)seed, hi = (uint32_t)(seed >> 32);
+    return (uint64_t)fmix32(lo ^ fmix32(hi ^ 0x9E3779B9u));
+}
+
 // ---- division by a launch-invariant divisor ---------------------------------------------------
 // Exact unsigned division by an invariant divisor (Granlund-Montgomery round-up multiplier).
 struct FastDiv {

@@ -180,19 +180,7 @@ QuantWs carve_quant_ws(void* base, int C, int N, int HW, int given_waves = 0, in
 // and the two int8 copies take disjoint halves of the word as 16-bit uniforms: the per-channel copy (t = 0) U = h >> 16,
 // the per-tensor copy (t = 1) U = h & 0xFFFF, u = U * 2^-16.  A kernel that writes both copies of an element pays for
 // one hash (the calls below are pure, the compiler merges them); nothing is carried from one element to the next.
-__host__ __device__ __forceinline__ uint32_t fmix32_rest(uint32_t h) {   // fmix32 behind its first step
-    h *= 0x85EBCA6Bu;
-    h ^= h >> 13;
-    h *= 0xC2B2AE35u;
-    h ^= h >> 16;
-    return h;
-}
-__host__ __device__ __forceinline__ uint32_t fmix32(uint32_t h) { return fmix32_rest(h ^ (h >> 16)); }
-// key = fmix32(seed_lo ^ fmix32(seed_hi ^ 0x9E3779B9)); it travels in the kernels' 64-bit seed argument
-inline uint64_t round_keys(uint64_t seed) {
-    const uint32_t lo = (uint32_t)seed, hi = (uint32_t)(seed >> 32);
-    return (uint64_t)fmix32(lo ^ fmix32(hi ^ 0x9E3779B9u));
-}
+// (fmix32 and the key are in daq_internal.h.)
 // What the kernels carry is the complement of the word: each half of it is then 65535 - U, the form the rounding below adds.
 __device__ __forceinline__ uint32_t draw_word(uint64_t keys, uint32_t idx) { return ~fmix32(idx ^ (uint32_t)keys); }
 // The words of elements idx .. idx + 3, idx a multiple of four: (idx + e) ^ key is (idx ^ key) ^ e, and as e < 4 touches no bit that

@@ -1,0 +1,320 @@
+"""Microscaled 4-bit products and 8-bit checkpoints on the GPU, through the binding, against the oracle in 64 bits.
+
+Codes, scales and whole buffers are compared byte for byte.  Sums: every product is exact, each fp32 addition is off by at most 2^-23 of the
+magnitudes added so far (to nearest or cut off), so a sum of n terms by at most n * 2^-23 * sum |products|; the matrix instructions add 64
+(4-bit) or 16 (bfloat16) products as trees, so n counts steps, with ten additions inside and behind them.  A bfloat16 result adds 2^-8 of itself."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import lowbits as ref
+from paper_2102_04782_amd import binding as daq
+
+pytestmark = pytest.mark.gpu
+
+DT = [torch.float32, torch.bfloat16]
+SIZES = [(1, 1), (1, 31), (3, 32), (31, 33), (32, 64), (33, 255), (64, 256), (65, 257), (7, 1000), (300, 130), (257, 515)]
+
+
+def _x(rows, cols, dtype, seed, spread=6):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g) * torch.exp2(torch.randint(-spread, spread + 1, (rows, cols), generator=g).float())
+    if rows > 1 and cols > 40:
+        x[1, :32] = 0                                # a block of zeros
+        x[0, 32:40] = 0.25 * torch.arange(8)          # ties, once the block's scale is a power of two above them
+        x[0, 40:min(cols, 64)] = 1.0
+    return x.to(dtype)
+
+
+def _strided(x, dev, pad=5, first=3):
+    """x inside a wider matrix of other values: rows start at any element."""
+    wide = torch.full((x.shape[0], x.shape[1] + pad), 7.0, dtype=x.dtype, device=dev)
+    v = wide[:, first:first + x.shape[1]]
+    v.copy_(x)
+    return v
+
+
+def _np(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _mx4(x, **kw):
+    codes, byte = ref.mx4_codes(_np(x), **kw)
+    return codes, byte
+
+
+def _values(x, **kw):
+    codes, byte = _mx4(x, **kw)
+    return ref.mx4_values(codes, byte, x.shape[0] if kw.get("transpose") else x.shape[1])
+
+
+def _saved(x, parts=1):
+    codes, byte = ref.ckpt8_codes(_np(x), parts)
+    return ref.ckpt8_values(codes, byte, x.shape[0], x.shape[1] // parts, parts)
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_mx4_codes_scales_and_padding(rows, cols, dtype, stochastic, transpose):
+    x = _x(rows, cols, dtype, rows * 1000 + cols)
+    for src in (x.cuda(), _strided(x, "cuda")):
+        out = daq.alloc_mx4(*((cols, rows) if transpose else (rows, cols)))
+        out.buf.fill_(0xA5)                           # every byte, padding included, must come from the call
+        q = daq.mx4_quantize(src, transpose=transpose, mode=daq.ROUND_STOCHASTIC if stochastic else daq.ROUND_NEAREST, seed=(5 << 40) + 77, out=out)
+        codes, byte = _mx4(x, stochastic=stochastic, seed=(5 << 40) + 77, transpose=transpose)
+        got, want = q.buf.cpu().numpy(), ref.mx4_buffer(codes, byte)
+        off = daq.layout_mx4(q.rows, q.cols).off_scales
+        assert np.array_equal(got[off:], want[off:])
+        # a code of zero may carry either sign
+        same = got[:off] == want[:off]
+        lo, hi = got[:off] & 15, got[:off] >> 4
+        zero = lambda a, b: (a == b) | ((a & 7 == 0) & (b & 7 == 0))
+        assert np.all(same | (zero(lo, want[:off] & 15) & zero(hi, want[:off] >> 4)))
+        for to in DT:
+            v = daq.mx4_dequantize(q, dtype=to)
+            assert np.array_equal(_np(v), ref.mx4_values(codes, byte, q.cols))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("stochastic", [False, True])
+def test_mx4_extremes(dtype, stochastic):
+    x = torch.zeros(9, 96, dtype=dtype)
+    big = torch.finfo(dtype).max
+    x[0, 0], x[0, 33], x[1, 5] = big, -big, 2.0 ** -126
+    x[2, 7], x[2, 40] = 2.0 ** -133, 2.0 ** -128          # below the normal range
+    x[3, 3], x[4, 50], x[5, 70] = float("nan"), float("inf"), float("-inf")
+    x[6] = torch.tensor([2.0 ** -129 * (i % 13) for i in range(96)])
+    x[7, 31], x[7, 0] = 3.0, 6.0
+    x[8, :8] = torch.tensor([6.0, 6.5, 7.0, 7.5, 5.0, 4.999, 1e-30, -7.9])
+    for transpose in (False, True):
+        q = daq.mx4_quantize(x.cuda(), transpose=transpose, mode=int(stochastic), seed=3)
+        codes, byte = _mx4(x, stochastic=stochastic, seed=3, transpose=transpose)
+        for to in DT:
+            # (2^128, which stochastic rounding can make of the largest values, is an infinity in either type)
+            with np.errstate(over="ignore"):
+                want = ref.mx4_values(codes, byte, q.cols).astype(np.float32)
+            assert np.array_equal(_np(daq.mx4_dequantize(q, dtype=to)), want, equal_nan=True)
+
+
+MATMUL = [(1, 1, 1), (1, 33, 65), (1, 512, 2048), (2, 70, 300), (5, 64, 256), (13, 100, 1030), (32, 256, 512), (33, 129, 64), (40, 2049, 96), (64, 64, 4096),
+          (100, 260, 700), (255, 257, 513), (256, 256, 256), (300, 600, 320), (513, 511, 1024), (1030, 770, 200)]
+
+
+def _bound(steps, absolute, exact, dtype):
+    return (steps + 10) * 2.0 ** -23 * absolute + (2.0 ** -8 * np.abs(exact) if dtype == torch.bfloat16 else 0) + 1e-40
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", MATMUL)
+def test_mx4_matmul(M, N, K, dtype):
+    a, b = _x(M, K, torch.bfloat16, M + K), _x(N, K, torch.float32, N + 3 * K)
+    va, vb = _values(a), _values(b)
+    exact, absolute = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    qa, qb = daq.mx4_quantize(a.cuda()), daq.mx4_quantize(b.cuda())
+    wide = torch.full((M, N + 7), 55.0, dtype=dtype, device="cuda")
+    for out in (torch.full((M, N), float("nan"), dtype=dtype, device="cuda"), wide[:, 3:3 + N]):
+        got = _np(daq.mx4_matmul(qa, qb, out=out))
+        assert np.all(np.abs(got - exact) <= _bound(-(-K // 64), absolute, exact, dtype))
+    assert bool((wide[:, :3] == 55).all()) and bool((wide[:, 3 + N:] == 55).all())     # nothing beside the result
+
+
+@pytest.mark.parametrize("stochastic", [False, True])
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", MATMUL)
+def test_mx4_linear(M, N, K, dtype, stochastic):
+    x, w = _x(M, K, dtype, M + 2 * K), _x(N, K, torch.bfloat16, N + 5 * K)
+    vx, vw = _values(x, stochastic=stochastic, seed=9), _values(w)
+    exact, absolute = vx @ vw.T, np.abs(vx) @ np.abs(vw).T
+    qw = daq.mx4_quantize(w.cuda())
+    for src in (x.cuda(), _strided(x, "cuda")):
+        for to in DT:
+            got = _np(daq.mx4_linear(src, qw, mode=int(stochastic), seed=9, dtype=to))
+            assert np.all(np.abs(got - exact) <= _bound(-(-K // 64), absolute, exact, to))
+
+
+def test_mx4_linear_data_gradient_is_the_product_with_the_weights_by_columns():
+    dy, w = _x(70, 200, torch.float32, 1), _x(200, 330, torch.bfloat16, 2)
+    vy, vw = _values(dy, stochastic=True, seed=4), _values(w, transpose=True)       # vw [330, 200]
+    exact, absolute = vy @ vw.T, np.abs(vy) @ np.abs(vw).T
+    got = _np(daq.mx4_linear(dy.cuda(), daq.mx4_quantize(w.cuda(), transpose=True), mode=daq.ROUND_STOCHASTIC, seed=4))
+    assert got.shape == (70, 330) and np.all(np.abs(got - exact) <= _bound(4, absolute, exact, torch.float32))
+
+
+@pytest.mark.parametrize("M", [1, 3, 40, 300])
+def test_mx4_linear_keeps_a_bad_row_to_itself(M):
+    x, w = _x(M, 300, torch.bfloat16, 11), _x(150, 300, torch.bfloat16, 12)
+    w[149, 299] = float("inf")
+    x[0, 7] = float("nan")
+    got = _np(daq.mx4_linear(x.cuda(), daq.mx4_quantize(w.cuda())))
+    assert np.isnan(got[0]).all() and np.isnan(got[:, 149]).all() and np.isfinite(got[1:, :149]).all()
+
+
+def test_no_rows():
+    w = daq.mx4_quantize(_x(64, 96, torch.bfloat16, 1).cuda())
+    x = torch.empty(0, 96, dtype=torch.bfloat16, device="cuda")
+    assert daq.mx4_linear(x, w).shape == (0, 64)
+    assert daq.mx4_dequantize(daq.mx4_quantize(x)).shape == (0, 96)
+    assert daq.mx4_dequantize(daq.mx4_quantize(x, transpose=True)).shape == (96, 0)
+    assert daq.ckpt8_restore(daq.ckpt8_save(x)).shape == (0, 96)
+    y, c = daq.ckpt8_act_forward(x, daq.ACT_SILU, gated=True)
+    assert y.shape == (0, 48) and daq.ckpt8_act_backward(y, c, daq.ACT_SILU).shape == (0, 96)
+    dy = torch.empty(0, 40, dtype=torch.bfloat16, device="cuda")
+    assert bool((daq.ckpt8_weight_grad(dy, daq.ckpt8_save(x)) == 0).all())
+    kept = torch.full((40, 96), 3.0, device="cuda")
+    daq.ckpt8_weight_grad(dy, daq.ckpt8_save(x), out=kept, accumulate=True)
+    assert bool((kept == 3).all())
+
+
+@pytest.mark.parametrize("parts", [1, 2])
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("rows,cols", SIZES + [(3, 5000)])
+def test_ckpt8_codes_scales_and_padding(rows, cols, dtype, parts):
+    x = _x(rows, parts * cols, dtype, rows + cols)
+    codes, byte = ref.ckpt8_codes(_np(x), parts)
+    n, L = rows * parts, daq.layout_ckpt8(rows, cols, parts)
+    want = ref.ckpt8_buffer(codes, byte)
+    for src in (x.cuda(), _strided(x, "cuda")):
+        c = daq.alloc_ckpt8(rows, cols, parts)
+        c.buf.fill_(0xA5)
+        daq.ckpt8_save(src, parts, out=c)
+        got = c.buf.cpu().numpy()
+        assert np.array_equal(got[:n * L.pitch], want[:n * L.pitch])
+        assert np.array_equal(got[L.off_scales:L.off_scales + n * L.pitch // 32], want[L.off_scales:L.off_scales + n * L.pitch // 32])
+        wide = torch.full((rows, parts * cols + 9), 55.0, dtype=dtype, device="cuda")
+        for out in (torch.empty_like(src), wide[:, 4:4 + parts * cols]):
+            assert np.array_equal(_np(daq.ckpt8_restore(c, out=out)), ref.ckpt8_values(codes, byte, rows, cols, parts))
+        assert bool((wide[:, :4] == 55).all()) and bool((wide[:, 4 + parts * cols:] == 55).all())
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_ckpt8_extremes(dtype):
+    x = torch.zeros(7, 96, dtype=dtype)
+    big = torch.finfo(dtype).max
+    x[0, 0], x[0, 33], x[1, 5] = big, -big, 2.0 ** -126
+    x[2, 7], x[2, 40] = 2.0 ** -133, 2.0 ** -128
+    x[3, 3], x[4, 50], x[5, 70] = float("nan"), float("inf"), float("-inf")
+    x[6, :9] = torch.tensor([127.0, 127.5, -127.5, 127.75, 0.5, 1.5, -2.5, 126.5, -0.5])
+    assert np.array_equal(_np(daq.ckpt8_restore(daq.ckpt8_save(x.cuda()))), _saved(x), equal_nan=True)
+
+
+ACTS = [("silu", daq.ACT_SILU), ("gelu", daq.ACT_GELU)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("name,act", ACTS)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 32), (5, 31), (33, 100), (64, 257), (3, 4100)])
+def test_act_forward_and_backward(rows, cols, name, act, dtype, gated):
+    """fp32 formulas: the exponential and the error function are good to some units in the last place, their sums and products to a unit
+    each; x times an error of the sigmoid or of Phi (an absolute one, at most 8 * 2^-24) bounds f, and as much times 1 + |x| its slope."""
+    parts = 2 if gated else 1
+    h, dy = _x(rows, parts * cols, dtype, rows + cols, 2), _x(rows, cols, dtype, rows + cols + 1, 2)
+    one = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+    eps = 8 * 2.0 ** -24
+    hv, hs, d = _np(h), _saved(h, parts), _np(dy)
+    f, _ = ref.act(hv[:, :cols], name)
+    fs, slope = ref.act(hs[:, :cols], name)
+    u, us = (hv[:, cols:], hs[:, cols:]) if gated else (1.0, 1.0)
+    for strided in (False, True):
+        src = _strided(h, "cuda") if strided else h.cuda()
+        y, kept = daq.ckpt8_act_forward(src, act, gated=gated)
+        assert y.dtype == dtype and np.all(np.abs(_np(y) - f * u) <= eps * np.abs(hv[:, :cols] * u) + one * np.abs(f * u) + 1e-37)
+        assert np.array_equal(_np(daq.ckpt8_restore(kept)), hs)
+        wide = torch.full((rows, parts * cols + 6), 55.0, dtype=dtype, device="cuda")
+        yk = daq.alloc_ckpt8(rows, cols)
+        dh = daq.ckpt8_act_backward(_strided(dy, "cuda") if strided else dy.cuda(), kept, act, out=wide[:, 2:2 + parts * cols], y_ckpt=yk)
+        got, want = _np(dh), d * us * slope
+        tol = eps * np.abs(d * us) * (1 + np.abs(hs[:, :cols])) ** 2
+        assert np.all(np.abs(got[:, :cols] - want) <= tol + one * np.abs(want) + 1e-37)
+        if gated:
+            assert np.all(np.abs(got[:, cols:] - d * fs) <= eps * np.abs(d * hs[:, :cols]) + one * np.abs(d * fs) + 1e-37)
+        assert bool((wide[:, :2] == 55).all()) and bool((wide[:, 2 + parts * cols:] == 55).all())
+        # the output saved again: within a code of what the oracle's value is, and the same gradient without it
+        ycodes, ybyte = ref.ckpt8_codes(fs * us)
+        step = np.repeat(np.exp2(ybyte - 127.0), 32, axis=1)[:, :cols]
+        assert np.all(np.abs(_np(daq.ckpt8_restore(yk)) - fs * us) <= 1.01 * step + eps * np.abs(hs[:, :cols] * us))
+        again = daq.ckpt8_act_backward(dy.cuda(), kept, act)
+        assert torch.equal(again, dh)
+
+
+@pytest.mark.parametrize("name,act", ACTS)
+def test_act_gradient_against_differences(name, act):
+    """(f(x + h) - f(x - h)) / 2h of the forward pass at points that 8 bits hold exactly; h = 2^-6: h^2 / 6 times a third derivative below 2,
+    and fp32 rounding of f over h."""
+    codes = torch.arange(-127, 128, dtype=torch.float32)
+    x = torch.zeros(8, 32)
+    x.view(-1)[:255] = codes / 16
+    x[:, 31] = 127 / 16                                  # the scale of every block
+    x, one = x.cuda(), torch.ones(8, 32, device="cuda")
+    h = 2.0 ** -6
+    up, _ = daq.ckpt8_act_forward(x + h, act)
+    down, _ = daq.ckpt8_act_forward(x - h, act)
+    _, kept = daq.ckpt8_act_forward(x, act)
+    assert torch.equal(daq.ckpt8_restore(kept), x)
+    slope = daq.ckpt8_act_backward(one, kept, act)
+    assert float((slope - (up - down) / (2 * h)).abs().max()) <= h * h / 3 + 16 * 8 * 2.0 ** -24 / h
+
+
+WGRAD = [(1, 1, 1), (1, 40, 70), (7, 33, 31), (16, 32, 32), (64, 128, 256), (100, 130, 260), (257, 300, 129), (1000, 64, 64), (513, 520, 400), (2048, 96, 1000)]
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", WGRAD)
+def test_weight_grad(M, N, K, dtype):
+    dy, x = _x(M, N, dtype, M + N), _x(M, K, torch.bfloat16, M + 7 * K)
+    xs, d = _saved(x), _np(dy)
+    exact, absolute = d.T @ xs, np.abs(d.T) @ np.abs(xs)
+    kept = daq.ckpt8_save(x.cuda())
+    bound = _bound((3 if dtype == torch.float32 else 1) * -(-M // 16), absolute, exact, torch.float32)
+    for src in (dy.cuda(), _strided(dy, "cuda")):
+        got = daq.ckpt8_weight_grad(src, kept)
+        assert np.all(np.abs(_np(got) - exact) <= bound)
+        wide = torch.full((N, K + 5), 2.0, device="cuda")
+        daq.ckpt8_weight_grad(src, kept, out=wide[:, 1:1 + K], accumulate=True)
+        assert bool((wide[:, 0] == 2).all()) and bool((wide[:, 1 + K:] == 2).all())
+        assert np.all(np.abs(_np(wide[:, 1:1 + K]) - 2 - exact) <= bound + 2.0 ** -22 * (2 + np.abs(exact)))
+        assert torch.equal(got, daq.ckpt8_weight_grad(src, kept))       # the same bits every time
+
+
+def test_weight_grad_against_differences():
+    """The loss sum(dy * (x^ w^T)) is linear in the weights: a step in one of them changes it by its gradient."""
+    g = torch.Generator().manual_seed(3)
+    x = daq.ckpt8_save(torch.randn(50, 40, generator=g).cuda())
+    xs, dy = daq.ckpt8_restore(x).double(), torch.randn(50, 24, generator=g).cuda()
+    dW, w = daq.ckpt8_weight_grad(dy, x), torch.randn(24, 40, generator=g).cuda().double()
+    loss = lambda w: float((dy.double() * (xs @ w.t().contiguous())).sum())
+    for n, k in [(0, 0), (5, 31), (23, 39), (11, 32)]:
+        up, down = w.clone(), w.clone()
+        up[n, k] += 0.5
+        down[n, k] -= 0.5
+        assert abs(loss(up) - loss(down) - float(dW[n, k])) <= 14 * 2.0 ** -23 * float((dy[:, n].abs().double() * xs[:, k].abs()).sum()) + 1e-9
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_weight_grad_keeps_what_is_not_finite_to_itself(dtype):
+    dy, x = _x(100, 40, dtype, 1), _x(100, 70, torch.bfloat16, 2)
+    dy[3, 5], dy[99, 39], x[50, 33] = float("nan"), float("inf"), float("inf")
+    got = _np(daq.ckpt8_weight_grad(dy.cuda(), daq.ckpt8_save(x.cuda())))
+    bad = np.zeros((40, 70), bool)
+    bad[5] = bad[39] = True
+    bad[:, 32:64] = True
+    assert np.isnan(got[5]).all() and np.isnan(got[:, 32:64]).all() and not np.isfinite(got[39]).any() and np.isfinite(got[~bad]).all()
+
+
+def test_calls_on_another_stream():
+    side = torch.cuda.Stream()
+    x, w = _x(200, 512, torch.bfloat16, 1).cuda(), _x(300, 512, torch.bfloat16, 2).cuda()
+    dy = _x(200, 300, torch.bfloat16, 3).cuda()
+    want = daq.mx4_linear(x, daq.mx4_quantize(w)), daq.ckpt8_weight_grad(dy, daq.ckpt8_save(x))
+    out, dW = torch.empty_like(want[0]), torch.empty_like(want[1])
+    qw, kept = daq.alloc_mx4(300, 512), daq.alloc_ckpt8(200, 512)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    daq.mx4_quantize(w, out=qw, stream=side)
+    daq.mx4_linear(x, qw, out=out, workspace=ws, stream=side)
+    daq.ckpt8_save(x, out=kept, stream=side)
+    daq.ckpt8_weight_grad(dy, kept, out=dW, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(dW, want[1])
