@@ -2,85 +2,245 @@
 //
 // A decoded code is an integer of at most seven bits times a power of two, so X^ is exact in bfloat16 and the products run on the
 // bfloat16 matrix cores with fp32 sums.  An fp32 gradient is the sum of three bfloat16 values of eight bits each.
-#include "lowbits.h"
+//
+// Both operands have their summed axis, the tokens, outermost.  A first launch brings them into the order of the matrix
+// instructions (eight tokens of a column in 16 bytes), decoding X^ and splitting an fp32 dY on the way: it reads and writes each once,
+// 0.1 of the time of the products at 16384 x 8192 x 4096.  The products then run on whole KiB tiles.
+#include "tile_product.h"
 
 namespace daq {
 
 namespace {
 
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef uint16_t v8u __attribute__((ext_vector_type(8)));
+constexpr int kStageM = 16 * kStageSteps;   // tokens of a stage
 
-struct WgradArgs {
+struct OrderArgs {
     const void* dy;
     int64_t lddy;
     const uint8_t* codes;
     const uint8_t* scales;
     int64_t pitch;
-    int64_t M, N, K;
-    float* dw;
-    int64_t ldw;
-    int accumulate;
+    int64_t M, N;
+    uint8_t* dy_tiles;
+    uint8_t* x_tiles;
+    int n_blocks, k_blocks;      // row blocks of 32 of either operand
+    int steps;                   // of 16 tokens, a multiple of kStageSteps
+    int64_t dy_waves, x_waves;
 };
 
 // x = hi + mid + lo, each the leading eight bits of what is left (a value that is not finite stays whole).
-__device__ __forceinline__ void split3(float x, uint16_t& hi, uint16_t& mid, uint16_t& lo) {
+__device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
     const uint32_t h = __float_as_uint(x) & 0xFFFF0000u;
-    hi = (uint16_t)(h >> 16);
+    hi = h >> 16;
     const bool finite = (h & 0x7F800000u) != 0x7F800000u;
     const float r = finite ? x - bits_as<float>(h) : 0.0f;
     const uint32_t m = __float_as_uint(r) & 0xFFFF0000u;
-    mid = (uint16_t)(m >> 16);
-    lo = (uint16_t)(__float_as_uint(r - bits_as<float>(m)) >> 16);
+    mid = m >> 16;
+    lo = __float_as_uint(r - bits_as<float>(m)) >> 16;
     if (!finite && x != x) hi |= 0x40;   // a NaN of low bits only
 }
 
+// Four columns of eight tokens, as words of two neighbouring columns, to the order of the tiles: 16 bytes a column.
+__device__ __forceinline__ void store_columns(uint8_t* to, const u32x2 (&v)[8]) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = __builtin_amdgcn_perm(v[2 * i + 1][c / 2], v[2 * i][c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
+        *reinterpret_cast<u32x4*>(to + c * 16) = w;
+    }
+}
+
+// A wave takes 128 columns x 16 tokens of either operand, a lane four columns of eight tokens.
 template <typename T>
-__global__ __launch_bounds__(256) void k_ckpt8_wgrad(WgradArgs p) {
+__global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
     const int lane = threadIdx.x % kWave;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    const int64_t tiles_k = (p.K + 31) / 32, tn = wave / tiles_k, tk = wave - tn * tiles_k;
-    if (tn * 32 >= p.N) return;
-    const int64_t n = tn * 32 + lane % 32, k = tk * 32 + lane % 32;
-    const T* dy = static_cast<const T*>(p.dy) + min(n, p.N - 1);
-    const uint8_t* code = p.codes + k;                        // inside the row's padding at least
-    const uint8_t* scale = p.scales + tk;
-    v16f acc = {};
-    for (int64_t m0 = 0; m0 < p.M; m0 += 16) {
-        v8u hi, mid, lo, x;
+    int64_t wave = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    const bool of_dy = wave < p.dy_waves;
+    if (!of_dy) wave -= p.dy_waves;
+    if (!of_dy && wave >= p.x_waves) return;
+    const int blocks = of_dy ? p.n_blocks : p.k_blocks;
+    const int wide = (blocks + 3) / 4;
+    const int64_t step = wave / wide;
+    const int64_t col = (wave - step * wide) * 128 + (lane % 32) * 4;
+    if (col / 32 >= blocks) return;
+    const int64_t m0 = step * 16 + (lane / 32) * 8;
+    const int64_t at = (col / 32 * p.steps + step) * 1024 + (lane / 32) * 512 + (col % 32) * 16;
+    if (of_dy) {
+        const T* src = static_cast<const T*>(p.dy) + col;
+        if constexpr (sizeof(T) == 2) {
+            u32x2 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = m0 + j < p.M;
+                const T* row = src + (in ? m0 + j : 0) * p.lddy;
+                if (col + 4 <= p.N) {
+                    const u32x2_a2 q = *reinterpret_cast<const u32x2_a2*>(row);
+                    v[j] = in ? u32x2{q[0], q[1]} : u32x2{0, 0};
+                } else {
+                    uint32_t e[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = in && col + i < p.N ? row[i] : 0u;
+                    v[j] = u32x2{e[0] | (e[1] << 16), e[2] | (e[3] << 16)};
+                }
+            }
+            store_columns(p.dy_tiles + at, v);
+        } else {
+            u32x2 v[3][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = m0 + j < p.M;
+                const T* row = src + (in ? m0 + j : 0) * p.lddy;
+                float e[4];
+                if (col + 4 <= p.N) {
+                    const u32x4_a4 q = *reinterpret_cast<const u32x4_a4*>(row);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = in ? bits_as<float>(q[i]) : 0.0f;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = in && col + i < p.N ? row[i] : 0.0f;
+                }
+                uint32_t h[4][3];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) split3(e[i], h[i][0], h[i][1], h[i][2]);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) v[k][j] = u32x2{h[0][k] | (h[1][k] << 16), h[2][k] | (h[3][k] << 16)};
+            }
+            // the three parts are stages of their own, one after the other, the smallest first: so the sums are long only in the last
+            // third, and as exact as those of the leading bits alone
+            uint8_t* to = p.dy_tiles + (col / 32 * 3 * p.steps + step) * 1024 + (lane / 32) * 512 + (col % 32) * 16;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) store_columns(to + (int64_t)(2 - k) * p.steps * 1024, v[k]);
+        }
+    } else {
+        u32x2 v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int64_t m = m0 + (lane / 32) * 8 + j;
-            const bool in = m < p.M;
-            const int64_t r = in ? m : 0;
-            const float xv = (float)(int8_t)code[r * p.pitch] * scale_of(scale[r * (p.pitch / kMxBlock)]);
-            x[j] = in ? (uint16_t)(__float_as_uint(xv) >> 16) : (uint16_t)0;
-            if constexpr (sizeof(T) == 4) {
-                uint16_t a, b, c;
-                split3(dy[r * p.lddy], a, b, c);
-                hi[j] = in ? a : (uint16_t)0;
-                mid[j] = in ? b : (uint16_t)0;
-                lo[j] = in ? c : (uint16_t)0;
-            } else {
-                hi[j] = in ? dy[r * p.lddy] : (uint16_t)0;
-            }
-        }
-        const v8bf xb = __builtin_bit_cast(v8bf, x);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, hi), xb, acc, 0, 0, 0);
-        if constexpr (sizeof(T) == 4) {
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, mid), xb, acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, lo), xb, acc, 0, 0, 0);
-        }
-    }
+            const bool in = m0 + j < p.M;
+            const int64_t r = in ? m0 + j : 0;
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(p.codes + r * p.pitch + col);
+            const float s = in ? scale_of(p.scales[r * (p.pitch / kMxBlock) + col / 32]) : 0.0f;
+            float e[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int64_t row = tn * 32 + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
-        if (row < p.N && k < p.K) {
-            float* z = p.dw + row * p.ldw + k;
-            *z = p.accumulate ? *z + acc[i] : acc[i];
+            for (int i = 0; i < 4; ++i) e[i] = in ? (float)(int8_t)(w >> (8 * i)) * s : 0.0f;
+            // (exact in bfloat16: the upper halves)
+            v[j] = u32x2{__builtin_amdgcn_perm(__float_as_uint(e[1]), __float_as_uint(e[0]), 0x07060302u),
+                         __builtin_amdgcn_perm(__float_as_uint(e[3]), __float_as_uint(e[2]), 0x07060302u)};
         }
+        store_columns(p.x_tiles + at, v);
     }
+}
+
+struct WgradArgs {
+    TileOperand dy, x;
+    int stages;              // of dy
+    int x_stages;            // of x: dy begins again every so many
+    int splits, per_split;   // parts of the stages, and stages of a part
+    int tiles_n, tiles_k, per_xcd;
+    int64_t N, K;
+    float* dw;
+    int64_t ldw;
+    int accumulate;
+    float* part;             // splits > 1: [split][N][pitch]
+    int64_t pitch;
+};
+
+// Tiles of 32 RB WR rows x 32 CB WC columns of dW, a workgroup each, for one part of the tokens.  Order of the workgroups as in the
+// 4-bit products; the parts of a tile are neighbours in it.
+template <int WR, int WC, int RB, int CB>
+__global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
+    using Product = TileProduct<WR, WC, RB, CB, false>;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int64_t b = (int64_t)(blockIdx.x % kXcd) * p.per_xcd + blockIdx.x / kXcd;
+    const int64_t t = b / p.splits;
+    const int split = (int)(b - t * p.splits);
+    if (t >= (int64_t)p.tiles_n * p.tiles_k) return;
+    const int64_t band = t / (4 * p.tiles_k);
+    const int rest = (int)(t - band * 4 * p.tiles_k), high = min(4, p.tiles_n - (int)band * 4);
+    const int tn = (int)band * 4 + rest % high, tk = rest / high;
+    Product prod;
+    prod.run(p.dy, p.x, tn * WR * RB, tk * WC * CB, split * p.per_split, min(p.stages, (split + 1) * p.per_split), p.x_stages, lds,
+             lds + Product::kStageBytes);
+    const int wave = threadIdx.x / kWave;
+    const int64_t n0 = ((int64_t)tn * WR + wave / WC) * RB * 32, k0 = ((int64_t)tk * WC + wave % WC) * CB * 32;
+    float* base = p.splits > 1 ? p.part + split * p.N * p.pitch : p.dw;
+    const int64_t ld = p.splits > 1 ? p.pitch : p.ldw;
+    const bool add = p.splits == 1 && p.accumulate;
+    prod.store(false, lds, [&](int row, int col, u32x4 v) {
+        const int64_t n = n0 + row, k = k0 + col;
+        if (n >= p.N || k >= p.K) return;
+        float* z = base + n * ld + k;
+        if (k + 4 <= p.K) {
+            u32x4_a4* q = reinterpret_cast<u32x4_a4*>(z);
+            if (add) {
+                const u32x4_a4 old = *q;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(bits_as<float>(old[i]) + bits_as<float>(v[i]));
+            }
+            *q = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (k + i < p.K) z[i] = add ? z[i] + bits_as<float>(v[i]) : bits_as<float>(v[i]);
+        }
+    });
+}
+
+// Sums of the parts, in their order; no parts: zeros.
+__global__ __launch_bounds__(256) void k_ckpt8_wgrad_sum(const float* part, int splits, int64_t N, int64_t K, int64_t pitch, float* dw, int64_t ldw,
+                                                         int accumulate) {
+    const int64_t units = (K + 3) / 4, u = (int64_t)blockIdx.x * 256 + threadIdx.x, n = u / units, k = (u - n * units) * 4;
+    if (n >= N) return;
+    f32x4 sum = {0, 0, 0, 0};
+    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(part + (s * N + n) * pitch + k);
+    float* z = dw + n * ldw + k;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (k + i < K) z[i] = accumulate ? z[i] + sum[i] : sum[i];
+}
+
+template <int WR, int WC, int RB, int CB>
+daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
+    using Product = TileProduct<WR, WC, RB, CB, false>;
+    p.tiles_n = (int)ceil_div(p.dy.blocks, WR * RB);
+    p.tiles_k = (int)ceil_div(p.x.blocks, WC * CB);
+    const int64_t per = ceil_div((int64_t)p.tiles_n * p.tiles_k * p.splits, kXcd);
+    if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
+    p.per_xcd = (int)per;
+    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB>;
+    if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
+    DAQ_LAUNCH("ckpt8_wgrad", st, hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcd)), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
+    return DAQ_OK;
+}
+
+// Sizes of a call and where its workspace holds what.
+struct WgradPlan {
+    int n_blocks, k_blocks, steps, parts;   // parts: of a value of dY
+    bool big;                               // tiles of 256 x 256 instead of 128 x 128
+    int splits, per_split;
+    int64_t off_x, off_part, pitch, bytes;
+};
+WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype) {
+    WgradPlan w{};
+    w.n_blocks = (int)ceil_div(N, 32);
+    w.k_blocks = (int)ceil_div(K, 32);
+    w.steps = (int)(ceil_div(M, kStageM) * kStageSteps);
+    w.parts = dtype == DAQ_BF16 ? 1 : 3;
+    const int stages = w.steps / kStageSteps * w.parts;
+    const int64_t big = ceil_div(w.n_blocks, 8) * ceil_div(w.k_blocks, 8), small = ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4);
+    w.big = big >= 128;
+    const int64_t tiles = w.big ? big : small, slots = w.big ? 256 : 512;
+    w.splits = 1;
+    while (tiles * w.splits * 2 <= slots && w.splits < stages / 2) w.splits *= 2;
+    w.splits = std::min(w.splits, stages);
+    w.per_split = (int)ceil_div(stages, w.splits);
+    w.splits = (int)ceil_div(stages, w.per_split);
+    w.pitch = round_up(K, 4);
+    w.off_x = round_up((int64_t)w.n_blocks * w.steps * w.parts * 1024, 256);
+    w.off_part = w.off_x + (int64_t)w.k_blocks * w.steps * 1024;
+    w.bytes = w.off_part + (w.splits > 1 ? round_up((int64_t)w.splits * N * w.pitch * 4, 256) : 0);
+    return w;
 }
 
 }  // namespace
@@ -101,24 +261,56 @@ extern "C" daq_status daq_ckpt8_weight_grad_workspace(int64_t M, int64_t N, int6
     if (!bytes) return DAQ_ERR_INVALID_ARG;
     *bytes = 0;
     if (!dtype_ok(dtype)) return DAQ_ERR_INVALID_ARG;
-    return wgrad_size(M, N, K);
+    const daq_status rc = wgrad_size(M, N, K);
+    if (rc == DAQ_OK && M > 0) *bytes = (size_t)wgrad_plan(M, N, K, dtype).bytes;
+    return rc;
 }
 
 extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, const void* dY, daq_dtype dtype, int64_t lddy,
                                             const uint8_t* x_ckpt, float* dW, int64_t ldw, int32_t accumulate, void* workspace,
                                             size_t workspace_bytes, void* stream) {
     if (!dtype_ok(dtype)) return DAQ_ERR_INVALID_ARG;
-    const daq_status rc = wgrad_size(M, N, K);
+    daq_status rc = wgrad_size(M, N, K);
     if (rc != DAQ_OK) return rc;
     if (!dW || !elem_aligned(dW, DAQ_FP32) || ldw < K) return DAQ_ERR_INVALID_ARG;
     if (M > 0 && (!dY || !elem_aligned(dY, dtype) || lddy < N || !x_ckpt || !aligned256(x_ckpt))) return DAQ_ERR_INVALID_ARG;
+    hipStream_t st = (hipStream_t)stream;
+    const int64_t sum_blocks = ceil_div(N * ceil_div(K, 4), 256);
+    if (!grid_ok(sum_blocks)) return DAQ_ERR_UNSUPPORTED;
+    if (M == 0) {   // a sum of nothing
+        if (!accumulate)
+            DAQ_LAUNCH("ckpt8_wgrad_sum", st, hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, nullptr, 0, N, K, 0, dW, ldw, 0));
+        return DAQ_OK;
+    }
+    const WgradPlan w = wgrad_plan(M, N, K, dtype);
+    if (!workspace || workspace_bytes < (size_t)w.bytes || !aligned256(workspace)) return DAQ_ERR_WORKSPACE;
     daq_ckpt8_layout L;
     daq_layout_ckpt8(M, K, 1, &L);
-    const WgradArgs p{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, K, dW, ldw, accumulate};
-    const int64_t blocks = ceil_div(ceil_div(N, 32) * ceil_div(K, 32), 4);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    OrderArgs o{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, ws, ws + w.off_x, w.n_blocks, w.k_blocks, w.steps, 0, 0};
+    o.dy_waves = round_up(ceil_div(w.n_blocks, 4) * w.steps, 4);
+    o.x_waves = ceil_div(w.k_blocks, 4) * w.steps;
+    const int64_t blocks = ceil_div(o.dy_waves + o.x_waves, 4);
     if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;
-    hipStream_t st = (hipStream_t)stream;
-    if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_wgrad", st, hipLaunchKernelGGL(k_ckpt8_wgrad<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, st, p));
-    else DAQ_LAUNCH("ckpt8_wgrad", st, hipLaunchKernelGGL(k_ckpt8_wgrad<float>, dim3((unsigned)blocks), dim3(256), 0, st, p));
+    if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, st, o));
+    else DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<float>, dim3((unsigned)blocks), dim3(256), 0, st, o));
+    WgradArgs p{};
+    p.dy = TileOperand{o.dy_tiles, nullptr, w.n_blocks, w.steps * w.parts};
+    p.x = TileOperand{o.x_tiles, nullptr, w.k_blocks, w.steps};
+    p.stages = w.steps / kStageSteps * w.parts;
+    p.x_stages = w.steps / kStageSteps;
+    p.splits = w.splits;
+    p.per_split = w.per_split;
+    p.N = N;
+    p.K = K;
+    p.dw = dW;
+    p.ldw = ldw;
+    p.accumulate = accumulate;
+    p.part = reinterpret_cast<float*>(ws + w.off_part);
+    p.pitch = w.pitch;
+    rc = w.big ? launch_wgrad<2, 4, 4, 2>(p, st) : launch_wgrad<2, 2, 2, 2>(p, st);
+    if (rc != DAQ_OK || w.splits == 1) return rc;
+    DAQ_LAUNCH("ckpt8_wgrad_sum", st,
+               hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, p.part, w.splits, N, K, w.pitch, dW, ldw, accumulate));
     return DAQ_OK;
 }

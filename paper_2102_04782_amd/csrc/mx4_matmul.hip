@@ -4,15 +4,11 @@
 // row l % 32 and block l / 32 of the 64 columns.  The packed layout holds operands in that order, so a wave loads a 32 x 64 tile
 // as one contiguous KiB and the scale bytes of four tiles as one contiguous 256 bytes.  B goes in as the instruction's first
 // operand, so that a lane holds four neighbouring columns of a row of D at a time.
-#include "lowbits.h"
+#include "tile_product.h"
 
 namespace daq {
 
 namespace {
-
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
 
 struct MatmulArgs {
     const uint8_t* a;       // codes
@@ -28,88 +24,61 @@ struct MatmulArgs {
     int bf16;
 };
 
-// One step: cbsz / blgp 4 say 4-bit elements; S picks the byte of the scale words.
-template <int S>
-__device__ __forceinline__ v16f mfma4(v4i x, v4i y, v16f c, int sx, int sy) {
-    const v8i a = {x[0], x[1], x[2], x[3], 0, 0, 0, 0}, b = {y[0], y[1], y[2], y[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, S, sx, S, sy);
-}
-
-// Four columns of row m of D from column n on.
-__device__ __forceinline__ void store4(const MatmulArgs& p, int64_t m, int64_t n, float a, float b, float c, float d) {
-    if (m >= p.M || n >= p.N) return;
-    const int left = (int)min(p.N - n, (int64_t)4);
+// Tiles of 32 RB WR x 32 CB WC results, a workgroup each.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles, in bands
+// of four row tiles, so that the 32 it holds at a time share twelve panels of the operands in its L2.
+template <int WR, int WC, int RB, int CB>
+__global__ __launch_bounds__(64 * WR * WC, 1) void k_mx4_tiles(MatmulArgs p, int tiles_m, int tiles_n, int per_xcd) {
+    using Product = TileProduct<WR, WC, RB, CB, true>;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int64_t t = (int64_t)(blockIdx.x % kXcd) * per_xcd + blockIdx.x / kXcd;
+    if (t >= (int64_t)tiles_m * tiles_n) return;
+    const int64_t band = t / (4 * tiles_n);
+    const int rest = (int)(t - band * 4 * tiles_n), high = min(4, tiles_m - (int)band * 4);
+    const int tm = (int)band * 4 + rest % high, tn = rest / high;
+    const TileOperand r{p.a, p.a_scales, p.a_blocks, p.groups * 4}, c{p.b, p.b_scales, p.b_blocks, p.groups * 4};
+    Product prod;
+    prod.run(r, c, tm * WR * RB, tn * WC * CB, 0, p.groups, p.groups, lds, lds + Product::kStageBytes);
+    const int wave = threadIdx.x / kWave;
+    const int64_t m0 = ((int64_t)tm * WR + wave / WC) * RB * 32, n0 = ((int64_t)tn * WC + wave % WC) * CB * 32;
     if (p.bf16) {
-        uint16_t* z = static_cast<uint16_t*>(p.d) + m * p.ldd + n;
-        const uint32_t w0 = pack_bf16(a, b), w1 = pack_bf16(c, d);
-        if (left == 4) {
-            *reinterpret_cast<u32x2_a2*>(z) = u32x2_a2{w0, w1};
-        } else {
-            z[0] = (uint16_t)w0;
-            if (left > 1) z[1] = (uint16_t)(w0 >> 16);
-            if (left > 2) z[2] = (uint16_t)w1;
-        }
+        prod.store(true, lds, [&](int row, int col, u32x4 v) {
+            const int64_t m = m0 + row, n = n0 + col;
+            if (m >= p.M || n >= p.N) return;
+            uint16_t* z = static_cast<uint16_t*>(p.d) + m * p.ldd + n;
+            if (n + 8 <= p.N) {
+                *reinterpret_cast<u32x4_a2*>(z) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 7; ++i)
+                    if (n + i < p.N) z[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+            }
+        });
     } else {
-        float* z = static_cast<float*>(p.d) + m * p.ldd + n;
-        if (left == 4) {
-            *reinterpret_cast<u32x4_a4*>(z) = u32x4_a4{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)};
-        } else {
-            z[0] = a;
-            if (left > 1) z[1] = b;
-            if (left > 2) z[2] = c;
-        }
+        prod.store(false, lds, [&](int row, int col, u32x4 v) {
+            const int64_t m = m0 + row, n = n0 + col;
+            if (m >= p.M || n >= p.N) return;
+            uint32_t* z = static_cast<uint32_t*>(p.d) + m * p.ldd + n;
+            if (n + 4 <= p.N) {
+                *reinterpret_cast<u32x4_a4*>(z) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (n + i < p.N) z[i] = v[i];
+            }
+        });
     }
 }
 
-// A wave takes 64 x 64 results, operands straight from memory.
-__global__ __launch_bounds__(256) void k_mx4_matmul(MatmulArgs p) {
-    const int lane = threadIdx.x % kWave;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    const int tiles_n = (p.b_blocks + 1) / 2;
-    const int64_t tm = wave / tiles_n;
-    const int tn = (int)(wave - tm * tiles_n);
-    if (tm * 2 >= p.a_blocks) return;
-    const uint8_t *a[2], *b[2], *sa[2], *sb[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t ra = min(tm * 2 + i, (int64_t)p.a_blocks - 1), rb = min(tn * 2 + i, p.b_blocks - 1);
-        a[i] = p.a + ra * p.groups * 4096 + lane * 16;
-        b[i] = p.b + rb * p.groups * 4096 + lane * 16;
-        sa[i] = p.a_scales + ra * p.groups * 256 + lane * 4;
-        sb[i] = p.b_scales + rb * p.groups * 256 + lane * 4;
-    }
-    v16f acc[2][2] = {};
-    for (int g = 0; g < p.groups; ++g) {
-        int wa[2], wb[2];
-        v4i va[2][4], vb[2][4];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            wa[i] = *reinterpret_cast<const int*>(sa[i] + (int64_t)g * 256);
-            wb[i] = *reinterpret_cast<const int*>(sb[i] + (int64_t)g * 256);
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                va[i][s] = *reinterpret_cast<const v4i*>(a[i] + ((int64_t)g * 4 + s) * 1024);
-                vb[i][s] = *reinterpret_cast<const v4i*>(b[i] + ((int64_t)g * 4 + s) * 1024);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                acc[i][j] = mfma4<0>(vb[j][0], va[i][0], acc[i][j], wb[j], wa[i]);
-                acc[i][j] = mfma4<1>(vb[j][1], va[i][1], acc[i][j], wb[j], wa[i]);
-                acc[i][j] = mfma4<2>(vb[j][2], va[i][2], acc[i][j], wb[j], wa[i]);
-                acc[i][j] = mfma4<3>(vb[j][3], va[i][3], acc[i][j], wb[j], wa[i]);
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                store4(p, (tm * 2 + i) * 32 + lane % 32, ((int64_t)tn * 2 + j) * 32 + q * 8 + (lane / 32) * 4, acc[i][j][4 * q], acc[i][j][4 * q + 1],
-                       acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+template <int WR, int WC, int RB, int CB>
+daq_status launch_tiles(const MatmulArgs& p, hipStream_t st) {
+    using Product = TileProduct<WR, WC, RB, CB, true>;
+    const int64_t tm = ceil_div(p.a_blocks, WR * RB), tn = ceil_div(p.b_blocks, WC * CB), per = ceil_div(tm * tn, kXcd);
+    if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
+    const auto kernel = k_mx4_tiles<WR, WC, RB, CB>;
+    if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
+    DAQ_LAUNCH("mx4_tiles", st,
+               hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcd)), dim3(64 * WR * WC), Product::kLdsBytes, st, p, (int)tm, (int)tn, (int)per));
+    return DAQ_OK;
 }
 
 }  // namespace
@@ -133,10 +102,8 @@ static daq_status mx4_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, 
     daq_layout_mx4(N, K, &lb);
     const MatmulArgs p{A, A + la.off_scales, B, B + lb.off_scales, M, N, la.row_blocks, lb.row_blocks, la.groups,
                        (int)ceil_div(K, 64), D, ldd, dtype == DAQ_BF16};
-    const int64_t waves = ceil_div(la.row_blocks, 2) * ceil_div(lb.row_blocks, 2), blocks = ceil_div(waves, 4);
-    if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;
-    DAQ_LAUNCH("mx4_matmul", st, hipLaunchKernelGGL(k_mx4_matmul, dim3((unsigned)blocks), dim3(256), 0, st, p));
-    return DAQ_OK;
+    const int64_t big = ceil_div(la.row_blocks, 8) * ceil_div(lb.row_blocks, 8);
+    return big >= 160 ? launch_tiles<2, 4, 4, 2>(p, st) : launch_tiles<2, 2, 2, 2>(p, st);
 }
 
 }  // namespace daq
