@@ -594,7 +594,7 @@ daq_status daq_mx4_dequantize(const uint8_t* src, int64_t rows, int64_t cols, vo
 daq_status daq_mx4_matmul_workspace(int64_t M, int64_t N, int64_t K, size_t* bytes);
 daq_status daq_mx4_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, daq_dtype dtype,
                           int64_t ldd, void* workspace, size_t workspace_bytes, void* stream);
-daq_status daq_mx4_linear_workspace(int64_t M, int64_t N, int64_t K, size_t* bytes);
+daq_status daq_mx4_linear_workspace(int64_t M, int64_t N, int64_t K, daq_dtype x_dtype, daq_round mode, size_t* bytes);
 daq_status daq_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, daq_dtype x_dtype, int64_t ldx, daq_round mode,
                           uint64_t seed, const uint8_t* W, void* Y, daq_dtype y_dtype, int64_t ldy, void* workspace,
                           size_t workspace_bytes, void* stream);

@@ -7,6 +7,7 @@ not been built -- there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -262,7 +263,7 @@ def lib():
         L.daq_mx4_dequantize.argtypes = [vp, i64, i64, vp, C.c_int, i64, vp]
         L.daq_mx4_matmul_workspace.argtypes = [i64, i64, i64, psz]
         L.daq_mx4_matmul.argtypes = [i64, i64, i64, vp, vp, vp, C.c_int, i64, vp, sz, vp]
-        L.daq_mx4_linear_workspace.argtypes = [i64, i64, i64, psz]
+        L.daq_mx4_linear_workspace.argtypes = [i64, i64, i64, C.c_int, C.c_int, psz]
         L.daq_mx4_linear.argtypes = [i64, i64, i64, vp, C.c_int, i64, C.c_int, u64, vp, vp, C.c_int, i64, vp, sz, vp]
         L.daq_ckpt8_save.argtypes = [vp, C.c_int, i64, i64, i32, i64, vp, vp]
         L.daq_ckpt8_restore.argtypes = [vp, i64, i64, i32, vp, C.c_int, i64, vp]
@@ -687,12 +688,14 @@ class Ckpt8:
     parts: int = 1
 
 
+@functools.lru_cache(maxsize=4096)
 def layout_mx4(rows: int, cols: int) -> Mx4Layout:
     L = Mx4Layout()
     _check(lib().daq_layout_mx4(rows, cols, C.byref(L)), "daq_layout_mx4")
     return L
 
 
+@functools.lru_cache(maxsize=4096)
 def layout_ckpt8(rows: int, cols: int, parts: int = 1) -> Ckpt8Layout:
     L = Ckpt8Layout()
     _check(lib().daq_layout_ckpt8(rows, cols, parts, C.byref(L)), "daq_layout_ckpt8")
@@ -761,17 +764,23 @@ def mx4_linear(x: torch.Tensor, w: Mx4, mode=ROUND_NEAREST, seed=0, dtype=None, 
         out = torch.empty((M, w.rows), dtype=dtype or x.dtype, device=x.device)
     assert _matrix(out) and tuple(out.shape) == (M, w.rows)
     if workspace is None:
-        workspace = _few_ws("daq_mx4_linear_workspace", x.device, M, w.rows, w.cols)
+        workspace = _few_ws("daq_mx4_linear_workspace", x.device, M, w.rows, w.cols, _DTYPES[x.dtype], mode)
     _check(lib().daq_mx4_linear(M, w.rows, w.cols, _ptr(x), _DTYPES[x.dtype], _ld(x), mode, seed, _ptr(w.buf), _ptr(out), _DTYPES[out.dtype],
                                 _ld(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_linear")
     return out
 
 
-def _few_ws(fn_name: str, device, *sizes) -> Optional[torch.Tensor]:
-    """The workspace a call of these sizes needs, None where it needs none."""
+@functools.lru_cache(maxsize=4096)
+def _few_ws_bytes(fn_name: str, *sizes) -> int:
     n = C.c_size_t(0)
     _check(getattr(lib(), fn_name)(*sizes, C.byref(n)), fn_name)
-    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+    return n.value
+
+
+def _few_ws(fn_name: str, device, *sizes) -> Optional[torch.Tensor]:
+    """The workspace a call of these sizes needs, None where it needs none."""
+    n = _few_ws_bytes(fn_name, *sizes)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
 def ckpt8_save(x: torch.Tensor, parts: int = 1, out: Optional[Ckpt8] = None, stream=None) -> Ckpt8:

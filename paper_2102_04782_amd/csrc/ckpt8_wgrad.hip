@@ -40,21 +40,36 @@ __device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uin
     if (!finite && x != x) hi |= 0x40;   // a NaN of low bits only
 }
 
-// Four columns of eight tokens, as words of two neighbouring columns, to the order of the tiles: 16 bytes a column.
-__device__ __forceinline__ void store_columns(uint8_t* to, const u32x2 (&v)[8]) {
+// Four columns of eight tokens a lane, as words of two neighbouring columns, to the order of the tiles, 16 bytes a column: through the
+// wave's share of LDS, so that every store of the wave is half a KiB in a row.  Pieces lie there in the order piece ^ piece / 8 % 4, which
+// keeps writes (every fourth piece) and reads off one another's banks.  to: the wave's 128 columns; col: the lane's first.
+__device__ __forceinline__ void store_columns(uint8_t* lds, uint8_t* to, int64_t block_bytes, int blocks, const u32x2 (&v)[8]) {
+    const int lane = threadIdx.x % kWave, half = lane / 32;
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         u32x4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             w[i] = __builtin_amdgcn_perm(v[2 * i + 1][c / 2], v[2 * i][c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
-        *reinterpret_cast<u32x4*>(to + c * 16) = w;
+        const int piece = half * 128 + (lane % 32) * 4 + c;
+        *reinterpret_cast<u32x4*>(lds + (piece ^ (piece / 8 & 3)) * 16) = w;
     }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int piece = half * 128 + k * 32 + lane % 32;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(lds + (piece ^ (piece / 8 & 3)) * 16);
+        if (k < blocks) *reinterpret_cast<u32x4*>(to + k * block_bytes + lane * 16) = w;
+    }
+    __builtin_amdgcn_wave_barrier();
 }
 
 // A wave takes 128 columns x 16 tokens of either operand, a lane four columns of eight tokens.
 template <typename T>
 __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
+    __shared__ __attribute__((aligned(16))) uint8_t shares[4][4096];
+    uint8_t* lds = shares[threadIdx.x / kWave];
     const int lane = threadIdx.x % kWave;
     int64_t wave = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
     const bool of_dy = wave < p.dy_waves;
@@ -63,10 +78,10 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
     const int blocks = of_dy ? p.n_blocks : p.k_blocks;
     const int wide = (blocks + 3) / 4;
     const int64_t step = wave / wide;
-    const int64_t col = (wave - step * wide) * 128 + (lane % 32) * 4;
-    if (col / 32 >= blocks) return;
+    const int b0 = (int)(wave - step * wide) * 4, nb = min(4, blocks - b0);     // row blocks of the tiles
+    const int64_t col = (int64_t)b0 * 32 + (lane % 32) * 4;
     const int64_t m0 = step * 16 + (lane / 32) * 8;
-    const int64_t at = (col / 32 * p.steps + step) * 1024 + (lane / 32) * 512 + (col % 32) * 16;
+    const int64_t block_bytes = (int64_t)p.steps * 1024 * (of_dy && sizeof(T) == 4 ? 3 : 1);
     if (of_dy) {
         const T* src = static_cast<const T*>(p.dy) + col;
         if constexpr (sizeof(T) == 2) {
@@ -85,7 +100,7 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
                     v[j] = u32x2{e[0] | (e[1] << 16), e[2] | (e[3] << 16)};
                 }
             }
-            store_columns(p.dy_tiles + at, v);
+            store_columns(lds, p.dy_tiles + b0 * block_bytes + step * 1024, block_bytes, nb, v);
         } else {
             u32x2 v[3][8];
 #pragma unroll
@@ -109,9 +124,9 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
             }
             // the three parts are stages of their own, one after the other, the smallest first: so the sums are long only in the last
             // third, and as exact as those of the leading bits alone
-            uint8_t* to = p.dy_tiles + (col / 32 * 3 * p.steps + step) * 1024 + (lane / 32) * 512 + (col % 32) * 16;
 #pragma unroll
-            for (int k = 0; k < 3; ++k) store_columns(to + (int64_t)(2 - k) * p.steps * 1024, v[k]);
+            for (int k = 0; k < 3; ++k)
+                store_columns(lds, p.dy_tiles + b0 * block_bytes + ((int64_t)(2 - k) * p.steps + step) * 1024, block_bytes, nb, v[k]);
         }
     } else {
         u32x2 v[8];
@@ -119,8 +134,9 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
         for (int j = 0; j < 8; ++j) {
             const bool in = m0 + j < p.M;
             const int64_t r = in ? m0 + j : 0;
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(p.codes + r * p.pitch + col);
-            const float s = in ? scale_of(p.scales[r * (p.pitch / kMxBlock) + col / 32]) : 0.0f;
+            const int64_t at = col < p.pitch ? col : 0;      // (columns behind the last block are not stored)
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(p.codes + r * p.pitch + at);
+            const float s = in ? scale_of(p.scales[r * (p.pitch / kMxBlock) + at / 32]) : 0.0f;
             float e[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) e[i] = in ? (float)(int8_t)(w >> (8 * i)) * s : 0.0f;
@@ -128,7 +144,7 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
             v[j] = u32x2{__builtin_amdgcn_perm(__float_as_uint(e[1]), __float_as_uint(e[0]), 0x07060302u),
                          __builtin_amdgcn_perm(__float_as_uint(e[3]), __float_as_uint(e[2]), 0x07060302u)};
         }
-        store_columns(p.x_tiles + at, v);
+        store_columns(lds, p.x_tiles + b0 * block_bytes + step * 1024, block_bytes, nb, v);
     }
 }
 
@@ -148,9 +164,9 @@ struct WgradArgs {
 
 // Tiles of 32 RB WR rows x 32 CB WC columns of dW, a workgroup each, for one part of the tokens.  Order of the workgroups as in the
 // 4-bit products; the parts of a tile are neighbours in it.
-template <int WR, int WC, int RB, int CB>
+template <int WR, int WC, int RB, int CB, int SLOTS>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
-    using Product = TileProduct<WR, WC, RB, CB, false>;
+    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int64_t b = (int64_t)(blockIdx.x % kXcd) * p.per_xcd + blockIdx.x / kXcd;
     const int64_t t = b / p.splits;
@@ -160,8 +176,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
     const int rest = (int)(t - band * 4 * p.tiles_k), high = min(4, p.tiles_n - (int)band * 4);
     const int tn = (int)band * 4 + rest % high, tk = rest / high;
     Product prod;
-    prod.run(p.dy, p.x, tn * WR * RB, tk * WC * CB, split * p.per_split, min(p.stages, (split + 1) * p.per_split), p.x_stages, lds,
-             lds + Product::kStageBytes);
+    prod.run(p.dy, p.x, tn * WR * RB, tk * WC * CB, split * p.per_split, min(p.stages, (split + 1) * p.per_split), p.x_stages, lds);
     const int wave = threadIdx.x / kWave;
     const int64_t n0 = ((int64_t)tn * WR + wave / WC) * RB * 32, k0 = ((int64_t)tk * WC + wave % WC) * CB * 32;
     float* base = p.splits > 1 ? p.part + split * p.N * p.pitch : p.dw;
@@ -200,15 +215,15 @@ __global__ __launch_bounds__(256) void k_ckpt8_wgrad_sum(const float* part, int 
         if (k + i < K) z[i] = accumulate ? z[i] + sum[i] : sum[i];
 }
 
-template <int WR, int WC, int RB, int CB>
+template <int WR, int WC, int RB, int CB, int SLOTS>
 daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
-    using Product = TileProduct<WR, WC, RB, CB, false>;
+    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS>;
     p.tiles_n = (int)ceil_div(p.dy.blocks, WR * RB);
     p.tiles_k = (int)ceil_div(p.x.blocks, WC * CB);
     const int64_t per = ceil_div((int64_t)p.tiles_n * p.tiles_k * p.splits, kXcd);
     if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
     p.per_xcd = (int)per;
-    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB>;
+    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, SLOTS>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("ckpt8_wgrad", st, hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcd)), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
     return DAQ_OK;
@@ -227,13 +242,17 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype) {
     w.k_blocks = (int)ceil_div(K, 32);
     w.steps = (int)(ceil_div(M, kStageM) * kStageSteps);
     w.parts = dtype == DAQ_BF16 ? 1 : 3;
+    // The form and the parts of the tokens that take the least time by what was measured of them (us): a workgroup to a CU, 6 + 1.5 a
+    // stage for tiles of 256 x 256, 4 + 0.62 for tiles of 128 x 128 with four stages in LDS; several parts: 3 for their sum, and each
+    // part's results written and read at 4 TB/s.  E.g. 2048 x 2048 x 2048 38.8 us on small tiles, 62 on large ones, 52 on small ones in
+    // two parts; 16384 x 256 x 256 from fp32 345 us in one part, 52 in sixteen.
     const int stages = w.steps / kStageSteps * w.parts;
-    const int64_t big = ceil_div(w.n_blocks, 8) * ceil_div(w.k_blocks, 8), small = ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4);
-    w.big = big >= 128;
-    const int64_t tiles = w.big ? big : small, slots = w.big ? 256 : 512;
-    w.splits = 1;
-    while (tiles * w.splits * 2 <= slots && w.splits < stages / 2) w.splits *= 2;
-    w.splits = std::min(w.splits, stages);
+    const double t_part = (double)N * K * 8 / 4e6;
+    SplitModel small{stages, ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4), stages, 0.62, 4.0, 0.0, 3.0, t_part};
+    SplitModel big{stages, ceil_div(w.n_blocks, 8) * ceil_div(w.k_blocks, 8), stages, 1.5, 6.0, 0.0, 3.0, t_part};
+    const int s_small = cheapest_split(small), s_big = cheapest_split(big);
+    w.big = big.cost(s_big) < small.cost(s_small);
+    w.splits = w.big ? s_big : s_small;
     w.per_split = (int)ceil_div(stages, w.splits);
     w.splits = (int)ceil_div(stages, w.per_split);
     w.pitch = round_up(K, 4);
@@ -308,7 +327,7 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     p.accumulate = accumulate;
     p.part = reinterpret_cast<float*>(ws + w.off_part);
     p.pitch = w.pitch;
-    rc = w.big ? launch_wgrad<2, 4, 4, 2>(p, st) : launch_wgrad<2, 2, 2, 2>(p, st);
+    rc = w.big ? launch_wgrad<2, 4, 4, 2, 2>(p, st) : launch_wgrad<2, 2, 2, 2, 4>(p, st);
     if (rc != DAQ_OK || w.splits == 1) return rc;
     DAQ_LAUNCH("ckpt8_wgrad_sum", st,
                hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, p.part, w.splits, N, K, w.pitch, dW, ldw, accumulate));

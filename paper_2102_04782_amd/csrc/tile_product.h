@@ -48,27 +48,32 @@ __device__ __forceinline__ void words_to_lds(__amdgpu_buffer_rsrc_t src, uint32_
 }
 
 // The results of a workgroup of WR x WC waves, each RB x CB tiles of 32 x 32: rows from row block `rb` of `r` on, columns from row block
-// `cb` of `c` on, summed over the stages s0 .. s1 - 1.  A stage of both operands is asked for while the one before it is multiplied,
+// `cb` of `c` on, summed over the stages s0 .. s1 - 1.  A stage of both operands is asked for while the SLOTS - 1 before it are multiplied,
 // straight into LDS, and the fragments of a step while the step before is multiplied, the first step of a stage among them:
 // the barrier stands before the last step's products, when that step's fragments are in registers already.
 // c_wrap: stages after which the second operand begins again.
-template <int WR, int WC, int RB, int CB, bool MX>
+template <int WR, int WC, int RB, int CB, bool MX, int SLOTS = 2>
 struct TileProduct {
     static constexpr int kWaves = WR * WC;
     static constexpr int kTiles = WR * RB + WC * CB;               // of a step
     static constexpr int kScales = MX ? kTiles * 256 : 0;          // bytes of a stage
     static constexpr int kStageBytes = kTiles * kStageSteps * 1024 + kScales;
-    static constexpr int kLdsBytes = 2 * kStageBytes;
+    static constexpr int kLdsBytes = SLOTS * kStageBytes;
     static constexpr int kShare = kTiles / kWaves;                    // operand row blocks that a wave fetches
+    static constexpr int kAsks = kShare * (kStageSteps + (MX ? 1 : 0));   // requests of a wave for a stage
 
+    static_assert(SLOTS == 2 || SLOTS == 4, "two or four stages in LDS");
     static_assert(kTiles % kWaves == 0, "every wave fetches the same number of row blocks");
 
     v16f acc[CB][RB];
 
-    // lds0, lds1: the two stages' places.  They are arguments so that the compiler knows them apart, and does not let a read of one
-    // wait for the requests into the other.
-    __device__ __forceinline__ void run(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, int c_wrap, uint8_t* __restrict__ lds0,
-                                        uint8_t* __restrict__ lds1) {
+    __device__ __forceinline__ void run(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, int c_wrap, uint8_t* lds) {
+        run_on(r, c, rb, cb, s0, s1, c_wrap, lds, lds + kStageBytes, lds + (SLOTS - 2) * kStageBytes, lds + (SLOTS - 1) * kStageBytes);
+    }
+    // lds0 ..: the stages' places (the last two are not used where there are two).  They are arguments so that the compiler knows them
+    // apart, and does not let a read of one wait for the requests into the others.
+    __device__ __forceinline__ void run_on(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, int c_wrap,
+                                           uint8_t* __restrict__ lds0, uint8_t* __restrict__ lds1, uint8_t* __restrict__ lds2, uint8_t* __restrict__ lds3) {
         const int lane = threadIdx.x % kWave;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const int wr = wave / WC, wc = wave % WC;
@@ -126,12 +131,17 @@ struct TileProduct {
 #pragma unroll
             for (int i = 0; i < RB; ++i) acc[j][i] = v16f{};
         if (s0 >= s1) return;
+        const int last = s1 - 1;
         ask(s0, lds0);
-        ask(min(s0 + 1, s1 - 1), lds1);
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kShare * (kStageSteps + (MX ? 1 : 0))) : "memory");
+        ask(min(s0 + 1, last), lds1);
+        if constexpr (SLOTS == 4) {
+            ask(min(s0 + 2, last), lds2);
+            ask(min(s0 + 3, last), lds3);
+        }
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * kAsks) : "memory");
         __builtin_amdgcn_s_barrier();
         read(lds0, 0, 0, 0);
-        // two stages a round, so that every register set has a number known here
+        // as many stages a round as there are places, so that these and the register sets have numbers known here
         auto stage = [&](int s, uint8_t* here, uint8_t* next, int sset) {
             read(here, 1, 1, sset);
             multiply(std::integral_constant<int, 0>{}, 0, sset);
@@ -142,19 +152,31 @@ struct TileProduct {
             read(here, 3, 1, sset);
             multiply(std::integral_constant<int, 2>{}, 0, sset);
             __builtin_amdgcn_sched_barrier(0);
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the next stage has landed, this one is read out
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");   // the next stage has landed, this one is read out
             __builtin_amdgcn_s_barrier();
             read(next, 0, 0, sset ^ 1);
-            ask(min(s + 2, s1 - 1), here);
+            ask(min(s + SLOTS, last), here);
             multiply(std::integral_constant<int, 3>{}, 1, sset);
             __builtin_amdgcn_sched_barrier(0);
         };
         int s = s0;
-        for (; s + 1 < s1; s += 2) {
-            stage(s, lds0, lds1, 0);
-            stage(s + 1, lds1, lds0, 1);
+        if constexpr (SLOTS == 2) {
+            for (; s + 1 < s1; s += 2) {
+                stage(s, lds0, lds1, 0);
+                stage(s + 1, lds1, lds0, 1);
+            }
+            if (s < s1) stage(s, lds0, lds1, 0);
+        } else {
+            for (; s + 3 < s1; s += 4) {
+                stage(s, lds0, lds1, 0);
+                stage(s + 1, lds1, lds2, 1);
+                stage(s + 2, lds2, lds3, 0);
+                stage(s + 3, lds3, lds0, 1);
+            }
+            if (s < s1) stage(s, lds0, lds1, 0);
+            if (s + 1 < s1) stage(s + 1, lds1, lds2, 1);
+            if (s + 2 < s1) stage(s + 2, lds2, lds3, 0);
         }
-        if (s < s1) stage(s, lds0, lds1, 0);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the requests past the end have landed before LDS is put to other use
     }
 

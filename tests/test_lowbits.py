@@ -105,7 +105,9 @@ def test_refusals_come_before_any_launch():
     assert L.daq_mx4_matmul_workspace(4, 0, 4, C.byref(n)) == L.daq_mx4_matmul_workspace(4, 4, 4, None) == INV
     li = lambda M=64, N=8, K=40, X=a, xd=0, ldx=40, mode=0, W=a, Y=a, yd=0, ldy=8, ws=a, wn=1 << 30: L.daq_mx4_linear(M, N, K, X, xd, ldx, mode, 0, W, Y, yd, ldy, ws, wn, None)
     assert li(X=None) == li(W=None) == li(Y=None) == li(ldx=39) == li(ldy=7) == li(xd=2) == li(yd=2) == li(mode=3) == li(X=odd) == li(N=0) == INV
-    assert L.daq_mx4_linear_workspace(4096, 4096, 4096, C.byref(n)) == daq.OK and n.value >= 4096 * 4096 // 2
+    assert L.daq_mx4_linear_workspace(4, 4, 4, 2, 0, C.byref(n)) == L.daq_mx4_linear_workspace(4, 4, 4, 0, 2, C.byref(n)) == INV
+    assert L.daq_mx4_linear_workspace(1, 8192, 2048, 1, 0, C.byref(n)) == daq.OK and n.value == 0          # one token: one launch
+    assert L.daq_mx4_linear_workspace(4096, 4096, 4096, 0, 0, C.byref(n)) == daq.OK and n.value >= 4096 * 4096 // 2
     big = dict(M=4096, N=4096, K=4096, ldx=4096, ldy=4096)
     assert li(ws=None, wn=0, **big) == li(ws=a, wn=n.value - 1, **big) == li(ws=a + 16, **big) == WS and li(M=0) == daq.OK
     for fn in (lambda x=a, dt=0, r=4, c=40, p=2, ld=80, k=a: L.daq_ckpt8_save(x, dt, r, c, p, ld, k, None),
