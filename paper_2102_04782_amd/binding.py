@@ -702,13 +702,22 @@ def layout_ckpt8(rows: int, cols: int, parts: int = 1) -> Ckpt8Layout:
     return L
 
 
-def _matrix(t: torch.Tensor) -> bool:
-    """On the GPU, fp32 or bfloat16, two axes, elements of a row next to each other, rows that do not overlap."""
-    return t.is_cuda and t.dtype in _DTYPES and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])
+def _matrix(t: torch.Tensor):
+    """(rows, cols, row stride, dtype code) of a matrix on the GPU: fp32 or bfloat16, elements of a row next to each other, rows that do
+    not overlap."""
+    assert t.is_cuda and t.dim() == 2
+    (rows, cols), (ld, one) = t.shape, t.stride()
+    assert (one == 1 or cols <= 1) and (ld >= cols or rows <= 1)
+    return rows, cols, ld if rows > 1 else max(cols, 1), _DTYPES[t.dtype]
 
 
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype, like: torch.Tensor):
+    """(result, row stride, dtype code): ``out``, checked, or a new matrix on the device of ``like``."""
+    if out is None:
+        return torch.empty((rows, cols), dtype=dtype, device=like.device), max(cols, 1), _DTYPES[dtype]
+    r, c, ld, code = _matrix(out)
+    assert (r, c) == (rows, cols) and (dtype is None or out.dtype == dtype)
+    return out, ld, code
 
 
 def alloc_mx4(rows: int, cols: int, device="cuda") -> Mx4:
@@ -721,52 +730,46 @@ def alloc_ckpt8(rows: int, cols: int, parts: int = 1, device="cuda") -> Ckpt8:
 
 def mx4_quantize(x: torch.Tensor, transpose: bool = False, mode=ROUND_NEAREST, seed=0, out: Optional[Mx4] = None, stream=None) -> Mx4:
     """daq_mx4_quantize: ``x`` [rows, cols] with blocks along its rows, or (``transpose``) its transpose, with blocks along its columns."""
-    assert _matrix(x)
-    rows, cols = x.shape
-    shape = (cols, rows) if transpose else (rows, cols)
+    rows, cols, ld, code = _matrix(x)
+    r, c = (cols, rows) if transpose else (rows, cols)
     if out is None:
-        out = alloc_mx4(*shape, x.device)
-    assert (out.rows, out.cols) == shape
-    _check(lib().daq_mx4_quantize(_ptr(x), _DTYPES[x.dtype], rows, cols, _ld(x), int(transpose), mode, seed, _ptr(out.buf), _stream(stream)),
+        out = alloc_mx4(r, c, x.device)
+    assert out.rows == r and out.cols == c
+    _check(lib().daq_mx4_quantize(x.data_ptr(), code, rows, cols, ld, int(transpose), mode, seed, out.buf.data_ptr(), _stream(stream)),
            "daq_mx4_quantize")
     return out
 
 
 def mx4_dequantize(q: Mx4, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """daq_mx4_dequantize: the values that ``q`` holds, exact in either type."""
-    if out is None:
-        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.buf.device)
-    assert _matrix(out) and tuple(out.shape) == (q.rows, q.cols)
-    _check(lib().daq_mx4_dequantize(_ptr(q.buf), q.rows, q.cols, _ptr(out), _DTYPES[out.dtype], _ld(out), _stream(stream)), "daq_mx4_dequantize")
+    """daq_mx4_dequantize: the values that ``q`` holds, exact in either type (that of ``out`` where it is given)."""
+    out, ld, code = _result(out, q.rows, q.cols, dtype if out is None else None, q.buf)
+    _check(lib().daq_mx4_dequantize(q.buf.data_ptr(), q.rows, q.cols, out.data_ptr(), code, ld, _stream(stream)), "daq_mx4_dequantize")
     return out
 
 
 def mx4_matmul(a: Mx4, b: Mx4, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
-    """daq_mx4_matmul: a b^T, [a.rows, b.rows]."""
+    """daq_mx4_matmul: a b^T, [a.rows, b.rows], of ``dtype`` (or that of ``out``)."""
     assert a.cols == b.cols
-    if out is None:
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=b.buf.device)
-    assert _matrix(out) and tuple(out.shape) == (a.rows, b.rows)
+    out, ld, code = _result(out, a.rows, b.rows, dtype if out is None else None, b.buf)
     if workspace is None:
         workspace = _few_ws("daq_mx4_matmul_workspace", b.buf.device, a.rows, b.rows, a.cols)
-    _check(lib().daq_mx4_matmul(a.rows, b.rows, a.cols, _ptr(a.buf), _ptr(b.buf), _ptr(out), _DTYPES[out.dtype], _ld(out), _ptr(workspace),
+    _check(lib().daq_mx4_matmul(a.rows, b.rows, a.cols, a.buf.data_ptr(), b.buf.data_ptr(), out.data_ptr(), code, ld, _ptr(workspace),
                                 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_matmul")
     return out
 
 
 def mx4_linear(x: torch.Tensor, w: Mx4, mode=ROUND_NEAREST, seed=0, dtype=None, out: Optional[torch.Tensor] = None,
                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """daq_mx4_linear: x w^T with ``x`` [M, w.cols] quantized in the call; the result is of ``dtype`` (that of ``x`` if not given)."""
-    assert _matrix(x) and x.shape[1] == w.cols
-    M = x.shape[0]
-    if out is None:
-        out = torch.empty((M, w.rows), dtype=dtype or x.dtype, device=x.device)
-    assert _matrix(out) and tuple(out.shape) == (M, w.rows)
+    """daq_mx4_linear: x w^T with ``x`` [M, w.cols] quantized in the call; the result is of ``dtype`` (that of ``out``, or of ``x``)."""
+    M, K, ldx, x_code = _matrix(x)
+    N = w.rows
+    assert K == w.cols
+    out, ldy, y_code = _result(out, M, N, (dtype or x.dtype) if out is None else dtype, x)
     if workspace is None:
-        workspace = _few_ws("daq_mx4_linear_workspace", x.device, M, w.rows, w.cols, _DTYPES[x.dtype], mode)
-    _check(lib().daq_mx4_linear(M, w.rows, w.cols, _ptr(x), _DTYPES[x.dtype], _ld(x), mode, seed, _ptr(w.buf), _ptr(out), _DTYPES[out.dtype],
-                                _ld(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_linear")
+        workspace = _few_ws("daq_mx4_linear_workspace", x.device, M, N, K, x_code, mode)
+    _check(lib().daq_mx4_linear(M, N, K, x.data_ptr(), x_code, ldx, mode, seed, w.buf.data_ptr(), out.data_ptr(), y_code, ldy, _ptr(workspace),
+                                0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_linear")
     return out
 
 
@@ -785,39 +788,35 @@ def _few_ws(fn_name: str, device, *sizes) -> Optional[torch.Tensor]:
 
 def ckpt8_save(x: torch.Tensor, parts: int = 1, out: Optional[Ckpt8] = None, stream=None) -> Ckpt8:
     """daq_ckpt8_save: ``x`` [rows, parts * cols] in 8 bits."""
-    assert _matrix(x) and x.shape[1] % parts == 0
-    rows, cols = x.shape[0], x.shape[1] // parts
+    rows, width, ld, code = _matrix(x)
+    assert width % parts == 0
+    cols = width // parts
     if out is None:
         out = alloc_ckpt8(rows, cols, parts, x.device)
-    assert (out.rows, out.cols, out.parts) == (rows, cols, parts)
-    _check(lib().daq_ckpt8_save(_ptr(x), _DTYPES[x.dtype], rows, cols, parts, _ld(x), _ptr(out.buf), _stream(stream)), "daq_ckpt8_save")
+    assert out.rows == rows and out.cols == cols and out.parts == parts
+    _check(lib().daq_ckpt8_save(x.data_ptr(), code, rows, cols, parts, ld, out.buf.data_ptr(), _stream(stream)), "daq_ckpt8_save")
     return out
 
 
 def ckpt8_restore(c: Ckpt8, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """daq_ckpt8_restore: the values that ``c`` holds, exact in either type."""
-    shape = (c.rows, c.parts * c.cols)
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=c.buf.device)
-    assert _matrix(out) and tuple(out.shape) == shape
-    _check(lib().daq_ckpt8_restore(_ptr(c.buf), c.rows, c.cols, c.parts, _ptr(out), _DTYPES[out.dtype], _ld(out), _stream(stream)),
-           "daq_ckpt8_restore")
+    """daq_ckpt8_restore: the values that ``c`` holds, exact in either type (that of ``out`` where it is given)."""
+    out, ld, code = _result(out, c.rows, c.parts * c.cols, dtype if out is None else None, c.buf)
+    _check(lib().daq_ckpt8_restore(c.buf.data_ptr(), c.rows, c.cols, c.parts, out.data_ptr(), code, ld, _stream(stream)), "daq_ckpt8_restore")
     return out
 
 
 def ckpt8_act_forward(h: torch.Tensor, act: int, gated: bool = False, out: Optional[torch.Tensor] = None, ckpt: Optional[Ckpt8] = None,
                       stream=None):
     """daq_ckpt8_act_forward: (y, the checkpoint of ``h``).  ``h`` [rows, cols], or [rows, 2 * cols] = gate | up when ``gated``."""
-    assert _matrix(h) and (not gated or h.shape[1] % 2 == 0)
+    rows, width, ldh, code = _matrix(h)
     parts = 2 if gated else 1
-    rows, cols = h.shape[0], h.shape[1] // parts
-    if out is None:
-        out = torch.empty((rows, cols), dtype=h.dtype, device=h.device)
-    assert _matrix(out) and out.dtype == h.dtype and tuple(out.shape) == (rows, cols)
+    assert width % parts == 0
+    cols = width // parts
+    out, ldy, _ = _result(out, rows, cols, h.dtype, h)
     if ckpt is None:
         ckpt = alloc_ckpt8(rows, cols, parts, h.device)
-    assert (ckpt.rows, ckpt.cols, ckpt.parts) == (rows, cols, parts)
-    _check(lib().daq_ckpt8_act_forward(_ptr(h), _DTYPES[h.dtype], rows, cols, _ld(h), act, int(gated), _ptr(out), _ld(out), _ptr(ckpt.buf),
+    assert ckpt.rows == rows and ckpt.cols == cols and ckpt.parts == parts
+    _check(lib().daq_ckpt8_act_forward(h.data_ptr(), code, rows, cols, ldh, act, int(gated), out.data_ptr(), ldy, ckpt.buf.data_ptr(),
                                        _stream(stream)), "daq_ckpt8_act_forward")
     return out, ckpt
 
@@ -826,30 +825,24 @@ def ckpt8_act_backward(dy: torch.Tensor, ckpt: Ckpt8, act: int, out: Optional[to
                        stream=None) -> torch.Tensor:
     """daq_ckpt8_act_backward: the gradient of the layer's input, of the type of ``dy``; ``y_ckpt`` receives the layer's output, recomputed, in
     8 bits."""
-    assert _matrix(dy) and tuple(dy.shape) == (ckpt.rows, ckpt.cols)
-    shape = (ckpt.rows, ckpt.parts * ckpt.cols)
-    if out is None:
-        out = torch.empty(shape, dtype=dy.dtype, device=dy.device)
-    assert _matrix(out) and out.dtype == dy.dtype and tuple(out.shape) == shape
-    assert y_ckpt is None or (y_ckpt.rows, y_ckpt.cols, y_ckpt.parts) == (ckpt.rows, ckpt.cols, 1)
-    _check(lib().daq_ckpt8_act_backward(_ptr(dy), _DTYPES[dy.dtype], ckpt.rows, ckpt.cols, _ld(dy), _ptr(ckpt.buf), act, int(ckpt.parts == 2),
-                                        _ptr(out), _ld(out), None if y_ckpt is None else _ptr(y_ckpt.buf), _stream(stream)),
-           "daq_ckpt8_act_backward")
+    rows, cols, lddy, code = _matrix(dy)
+    assert rows == ckpt.rows and cols == ckpt.cols
+    out, lddh, _ = _result(out, rows, ckpt.parts * cols, dy.dtype, dy)
+    assert y_ckpt is None or (y_ckpt.rows, y_ckpt.cols, y_ckpt.parts) == (rows, cols, 1)
+    _check(lib().daq_ckpt8_act_backward(dy.data_ptr(), code, rows, cols, lddy, ckpt.buf.data_ptr(), act, int(ckpt.parts == 2), out.data_ptr(), lddh,
+                                        None if y_ckpt is None else y_ckpt.buf.data_ptr(), _stream(stream)), "daq_ckpt8_act_backward")
     return out
 
 
 def ckpt8_weight_grad(dy: torch.Tensor, x: Ckpt8, out: Optional[torch.Tensor] = None, accumulate: bool = False,
                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """daq_ckpt8_weight_grad: dy^T x^, fp32 [N, K]; ``accumulate`` adds it to ``out``."""
-    assert _matrix(dy) and x.parts == 1 and dy.shape[0] == x.rows
-    N = dy.shape[1]
-    assert out is not None or not accumulate
-    if out is None:
-        out = torch.empty((N, x.cols), dtype=torch.float32, device=dy.device)
-    assert _matrix(out) and out.dtype == torch.float32 and tuple(out.shape) == (N, x.cols)
+    M, N, lddy, code = _matrix(dy)
+    assert x.parts == 1 and M == x.rows and (out is not None or not accumulate)
+    out, ldw, _ = _result(out, N, x.cols, torch.float32, dy)
     if workspace is None:
-        workspace = _few_ws("daq_ckpt8_weight_grad_workspace", dy.device, x.rows, N, x.cols, _DTYPES[dy.dtype])
-    _check(lib().daq_ckpt8_weight_grad(x.rows, N, x.cols, _ptr(dy), _DTYPES[dy.dtype], _ld(dy), _ptr(x.buf), _ptr(out), _ld(out), int(accumulate),
+        workspace = _few_ws("daq_ckpt8_weight_grad_workspace", dy.device, M, N, x.cols, code)
+    _check(lib().daq_ckpt8_weight_grad(M, N, x.cols, dy.data_ptr(), code, lddy, x.buf.data_ptr(), out.data_ptr(), ldw, int(accumulate),
                                        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_ckpt8_weight_grad")
     return out
 
