@@ -141,23 +141,34 @@ struct TileProduct {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * kAsks) : "memory");
         __builtin_amdgcn_s_barrier();
         read(lds0, 0, 0, 0);
+        // The reads of a step stand between the products of the step before, one each, from its beginning on: left to itself the compiler
+        // moves them behind the last one, where every wave then waits for them.
+        auto interleave = [&] {
+#pragma unroll
+            for (int i = 0; i < RB + CB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, RB * CB, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
         // as many stages a round as there are places, so that these and the register sets have numbers known here
         auto stage = [&](int s, uint8_t* here, uint8_t* next, int sset) {
             read(here, 1, 1, sset);
             multiply(std::integral_constant<int, 0>{}, 0, sset);
-            __builtin_amdgcn_sched_barrier(0);
+            interleave();
             read(here, 2, 0, sset);
             multiply(std::integral_constant<int, 1>{}, 1, sset);
-            __builtin_amdgcn_sched_barrier(0);
+            interleave();
             read(here, 3, 1, sset);
             multiply(std::integral_constant<int, 2>{}, 0, sset);
-            __builtin_amdgcn_sched_barrier(0);
+            interleave();
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");   // the next stage has landed, this one is read out
             __builtin_amdgcn_s_barrier();
             read(next, 0, 0, sset ^ 1);
             ask(min(s + SLOTS, last), here);
             multiply(std::integral_constant<int, 3>{}, 1, sset);
-            __builtin_amdgcn_sched_barrier(0);
+            interleave();
         };
         int s = s0;
         if constexpr (SLOTS == 2) {
