@@ -1,4 +1,6 @@
 // Matrices saved in 8 bits, and activation layers that keep their input so.
+#include <type_traits>
+
 #include "lowbits.h"
 
 namespace daq {
@@ -6,8 +8,14 @@ namespace daq {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kPer = 8;                        // elements of a thread; four neighbouring threads hold a block
+constexpr int kPer = 8;                         // elements of a thread; four neighbouring threads hold a block
 constexpr int kLanes = kMxBlock / kPer;
+
+// Matrices of 48 MiB and more pass the caches by (NT); the codes are read so too but written into them.  us with and without, bfloat16:
+// 32768 x 8192 saved and restored 256 and 316; gated, 16384 x 8192, forward and backward 335 and 432 (with the codes' stores past the caches
+// as well 281 and 371).  Between a producer and a consumer of the matrices, gated of 34 MB 64.7 and 62.3 for the whole, 67 MB 114 and
+// 116, 134 MB 214 and 228, 268 MB 429 and 473.
+constexpr int64_t kPassBytes = 2 * kStreamBytes;
 
 // How the rows of a launch are dealt out: `tpr` threads (a power of two, at most a workgroup) to a row, several rows to a workgroup
 // where they are short, several workgroups to a row (blockIdx.y) where they are long.
@@ -34,11 +42,13 @@ bool rows_grid(int64_t rows, int64_t pitch, Rows& r, dim3& grid) {
 }
 
 // kPer elements from column c on, as fp32; those behind the last column are zero.
+template <bool NT>
 __device__ __forceinline__ void load_unit(const float* p, int64_t left, float (&v)[kPer]) {
     if (left >= kPer) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const u32x4_a4 q = *reinterpret_cast<const u32x4_a4*>(p + 4 * i);
+        for (int i = 0; i < kPer / 4; ++i) {
+            const u32x4_a4* at = reinterpret_cast<const u32x4_a4*>(p + 4 * i);
+            const u32x4_a4 q = NT ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[4 * i + j] = bits_as<float>(q[j]);
         }
@@ -47,38 +57,57 @@ __device__ __forceinline__ void load_unit(const float* p, int64_t left, float (&
         for (int i = 0; i < kPer; ++i) v[i] = i < left ? p[i] : 0.0f;
     }
 }
+template <bool NT>
 __device__ __forceinline__ void load_unit(const uint16_t* p, int64_t left, float (&v)[kPer]) {
     if (left >= kPer) {
-        const u32x4_a2 q = *reinterpret_cast<const u32x4_a2*>(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = bf16_lo(q[i]);
-            v[2 * i + 1] = bf16_hi(q[i]);
+        for (int k = 0; k < kPer / 8; ++k) {
+            const u32x4_a2* at = reinterpret_cast<const u32x4_a2*>(p + 8 * k);
+            const u32x4_a2 q = NT ? __builtin_nontemporal_load(at) : *at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[8 * k + 2 * i] = bf16_lo(q[i]);
+                v[8 * k + 2 * i + 1] = bf16_hi(q[i]);
+            }
         }
     } else {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) v[i] = i < left ? bits_as<float>((uint32_t)p[i] << 16) : 0.0f;
     }
 }
+template <bool NT>
 __device__ __forceinline__ void store_unit(float* p, int64_t left, const float (&v)[kPer]) {
     if (left >= kPer) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<u32x4_a4*>(p + 4 * i) = u32x4_a4{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+        for (int i = 0; i < kPer / 4; ++i) {
+            const u32x4_a4 q = {__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+            u32x4_a4* at = reinterpret_cast<u32x4_a4*>(p + 4 * i);
+            if constexpr (NT) __builtin_nontemporal_store(q, at);
+            else *at = q;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
             if (i < left) p[i] = v[i];
     }
 }
+template <bool NT>
 __device__ __forceinline__ void store_unit(uint16_t* p, int64_t left, const float (&v)[kPer]) {
-    const u32x4_a2 q = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    uint32_t w[kPer / 2];
+#pragma unroll
+    for (int i = 0; i < kPer / 2; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
     if (left >= kPer) {
-        *reinterpret_cast<u32x4_a2*>(p) = q;
+#pragma unroll
+        for (int i = 0; i < kPer / 8; ++i) {
+            const u32x4_a2 q = {w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+            u32x4_a2* at = reinterpret_cast<u32x4_a2*>(p + 8 * i);
+            if constexpr (NT) __builtin_nontemporal_store(q, at);
+            else *at = q;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
-            if (i < left) p[i] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
+            if (i < left) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
     }
 }
 
@@ -112,13 +141,15 @@ __device__ __forceinline__ void save_unit(const Saved& to, int64_t part_row, int
     }
     u32x2 w;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kPer / 4; ++i)
         w[i] = (c[4 * i] & 255u) | ((c[4 * i + 1] & 255u) << 8) | ((c[4 * i + 2] & 255u) << 16) | (c[4 * i + 3] << 24);
     *reinterpret_cast<u32x2*>(to.code(part_row, unit)) = w;
     if (unit % kLanes == 0) *to.scale(part_row, unit) = (uint8_t)byte;
 }
+template <bool NT>
 __device__ __forceinline__ void read_unit(const Saved& from, int64_t part_row, int64_t unit, float (&v)[kPer]) {
-    const u32x2 w = *reinterpret_cast<const u32x2*>(from.code(part_row, unit));
+    const u32x2* at = reinterpret_cast<const u32x2*>(from.code(part_row, unit));
+    const u32x2 w = NT ? __builtin_nontemporal_load(at) : *at;
     const float s = scale_of(*from.scale(part_row, unit));
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * s;
@@ -133,24 +164,24 @@ struct SaveArgs {
 };
 
 // The parts are rows of their own here.
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(kBlock) void k_ckpt8_save(Rows rows, SaveArgs p) {
     int64_t row, unit;
     if (!rows.place(row, unit)) return;
     const int64_t r = p.parts == 1 ? row : row >> 1, part = p.parts == 1 ? 0 : row & 1, c = unit * kPer;
     float v[kPer];
-    load_unit(static_cast<const T*>(p.src) + r * p.ld + part * p.cols + c, p.cols - c, v);
+    load_unit<NT>(static_cast<const T*>(p.src) + r * p.ld + part * p.cols + c, p.cols - c, v);
     save_unit(p.ckpt, row, unit, v);
 }
 
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(kBlock) void k_ckpt8_restore(Rows rows, SaveArgs p) {
     int64_t row, unit;
     if (!rows.place(row, unit)) return;
     const int64_t r = p.parts == 1 ? row : row >> 1, part = p.parts == 1 ? 0 : row & 1, c = unit * kPer;
     float v[kPer];
-    read_unit(p.ckpt, row, unit, v);
-    store_unit(static_cast<T*>(p.dst) + r * p.ld + part * p.cols + c, p.cols - c, v);
+    read_unit<NT>(p.ckpt, row, unit, v);
+    store_unit<NT>(static_cast<T*>(p.dst) + r * p.ld + part * p.cols + c, p.cols - c, v);
 }
 
 // f(x), and f'(x) where `slope` is asked for.
@@ -175,34 +206,34 @@ struct ActArgs {
     Saved y;             // backward: y saved again, where asked for
 };
 
-template <typename T, int ACT, bool GATED>
+template <typename T, int ACT, bool GATED, bool NT>
 __global__ __launch_bounds__(kBlock) void k_ckpt8_act_forward(Rows rows, ActArgs p) {
     int64_t row, unit;
     if (!rows.place(row, unit)) return;
     const int64_t c = unit * kPer;
     const T* h = static_cast<const T*>(p.in) + row * p.ld_in + c;
     float g[kPer], u[kPer], y[kPer];
-    load_unit(h, p.cols - c, g);
-    if constexpr (GATED) load_unit(h + p.cols, p.cols - c, u);
+    load_unit<NT>(h, p.cols - c, g);
+    if constexpr (GATED) load_unit<NT>(h + p.cols, p.cols - c, u);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         y[i] = act_value(ACT, g[i], nullptr);
         if constexpr (GATED) y[i] *= u[i];
     }
-    store_unit(static_cast<T*>(p.out) + row * p.ld_out + c, p.cols - c, y);
+    store_unit<NT>(static_cast<T*>(p.out) + row * p.ld_out + c, p.cols - c, y);
     save_unit(p.ckpt, GATED ? 2 * row : row, unit, g);
     if constexpr (GATED) save_unit(p.ckpt, 2 * row + 1, unit, u);
 }
 
-template <typename T, int ACT, bool GATED, bool SAVE>
+template <typename T, int ACT, bool GATED, bool SAVE, bool NT>
 __global__ __launch_bounds__(kBlock) void k_ckpt8_act_backward(Rows rows, ActArgs p) {
     int64_t row, unit;
     if (!rows.place(row, unit)) return;
     const int64_t c = unit * kPer;
     float dy[kPer], g[kPer], u[kPer], y[kPer];
-    load_unit(static_cast<const T*>(p.in) + row * p.ld_in + c, p.cols - c, dy);
-    read_unit(p.ckpt, GATED ? 2 * row : row, unit, g);
-    if constexpr (GATED) read_unit(p.ckpt, 2 * row + 1, unit, u);
+    load_unit<NT>(static_cast<const T*>(p.in) + row * p.ld_in + c, p.cols - c, dy);
+    read_unit<NT>(p.ckpt, GATED ? 2 * row : row, unit, g);
+    if constexpr (GATED) read_unit<NT>(p.ckpt, 2 * row + 1, unit, u);
     float dg[kPer], du[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -218,8 +249,8 @@ __global__ __launch_bounds__(kBlock) void k_ckpt8_act_backward(Rows rows, ActArg
         }
     }
     T* dh = static_cast<T*>(p.out) + row * p.ld_out + c;
-    store_unit(dh, p.cols - c, dg);
-    if constexpr (GATED) store_unit(dh + p.cols, p.cols - c, du);
+    store_unit<NT>(dh, p.cols - c, dg);
+    if constexpr (GATED) store_unit<NT>(dh + p.cols, p.cols - c, du);
     if constexpr (SAVE) save_unit(p.y, row, unit, y);
 }
 
@@ -230,29 +261,29 @@ Saved saved_at(const uint8_t* ckpt, int64_t rows, int64_t cols, int parts) {
     return Saved{base, base + L.off_scales, L.pitch};
 }
 
-template <typename T, int ACT, bool GATED>
+template <typename T, int ACT, bool GATED, bool NT>
 daq_status act_backward(const Rows& rows, const dim3& grid, const ActArgs& p, hipStream_t st) {
     if (p.y.codes)
-        DAQ_LAUNCH("ckpt8_act_backward", st, hipLaunchKernelGGL((k_ckpt8_act_backward<T, ACT, GATED, true>), grid, dim3(kBlock), 0, st, rows, p));
+        DAQ_LAUNCH("ckpt8_act_backward", st, hipLaunchKernelGGL((k_ckpt8_act_backward<T, ACT, GATED, true, NT>), grid, dim3(kBlock), 0, st, rows, p));
     else
-        DAQ_LAUNCH("ckpt8_act_backward", st, hipLaunchKernelGGL((k_ckpt8_act_backward<T, ACT, GATED, false>), grid, dim3(kBlock), 0, st, rows, p));
+        DAQ_LAUNCH("ckpt8_act_backward", st, hipLaunchKernelGGL((k_ckpt8_act_backward<T, ACT, GATED, false, NT>), grid, dim3(kBlock), 0, st, rows, p));
     return DAQ_OK;
 }
-template <typename T, int ACT, bool GATED>
+template <typename T, int ACT, bool GATED, bool NT>
 daq_status act_forward(const Rows& rows, const dim3& grid, const ActArgs& p, hipStream_t st) {
-    DAQ_LAUNCH("ckpt8_act_forward", st, hipLaunchKernelGGL((k_ckpt8_act_forward<T, ACT, GATED>), grid, dim3(kBlock), 0, st, rows, p));
+    DAQ_LAUNCH("ckpt8_act_forward", st, hipLaunchKernelGGL((k_ckpt8_act_forward<T, ACT, GATED, NT>), grid, dim3(kBlock), 0, st, rows, p));
     return DAQ_OK;
 }
-// One of the eight instances of a kernel.
-#define DAQ_ACT_PICK(FN, dtype, act, gated, ...)                                                             \
-    ((dtype) == DAQ_BF16 ? ((act) == DAQ_ACT_SILU ? ((gated) ? FN<uint16_t, DAQ_ACT_SILU, true>(__VA_ARGS__)  \
-                                                             : FN<uint16_t, DAQ_ACT_SILU, false>(__VA_ARGS__)) \
-                                                  : ((gated) ? FN<uint16_t, DAQ_ACT_GELU, true>(__VA_ARGS__)  \
-                                                             : FN<uint16_t, DAQ_ACT_GELU, false>(__VA_ARGS__))) \
-                         : ((act) == DAQ_ACT_SILU ? ((gated) ? FN<float, DAQ_ACT_SILU, true>(__VA_ARGS__)     \
-                                                             : FN<float, DAQ_ACT_SILU, false>(__VA_ARGS__))   \
-                                                  : ((gated) ? FN<float, DAQ_ACT_GELU, true>(__VA_ARGS__)     \
-                                                             : FN<float, DAQ_ACT_GELU, false>(__VA_ARGS__))))
+// f(type, act, gated, streaming) with one of the sixteen combinations as constants.
+template <typename F>
+daq_status act_pick(int dtype, int act, bool gated, bool nt, F f) {
+    auto with_nt = [&](auto t, auto a, auto g) { return nt ? f(t, a, g, std::true_type{}) : f(t, a, g, std::false_type{}); };
+    auto with_gate = [&](auto t, auto a) { return gated ? with_nt(t, a, std::true_type{}) : with_nt(t, a, std::false_type{}); };
+    auto with_act = [&](auto t) {
+        return act == DAQ_ACT_SILU ? with_gate(t, std::integral_constant<int, DAQ_ACT_SILU>{}) : with_gate(t, std::integral_constant<int, DAQ_ACT_GELU>{});
+    };
+    return dtype == DAQ_BF16 ? with_act(uint16_t{}) : with_act(float{});
+}
 
 // The sizes of a matrix of `parts` parts.
 daq_status parts_size(int64_t rows, int64_t cols, int parts) {
@@ -293,14 +324,16 @@ static daq_status save_or_restore(bool save, const void* src, void* dst, int dty
     Rows r;
     dim3 grid;
     if (!rows_grid(rows * parts, p.ckpt.pitch, r, grid)) return DAQ_ERR_UNSUPPORTED;
-    if (save) {
-        if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_save", st, hipLaunchKernelGGL(k_ckpt8_save<uint16_t>, grid, dim3(kBlock), 0, st, r, p));
-        else DAQ_LAUNCH("ckpt8_save", st, hipLaunchKernelGGL(k_ckpt8_save<float>, grid, dim3(kBlock), 0, st, r, p));
-    } else {
-        if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_restore", st, hipLaunchKernelGGL(k_ckpt8_restore<uint16_t>, grid, dim3(kBlock), 0, st, r, p));
-        else DAQ_LAUNCH("ckpt8_restore", st, hipLaunchKernelGGL(k_ckpt8_restore<float>, grid, dim3(kBlock), 0, st, r, p));
-    }
-    return DAQ_OK;
+    auto launch = [&](auto t, auto n) -> daq_status {
+        using T = decltype(t);
+        constexpr bool NT = decltype(n)::value;
+        if (save) DAQ_LAUNCH("ckpt8_save", st, hipLaunchKernelGGL((k_ckpt8_save<T, NT>), grid, dim3(kBlock), 0, st, r, p));
+        else DAQ_LAUNCH("ckpt8_restore", st, hipLaunchKernelGGL((k_ckpt8_restore<T, NT>), grid, dim3(kBlock), 0, st, r, p));
+        return DAQ_OK;
+    };
+    const bool nt = rows * cols * parts * dtype_size(dtype) >= kPassBytes;
+    if (dtype == DAQ_BF16) return nt ? launch(uint16_t{}, std::true_type{}) : launch(uint16_t{}, std::false_type{});
+    return nt ? launch(float{}, std::true_type{}) : launch(float{}, std::false_type{});
 }
 
 extern "C" daq_status daq_ckpt8_save(const void* src, daq_dtype dtype, int64_t rows, int64_t cols, int32_t parts, int64_t ld,
@@ -325,7 +358,10 @@ extern "C" daq_status daq_ckpt8_act_forward(const void* h, daq_dtype dtype, int6
     Rows r;
     dim3 grid;
     if (!rows_grid(rows, p.ckpt.pitch, r, grid)) return DAQ_ERR_UNSUPPORTED;
-    return DAQ_ACT_PICK(act_forward, dtype, act, gated, r, grid, p, (hipStream_t)stream);
+    const bool nt = rows * cols * parts * dtype_size(dtype) >= kPassBytes;
+    return act_pick(dtype, act, gated != 0, nt, [&](auto t, auto a, auto g, auto n) {
+        return act_forward<decltype(t), decltype(a)::value, decltype(g)::value, decltype(n)::value>(r, grid, p, (hipStream_t)stream);
+    });
 }
 
 extern "C" daq_status daq_ckpt8_act_backward(const void* dy, daq_dtype dtype, int64_t rows, int64_t cols, int64_t lddy, const uint8_t* ckpt,
@@ -341,5 +377,8 @@ extern "C" daq_status daq_ckpt8_act_backward(const void* dy, daq_dtype dtype, in
     Rows r;
     dim3 grid;
     if (!rows_grid(rows, p.ckpt.pitch, r, grid)) return DAQ_ERR_UNSUPPORTED;
-    return DAQ_ACT_PICK(act_backward, dtype, act, gated, r, grid, p, (hipStream_t)stream);
+    const bool nt = rows * cols * parts * dtype_size(dtype) >= kPassBytes;
+    return act_pick(dtype, act, gated != 0, nt, [&](auto t, auto a, auto g, auto n) {
+        return act_backward<decltype(t), decltype(a)::value, decltype(g)::value, decltype(n)::value>(r, grid, p, (hipStream_t)stream);
+    });
 }
