@@ -145,67 +145,57 @@ struct ValuesArgs {
     int64_t ld;
 };
 
-// Workgroups, waves and lanes as in k_mx4_rows.
+// Workgroups and waves as in k_mx4_rows; a lane takes a piece of 16 bytes of a row of dst, so that every store of the wave fills whole
+// lines: 8 rows of 64 bfloat16, 4 rows of 64 fp32 at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void k_mx4_values(ValuesArgs p) {
+    constexpr int kPiece = 16 / sizeof(T), kAcross = 64 / kPiece, kRows = kWave / kAcross;
     const int lane = threadIdx.x % kWave, s = threadIdx.x / kWave;
     const int64_t rb = blockIdx.x / p.groups;
     const int g = (int)(blockIdx.x - rb * p.groups);
-    const int half = lane / 32, r32 = lane % 32;
-    const int64_t r = rb * 32 + r32, c0 = (int64_t)g * kMxGroup + s * 64 + half * 32, left = p.cols - c0;
-    if (r >= p.rows || left <= 0) return;
-    const u32x4 codes = *reinterpret_cast<const u32x4*>(p.codes + ((blockIdx.x * 4 + s) * (int64_t)2 + half) * 512 + r32 * 16);
-    const uint32_t byte = p.scales[(int64_t)blockIdx.x * 256 + lane * 4 + s];
-    T* row = static_cast<T*>(p.dst) + r * p.ld;
-    const float scale = scale_of(byte);
-    const bool nan = byte == 255u;
-    if constexpr (sizeof(T) == 4) {
-        float v[32];
+    const int col = (lane % kAcross) * kPiece, half = col / 32;
+    const int64_t c = (int64_t)g * kMxGroup + s * 64 + col, left = p.cols - c;
+    if (left <= 0) return;
+    const uint8_t* codes = p.codes + ((blockIdx.x * 4 + s) * (int64_t)2 + half) * 512 + (col % 32) / 2;
+    const uint8_t* scales = p.scales + (int64_t)blockIdx.x * 256 + half * 128 + s;
+    uint32_t word[32 / kRows], byte[32 / kRows];
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            f32x2 q[4];
-            q[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[d], scale, 0);
-            q[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[d], scale, 1);
-            q[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[d], scale, 2);
-            q[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[d], scale, 3);
+    for (int i = 0; i < 32 / kRows; ++i) {
+        const int r32 = i * kRows + lane / kAcross;
+        word[i] = kPiece == 8 ? *reinterpret_cast<const uint32_t*>(codes + r32 * 16) : (uint32_t)*reinterpret_cast<const uint16_t*>(codes + r32 * 16);
+        byte[i] = scales[r32 * 4];
+    }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[8 * d + 2 * i] = nan ? scale : q[i][0];
-                v[8 * d + 2 * i + 1] = nan ? scale : q[i][1];
-            }
+    for (int i = 0; i < 32 / kRows; ++i) {
+        const int64_t r = rb * 32 + i * kRows + lane / kAcross;
+        if (r >= p.rows) return;
+        const float scale = scale_of(byte[i]);
+        const bool nan = byte[i] == 255u;
+        u32x4 v;
+        if constexpr (sizeof(T) == 4) {
+            const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 0), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word[i], scale, 1);
+            v = u32x4{__float_as_uint(lo[0]), __float_as_uint(lo[1]), __float_as_uint(hi[0]), __float_as_uint(hi[1])};
+        } else {
+            v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 0));
+            v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 1));
+            v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 2));
+            v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word[i], scale, 3));
         }
-        if (left >= 32) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                *reinterpret_cast<u32x4_a4*>(row + c0 + 4 * i) =
-                    u32x4_a4{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+        if (nan) v = sizeof(T) == 4 ? u32x4{0x7FC00000u, 0x7FC00000u, 0x7FC00000u, 0x7FC00000u} : u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+        T* z = static_cast<T*>(p.dst) + r * p.ld + c;
+        if (left >= kPiece) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_a4*>(z) = v;
+            else *reinterpret_cast<u32x4_a2*>(z) = v;
         } else {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) row[c0 + i] = v[i];
-        }
-    } else {
-        uint32_t v[16];
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            v[4 * d] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[d], scale, 0));
-            v[4 * d + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[d], scale, 1));
-            v[4 * d + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[d], scale, 2));
-            v[4 * d + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[d], scale, 3));
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = nan ? 0x7FC07FC0u : v[i];
-        if (left >= 32) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<u32x4_a2*>(row + c0 + 8 * i) = u32x4_a2{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) row[c0 + i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+            for (int k = 0; k < kPiece - 1; ++k)
+                if (k < left) {
+                    if constexpr (sizeof(T) == 4) z[k] = bits_as<float>(v[k]);
+                    else z[k] = (uint16_t)(v[k / 2] >> (16 * (k & 1)));
+                }
         }
     }
-    }
+}
 
 }  // namespace
 
