@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void k_mx4_rows(PackArgs p) {
         const uint32_t first = (uint32_t)r * p.half + (uint32_t)(c / 2);
         uint32_t word = 0;
         codes = stochastic_codes(v, byte, [&](int i) {
-            if ((i & 1) == 0) word = ~fmix32((first + (uint32_t)(i / 2)) ^ p.key);
+            if (i & 1) word = ~fmix32((first + (uint32_t)(i / 2)) ^ p.key);   // (asked for from the last one on)
             return (i & 1) ? word & 0xFFFFu : word >> 16;
         });
     } else {

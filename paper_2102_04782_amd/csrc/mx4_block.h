@@ -50,27 +50,44 @@ __device__ __forceinline__ u32x4 nearest_codes(const uint32_t (&v)[16], uint32_t
     }
     return c;
 }
-// The code of one element, stochastically, from the complement V = 65535 - U of its draw.  With t = |x| * 2^-e, at most 6, as a fixed-point
-// number of 23 places, or from t = 2 on as the bits of the float themselves, the bits from 22 on count the elements up to t and the
-// 16 below them are the fraction of the step to the next, so that adding V there carries exactly if the fraction is above U.
-__device__ __forceinline__ uint32_t stochastic_code(float x, int shift, uint32_t v16) {
-    const float t = ldexpf(fabsf(x), shift);                                  // t * 2^23
-    const uint32_t bits = __float_as_uint(t) - (uint32_t)((252 + 46) << 22);
-    const uint32_t w = t < 16777216.0f ? (uint32_t)t : bits;
-    return ((w + (v16 << 6)) >> 22) | ((__float_as_uint(x) >> 28) & 8u);
+// The code of one element in the upper four bits, stochastically, from the complement V = 65535 - U of its draw.  With t = |x| * 2^-e, at most
+// 6, as a fixed-point number of 29 places, or from t = 2 on as the bits of the float themselves moved there, the bits from 28 on count
+// the elements up to t and the 16 below them are the fraction of the step to the next, so that adding V there carries exactly if the
+// fraction is above U.
+__device__ __forceinline__ uint32_t stochastic_code(float x, float up, uint32_t v16) {
+    const float t = fabsf(x) * up;                                            // t * 2^29
+    const uint32_t bits = (__float_as_uint(t) << 6) - (uint32_t)((252u + 58u) << 28);
+    const uint32_t w = (t < 1073741824.0f ? (uint32_t)t : bits) + (v16 << 12);
+    return (w & 0x7FFFFFFFu) | (__float_as_uint(x) & 0x80000000u);
 }
 __device__ __forceinline__ float elem_f32(const uint32_t (&v)[32], int i) { return bits_as<float>(v[i]); }
 __device__ __forceinline__ float elem_f32(const uint32_t (&v)[16], int i) { return (i & 1) ? bf16_hi(v[i / 2]) : bf16_lo(v[i / 2]); }
-// draw(i): the complement of element i's draw
+__device__ __forceinline__ void scale_up(uint32_t (&v)[32], float f) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(bits_as<float>(v[i]) * f);
+}
+__device__ __forceinline__ void scale_up(uint32_t (&v)[16], float f) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = pack_bf16(bf16_lo(v[i]) * f, bf16_hi(v[i]) * f);
+}
+// draw(i): the complement of element i's draw, asked for from the last one on.  v is used up.
 template <int W, typename F>
-__device__ __forceinline__ u32x4 stochastic_codes(const uint32_t (&v)[W], uint32_t byte, F draw) {
-    const int shift = 127 + 23 - (int)byte;
+__device__ __forceinline__ u32x4 stochastic_codes(uint32_t (&v)[W], uint32_t byte, F draw) {
+    // 2^(156 - byte) exceeds fp32 for the smallest scales: such elements are brought up by 2^64 first (exactly, also from below the normal
+    // range); a block of zeros, of scale byte 1, is so too
+    uint32_t from = byte;
+    if (__any(byte < 29u)) {
+        const bool tiny = byte < 29u;
+        scale_up(v, tiny ? 0x1p64f : 1.0f);
+        from += tiny ? 64u : 0u;
+    }
+    const float up = bits_as<float>((283u - from) << 23);
     u32x4 c;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
         uint32_t w = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w |= stochastic_code(elem_f32(v, 8 * d + i), shift, draw(8 * d + i)) << (4 * i);
+        for (int i = 7; i >= 0; --i) w = __builtin_amdgcn_alignbit(w, stochastic_code(elem_f32(v, 8 * d + i), up, draw(8 * d + i)), 28);
         c[d] = w;
     }
     return byte == 255u ? u32x4{0, 0, 0, 0} : c;
