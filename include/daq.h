@@ -630,9 +630,11 @@ daq_status daq_ckpt8_act_backward(const void* dy, daq_dtype dtype, int64_t rows,
  * layer: products on the bfloat16 matrix cores, where X^ is exact, and fp32 sums.  An fp32 dY enters as the sum of three
  * bfloat16 values (its 24 bits).  accumulate != 0 adds to dW.
  *   dW         i/o  fp32 [N][K], row stride ldw
- *   workspace  of the bytes daq_ckpt8_weight_grad_workspace reports; may be NULL where that is 0
+ *   workspace  of the bytes daq_ckpt8_weight_grad_workspace reports (dy_misaligned: the address of dY modulo 16; a bfloat16 dY
+ *              of 16-byte aligned rows needs less); may be NULL where that is 0
  * ------------------------------------------------------------------------------------------- */
-daq_status daq_ckpt8_weight_grad_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, size_t* bytes);
+daq_status daq_ckpt8_weight_grad_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, int64_t lddy, int32_t dy_misaligned,
+                                           size_t* bytes);
 daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, const void* dY, daq_dtype dtype, int64_t lddy,
                                  const uint8_t* x_ckpt, float* dW, int64_t ldw, int32_t accumulate, void* workspace,
                                  size_t workspace_bytes, void* stream);

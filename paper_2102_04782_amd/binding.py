@@ -269,7 +269,7 @@ def lib():
         L.daq_ckpt8_restore.argtypes = [vp, i64, i64, i32, vp, C.c_int, i64, vp]
         L.daq_ckpt8_act_forward.argtypes = [vp, C.c_int, i64, i64, i64, C.c_int, i32, vp, i64, vp, vp]
         L.daq_ckpt8_act_backward.argtypes = [vp, C.c_int, i64, i64, i64, vp, C.c_int, i32, vp, i64, vp, vp]
-        L.daq_ckpt8_weight_grad_workspace.argtypes = [i64, i64, i64, C.c_int, psz]
+        L.daq_ckpt8_weight_grad_workspace.argtypes = [i64, i64, i64, C.c_int, i64, i32, psz]
         L.daq_ckpt8_weight_grad.argtypes = [i64, i64, i64, vp, C.c_int, i64, vp, vp, i64, i32, vp, sz, vp]
         L.daq_prof_end.argtypes = [C.POINTER(ProfRow), C.c_int32, C.POINTER(C.c_int32)]
         L.daq_ceiling_mfma_i8.argtypes = [C.c_int32, C.c_int32, vp, C.POINTER(C.c_double), vp]
@@ -841,7 +841,7 @@ def ckpt8_weight_grad(dy: torch.Tensor, x: Ckpt8, out: Optional[torch.Tensor] = 
     assert x.parts == 1 and M == x.rows and (out is not None or not accumulate)
     out, ldw, _ = _result(out, N, x.cols, torch.float32, dy)
     if workspace is None:
-        workspace = _few_ws("daq_ckpt8_weight_grad_workspace", dy.device, M, N, x.cols, code)
+        workspace = _few_ws("daq_ckpt8_weight_grad_workspace", dy.device, M, N, x.cols, code, lddy, dy.data_ptr() % 16)
     _check(lib().daq_ckpt8_weight_grad(M, N, x.cols, dy.data_ptr(), code, lddy, x.buf.data_ptr(), out.data_ptr(), ldw, int(accumulate),
                                        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_ckpt8_weight_grad")
     return out

@@ -164,9 +164,9 @@ struct WgradArgs {
 
 // Tiles of 32 RB WR rows x 32 CB WC columns of dW, a workgroup each, for one part of the tokens.  Order of the workgroups as in the
 // 4-bit products; the parts of a tile are neighbours in it.
-template <int WR, int WC, int RB, int CB, int SLOTS>
+template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
-    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS>;
+    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int64_t b = (int64_t)(blockIdx.x % kXcd) * p.per_xcd + blockIdx.x / kXcd;
     const int64_t t = b / p.splits;
@@ -215,15 +215,15 @@ __global__ __launch_bounds__(256) void k_ckpt8_wgrad_sum(const float* part, int 
         if (k + i < K) z[i] = accumulate ? z[i] + sum[i] : sum[i];
 }
 
-template <int WR, int WC, int RB, int CB, int SLOTS>
+template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT>
 daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
-    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS>;
+    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT>;
     p.tiles_n = (int)ceil_div(p.dy.blocks, WR * RB);
     p.tiles_k = (int)ceil_div(p.x.blocks, WC * CB);
     const int64_t per = ceil_div((int64_t)p.tiles_n * p.tiles_k * p.splits, kXcd);
     if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
     p.per_xcd = (int)per;
-    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, SLOTS>;
+    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, SLOTS, FLAT>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("ckpt8_wgrad", st, hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcd)), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
     return DAQ_OK;
@@ -232,11 +232,12 @@ daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
 // Sizes of a call and where its workspace holds what.
 struct WgradPlan {
     int n_blocks, k_blocks, steps, parts;   // parts: of a value of dY
+    bool flat;                              // dY as it is, not in tiles
     bool big;                               // tiles of 256 x 256 instead of 128 x 128
     int splits, per_split;
     int64_t off_x, off_part, pitch, bytes;
 };
-WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype) {
+WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, int dy_misaligned) {
     WgradPlan w{};
     w.n_blocks = (int)ceil_div(N, 32);
     w.k_blocks = (int)ceil_div(K, 32);
@@ -253,10 +254,15 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype) {
     const int s_small = cheapest_split(small), s_big = cheapest_split(big);
     w.big = big.cost(s_big) < small.cost(s_small);
     w.splits = w.big ? s_big : s_small;
+    // A bfloat16 dY of whole 16-byte pieces can be read by the products as it is (what they reach of it at a time is within 31 bits): that
+    // spares its way into tiles, and the fragments' transposing reads cost the products some.  us with it and without: 16384 x 8192 x 4096
+    // 941 and 976, 4096 x 4096 x 4096 133 and 133, 16384 x 4096 x 512 103 and 141; on small tiles 2048 x 2048 x 2048 37.3 and 35.1,
+    // 8192 x 1024 x 1024 42.2 and 42.3, 16384 x 256 x 256 29.9 and 31.6.
+    w.flat = dtype == DAQ_BF16 && dy_misaligned == 0 && lddy % 8 == 0 && N % 8 == 0 && lddy < ((int64_t)1 << 24) && K <= (w.big ? 8192 : 1024);
     w.per_split = (int)ceil_div(stages, w.splits);
     w.splits = (int)ceil_div(stages, w.per_split);
     w.pitch = round_up(K, 4);
-    w.off_x = round_up((int64_t)w.n_blocks * w.steps * w.parts * 1024, 256);
+    w.off_x = w.flat ? 0 : (int64_t)w.n_blocks * w.steps * w.parts * 1024;
     w.off_part = w.off_x + (int64_t)w.k_blocks * w.steps * 1024;
     w.bytes = w.off_part + (w.splits > 1 ? round_up((int64_t)w.splits * N * w.pitch * 4, 256) : 0);
     return w;
@@ -276,12 +282,13 @@ static daq_status wgrad_size(int64_t M, int64_t N, int64_t K) {
     return rc;
 }
 
-extern "C" daq_status daq_ckpt8_weight_grad_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, size_t* bytes) {
+extern "C" daq_status daq_ckpt8_weight_grad_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, int64_t lddy, int32_t dy_misaligned,
+                                                      size_t* bytes) {
     if (!bytes) return DAQ_ERR_INVALID_ARG;
     *bytes = 0;
-    if (!dtype_ok(dtype)) return DAQ_ERR_INVALID_ARG;
+    if (!dtype_ok(dtype) || dy_misaligned < 0) return DAQ_ERR_INVALID_ARG;
     const daq_status rc = wgrad_size(M, N, K);
-    if (rc == DAQ_OK && M > 0) *bytes = (size_t)wgrad_plan(M, N, K, dtype).bytes;
+    if (rc == DAQ_OK && M > 0) *bytes = (size_t)wgrad_plan(M, N, K, dtype, lddy, dy_misaligned).bytes;
     return rc;
 }
 
@@ -301,21 +308,22 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
             DAQ_LAUNCH("ckpt8_wgrad_sum", st, hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, nullptr, 0, N, K, 0, dW, ldw, 0));
         return DAQ_OK;
     }
-    const WgradPlan w = wgrad_plan(M, N, K, dtype);
+    const WgradPlan w = wgrad_plan(M, N, K, dtype, lddy, (int)((uintptr_t)dY & 15u));
     if (!workspace || workspace_bytes < (size_t)w.bytes || !aligned256(workspace)) return DAQ_ERR_WORKSPACE;
     daq_ckpt8_layout L;
     daq_layout_ckpt8(M, K, 1, &L);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     OrderArgs o{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, ws, ws + w.off_x, w.n_blocks, w.k_blocks, w.steps, 0, 0};
-    o.dy_waves = round_up(ceil_div(w.n_blocks, 4) * w.steps, 4);
+    o.dy_waves = w.flat ? 0 : round_up(ceil_div(w.n_blocks, 4) * w.steps, 4);
     o.x_waves = ceil_div(w.k_blocks, 4) * w.steps;
     const int64_t blocks = ceil_div(o.dy_waves + o.x_waves, 4);
     if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;
     if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, st, o));
     else DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<float>, dim3((unsigned)blocks), dim3(256), 0, st, o));
     WgradArgs p{};
-    p.dy = TileOperand{o.dy_tiles, nullptr, w.n_blocks, w.steps * w.parts};
-    p.x = TileOperand{o.x_tiles, nullptr, w.k_blocks, w.steps};
+    if (w.flat) p.dy = TileOperand{static_cast<const uint8_t*>(dY), nullptr, w.n_blocks, w.steps, lddy * 2, N * 2, M};
+    else p.dy = TileOperand{o.dy_tiles, nullptr, w.n_blocks, w.steps * w.parts, 0, 0, 0};
+    p.x = TileOperand{o.x_tiles, nullptr, w.k_blocks, w.steps, 0, 0, 0};
     p.stages = w.steps / kStageSteps * w.parts;
     p.x_stages = w.steps / kStageSteps;
     p.splits = w.splits;
@@ -327,7 +335,8 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     p.accumulate = accumulate;
     p.part = reinterpret_cast<float*>(ws + w.off_part);
     p.pitch = w.pitch;
-    rc = w.big ? launch_wgrad<2, 4, 4, 2, 2>(p, st) : launch_wgrad<2, 2, 2, 2, 4>(p, st);
+    if (w.flat) rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, true>(p, st) : launch_wgrad<2, 2, 2, 2, 4, true>(p, st);
+    else rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, false>(p, st) : launch_wgrad<2, 2, 2, 2, 4, false>(p, st);
     if (rc != DAQ_OK || w.splits == 1) return rc;
     DAQ_LAUNCH("ckpt8_wgrad_sum", st,
                hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, p.part, w.splits, N, K, w.pitch, dW, ldw, accumulate));

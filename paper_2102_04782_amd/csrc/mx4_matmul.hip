@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_mx4_tiles(MatmulArgs p, int
     const int64_t band = t / (4 * tiles_n);
     const int rest = (int)(t - band * 4 * tiles_n), high = min(4, tiles_m - (int)band * 4);
     const int tm = (int)band * 4 + rest % high, tn = rest / high;
-    const TileOperand r{p.a, p.a_scales, p.a_blocks, p.groups * 4}, c{p.b, p.b_scales, p.b_blocks, p.groups * 4};
+    const TileOperand r{p.a, p.a_scales, p.a_blocks, p.groups * 4, 0, 0, 0}, c{p.b, p.b_scales, p.b_blocks, p.groups * 4, 0, 0, 0};
     Product prod;
     prod.run(r, c, tm * WR * RB, tn * WC * CB, 0, p.groups, p.groups, lds);
     const int wave = threadIdx.x / kWave;

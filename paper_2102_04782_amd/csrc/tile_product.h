@@ -16,6 +16,9 @@ struct TileOperand {
     const uint8_t* scales;
     int blocks;         // row blocks
     int steps;          // of a row block, a multiple of kStageSteps
+    // Or, for the first operand of bfloat16 products (FLAT), not tiles but the matrix itself, its columns being the rows of the
+    // product: row m of the sum's axis is `width` bytes at tiles + m * pitch, for m < depth.  16-byte aligned, pitch included.
+    int64_t pitch, width, depth;
 };
 constexpr int kStageSteps = 4;
 
@@ -52,7 +55,7 @@ __device__ __forceinline__ void words_to_lds(__amdgpu_buffer_rsrc_t src, uint32_
 // straight into LDS, and the fragments of a step while the step before is multiplied, the first step of a stage among them:
 // the barrier stands before the last step's products, when that step's fragments are in registers already.
 // c_wrap: stages after which the second operand begins again.
-template <int WR, int WC, int RB, int CB, bool MX, int SLOTS = 2>
+template <int WR, int WC, int RB, int CB, bool MX, int SLOTS = 2, bool FLAT = false>
 struct TileProduct {
     static constexpr int kWaves = WR * WC;
     static constexpr int kTiles = WR * RB + WC * CB;               // of a step
@@ -62,6 +65,11 @@ struct TileProduct {
     static constexpr int kShare = kTiles / kWaves;                    // operand row blocks that a wave fetches
     static constexpr int kAsks = kShare * (kStageSteps + (MX ? 1 : 0));   // requests of a wave for a stage
 
+    // FLAT: a stage of the first operand lies in LDS as its 64 rows, 16-byte pieces of a row in the order piece ^ place(row): the fragment
+    // reads, which transpose, take 64 bytes each of eight rows, four of them neighbours and four more eight on.
+    static constexpr int kRowBytes = WR * RB * 64, kRowPieces = kRowBytes / 16, kRowsAsked = 1024 / kRowBytes;   // (a request is a KiB)
+    static __device__ __forceinline__ int place(int row) { return ((row & 3) * 4 + (row & 8) * 2) & (kRowPieces - 1); }
+    static_assert(!FLAT || (!MX && (WR * RB) % kShare == 0), "a wave fetches of one operand only");
     static_assert(SLOTS == 2 || SLOTS == 4, "two or four stages in LDS");
     static_assert(kTiles % kWaves == 0, "every wave fetches the same number of row blocks");
 
@@ -86,10 +94,29 @@ struct TileProduct {
             of_c[i] = t >= WR * RB;
             const TileOperand& o = of_c[i] ? c : r;
             const int64_t b = min(of_c[i] ? cb + t - WR * RB : rb + t, o.blocks - 1);     // (blocks behind the last one are not stored)
-            src[i] = bytes_from(o.tiles + b * o.steps * 1024);
+            if (!FLAT || of_c[i]) src[i] = bytes_from(o.tiles + b * o.steps * 1024);
             if constexpr (MX) ssrc[i] = bytes_from(o.scales + b * (o.steps / 4) * 256);
         }
+        // FLAT: the rows of a stage that this wave asks for, request by request, and where in them a lane reads
+        constexpr int kAskedRows = kShare * kStageSteps * kRowsAsked;
+        uint32_t flat_off[kShare * kStageSteps];
+        if constexpr (FLAT) {
+#pragma unroll
+            for (int k = 0; k < kShare * kStageSteps; ++k) {
+                const int in = lane / kRowPieces, row = wave * kAskedRows + k * kRowsAsked + in;
+                flat_off[k] = (uint32_t)(row * (int)r.pitch) + (uint32_t)((lane % kRowPieces) ^ place(row)) * 16u;
+            }
+        }
         auto ask = [&](int s, uint8_t* to) {
+            if (FLAT && !of_c[0]) {
+                // rows behind the last one are beyond the descriptor's end and read as zeros
+                const int64_t first = (int64_t)s * kStageSteps * 16 * r.pitch + (int64_t)rb * 64;
+                const int64_t bytes = max((r.depth - 1) * r.pitch + r.width - first, (int64_t)0);
+                const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc((void*)(r.tiles + first), 0, (int)(uint32_t)min(bytes, (int64_t)0xFFFFFF00u), 0x00020000);
+#pragma unroll
+                for (int k = 0; k < kShare * kStageSteps; ++k) tile_to_lds(rows, flat_off[k], 0, to + (wave * kShare * kStageSteps + k) * 1024);
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < kShare; ++i) {
                 const int st = of_c[i] ? (s >= 2 * c_wrap ? s - 2 * c_wrap : s >= c_wrap ? s - c_wrap : s) : s;
@@ -103,11 +130,56 @@ struct TileProduct {
         int sr[2][RB], sc[2][CB];
         const int at_r = wr * RB * kStageSteps * 1024 + lane * 16, at_c = (WR * RB + wc * CB) * kStageSteps * 1024 + lane * 16;
         const int at_sr = kTiles * kStageSteps * 1024 + wr * RB * 256 + lane * 4, at_sc = kTiles * kStageSteps * 1024 + (WR * RB + wc * CB) * 256 + lane * 4;
+        // FLAT: lane l takes column l % 16 of the 16 of its quarter wave and four rows at a time; the quarters are 16 columns and 8 rows apart
+        int at_flat[RB];
+        if constexpr (FLAT) {
+            const int row = (lane / 32) * 8 + (lane % 16) / 4;
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                const int piece = (wr * RB + i) * 4 + (lane / 16 & 1) * 2 + (lane & 3) / 2;
+                at_flat[i] = row * kRowBytes + (piece ^ place(row)) * 16 + (lane & 1) * 8;
+            }
+        }
+        // FLAT: the transposing reads are written out, with their wait, as the compiler would have each wait for the requests under way
+        auto read_flat = [&](const uint8_t* from, auto step, int set) {
+            if constexpr (FLAT) {
+                typedef short v4s __attribute__((ext_vector_type(4)));
+                constexpr int kAt = decltype(step)::value * 16 * kRowBytes;
+                const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)from;
+                v4s part[2 * RB];
+                uint32_t at[RB];
+#pragma unroll
+                for (int i = 0; i < RB; ++i) at[i] = base + (uint32_t)at_flat[i];
+                if constexpr (RB == 4)
+                    asm volatile(
+                        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+                        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+                        "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+                        "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
+                        "s_waitcnt lgkmcnt(0)"
+                        : "=&v"(part[0]), "=&v"(part[1]), "=&v"(part[2]), "=&v"(part[3]), "=&v"(part[2 * RB - 4]), "=&v"(part[2 * RB - 3]),
+                          "=&v"(part[2 * RB - 2]), "=&v"(part[2 * RB - 1])
+                        : "v"(at[0]), "v"(at[1]), "v"(at[RB - 2]), "v"(at[RB - 1]), "n"(kAt), "n"(kAt + 4 * kRowBytes)
+                        : "memory");
+                else
+                    asm volatile(
+                        "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                        "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                        "s_waitcnt lgkmcnt(0)"
+                        : "=&v"(part[0]), "=&v"(part[1]), "=&v"(part[2]), "=&v"(part[3])
+                        : "v"(at[0]), "v"(at[1]), "n"(kAt), "n"(kAt + 4 * kRowBytes)
+                        : "memory");
+#pragma unroll
+                for (int i = 0; i < RB; ++i) fr[set][i] = __builtin_bit_cast(v4i, __builtin_shufflevector(part[2 * i], part[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
         auto read = [&](const uint8_t* from, int k, int set, int sset) {
 #pragma unroll
             for (int i = 0; i < CB; ++i) fc[set][i] = *reinterpret_cast<const v4i*>(from + at_c + (i * kStageSteps + k) * 1024);
+            if constexpr (!FLAT) {
 #pragma unroll
-            for (int i = 0; i < RB; ++i) fr[set][i] = *reinterpret_cast<const v4i*>(from + at_r + (i * kStageSteps + k) * 1024);
+                for (int i = 0; i < RB; ++i) fr[set][i] = *reinterpret_cast<const v4i*>(from + at_r + (i * kStageSteps + k) * 1024);
+            }
             if constexpr (MX) {
                 if (k == 0) {
 #pragma unroll
@@ -141,34 +213,40 @@ struct TileProduct {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * kAsks) : "memory");
         __builtin_amdgcn_s_barrier();
         read(lds0, 0, 0, 0);
+        read_flat(lds0, std::integral_constant<int, 0>{}, 0);
         // The reads of a step stand between the products of the step before, one each, from its beginning on: left to itself the compiler
-        // moves them behind the last one, where every wave then waits for them.
-        auto interleave = [&] {
+        // moves them behind the last one, where every wave then waits for them.  (FLAT: the written ones do follow the products, and the
+        // wave that shares the SIMD multiplies meanwhile.)
+        auto then = [&](const uint8_t* from, auto step, int set) {
+            if constexpr (FLAT) {
+                __builtin_amdgcn_sched_barrier(0);
+                read_flat(from, step, set);
+            } else {
 #pragma unroll
-            for (int i = 0; i < RB + CB; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
+                for (int i = 0; i < RB * CB; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
+                }
             }
-            __builtin_amdgcn_sched_group_barrier(0x008, RB * CB, 0);
             __builtin_amdgcn_sched_barrier(0);
         };
         // as many stages a round as there are places, so that these and the register sets have numbers known here
         auto stage = [&](int s, uint8_t* here, uint8_t* next, int sset) {
             read(here, 1, 1, sset);
             multiply(std::integral_constant<int, 0>{}, 0, sset);
-            interleave();
+            then(here, std::integral_constant<int, 1>{}, 1);
             read(here, 2, 0, sset);
             multiply(std::integral_constant<int, 1>{}, 1, sset);
-            interleave();
+            then(here, std::integral_constant<int, 2>{}, 0);
             read(here, 3, 1, sset);
             multiply(std::integral_constant<int, 2>{}, 0, sset);
-            interleave();
+            then(here, std::integral_constant<int, 3>{}, 1);
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");   // the next stage has landed, this one is read out
             __builtin_amdgcn_s_barrier();
             read(next, 0, 0, sset ^ 1);
             ask(min(s + SLOTS, last), here);
             multiply(std::integral_constant<int, 3>{}, 1, sset);
-            interleave();
+            then(next, std::integral_constant<int, 0>{}, 0);
         };
         int s = s0;
         if constexpr (SLOTS == 2) {
