@@ -13,6 +13,7 @@ namespace daq {
 namespace {
 
 constexpr int kStageM = 16 * kStageSteps;   // tokens of a stage
+constexpr int kParts = 3;                   // bfloat16 values that an fp32 value is the sum of
 
 struct OrderArgs {
     const void* dy;
@@ -81,65 +82,89 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
     const int b0 = (int)(wave - step * wide) * 4, nb = min(4, blocks - b0);     // row blocks of the tiles
     const int64_t col = (int64_t)b0 * 32 + (lane % 32) * 4;
     const int64_t m0 = step * 16 + (lane / 32) * 8;
-    const int64_t block_bytes = (int64_t)p.steps * 1024 * (of_dy && sizeof(T) == 4 ? 3 : 1);
+    const int64_t block_bytes = (int64_t)p.steps * 1024 * (of_dy && sizeof(T) == 4 ? kParts : 1);
+    // Rows and columns behind the last ones are read from places that exist and cleared afterwards, so that a lane has all its reads
+    // under way before it waits for the first.
+    int64_t row[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) row[j] = min(m0 + j, p.M - 1);
+    const bool cut = m0 + 8 > p.M;
     if (of_dy) {
         const T* src = static_cast<const T*>(p.dy) + col;
+        constexpr int kWords = sizeof(T) == 2 ? 2 : 4;
+        uint32_t q[8][kWords];
+        if (col + 4 <= p.N) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (sizeof(T) == 2) {
+                    const u32x2_a2 v = *reinterpret_cast<const u32x2_a2*>(src + row[j] * p.lddy);
+                    q[j][0] = v[0], q[j][1] = v[1];
+                } else {
+                    const u32x4_a4 v = *reinterpret_cast<const u32x4_a4*>(src + row[j] * p.lddy);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q[j][i] = v[i];
+                }
+            }
+        } else {
+            const int left = (int)max(p.N - col, (int64_t)0);
+            const T* last = static_cast<const T*>(p.dy) + p.N - 1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t e[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const T v = (i < left ? src + i : last)[row[j] * p.lddy];
+                    if constexpr (sizeof(T) == 2) e[i] = i < left ? v : 0u;
+                    else e[i] = i < left ? __float_as_uint(v) : 0u;
+                }
+                if constexpr (sizeof(T) == 2) {
+                    q[j][0] = e[0] | (e[1] << 16), q[j][1] = e[2] | (e[3] << 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q[j][i] = e[i];
+                }
+            }
+        }
+        if (cut) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) q[j][i] = m0 + j < p.M ? q[j][i] : 0u;
+        }
         if constexpr (sizeof(T) == 2) {
             u32x2 v[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = m0 + j < p.M;
-                const T* row = src + (in ? m0 + j : 0) * p.lddy;
-                if (col + 4 <= p.N) {
-                    const u32x2_a2 q = *reinterpret_cast<const u32x2_a2*>(row);
-                    v[j] = in ? u32x2{q[0], q[1]} : u32x2{0, 0};
-                } else {
-                    uint32_t e[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = in && col + i < p.N ? row[i] : 0u;
-                    v[j] = u32x2{e[0] | (e[1] << 16), e[2] | (e[3] << 16)};
-                }
-            }
+            for (int j = 0; j < 8; ++j) v[j] = u32x2{q[j][0], q[j][1]};
             store_columns(lds, p.dy_tiles + b0 * block_bytes + step * 1024, block_bytes, nb, v);
         } else {
-            u32x2 v[3][8];
+            u32x2 v[kParts][8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool in = m0 + j < p.M;
-                const T* row = src + (in ? m0 + j : 0) * p.lddy;
-                float e[4];
-                if (col + 4 <= p.N) {
-                    const u32x4_a4 q = *reinterpret_cast<const u32x4_a4*>(row);
+                uint32_t h[4][kParts];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = in ? bits_as<float>(q[i]) : 0.0f;
-                } else {
+                for (int i = 0; i < 4; ++i) split3(bits_as<float>(q[j][i]), h[i][0], h[i][1], h[i][2]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = in && col + i < p.N ? row[i] : 0.0f;
-                }
-                uint32_t h[4][3];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) split3(e[i], h[i][0], h[i][1], h[i][2]);
-#pragma unroll
-                for (int k = 0; k < 3; ++k) v[k][j] = u32x2{h[0][k] | (h[1][k] << 16), h[2][k] | (h[3][k] << 16)};
+                for (int k = 0; k < kParts; ++k) v[k][j] = u32x2{h[0][k] | (h[1][k] << 16), h[2][k] | (h[3][k] << 16)};
             }
-            // the three parts are stages of their own, one after the other, the smallest first: so the sums are long only in the last
-            // third, and as exact as those of the leading bits alone
+            // the three parts of a step are tiles one after the other
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
-                store_columns(lds, p.dy_tiles + b0 * block_bytes + ((int64_t)(2 - k) * p.steps + step) * 1024, block_bytes, nb, v[k]);
+            for (int k = 0; k < kParts; ++k) store_columns(lds, p.dy_tiles + b0 * block_bytes + (step * kParts + k) * 1024, block_bytes, nb, v[k]);
         }
     } else {
+        const int64_t at = col < p.pitch ? col : 0;      // (columns behind the last block are not stored)
+        uint32_t w[8], byte[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const uint32_t*>(p.codes + row[j] * p.pitch + at);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) byte[j] = p.scales[row[j] * (p.pitch / kMxBlock) + at / kMxBlock];
         u32x2 v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const bool in = m0 + j < p.M;
-            const int64_t r = in ? m0 + j : 0;
-            const int64_t at = col < p.pitch ? col : 0;      // (columns behind the last block are not stored)
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(p.codes + r * p.pitch + at);
-            const float s = in ? scale_of(p.scales[r * (p.pitch / kMxBlock) + at / 32]) : 0.0f;
+            const float s = scale_of(byte[j]);
             float e[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = in ? (float)(int8_t)(w >> (8 * i)) * s : 0.0f;
+            for (int i = 0; i < 4; ++i) e[i] = in ? (float)(int8_t)(w[j] >> (8 * i)) * s : 0.0f;
             // (exact in bfloat16: the upper halves)
             v[j] = u32x2{__builtin_amdgcn_perm(__float_as_uint(e[1]), __float_as_uint(e[0]), 0x07060302u),
                          __builtin_amdgcn_perm(__float_as_uint(e[3]), __float_as_uint(e[2]), 0x07060302u)};
@@ -150,8 +175,7 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
 
 struct WgradArgs {
     TileOperand dy, x;
-    int stages;              // of dy
-    int x_stages;            // of x: dy begins again every so many
+    int stages;
     int splits, per_split;   // parts of the stages, and stages of a part
     int tiles_n, tiles_k, per_xcd;
     int64_t N, K;
@@ -164,9 +188,9 @@ struct WgradArgs {
 
 // Tiles of 32 RB WR rows x 32 CB WC columns of dW, a workgroup each, for one part of the tokens.  Order of the workgroups as in the
 // 4-bit products; the parts of a tile are neighbours in it.
-template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT>
+template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT, int PARTS>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
-    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT>;
+    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT, PARTS>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int64_t b = (int64_t)(blockIdx.x % kXcd) * p.per_xcd + blockIdx.x / kXcd;
     const int64_t t = b / p.splits;
@@ -176,7 +200,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
     const int rest = (int)(t - band * 4 * p.tiles_k), high = min(4, p.tiles_n - (int)band * 4);
     const int tn = (int)band * 4 + rest % high, tk = rest / high;
     Product prod;
-    prod.run(p.dy, p.x, tn * WR * RB, tk * WC * CB, split * p.per_split, min(p.stages, (split + 1) * p.per_split), p.x_stages, lds);
+    prod.run(p.dy, p.x, tn * WR * RB, tk * WC * CB, split * p.per_split, min(p.stages, (split + 1) * p.per_split), lds);
     const int wave = threadIdx.x / kWave;
     const int64_t n0 = ((int64_t)tn * WR + wave / WC) * RB * 32, k0 = ((int64_t)tk * WC + wave % WC) * CB * 32;
     float* base = p.splits > 1 ? p.part + split * p.N * p.pitch : p.dw;
@@ -215,15 +239,15 @@ __global__ __launch_bounds__(256) void k_ckpt8_wgrad_sum(const float* part, int 
         if (k + i < K) z[i] = accumulate ? z[i] + sum[i] : sum[i];
 }
 
-template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT>
+template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT, int PARTS>
 daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
-    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT>;
+    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT, PARTS>;
     p.tiles_n = (int)ceil_div(p.dy.blocks, WR * RB);
     p.tiles_k = (int)ceil_div(p.x.blocks, WC * CB);
     const int64_t per = ceil_div((int64_t)p.tiles_n * p.tiles_k * p.splits, kXcd);
     if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
     p.per_xcd = (int)per;
-    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, SLOTS, FLAT>;
+    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, SLOTS, FLAT, PARTS>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("ckpt8_wgrad", st, hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcd)), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
     return DAQ_OK;
@@ -242,17 +266,17 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, i
     w.n_blocks = (int)ceil_div(N, 32);
     w.k_blocks = (int)ceil_div(K, 32);
     w.steps = (int)(ceil_div(M, kStageM) * kStageSteps);
-    w.parts = dtype == DAQ_BF16 ? 1 : 3;
+    w.parts = dtype == DAQ_BF16 ? 1 : kParts;
     // The form and the parts of the tokens that take the least time by what was measured of them (us): a workgroup to a CU, 6 + 1.5 a
     // stage for tiles of 256 x 256, 4 + 0.62 for tiles of 128 x 128 with four stages in LDS; several parts: 3 for their sum, and each
     // part's results written and read at 4 TB/s.  E.g. 2048 x 2048 x 2048 38.8 us on small tiles, 62 on large ones, 52 on small ones in
     // two parts; 16384 x 256 x 256 from fp32 345 us in one part, 52 in sixteen.
-    const int stages = w.steps / kStageSteps * w.parts;
+    const int stages = w.steps / kStageSteps;
     const double t_part = (double)N * K * 8 / 4e6;
-    SplitModel small{stages, ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4), stages, 0.62, 4.0, 0.0, 3.0, t_part};
+    SplitModel small{stages, ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4), stages, w.parts > 1 ? 1.3 : 0.62, 4.0, 0.0, 3.0, t_part};
     SplitModel big{stages, ceil_div(w.n_blocks, 8) * ceil_div(w.k_blocks, 8), stages, 1.5, 6.0, 0.0, 3.0, t_part};
     const int s_small = cheapest_split(small), s_big = cheapest_split(big);
-    w.big = big.cost(s_big) < small.cost(s_small);
+    w.big = w.parts == 1 && big.cost(s_big) < small.cost(s_small);
     w.splits = w.big ? s_big : s_small;
     // A bfloat16 dY of whole 16-byte pieces can be read by the products as it is (what they reach of it at a time is within 31 bits): that
     // spares its way into tiles, and the fragments' transposing reads cost the products some.  us with it and without: 16384 x 8192 x 4096
@@ -324,8 +348,7 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     if (w.flat) p.dy = TileOperand{static_cast<const uint8_t*>(dY), nullptr, w.n_blocks, w.steps, lddy * 2, N * 2, M};
     else p.dy = TileOperand{o.dy_tiles, nullptr, w.n_blocks, w.steps * w.parts, 0, 0, 0};
     p.x = TileOperand{o.x_tiles, nullptr, w.k_blocks, w.steps, 0, 0, 0};
-    p.stages = w.steps / kStageSteps * w.parts;
-    p.x_stages = w.steps / kStageSteps;
+    p.stages = w.steps / kStageSteps;
     p.splits = w.splits;
     p.per_split = w.per_split;
     p.N = N;
@@ -335,8 +358,9 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     p.accumulate = accumulate;
     p.part = reinterpret_cast<float*>(ws + w.off_part);
     p.pitch = w.pitch;
-    if (w.flat) rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, true>(p, st) : launch_wgrad<2, 2, 2, 2, 4, true>(p, st);
-    else rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, false>(p, st) : launch_wgrad<2, 2, 2, 2, 4, false>(p, st);
+    if (w.parts > 1) rc = launch_wgrad<2, 2, 2, 2, 2, false, kParts>(p, st);
+    else if (w.flat) rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, true, 1>(p, st) : launch_wgrad<2, 2, 2, 2, 4, true, 1>(p, st);
+    else rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, false, 1>(p, st) : launch_wgrad<2, 2, 2, 2, 4, false, 1>(p, st);
     if (rc != DAQ_OK || w.splits == 1) return rc;
     DAQ_LAUNCH("ckpt8_wgrad_sum", st,
                hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, p.part, w.splits, N, K, w.pitch, dW, ldw, accumulate));

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_mx4_tiles(MatmulArgs p, int
     const int tm = (int)band * 4 + rest % high, tn = rest / high;
     const TileOperand r{p.a, p.a_scales, p.a_blocks, p.groups * 4, 0, 0, 0}, c{p.b, p.b_scales, p.b_blocks, p.groups * 4, 0, 0, 0};
     Product prod;
-    prod.run(r, c, tm * WR * RB, tn * WC * CB, 0, p.groups, p.groups, lds);
+    prod.run(r, c, tm * WR * RB, tn * WC * CB, 0, p.groups, lds);
     const int wave = threadIdx.x / kWave;
     const int64_t m0 = ((int64_t)tm * WR + wave / WC) * RB * 32, n0 = ((int64_t)tn * WC + wave % WC) * CB * 32;
     if (p.bf16) {

@@ -54,47 +54,50 @@ __device__ __forceinline__ void words_to_lds(__amdgpu_buffer_rsrc_t src, uint32_
 // `cb` of `c` on, summed over the stages s0 .. s1 - 1.  A stage of both operands is asked for while the SLOTS - 1 before it are multiplied,
 // straight into LDS, and the fragments of a step while the step before is multiplied, the first step of a stage among them:
 // the barrier stands before the last step's products, when that step's fragments are in registers already.
-// c_wrap: stages after which the second operand begins again.
-template <int WR, int WC, int RB, int CB, bool MX, int SLOTS = 2, bool FLAT = false>
+// PARTS: the first operand is the sum of so many, whose tiles of a step follow one another, the leading one first; the others' products
+// have sums of their own, which stay small, until the end.
+template <int WR, int WC, int RB, int CB, bool MX, int SLOTS = 2, bool FLAT = false, int PARTS = 1>
 struct TileProduct {
     static constexpr int kWaves = WR * WC;
-    static constexpr int kTiles = WR * RB + WC * CB;               // of a step
+    static constexpr int kTiles = WR * RB * PARTS + WC * CB;       // of a step
     static constexpr int kScales = MX ? kTiles * 256 : 0;          // bytes of a stage
     static constexpr int kStageBytes = kTiles * kStageSteps * 1024 + kScales;
     static constexpr int kLdsBytes = SLOTS * kStageBytes;
-    static constexpr int kShare = kTiles / kWaves;                    // operand row blocks that a wave fetches
+    static constexpr int kStrips = WR * RB * PARTS;                // of the first operand: strips of kStageSteps tiles of a row block
+    static constexpr int kShare = kTiles / kWaves;                 // strips that a wave fetches
     static constexpr int kAsks = kShare * (kStageSteps + (MX ? 1 : 0));   // requests of a wave for a stage
 
     // FLAT: a stage of the first operand lies in LDS as its 64 rows, 16-byte pieces of a row in the order piece ^ place(row): the fragment
     // reads, which transpose, take 64 bytes each of eight rows, four of them neighbours and four more eight on.
     static constexpr int kRowBytes = WR * RB * 64, kRowPieces = kRowBytes / 16, kRowsAsked = 1024 / kRowBytes;   // (a request is a KiB)
     static __device__ __forceinline__ int place(int row) { return ((row & 3) * 4 + (row & 8) * 2) & (kRowPieces - 1); }
-    static_assert(!FLAT || (!MX && (WR * RB) % kShare == 0), "a wave fetches of one operand only");
+    static_assert(!FLAT || (!MX && kStrips % kShare == 0), "a wave fetches of one operand only");
     static_assert(SLOTS == 2 || SLOTS == 4, "two or four stages in LDS");
-    static_assert(kTiles % kWaves == 0, "every wave fetches the same number of row blocks");
+    static_assert(kTiles % kWaves == 0, "every wave fetches the same number of strips");
+    static_assert(PARTS == 1 || (!MX && !FLAT), "parts are of bfloat16 tiles");
 
     v16f acc[CB][RB];
 
-    __device__ __forceinline__ void run(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, int c_wrap, uint8_t* lds) {
-        run_on(r, c, rb, cb, s0, s1, c_wrap, lds, lds + kStageBytes, lds + (SLOTS - 2) * kStageBytes, lds + (SLOTS - 1) * kStageBytes);
+    __device__ __forceinline__ void run(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, uint8_t* lds) {
+        run_on(r, c, rb, cb, s0, s1, lds, lds + kStageBytes, lds + (SLOTS - 2) * kStageBytes, lds + (SLOTS - 1) * kStageBytes);
     }
     // lds0 ..: the stages' places (the last two are not used where there are two).  They are arguments so that the compiler knows them
     // apart, and does not let a read of one wait for the requests into the others.
-    __device__ __forceinline__ void run_on(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, int c_wrap,
-                                           uint8_t* __restrict__ lds0, uint8_t* __restrict__ lds1, uint8_t* __restrict__ lds2, uint8_t* __restrict__ lds3) {
+    __device__ __forceinline__ void run_on(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, uint8_t* __restrict__ lds0,
+                                           uint8_t* __restrict__ lds1, uint8_t* __restrict__ lds2, uint8_t* __restrict__ lds3) {
         const int lane = threadIdx.x % kWave;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const int wr = wave / WC, wc = wave % WC;
-        // what this wave fetches: row blocks wave * kShare .. of the rows' WR * RB and the columns' WC * CB
+        // what this wave fetches: strips wave * kShare .. of the rows' kStrips and the columns' WC * CB
         __amdgpu_buffer_rsrc_t src[kShare], ssrc[kShare];
         bool of_c[kShare];
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
             const int t = wave * kShare + i;
-            of_c[i] = t >= WR * RB;
+            of_c[i] = t >= kStrips;
             const TileOperand& o = of_c[i] ? c : r;
-            const int64_t b = min(of_c[i] ? cb + t - WR * RB : rb + t, o.blocks - 1);     // (blocks behind the last one are not stored)
-            if (!FLAT || of_c[i]) src[i] = bytes_from(o.tiles + b * o.steps * 1024);
+            const int64_t b = min(of_c[i] ? cb + t - kStrips : rb + t / PARTS, o.blocks - 1);     // (blocks behind the last one are not stored)
+            if (!FLAT || of_c[i]) src[i] = bytes_from(o.tiles + (b * o.steps + (of_c[i] ? 0 : t % PARTS * kStageSteps)) * 1024);
             if constexpr (MX) ssrc[i] = bytes_from(o.scales + b * (o.steps / 4) * 256);
         }
         // FLAT: the rows of a stage that this wave asks for, request by request, and where in them a lane reads
@@ -119,16 +122,16 @@ struct TileProduct {
             }
 #pragma unroll
             for (int i = 0; i < kShare; ++i) {
-                const int st = of_c[i] ? (s >= 2 * c_wrap ? s - 2 * c_wrap : s >= c_wrap ? s - c_wrap : s) : s;
+                const uint32_t first = (uint32_t)s * (kStageSteps * 1024u) * (of_c[i] ? 1u : (uint32_t)PARTS);
                 uint8_t* at = to + (wave * kShare + i) * kStageSteps * 1024;
 #pragma unroll
-                for (int k = 0; k < kStageSteps; ++k) tile_to_lds(src[i], lane * 16, (uint32_t)(st * kStageSteps + k) * 1024u, at + k * 1024);
-                if constexpr (MX) words_to_lds(ssrc[i], lane * 4, (uint32_t)st * 256u, to + kTiles * kStageSteps * 1024 + (wave * kShare + i) * 256);
+                for (int k = 0; k < kStageSteps; ++k) tile_to_lds(src[i], lane * 16, first + k * 1024u, at + k * 1024);
+                if constexpr (MX) words_to_lds(ssrc[i], lane * 4, (uint32_t)s * 256u, to + kTiles * kStageSteps * 1024 + (wave * kShare + i) * 256);
             }
         };
-        v4i fr[2][RB], fc[2][CB];
+        v4i fr[2][PARTS][RB], fc[2][CB];
         int sr[2][RB], sc[2][CB];
-        const int at_r = wr * RB * kStageSteps * 1024 + lane * 16, at_c = (WR * RB + wc * CB) * kStageSteps * 1024 + lane * 16;
+        const int at_r = wr * RB * PARTS * kStageSteps * 1024 + lane * 16, at_c = (kStrips + wc * CB) * kStageSteps * 1024 + lane * 16;
         const int at_sr = kTiles * kStageSteps * 1024 + wr * RB * 256 + lane * 4, at_sc = kTiles * kStageSteps * 1024 + (WR * RB + wc * CB) * 256 + lane * 4;
         // FLAT: lane l takes column l % 16 of the 16 of its quarter wave and four rows at a time; the quarters are 16 columns and 8 rows apart
         int at_flat[RB];
@@ -170,7 +173,7 @@ struct TileProduct {
                         : "v"(at[0]), "v"(at[1]), "n"(kAt), "n"(kAt + 4 * kRowBytes)
                         : "memory");
 #pragma unroll
-                for (int i = 0; i < RB; ++i) fr[set][i] = __builtin_bit_cast(v4i, __builtin_shufflevector(part[2 * i], part[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                for (int i = 0; i < RB; ++i) fr[set][0][i] = __builtin_bit_cast(v4i, __builtin_shufflevector(part[2 * i], part[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };
         auto read = [&](const uint8_t* from, int k, int set, int sset) {
@@ -178,7 +181,10 @@ struct TileProduct {
             for (int i = 0; i < CB; ++i) fc[set][i] = *reinterpret_cast<const v4i*>(from + at_c + (i * kStageSteps + k) * 1024);
             if constexpr (!FLAT) {
 #pragma unroll
-                for (int i = 0; i < RB; ++i) fr[set][i] = *reinterpret_cast<const v4i*>(from + at_r + (i * kStageSteps + k) * 1024);
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q)
+                        fr[set][q][i] = *reinterpret_cast<const v4i*>(from + at_r + ((i * kStageSteps + k) * PARTS + q) * 1024);
             }
             if constexpr (MX) {
                 if (k == 0) {
@@ -189,19 +195,27 @@ struct TileProduct {
                 }
             }
         };
+        v16f small[PARTS > 1 ? CB : 1][PARTS > 1 ? RB : 1];
         auto multiply = [&](auto step, int set, int sset) {
 #pragma unroll
             for (int j = 0; j < CB; ++j)
 #pragma unroll
                 for (int i = 0; i < RB; ++i) {
-                    if constexpr (MX) acc[j][i] = mfma4<decltype(step)::value>(fc[set][j], fr[set][i], acc[j][i], sc[sset][j], sr[sset][i]);
-                    else acc[j][i] = mfma16(fc[set][j], fr[set][i], acc[j][i]);
+                    if constexpr (MX) acc[j][i] = mfma4<decltype(step)::value>(fc[set][j], fr[set][0][i], acc[j][i], sc[sset][j], sr[sset][i]);
+                    else acc[j][i] = mfma16(fc[set][j], fr[set][0][i], acc[j][i]);
+                    if constexpr (PARTS > 1) {
+#pragma unroll
+                        for (int q = PARTS - 1; q > 0; --q) small[j][i] = mfma16(fc[set][j], fr[set][q][i], small[j][i]);
+                    }
                 }
         };
 #pragma unroll
         for (int j = 0; j < CB; ++j)
 #pragma unroll
-            for (int i = 0; i < RB; ++i) acc[j][i] = v16f{};
+            for (int i = 0; i < RB; ++i) {
+                acc[j][i] = v16f{};
+                if constexpr (PARTS > 1) small[j][i] = v16f{};
+            }
         if (s0 >= s1) return;
         const int last = s1 - 1;
         ask(s0, lds0);
@@ -223,7 +237,7 @@ struct TileProduct {
                 read_flat(from, step, set);
             } else {
 #pragma unroll
-                for (int i = 0; i < RB * CB; ++i) {
+                for (int i = 0; i < RB * CB * PARTS; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // a matrix instruction
                     __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // an LDS read
                 }
@@ -265,6 +279,12 @@ struct TileProduct {
             if (s < s1) stage(s, lds0, lds1, 0);
             if (s + 1 < s1) stage(s + 1, lds1, lds2, 1);
             if (s + 2 < s1) stage(s + 2, lds2, lds3, 0);
+        }
+        if constexpr (PARTS > 1) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                for (int i = 0; i < RB; ++i) acc[j][i] += small[j][i];
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the requests past the end have landed before LDS is put to other use
     }
