@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
     __shared__ __attribute__((aligned(16))) uint8_t shares[4][4096];
     uint8_t* lds = shares[threadIdx.x / kWave];
     const int lane = threadIdx.x % kWave;
-    int64_t wave = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const bool of_dy = wave < p.dy_waves;
     if (!of_dy) wave -= p.dy_waves;
     if (!of_dy && wave >= p.x_waves) return;
@@ -93,7 +93,10 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
         const T* src = static_cast<const T*>(p.dy) + col;
         constexpr int kWords = sizeof(T) == 2 ? 2 : 4;
         uint32_t q[8][kWords];
-        if (col + 4 <= p.N) {
+        if (p.N >= 4) {
+            // (a lane at the last columns reads the last four, and moves its own to the front)
+            const int64_t from = min(col, p.N - 4);
+            src = static_cast<const T*>(p.dy) + from;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if constexpr (sizeof(T) == 2) {
@@ -105,17 +108,36 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
                     for (int i = 0; i < 4; ++i) q[j][i] = v[i];
                 }
             }
+            const int64_t d = col - from;
+            if (d > 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (sizeof(T) == 2) {
+                        const uint64_t v = d < 4 ? (((uint64_t)q[j][1] << 32) | q[j][0]) >> (16 * (d & 3)) : 0;
+                        q[j][0] = (uint32_t)v, q[j][1] = (uint32_t)(v >> 32);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t v = 0;
+#pragma unroll
+                            for (int k = 1; i + k < 4; ++k) v = d == k ? q[j][i + k] : v;
+                            q[j][i] = v;
+                        }
+                    }
+                }
+            }
         } else {
-            const int left = (int)max(p.N - col, (int64_t)0);
-            const T* last = static_cast<const T*>(p.dy) + p.N - 1;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 uint32_t e[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const T v = (i < left ? src + i : last)[row[j] * p.lddy];
-                    if constexpr (sizeof(T) == 2) e[i] = i < left ? v : 0u;
-                    else e[i] = i < left ? __float_as_uint(v) : 0u;
+                    e[i] = 0;
+                    if (col + i < p.N) {
+                        const T v = src[row[j] * p.lddy + i];
+                        if constexpr (sizeof(T) == 2) e[i] = v;
+                        else e[i] = __float_as_uint(v);
+                    }
                 }
                 if constexpr (sizeof(T) == 2) {
                     q[j][0] = e[0] | (e[1] << 16), q[j][1] = e[2] | (e[3] << 16);
