@@ -275,14 +275,8 @@ daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
     return DAQ_OK;
 }
 
-// Sizes of a call and where its workspace holds what.
-struct WgradPlan {
-    int n_blocks, k_blocks, steps, parts;   // parts: of a value of dY
-    bool flat;                              // dY as it is, not in tiles
-    bool big;                               // tiles of 256 x 256 instead of 128 x 128
-    int splits, per_split;
-    int64_t off_x, off_part, pitch, bytes;
-};
+}  // namespace
+
 WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, int dy_misaligned) {
     WgradPlan w{};
     w.n_blocks = (int)ceil_div(N, 32);
@@ -314,8 +308,6 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, i
     return w;
 }
 
-}  // namespace
-
 }  // namespace daq
 
 using namespace daq;
@@ -325,6 +317,8 @@ static daq_status wgrad_size(int64_t M, int64_t N, int64_t K) {
     daq_status rc = matrix_size(M, K);
     if (rc == DAQ_OK) rc = matrix_size(M, N);
     if (rc == DAQ_OK) rc = matrix_size(N, K);
+    // a row block's tiles are within 32 bits, with three parts of dY too
+    if (rc == DAQ_OK && ceil_div(M, kStageM) >= (int64_t)1 << 18) rc = DAQ_ERR_UNSUPPORTED;
     return rc;
 }
 

@@ -28,6 +28,21 @@ daq_status mx4_quantize_check(const void* src, int dtype, int64_t rows, int64_t 
 daq_status mx4_quantize(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, bool transpose, bool stochastic,
                         uint64_t seed, uint8_t* dst, hipStream_t st);
 
+// mx4_matmul.hip: the form of a product (row blocks of 32 of either operand, groups of 256 along k), and whether a linear layer's
+// workgroups quantize its rows themselves
+enum class MatmulForm { kFew, kDeep, kTwo, kBig };
+MatmulForm matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups);
+bool raw_rows(int64_t M, int64_t K, int dtype, int mode);
+// ckpt8_wgrad.hip: sizes of a weight gradient and where its workspace holds what
+struct WgradPlan {
+    int n_blocks, k_blocks, steps, parts;   // parts: of a value of dY
+    bool flat;                              // dY as it is, not in tiles
+    bool big;                               // tiles of 256 x 256 instead of 128 x 128
+    int splits, per_split;                  // parts of the tokens, and stages of one
+    int64_t off_x, off_part, pitch, bytes;
+};
+WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, int dy_misaligned);
+
 #if defined(__HIPCC__)
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

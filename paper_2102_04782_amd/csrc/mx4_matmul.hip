@@ -213,23 +213,22 @@ daq_status launch_few(const FewArgs& f, hipStream_t st) {
     return DAQ_OK;
 }
 
+}  // namespace
+
 // Which form a product takes: the one of the least time by what was measured of each (us, launch included).
 //   small products   2 + the longest of: 0.55 a group that a wave goes through; what the workgroups read at 19 TB/s (L2); B at 5 TB/s
 //   128 x 128 tiles  with four stages in LDS, a workgroup to a CU: 4 + 0.62 a group for every 256 tiles
 //   128 x 128 tiles  with two, two to a CU: 3.4 + 1.22 a group for every 512 tiles
 //   256 x 256 tiles  5.5 + 1.5 a group for every 256 tiles
 // e.g. 512 x 512 x 8192: 5.3, 18, 21, 42; 1777 x 2080 x 4096: 30, 13.9, 15.1, 26; 2048 x 4096 x 4096: -, 26, 24, 29;
-// 16384 x 8192 x 8192: -, 1020, 560, 490.
-enum class Form { kFew, kDeep, kTwo, kBig };
-Form matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups) {
+// 16384 x 8192 x 8192: -, -, 563, 490.
+MatmulForm matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups) {
     const double g = (double)groups, small = (double)(ceil_div(a_blocks, 4) * ceil_div(b_blocks, 4)), big = (double)(ceil_div(a_blocks, 8) * ceil_div(b_blocks, 8));
     const double few = a_blocks > 65535 ? 1e30 : 2.0 + std::max({0.55 * std::ceil(g / kFewWaves), (double)a_blocks * b_blocks * g * 8704 / 19e6, b_blocks * g * 4352 / 5e6});
     const double deep = std::ceil(small / 256) * (4.0 + 0.62 * g), two = std::ceil(small / 512) * (3.4 + 1.22 * g), wide = std::ceil(big / 256) * (5.5 + 1.5 * g);
     const double least = std::min({few, deep, two, wide});
-    return few == least ? Form::kFew : deep == least ? Form::kDeep : two == least ? Form::kTwo : Form::kBig;
+    return few == least ? MatmulForm::kFew : deep == least ? MatmulForm::kDeep : two == least ? MatmulForm::kTwo : MatmulForm::kBig;
 }
-
-}  // namespace
 
 // What the packed operands, the sizes and the result have to be.
 static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, const void* D, int dtype, int64_t ldd) {
@@ -239,6 +238,7 @@ static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, c
     if (rc == DAQ_OK) rc = matrix_size(M, N > 0 ? N : 1);
     if (rc != DAQ_OK) return rc;
     if (N <= 0) return DAQ_ERR_INVALID_ARG;
+    if (ceil_div(K, kMxGroup) >= (int64_t)1 << 20) return DAQ_ERR_UNSUPPORTED;   // a row block's tiles are within 32 bits
     if (M > 0 && (!B || !aligned256(B) || !D || !elem_aligned(D, dtype) || ldd < N)) return DAQ_ERR_INVALID_ARG;
     return DAQ_OK;
 }
@@ -246,7 +246,7 @@ static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, c
 // Whether the workgroups of the product quantize the rows themselves: nearest codes, one block a thread or two (bfloat16).  us with it and
 // in two launches: 1 x 8192 x 2048 4.4 and 6.8, 4 x 8192 x 8192 9.8 and 12.3, 16 x 2048 x 2048 4.3 and 5.8, from fp32 6.7 and 6.1;
 // 32 x 8192 x 2048 7.2 and 6.5.
-static bool raw_rows(int64_t M, int64_t K, int dtype, int mode) {
+bool raw_rows(int64_t M, int64_t K, int dtype, int mode) {
     return M <= 32 && mode == DAQ_ROUND_NEAREST && M * ceil_div(K, kMxGroup) * 8 * dtype_size(dtype) <= 2048;
 }
 
@@ -258,10 +258,10 @@ static daq_status mx4_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, 
     const MatmulArgs p{A, A + la.off_scales, B, B + lb.off_scales, M, N, la.row_blocks, lb.row_blocks, la.groups,
                        D, ldd, dtype == DAQ_BF16};
     switch (matmul_form(la.row_blocks, lb.row_blocks, la.groups)) {
-        case Form::kFew: return launch_few<void>(FewArgs{p, nullptr, 0, K}, st);
-        case Form::kDeep: return launch_tiles<2, 2, 2, 2, 4>(p, st);
-        case Form::kTwo: return launch_tiles<2, 2, 2, 2, 2>(p, st);
-        case Form::kBig: break;
+        case MatmulForm::kFew: return launch_few<void>(FewArgs{p, nullptr, 0, K}, st);
+        case MatmulForm::kDeep: return launch_tiles<2, 2, 2, 2, 4>(p, st);
+        case MatmulForm::kTwo: return launch_tiles<2, 2, 2, 2, 2>(p, st);
+        case MatmulForm::kBig: break;
     }
     return launch_tiles<2, 4, 4, 2, 2>(p, st);
 }
