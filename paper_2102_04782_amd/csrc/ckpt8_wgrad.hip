@@ -12,7 +12,7 @@ namespace daq {
 
 namespace {
 
-constexpr int kStageM = 16 * kStageSteps;   // tokens of a stage
+constexpr int kStageM = 16 * kGroupSteps;   // tokens of a stage
 constexpr int kParts = 3;                   // bfloat16 values that an fp32 value is the sum of
 
 struct OrderArgs {
@@ -25,7 +25,7 @@ struct OrderArgs {
     uint8_t* dy_tiles;
     uint8_t* x_tiles;
     int n_blocks, k_blocks;      // row blocks of 32 of either operand
-    int steps;                   // of 16 tokens, a multiple of kStageSteps
+    int steps;                   // of 16 tokens, a multiple of kGroupSteps
     int64_t dy_waves, x_waves;
 };
 
@@ -210,9 +210,9 @@ struct WgradArgs {
 
 // Tiles of 32 RB WR rows x 32 CB WC columns of dW, a workgroup each, for one part of the tokens.  Order of the workgroups as in the
 // 4-bit products; the parts of a tile are neighbours in it.
-template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT, int PARTS>
+template <int WR, int WC, int RB, int CB, bool FLAT, int PARTS>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
-    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT, PARTS>;
+    using Product = TileProduct<WR, WC, RB, CB, false, FLAT, PARTS>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int64_t b = (int64_t)(blockIdx.x % kXcd) * p.per_xcd + blockIdx.x / kXcd;
     const int64_t t = b / p.splits;
@@ -221,8 +221,9 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
     const int64_t band = t / (4 * p.tiles_k);
     const int rest = (int)(t - band * 4 * p.tiles_k), high = min(4, p.tiles_n - (int)band * 4);
     const int tn = (int)band * 4 + rest % high, tk = rest / high;
+    constexpr int kPer = kGroupSteps / Product::kSteps;   // the plan's stages are of four steps
     Product prod;
-    prod.run(p.dy, p.x, tn * WR * RB, tk * WC * CB, split * p.per_split, min(p.stages, (split + 1) * p.per_split), lds);
+    prod.run(p.dy, p.x, tn * WR * RB, tk * WC * CB, split * p.per_split * kPer, min(p.stages, (split + 1) * p.per_split) * kPer, lds);
     const int wave = threadIdx.x / kWave;
     const int64_t n0 = ((int64_t)tn * WR + wave / WC) * RB * 32, k0 = ((int64_t)tk * WC + wave % WC) * CB * 32;
     float* base = p.splits > 1 ? p.part + split * p.N * p.pitch : p.dw;
@@ -261,15 +262,15 @@ __global__ __launch_bounds__(256) void k_ckpt8_wgrad_sum(const float* part, int 
         if (k + i < K) z[i] = accumulate ? z[i] + sum[i] : sum[i];
 }
 
-template <int WR, int WC, int RB, int CB, int SLOTS, bool FLAT, int PARTS>
+template <int WR, int WC, int RB, int CB, bool FLAT, int PARTS>
 daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
-    using Product = TileProduct<WR, WC, RB, CB, false, SLOTS, FLAT, PARTS>;
+    using Product = TileProduct<WR, WC, RB, CB, false, FLAT, PARTS>;
     p.tiles_n = (int)ceil_div(p.dy.blocks, WR * RB);
     p.tiles_k = (int)ceil_div(p.x.blocks, WC * CB);
     const int64_t per = ceil_div((int64_t)p.tiles_n * p.tiles_k * p.splits, kXcd);
     if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
     p.per_xcd = (int)per;
-    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, SLOTS, FLAT, PARTS>;
+    const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, FLAT, PARTS>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("ckpt8_wgrad", st, hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcd)), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
     return DAQ_OK;
@@ -281,16 +282,16 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, i
     WgradPlan w{};
     w.n_blocks = (int)ceil_div(N, 32);
     w.k_blocks = (int)ceil_div(K, 32);
-    w.steps = (int)(ceil_div(M, kStageM) * kStageSteps);
+    w.steps = (int)(ceil_div(M, kStageM) * kGroupSteps);
     w.parts = dtype == DAQ_BF16 ? 1 : kParts;
-    // The form and the parts of the tokens that take the least time by what was measured of them (us): a workgroup to a CU, 6 + 1.5 a
-    // stage for tiles of 256 x 256, 4 + 0.62 for tiles of 128 x 128 with four stages in LDS; several parts: 3 for their sum, and each
-    // part's results written and read at 4 TB/s.  E.g. 2048 x 2048 x 2048 38.8 us on small tiles, 62 on large ones, 52 on small ones in
-    // two parts; 16384 x 256 x 256 from fp32 345 us in one part, 52 in sixteen.
-    const int stages = w.steps / kStageSteps;
+    // The form and the parts of the tokens that take the least time by what was measured of them (us): a workgroup to a CU, 6 + 1.7 a
+    // stage of 64 tokens for tiles of 256 x 256, 3.2 + 0.65 for tiles of 128 x 128 (1.3 with three parts of dY, which have that form
+    // only); several parts of the tokens: 3 for their sum, and each part's results written and read at 4 TB/s.  E.g. 2048 x 2048 x 2048
+    // 31.5 us on small tiles, 62 on large ones, 52 on small ones in two parts; 16384 x 256 x 256 from fp32 345 us in one part, 43 in 32.
+    const int stages = w.steps / kGroupSteps;
     const double t_part = (double)N * K * 8 / 4e6;
-    SplitModel small{stages, ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4), stages, w.parts > 1 ? 1.3 : 0.62, 4.0, 0.0, 3.0, t_part};
-    SplitModel big{stages, ceil_div(w.n_blocks, 8) * ceil_div(w.k_blocks, 8), stages, 1.5, 6.0, 0.0, 3.0, t_part};
+    SplitModel small{stages, ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4), stages, w.parts > 1 ? 1.3 : 0.65, 3.2, 0.0, 3.0, t_part};
+    SplitModel big{stages, ceil_div(w.n_blocks, 8) * ceil_div(w.k_blocks, 8), stages, 1.7, 6.0, 0.0, 3.0, t_part};
     const int s_small = cheapest_split(small), s_big = cheapest_split(big);
     w.big = w.parts == 1 && big.cost(s_big) < small.cost(s_small);
     w.splits = w.big ? s_big : s_small;
@@ -364,7 +365,7 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     if (w.flat) p.dy = TileOperand{static_cast<const uint8_t*>(dY), nullptr, w.n_blocks, w.steps, lddy * 2, N * 2, M};
     else p.dy = TileOperand{o.dy_tiles, nullptr, w.n_blocks, w.steps * w.parts, 0, 0, 0};
     p.x = TileOperand{o.x_tiles, nullptr, w.k_blocks, w.steps, 0, 0, 0};
-    p.stages = w.steps / kStageSteps;
+    p.stages = w.steps / kGroupSteps;
     p.splits = w.splits;
     p.per_split = w.per_split;
     p.N = N;
@@ -374,9 +375,9 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     p.accumulate = accumulate;
     p.part = reinterpret_cast<float*>(ws + w.off_part);
     p.pitch = w.pitch;
-    if (w.parts > 1) rc = launch_wgrad<2, 2, 2, 2, 2, false, kParts>(p, st);
-    else if (w.flat) rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, true, 1>(p, st) : launch_wgrad<2, 2, 2, 2, 4, true, 1>(p, st);
-    else rc = w.big ? launch_wgrad<2, 4, 4, 2, 2, false, 1>(p, st) : launch_wgrad<2, 2, 2, 2, 4, false, 1>(p, st);
+    if (w.parts > 1) rc = launch_wgrad<2, 2, 2, 2, false, kParts>(p, st);
+    else if (w.flat) rc = w.big ? launch_wgrad<2, 4, 4, 2, true, 1>(p, st) : launch_wgrad<2, 2, 2, 2, true, 1>(p, st);
+    else rc = w.big ? launch_wgrad<2, 4, 4, 2, false, 1>(p, st) : launch_wgrad<2, 2, 2, 2, false, 1>(p, st);
     if (rc != DAQ_OK || w.splits == 1) return rc;
     DAQ_LAUNCH("ckpt8_wgrad_sum", st,
                hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, p.part, w.splits, N, K, w.pitch, dW, ldw, accumulate));

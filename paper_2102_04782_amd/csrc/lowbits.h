@@ -30,7 +30,7 @@ daq_status mx4_quantize(const void* src, int dtype, int64_t rows, int64_t cols, 
 
 // mx4_matmul.hip: the form of a product (row blocks of 32 of either operand, groups of 256 along k), and whether a linear layer's
 // workgroups quantize its rows themselves
-enum class MatmulForm { kFew, kDeep, kTwo, kBig };
+enum class MatmulForm { kFew, kSmall, kBig };
 MatmulForm matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups);
 bool raw_rows(int64_t M, int64_t K, int dtype, int mode);
 // ckpt8_wgrad.hip: sizes of a weight gradient and where its workspace holds what

@@ -45,9 +45,9 @@ __device__ __forceinline__ void store4(const MatmulArgs& p, int64_t row, int64_t
 
 // Tiles of 32 RB WR x 32 CB WC results, a workgroup each.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles, in bands
 // of four row tiles, so that the 32 it holds at a time share twelve panels of the operands in its L2.
-template <int WR, int WC, int RB, int CB, int SLOTS>
+template <int WR, int WC, int RB, int CB>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_mx4_tiles(MatmulArgs p, int tiles_m, int tiles_n, int per_xcd) {
-    using Product = TileProduct<WR, WC, RB, CB, true, SLOTS>;
+    using Product = TileProduct<WR, WC, RB, CB, true>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int64_t t = (int64_t)(blockIdx.x % kXcd) * per_xcd + blockIdx.x / kXcd;
     if (t >= (int64_t)tiles_m * tiles_n) return;
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_mx4_tiles(MatmulArgs p, int
     const int tm = (int)band * 4 + rest % high, tn = rest / high;
     const TileOperand r{p.a, p.a_scales, p.a_blocks, p.groups * 4, 0, 0, 0}, c{p.b, p.b_scales, p.b_blocks, p.groups * 4, 0, 0, 0};
     Product prod;
-    prod.run(r, c, tm * WR * RB, tn * WC * CB, 0, p.groups, lds);
+    prod.run(r, c, tm * WR * RB, tn * WC * CB, 0, p.groups * (kGroupSteps / Product::kSteps), lds);
     const int wave = threadIdx.x / kWave;
     const int64_t m0 = ((int64_t)tm * WR + wave / WC) * RB * 32, n0 = ((int64_t)tn * WC + wave % WC) * CB * 32;
     if (p.bf16) {
@@ -88,12 +88,12 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_mx4_tiles(MatmulArgs p, int
     }
 }
 
-template <int WR, int WC, int RB, int CB, int SLOTS>
+template <int WR, int WC, int RB, int CB>
 daq_status launch_tiles(const MatmulArgs& p, hipStream_t st) {
-    using Product = TileProduct<WR, WC, RB, CB, true, SLOTS>;
+    using Product = TileProduct<WR, WC, RB, CB, true>;
     const int64_t tm = ceil_div(p.a_blocks, WR * RB), tn = ceil_div(p.b_blocks, WC * CB), per = ceil_div(tm * tn, kXcd);
     if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
-    const auto kernel = k_mx4_tiles<WR, WC, RB, CB, SLOTS>;
+    const auto kernel = k_mx4_tiles<WR, WC, RB, CB>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("mx4_tiles", st,
                hipLaunchKernelGGL(kernel, dim3((unsigned)(per * kXcd)), dim3(64 * WR * WC), Product::kLdsBytes, st, p, (int)tm, (int)tn, (int)per));
@@ -217,17 +217,16 @@ daq_status launch_few(const FewArgs& f, hipStream_t st) {
 
 // Which form a product takes: the one of the least time by what was measured of each (us, launch included).
 //   small products   2 + the longest of: 0.55 a group that a wave goes through; what the workgroups read at 19 TB/s (L2); B at 5 TB/s
-//   128 x 128 tiles  with four stages in LDS, a workgroup to a CU: 4 + 0.62 a group for every 256 tiles
-//   128 x 128 tiles  with two, two to a CU: 3.4 + 1.22 a group for every 512 tiles
-//   256 x 256 tiles  5.5 + 1.5 a group for every 256 tiles
-// e.g. 512 x 512 x 8192: 5.3, 18, 21, 42; 1777 x 2080 x 4096: 30, 13.9, 15.1, 26; 2048 x 4096 x 4096: -, 26, 24, 29;
-// 16384 x 8192 x 8192: -, -, 563, 490.
+//   128 x 128 tiles  up to a tile for each CU 3.2 + 0.55 a group; more, two to a CU: 3 + 1.17 a group for every 512
+//   256 x 256 tiles  6 + 1.7 a group for every 256
+// e.g. 512 x 512 x 8192: 5.3, 18, 41; 128 x 8192 x 8192: 18.6, 20, 44; 1777 x 2080 x 4096: 28, 12.4, 26; 2048 x 4096 x 4096: -, 22, 29;
+// 4096 x 4096 x 4096: -, 42, 35.5; 16384 x 8192 x 8192: -, 563, 484.
 MatmulForm matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups) {
     const double g = (double)groups, small = (double)(ceil_div(a_blocks, 4) * ceil_div(b_blocks, 4)), big = (double)(ceil_div(a_blocks, 8) * ceil_div(b_blocks, 8));
     const double few = a_blocks > 65535 ? 1e30 : 2.0 + std::max({0.55 * std::ceil(g / kFewWaves), (double)a_blocks * b_blocks * g * 8704 / 19e6, b_blocks * g * 4352 / 5e6});
-    const double deep = std::ceil(small / 256) * (4.0 + 0.62 * g), two = std::ceil(small / 512) * (3.4 + 1.22 * g), wide = std::ceil(big / 256) * (5.5 + 1.5 * g);
-    const double least = std::min({few, deep, two, wide});
-    return few == least ? MatmulForm::kFew : deep == least ? MatmulForm::kDeep : two == least ? MatmulForm::kTwo : MatmulForm::kBig;
+    const double tiles = small <= 256 ? 3.2 + 0.55 * g : std::ceil(small / 512) * (3.0 + 1.17 * g), wide = std::ceil(big / 256) * (6.0 + 1.7 * g);
+    const double least = std::min({few, tiles, wide});
+    return few == least ? MatmulForm::kFew : tiles == least ? MatmulForm::kSmall : MatmulForm::kBig;
 }
 
 // What the packed operands, the sizes and the result have to be.
@@ -259,11 +258,10 @@ static daq_status mx4_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, 
                        D, ldd, dtype == DAQ_BF16};
     switch (matmul_form(la.row_blocks, lb.row_blocks, la.groups)) {
         case MatmulForm::kFew: return launch_few<void>(FewArgs{p, nullptr, 0, K}, st);
-        case MatmulForm::kDeep: return launch_tiles<2, 2, 2, 2, 4>(p, st);
-        case MatmulForm::kTwo: return launch_tiles<2, 2, 2, 2, 2>(p, st);
+        case MatmulForm::kSmall: return launch_tiles<2, 2, 2, 2>(p, st);
         case MatmulForm::kBig: break;
     }
-    return launch_tiles<2, 4, 4, 2, 2>(p, st);
+    return launch_tiles<2, 4, 4, 2>(p, st);
 }
 
 }  // namespace daq

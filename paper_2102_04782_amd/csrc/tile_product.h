@@ -15,12 +15,12 @@ struct TileOperand {
     const uint8_t* tiles;
     const uint8_t* scales;
     int blocks;         // row blocks
-    int steps;          // of a row block, a multiple of kStageSteps
+    int steps;          // of a row block, a multiple of kGroupSteps
     // Or, for the first operand of bfloat16 products (FLAT), not tiles but the matrix itself, its columns being the rows of the
     // product: row m of the sum's axis is `width` bytes at tiles + m * pitch, for m < depth.  16-byte aligned, pitch included.
     int64_t pitch, width, depth;
 };
-constexpr int kStageSteps = 4;
+constexpr int kGroupSteps = 4;
 
 namespace {
 
@@ -51,38 +51,40 @@ __device__ __forceinline__ void words_to_lds(__amdgpu_buffer_rsrc_t src, uint32_
 }
 
 // The results of a workgroup of WR x WC waves, each RB x CB tiles of 32 x 32: rows from row block `rb` of `r` on, columns from row block
-// `cb` of `c` on, summed over the stages s0 .. s1 - 1.  A stage of both operands is asked for while the SLOTS - 1 before it are multiplied,
+// `cb` of `c` on, summed over the stages s0 .. s1 - 1.  A stage, two steps of both operands, is asked for while the three before it are multiplied,
 // straight into LDS, and the fragments of a step while the step before is multiplied, the first step of a stage among them:
 // the barrier stands before the last step's products, when that step's fragments are in registers already.
 // PARTS: the first operand is the sum of so many, whose tiles of a step follow one another, the leading one first; the others' products
 // have sums of their own, which stay small, until the end.
-template <int WR, int WC, int RB, int CB, bool MX, int SLOTS = 2, bool FLAT = false, int PARTS = 1>
+template <int WR, int WC, int RB, int CB, bool MX, bool FLAT = false, int PARTS = 1>
 struct TileProduct {
+    static constexpr int kSteps = 2, kSlots = 4;                   // steps of a stage, stages in LDS
     static constexpr int kWaves = WR * WC;
     static constexpr int kTiles = WR * RB * PARTS + WC * CB;       // of a step
-    static constexpr int kScales = MX ? kTiles * 256 : 0;          // bytes of a stage
-    static constexpr int kStageBytes = kTiles * kStageSteps * 1024 + kScales;
-    static constexpr int kLdsBytes = SLOTS * kStageBytes;
-    static constexpr int kStrips = WR * RB * PARTS;                // of the first operand: strips of kStageSteps tiles of a row block
+    static constexpr int kScales = MX ? kTiles * 256 : 0;          // bytes of a group's scale words, with the group's first stage
+    static constexpr int kStageBytes = kTiles * kSteps * 1024 + kScales;
+    static constexpr int kLdsBytes = kSlots * kStageBytes;
+    static constexpr int kStrips = WR * RB * PARTS;                // of the first operand: strips of two tiles of a row block
     static constexpr int kShare = kTiles / kWaves;                 // strips that a wave fetches
-    static constexpr int kAsks = kShare * (kStageSteps + (MX ? 1 : 0));   // requests of a wave for a stage
+    // whether stage i begins a group of scale words, and the requests of a wave for it
+    static constexpr bool begins(int i) { return MX && i % (kGroupSteps / kSteps) == 0; }
+    static constexpr int asks(int i) { return kShare * (kSteps + (begins(i) ? 1 : 0)); }
 
-    // FLAT: a stage of the first operand lies in LDS as its 64 rows, 16-byte pieces of a row in the order piece ^ place(row): the fragment
+    // FLAT: a stage of the first operand lies in LDS as its 32 rows, 16-byte pieces of a row in the order piece ^ place(row): the fragment
     // reads, which transpose, take 64 bytes each of eight rows, four of them neighbours and four more eight on.
     static constexpr int kRowBytes = WR * RB * 64, kRowPieces = kRowBytes / 16, kRowsAsked = 1024 / kRowBytes;   // (a request is a KiB)
     static __device__ __forceinline__ int place(int row) { return ((row & 3) * 4 + (row & 8) * 2) & (kRowPieces - 1); }
     static_assert(!FLAT || (!MX && kStrips % kShare == 0), "a wave fetches of one operand only");
-    static_assert(SLOTS == 2 || SLOTS == 4, "two or four stages in LDS");
     static_assert(kTiles % kWaves == 0, "every wave fetches the same number of strips");
     static_assert(PARTS == 1 || (!MX && !FLAT), "parts are of bfloat16 tiles");
 
     v16f acc[CB][RB];
 
     __device__ __forceinline__ void run(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, uint8_t* lds) {
-        run_on(r, c, rb, cb, s0, s1, lds, lds + kStageBytes, lds + (SLOTS - 2) * kStageBytes, lds + (SLOTS - 1) * kStageBytes);
+        run_on(r, c, rb, cb, s0, s1, lds, lds + kStageBytes, lds + 2 * kStageBytes, lds + 3 * kStageBytes);
     }
-    // lds0 ..: the stages' places (the last two are not used where there are two).  They are arguments so that the compiler knows them
-    // apart, and does not let a read of one wait for the requests into the others.
+    // lds0 ..: the stages' places.  They are arguments so that the compiler knows them apart, and does not let a read of one wait for the
+    // requests into the others.
     __device__ __forceinline__ void run_on(const TileOperand& r, const TileOperand& c, int rb, int cb, int s0, int s1, uint8_t* __restrict__ lds0,
                                            uint8_t* __restrict__ lds1, uint8_t* __restrict__ lds2, uint8_t* __restrict__ lds3) {
         const int lane = threadIdx.x % kWave;
@@ -97,42 +99,42 @@ struct TileProduct {
             of_c[i] = t >= kStrips;
             const TileOperand& o = of_c[i] ? c : r;
             const int64_t b = min(of_c[i] ? cb + t - kStrips : rb + t / PARTS, o.blocks - 1);     // (blocks behind the last one are not stored)
-            if (!FLAT || of_c[i]) src[i] = bytes_from(o.tiles + (b * o.steps + (of_c[i] ? 0 : t % PARTS * kStageSteps)) * 1024);
+            if (!FLAT || of_c[i]) src[i] = bytes_from(o.tiles + (b * o.steps + (of_c[i] ? 0 : t % PARTS * kSteps)) * 1024);
             if constexpr (MX) ssrc[i] = bytes_from(o.scales + b * (o.steps / 4) * 256);
         }
         // FLAT: the rows of a stage that this wave asks for, request by request, and where in them a lane reads
-        constexpr int kAskedRows = kShare * kStageSteps * kRowsAsked;
-        uint32_t flat_off[kShare * kStageSteps];
+        constexpr int kAskedRows = kShare * kSteps * kRowsAsked;
+        uint32_t flat_off[kShare * kSteps];
         if constexpr (FLAT) {
 #pragma unroll
-            for (int k = 0; k < kShare * kStageSteps; ++k) {
+            for (int k = 0; k < kShare * kSteps; ++k) {
                 const int in = lane / kRowPieces, row = wave * kAskedRows + k * kRowsAsked + in;
                 flat_off[k] = (uint32_t)(row * (int)r.pitch) + (uint32_t)((lane % kRowPieces) ^ place(row)) * 16u;
             }
         }
-        auto ask = [&](int s, uint8_t* to) {
+        auto ask = [&](int s, uint8_t* to, bool scales) {
             if (FLAT && !of_c[0]) {
                 // rows behind the last one are beyond the descriptor's end and read as zeros
-                const int64_t first = (int64_t)s * kStageSteps * 16 * r.pitch + (int64_t)rb * 64;
+                const int64_t first = (int64_t)s * kSteps * 16 * r.pitch + (int64_t)rb * 64;
                 const int64_t bytes = max((r.depth - 1) * r.pitch + r.width - first, (int64_t)0);
                 const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc((void*)(r.tiles + first), 0, (int)(uint32_t)min(bytes, (int64_t)0xFFFFFF00u), 0x00020000);
 #pragma unroll
-                for (int k = 0; k < kShare * kStageSteps; ++k) tile_to_lds(rows, flat_off[k], 0, to + (wave * kShare * kStageSteps + k) * 1024);
+                for (int k = 0; k < kShare * kSteps; ++k) tile_to_lds(rows, flat_off[k], 0, to + (wave * kShare * kSteps + k) * 1024);
                 return;
             }
 #pragma unroll
             for (int i = 0; i < kShare; ++i) {
-                const uint32_t first = (uint32_t)s * (kStageSteps * 1024u) * (of_c[i] ? 1u : (uint32_t)PARTS);
-                uint8_t* at = to + (wave * kShare + i) * kStageSteps * 1024;
+                const uint32_t first = (uint32_t)s * (kSteps * 1024u) * (of_c[i] ? 1u : (uint32_t)PARTS);
+                uint8_t* at = to + (wave * kShare + i) * kSteps * 1024;
 #pragma unroll
-                for (int k = 0; k < kStageSteps; ++k) tile_to_lds(src[i], lane * 16, first + k * 1024u, at + k * 1024);
-                if constexpr (MX) words_to_lds(ssrc[i], lane * 4, (uint32_t)s * 256u, to + kTiles * kStageSteps * 1024 + (wave * kShare + i) * 256);
+                for (int k = 0; k < kSteps; ++k) tile_to_lds(src[i], lane * 16, first + k * 1024u, at + k * 1024);
+                if (MX && scales) words_to_lds(ssrc[i], lane * 4, (uint32_t)s / (kGroupSteps / kSteps) * 256u, to + kTiles * kSteps * 1024 + (wave * kShare + i) * 256);
             }
         };
         v4i fr[2][PARTS][RB], fc[2][CB];
         int sr[2][RB], sc[2][CB];
-        const int at_r = wr * RB * PARTS * kStageSteps * 1024 + lane * 16, at_c = (kStrips + wc * CB) * kStageSteps * 1024 + lane * 16;
-        const int at_sr = kTiles * kStageSteps * 1024 + wr * RB * 256 + lane * 4, at_sc = kTiles * kStageSteps * 1024 + (WR * RB + wc * CB) * 256 + lane * 4;
+        const int at_r = wr * RB * PARTS * kSteps * 1024 + lane * 16, at_c = (kStrips + wc * CB) * kSteps * 1024 + lane * 16;
+        const int at_sr = kTiles * kSteps * 1024 + wr * RB * 256 + lane * 4, at_sc = kTiles * kSteps * 1024 + (WR * RB + wc * CB) * 256 + lane * 4;
         // FLAT: lane l takes column l % 16 of the 16 of its quarter wave and four rows at a time; the quarters are 16 columns and 8 rows apart
         int at_flat[RB];
         if constexpr (FLAT) {
@@ -176,18 +178,18 @@ struct TileProduct {
                 for (int i = 0; i < RB; ++i) fr[set][0][i] = __builtin_bit_cast(v4i, __builtin_shufflevector(part[2 * i], part[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };
-        auto read = [&](const uint8_t* from, int k, int set, int sset) {
+        auto read = [&](const uint8_t* from, int k, int set, bool scales, int sset) {
 #pragma unroll
-            for (int i = 0; i < CB; ++i) fc[set][i] = *reinterpret_cast<const v4i*>(from + at_c + (i * kStageSteps + k) * 1024);
+            for (int i = 0; i < CB; ++i) fc[set][i] = *reinterpret_cast<const v4i*>(from + at_c + (i * kSteps + k) * 1024);
             if constexpr (!FLAT) {
 #pragma unroll
                 for (int i = 0; i < RB; ++i)
 #pragma unroll
                     for (int q = 0; q < PARTS; ++q)
-                        fr[set][q][i] = *reinterpret_cast<const v4i*>(from + at_r + ((i * kStageSteps + k) * PARTS + q) * 1024);
+                        fr[set][q][i] = *reinterpret_cast<const v4i*>(from + at_r + ((i * kSteps + k) * PARTS + q) * 1024);
             }
             if constexpr (MX) {
-                if (k == 0) {
+                if (scales) {
 #pragma unroll
                     for (int i = 0; i < RB; ++i) sr[sset][i] = *reinterpret_cast<const int*>(from + at_sr + i * 256);
 #pragma unroll
@@ -218,15 +220,13 @@ struct TileProduct {
             }
         if (s0 >= s1) return;
         const int last = s1 - 1;
-        ask(s0, lds0);
-        ask(min(s0 + 1, last), lds1);
-        if constexpr (SLOTS == 4) {
-            ask(min(s0 + 2, last), lds2);
-            ask(min(s0 + 3, last), lds3);
-        }
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * kAsks) : "memory");
+        ask(s0, lds0, true);
+        ask(min(s0 + 1, last), lds1, begins(1));
+        ask(min(s0 + 2, last), lds2, begins(2));
+        ask(min(s0 + 3, last), lds3, begins(3));
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(asks(1) + asks(2) + asks(3)) : "memory");
         __builtin_amdgcn_s_barrier();
-        read(lds0, 0, 0, 0);
+        read(lds0, 0, 0, true, 0);
         read_flat(lds0, std::integral_constant<int, 0>{}, 0);
         // The reads of a step stand between the products of the step before, one each, from its beginning on: left to itself the compiler
         // moves them behind the last one, where every wave then waits for them.  (FLAT: the written ones do follow the products, and the
@@ -244,42 +244,30 @@ struct TileProduct {
             }
             __builtin_amdgcn_sched_barrier(0);
         };
-        // as many stages a round as there are places, so that these and the register sets have numbers known here
-        auto stage = [&](int s, uint8_t* here, uint8_t* next, int sset) {
-            read(here, 1, 1, sset);
-            multiply(std::integral_constant<int, 0>{}, 0, sset);
+        // as many stages a round as there are places, so that these, the register sets and the bytes of a scale word have numbers known here
+        auto stage = [&](int s, uint8_t* here, uint8_t* next, auto index) {
+            constexpr int kIndex = decltype(index)::value, kPer = kGroupSteps / kSteps, kScaleSet = kIndex / kPer & 1, kFirst = kIndex % kPer * kSteps;
+            read(here, 1, 1, false, 0);
+            multiply(std::integral_constant<int, kFirst>{}, 0, kScaleSet);
             then(here, std::integral_constant<int, 1>{}, 1);
-            read(here, 2, 0, sset);
-            multiply(std::integral_constant<int, 1>{}, 1, sset);
-            then(here, std::integral_constant<int, 2>{}, 0);
-            read(here, 3, 1, sset);
-            multiply(std::integral_constant<int, 2>{}, 0, sset);
-            then(here, std::integral_constant<int, 3>{}, 1);
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");   // the next stage has landed, this one is read out
+            // the next stage has landed, this one is read out
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(asks(kIndex + 2) + asks(kIndex + 3)) : "memory");
             __builtin_amdgcn_s_barrier();
-            read(next, 0, 0, sset ^ 1);
-            ask(min(s + SLOTS, last), here);
-            multiply(std::integral_constant<int, 3>{}, 1, sset);
+            read(next, 0, 0, begins(kIndex + 1), (kIndex + 1) / kPer & 1);
+            ask(min(s + kSlots, last), here, begins(kIndex));
+            multiply(std::integral_constant<int, kFirst + kSteps - 1>{}, 1, kScaleSet);
             then(next, std::integral_constant<int, 0>{}, 0);
         };
         int s = s0;
-        if constexpr (SLOTS == 2) {
-            for (; s + 1 < s1; s += 2) {
-                stage(s, lds0, lds1, 0);
-                stage(s + 1, lds1, lds0, 1);
-            }
-            if (s < s1) stage(s, lds0, lds1, 0);
-        } else {
-            for (; s + 3 < s1; s += 4) {
-                stage(s, lds0, lds1, 0);
-                stage(s + 1, lds1, lds2, 1);
-                stage(s + 2, lds2, lds3, 0);
-                stage(s + 3, lds3, lds0, 1);
-            }
-            if (s < s1) stage(s, lds0, lds1, 0);
-            if (s + 1 < s1) stage(s + 1, lds1, lds2, 1);
-            if (s + 2 < s1) stage(s + 2, lds2, lds3, 0);
+        for (; s + 3 < s1; s += 4) {
+            stage(s, lds0, lds1, std::integral_constant<int, 0>{});
+            stage(s + 1, lds1, lds2, std::integral_constant<int, 1>{});
+            stage(s + 2, lds2, lds3, std::integral_constant<int, 2>{});
+            stage(s + 3, lds3, lds0, std::integral_constant<int, 3>{});
         }
+        if (s < s1) stage(s, lds0, lds1, std::integral_constant<int, 0>{});
+        if (s + 1 < s1) stage(s + 1, lds1, lds2, std::integral_constant<int, 1>{});
+        if (s + 2 < s1) stage(s + 2, lds2, lds3, std::integral_constant<int, 2>{});
         if constexpr (PARTS > 1) {
 #pragma unroll
             for (int j = 0; j < CB; ++j)

@@ -15,8 +15,8 @@ static void products() {
     auto form = [](int64_t M, int64_t N, int64_t K) { return matmul_form(ceil_div(M, 32), ceil_div(N, 32), ceil_div(K, 256)); };
     for (int64_t M : {1, 13, 32, 64, 128}) EXPECT(form(M, 2048, 2048) == MatmulForm::kFew && form(M, 512, 8192) == MatmulForm::kFew);
     EXPECT(form(512, 512, 8192) == MatmulForm::kFew && form(200, 64, 8192) == MatmulForm::kFew && form(128, 8192, 8192) == MatmulForm::kFew);
-    EXPECT(form(512, 4096, 4096) == MatmulForm::kDeep && form(1777, 2080, 4096) == MatmulForm::kDeep && form(512, 8192, 8192) == MatmulForm::kDeep);
-    EXPECT(form(2048, 4096, 4096) == MatmulForm::kTwo);
+    EXPECT(form(512, 4096, 4096) == MatmulForm::kSmall && form(1777, 2080, 4096) == MatmulForm::kSmall && form(512, 8192, 8192) == MatmulForm::kSmall);
+    EXPECT(form(2048, 4096, 4096) == MatmulForm::kSmall);
     EXPECT(form(16384, 8192, 8192) == MatmulForm::kBig && form(4096, 4096, 4096) == MatmulForm::kBig && form(3000, 4096, 8192) == MatmulForm::kBig);
     EXPECT(form(((int64_t)1 << 31) - 1, 32, 256) != MatmulForm::kFew);   // a grid's second axis ends at 65535
     EXPECT(raw_rows(1, 8192, DAQ_BF16, DAQ_ROUND_NEAREST) && raw_rows(16, 2048, DAQ_BF16, DAQ_ROUND_NEAREST) && raw_rows(2, 8192, DAQ_FP32, DAQ_ROUND_NEAREST));
