@@ -316,8 +316,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream(stream) -> int:
-    if stream is None:   # the handle of the current stream, without a Stream object around it (2.9 against 0.4 us)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if stream is None:   # the handle of the current stream, without a Stream object around it (2.9 against 0.2 us)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream
 
 
@@ -711,21 +711,34 @@ def _matrix(t: torch.Tensor):
     return rows, cols, ld if rows > 1 else max(cols, 1), _DTYPES[t.dtype]
 
 
-def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype, like: torch.Tensor):
-    """(result, row stride, dtype code): ``out``, checked, or a new matrix on the device of ``like``."""
+def _bytes_on(stream, n: int, device) -> torch.Tensor:
+    """Device memory of the stream that the call runs on: given back, it is only handed out again behind the call."""
+    if stream is None:
+        return torch.empty(n, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype, like: torch.Tensor, stream):
+    """(result, row stride, dtype code): ``out``, checked, or a new matrix on the device of ``like``, in the order of ``stream``."""
     if out is None:
-        return torch.empty((rows, cols), dtype=dtype, device=like.device), max(cols, 1), _DTYPES[dtype]
+        if stream is None:
+            out = torch.empty(rows, cols, dtype=dtype, device=like.device)
+        else:
+            with torch.cuda.stream(stream):
+                out = torch.empty(rows, cols, dtype=dtype, device=like.device)
+        return out, max(cols, 1), _DTYPES[dtype]
     r, c, ld, code = _matrix(out)
     assert (r, c) == (rows, cols) and (dtype is None or out.dtype == dtype)
     return out, ld, code
 
 
-def alloc_mx4(rows: int, cols: int, device="cuda") -> Mx4:
-    return Mx4(torch.empty(layout_mx4(rows, cols).bytes, dtype=torch.uint8, device=device), rows, cols)
+def alloc_mx4(rows: int, cols: int, device="cuda", stream=None) -> Mx4:
+    return Mx4(_bytes_on(stream, layout_mx4(rows, cols).bytes, device), rows, cols)
 
 
-def alloc_ckpt8(rows: int, cols: int, parts: int = 1, device="cuda") -> Ckpt8:
-    return Ckpt8(torch.empty(layout_ckpt8(rows, cols, parts).bytes, dtype=torch.uint8, device=device), rows, cols, parts)
+def alloc_ckpt8(rows: int, cols: int, parts: int = 1, device="cuda", stream=None) -> Ckpt8:
+    return Ckpt8(_bytes_on(stream, layout_ckpt8(rows, cols, parts).bytes, device), rows, cols, parts)
 
 
 def mx4_quantize(x: torch.Tensor, transpose: bool = False, mode=ROUND_NEAREST, seed=0, out: Optional[Mx4] = None, stream=None) -> Mx4:
@@ -733,7 +746,7 @@ def mx4_quantize(x: torch.Tensor, transpose: bool = False, mode=ROUND_NEAREST, s
     rows, cols, ld, code = _matrix(x)
     r, c = (cols, rows) if transpose else (rows, cols)
     if out is None:
-        out = alloc_mx4(r, c, x.device)
+        out = alloc_mx4(r, c, x.device, stream)
     assert out.rows == r and out.cols == c
     _check(lib().daq_mx4_quantize(x.data_ptr(), code, rows, cols, ld, int(transpose), mode, seed, out.buf.data_ptr(), _stream(stream)),
            "daq_mx4_quantize")
@@ -742,7 +755,7 @@ def mx4_quantize(x: torch.Tensor, transpose: bool = False, mode=ROUND_NEAREST, s
 
 def mx4_dequantize(q: Mx4, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """daq_mx4_dequantize: the values that ``q`` holds, exact in either type (that of ``out`` where it is given)."""
-    out, ld, code = _result(out, q.rows, q.cols, dtype if out is None else None, q.buf)
+    out, ld, code = _result(out, q.rows, q.cols, dtype if out is None else None, q.buf, stream)
     _check(lib().daq_mx4_dequantize(q.buf.data_ptr(), q.rows, q.cols, out.data_ptr(), code, ld, _stream(stream)), "daq_mx4_dequantize")
     return out
 
@@ -751,9 +764,9 @@ def mx4_matmul(a: Mx4, b: Mx4, dtype=torch.bfloat16, out: Optional[torch.Tensor]
                stream=None) -> torch.Tensor:
     """daq_mx4_matmul: a b^T, [a.rows, b.rows], of ``dtype`` (or that of ``out``)."""
     assert a.cols == b.cols
-    out, ld, code = _result(out, a.rows, b.rows, dtype if out is None else None, b.buf)
+    out, ld, code = _result(out, a.rows, b.rows, dtype if out is None else None, b.buf, stream)
     if workspace is None:
-        workspace = _few_ws("daq_mx4_matmul_workspace", b.buf.device, a.rows, b.rows, a.cols)
+        workspace = _few_ws("daq_mx4_matmul_workspace", stream, b.buf.device, a.rows, b.rows, a.cols)
     _check(lib().daq_mx4_matmul(a.rows, b.rows, a.cols, a.buf.data_ptr(), b.buf.data_ptr(), out.data_ptr(), code, ld, _ptr(workspace),
                                 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_matmul")
     return out
@@ -765,9 +778,9 @@ def mx4_linear(x: torch.Tensor, w: Mx4, mode=ROUND_NEAREST, seed=0, dtype=None, 
     M, K, ldx, x_code = _matrix(x)
     N = w.rows
     assert K == w.cols
-    out, ldy, y_code = _result(out, M, N, (dtype or x.dtype) if out is None else dtype, x)
+    out, ldy, y_code = _result(out, M, N, (dtype or x.dtype) if out is None else dtype, x, stream)
     if workspace is None:
-        workspace = _few_ws("daq_mx4_linear_workspace", x.device, M, N, K, x_code, mode)
+        workspace = _few_ws("daq_mx4_linear_workspace", stream, x.device, M, N, K, x_code, mode)
     _check(lib().daq_mx4_linear(M, N, K, x.data_ptr(), x_code, ldx, mode, seed, w.buf.data_ptr(), out.data_ptr(), y_code, ldy, _ptr(workspace),
                                 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_linear")
     return out
@@ -780,10 +793,10 @@ def _few_ws_bytes(fn_name: str, *sizes) -> int:
     return n.value
 
 
-def _few_ws(fn_name: str, device, *sizes) -> Optional[torch.Tensor]:
+def _few_ws(fn_name: str, stream, device, *sizes) -> Optional[torch.Tensor]:
     """The workspace a call of these sizes needs, None where it needs none."""
     n = _few_ws_bytes(fn_name, *sizes)
-    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    return _bytes_on(stream, n, device) if n else None
 
 
 def ckpt8_save(x: torch.Tensor, parts: int = 1, out: Optional[Ckpt8] = None, stream=None) -> Ckpt8:
@@ -792,7 +805,7 @@ def ckpt8_save(x: torch.Tensor, parts: int = 1, out: Optional[Ckpt8] = None, str
     assert width % parts == 0
     cols = width // parts
     if out is None:
-        out = alloc_ckpt8(rows, cols, parts, x.device)
+        out = alloc_ckpt8(rows, cols, parts, x.device, stream)
     assert out.rows == rows and out.cols == cols and out.parts == parts
     _check(lib().daq_ckpt8_save(x.data_ptr(), code, rows, cols, parts, ld, out.buf.data_ptr(), _stream(stream)), "daq_ckpt8_save")
     return out
@@ -800,7 +813,7 @@ def ckpt8_save(x: torch.Tensor, parts: int = 1, out: Optional[Ckpt8] = None, str
 
 def ckpt8_restore(c: Ckpt8, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """daq_ckpt8_restore: the values that ``c`` holds, exact in either type (that of ``out`` where it is given)."""
-    out, ld, code = _result(out, c.rows, c.parts * c.cols, dtype if out is None else None, c.buf)
+    out, ld, code = _result(out, c.rows, c.parts * c.cols, dtype if out is None else None, c.buf, stream)
     _check(lib().daq_ckpt8_restore(c.buf.data_ptr(), c.rows, c.cols, c.parts, out.data_ptr(), code, ld, _stream(stream)), "daq_ckpt8_restore")
     return out
 
@@ -812,9 +825,9 @@ def ckpt8_act_forward(h: torch.Tensor, act: int, gated: bool = False, out: Optio
     parts = 2 if gated else 1
     assert width % parts == 0
     cols = width // parts
-    out, ldy, _ = _result(out, rows, cols, h.dtype, h)
+    out, ldy, _ = _result(out, rows, cols, h.dtype, h, stream)
     if ckpt is None:
-        ckpt = alloc_ckpt8(rows, cols, parts, h.device)
+        ckpt = alloc_ckpt8(rows, cols, parts, h.device, stream)
     assert ckpt.rows == rows and ckpt.cols == cols and ckpt.parts == parts
     _check(lib().daq_ckpt8_act_forward(h.data_ptr(), code, rows, cols, ldh, act, int(gated), out.data_ptr(), ldy, ckpt.buf.data_ptr(),
                                        _stream(stream)), "daq_ckpt8_act_forward")
@@ -827,7 +840,7 @@ def ckpt8_act_backward(dy: torch.Tensor, ckpt: Ckpt8, act: int, out: Optional[to
     8 bits."""
     rows, cols, lddy, code = _matrix(dy)
     assert rows == ckpt.rows and cols == ckpt.cols
-    out, lddh, _ = _result(out, rows, ckpt.parts * cols, dy.dtype, dy)
+    out, lddh, _ = _result(out, rows, ckpt.parts * cols, dy.dtype, dy, stream)
     assert y_ckpt is None or (y_ckpt.rows, y_ckpt.cols, y_ckpt.parts) == (rows, cols, 1)
     _check(lib().daq_ckpt8_act_backward(dy.data_ptr(), code, rows, cols, lddy, ckpt.buf.data_ptr(), act, int(ckpt.parts == 2), out.data_ptr(), lddh,
                                         None if y_ckpt is None else y_ckpt.buf.data_ptr(), _stream(stream)), "daq_ckpt8_act_backward")
@@ -839,9 +852,9 @@ def ckpt8_weight_grad(dy: torch.Tensor, x: Ckpt8, out: Optional[torch.Tensor] = 
     """daq_ckpt8_weight_grad: dy^T x^, fp32 [N, K]; ``accumulate`` adds it to ``out``."""
     M, N, lddy, code = _matrix(dy)
     assert x.parts == 1 and M == x.rows and (out is not None or not accumulate)
-    out, ldw, _ = _result(out, N, x.cols, torch.float32, dy)
+    out, ldw, _ = _result(out, N, x.cols, torch.float32, dy, stream)
     if workspace is None:
-        workspace = _few_ws("daq_ckpt8_weight_grad_workspace", dy.device, M, N, x.cols, code, lddy, dy.data_ptr() % 16)
+        workspace = _few_ws("daq_ckpt8_weight_grad_workspace", stream, dy.device, M, N, x.cols, code, lddy, dy.data_ptr() % 16)
     _check(lib().daq_ckpt8_weight_grad(M, N, x.cols, dy.data_ptr(), code, lddy, x.buf.data_ptr(), out.data_ptr(), ldw, int(accumulate),
                                        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_ckpt8_weight_grad")
     return out

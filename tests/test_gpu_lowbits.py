@@ -438,3 +438,22 @@ def test_the_example_learns(capsys):
     feed_forward.main(steps=41)
     said = [float(l.split()[-1]) for l in capsys.readouterr().out.splitlines() if l.startswith("step")]
     assert said[-1] < 0.75 * said[0]
+
+
+def test_results_and_workspaces_of_another_stream():
+    """Nothing is given: what a call allocates belongs to its stream, also while the current stream takes and fills memory of the same sizes."""
+    side = torch.cuda.Stream()
+    x, w, dy = _x(500, 1024, torch.bfloat16, 1).cuda(), _x(700, 1024, torch.bfloat16, 2).cuda(), _x(500, 700, torch.float32, 3).cuda()
+    h = _x(500, 1400, torch.bfloat16, 4).cuda()
+    y, kept = daq.ckpt8_act_forward(h, daq.ACT_GELU, gated=True)
+    want = (daq.mx4_linear(x, daq.mx4_quantize(w)), daq.ckpt8_weight_grad(dy, daq.ckpt8_save(x)), y, daq.ckpt8_act_backward(y, kept, daq.ACT_GELU))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        a = daq.mx4_linear(x, daq.mx4_quantize(w, stream=side), stream=side)
+        b = daq.ckpt8_weight_grad(dy, daq.ckpt8_save(x, stream=side), stream=side)
+        c, k = daq.ckpt8_act_forward(h, daq.ACT_GELU, gated=True, stream=side)
+        d = daq.ckpt8_act_backward(c, k, daq.ACT_GELU, stream=side)
+        for n in (1 << 18, 1 << 20, 3 << 20):
+            torch.empty(n, dtype=torch.uint8, device="cuda").fill_(0xEE)
+        side.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip((a, b, c, d), want))
