@@ -3,9 +3,11 @@
 // A decoded code is an integer of at most seven bits times a power of two, so X^ is exact in bfloat16 and the products run on the
 // bfloat16 matrix cores with fp32 sums.  An fp32 gradient is the sum of three bfloat16 values of eight bits each.
 //
-// Both operands have their summed axis, the tokens, outermost.  A first launch brings them into the order of the matrix
-// instructions (eight tokens of a column in 16 bytes), decoding X^ and splitting an fp32 dY on the way: it reads and writes each once,
-// 0.1 of the time of the products at 16384 x 8192 x 4096.  The products then run on whole KiB tiles.
+// Both operands have their summed axis, the tokens, outermost.  A first launch brings X^, and dY where the products do not read it as it is,
+// into the order of the matrix instructions (eight tokens of a column in 16 bytes), decoding the one and splitting an fp32 dY on
+// the way: each is read and written once, at 5.4 TB/s (X^ of 16384 x 4096 35 us, with a dY of 8192 columns 137).  The products then run on
+// whole KiB tiles: 16384 x 8192 x 4096 890-940 us, 1.2 PFLOP/s, against 1.85 of the same instructions on registers alone, both at
+// what clock the power limit leaves; torch's bfloat16 product of 8192 x 8192 x 8192 makes 1.2.
 #include "tile_product.h"
 
 namespace daq {
