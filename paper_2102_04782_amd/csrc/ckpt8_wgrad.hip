@@ -6,7 +6,7 @@
 // Both operands have their summed axis, the tokens, outermost.  A first launch brings X^, and dY where the products do not read it as it is,
 // into the order of the matrix instructions (eight tokens of a column in 16 bytes), decoding the one and splitting an fp32 dY on
 // the way: each is read and written once, at 5.4 TB/s (X^ of 16384 x 4096 35 us, with a dY of 8192 columns 137).  The products then run on
-// whole KiB tiles: 16384 x 8192 x 4096 890-940 us, 1.2 PFLOP/s, against 1.85 of the same instructions on registers alone, both at
+// whole KiB tiles: 16384 x 8192 x 4096 840-930 us, 1.2 to 1.3 PFLOP/s, against 1.85 of the same instructions on registers alone, both at
 // what clock the power limit leaves; torch's bfloat16 product of 8192 x 8192 x 8192 makes 1.2.
 #include "tile_product.h"
 
@@ -378,7 +378,7 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     p.part = reinterpret_cast<float*>(ws + w.off_part);
     p.pitch = w.pitch;
     if (w.parts > 1) rc = launch_wgrad<2, 2, 2, 2, false, kParts>(p, st);
-    else if (w.flat) rc = w.big ? launch_wgrad<2, 4, 4, 2, true, 1>(p, st) : launch_wgrad<2, 2, 2, 2, true, 1>(p, st);
+    else if (w.flat) rc = w.big ? launch_wgrad<4, 2, 2, 4, true, 1>(p, st) : launch_wgrad<2, 2, 2, 2, true, 1>(p, st);
     else rc = w.big ? launch_wgrad<2, 4, 4, 2, false, 1>(p, st) : launch_wgrad<2, 2, 2, 2, false, 1>(p, st);
     if (rc != DAQ_OK || w.splits == 1) return rc;
     DAQ_LAUNCH("ckpt8_wgrad_sum", st,

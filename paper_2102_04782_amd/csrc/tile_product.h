@@ -74,7 +74,7 @@ struct TileProduct {
     // reads, which transpose, take 64 bytes each of eight rows, four of them neighbours and four more eight on.
     static constexpr int kRowBytes = WR * RB * 64, kRowPieces = kRowBytes / 16, kRowsAsked = 1024 / kRowBytes;   // (a request is a KiB)
     static __device__ __forceinline__ int place(int row) { return ((row & 3) * 4 + (row & 8) * 2) & (kRowPieces - 1); }
-    static_assert(!FLAT || (!MX && kStrips % kShare == 0), "a wave fetches of one operand only");
+    static_assert(!FLAT || (!MX && RB == 2 && kStrips % kShare == 0), "two row blocks to a wave, which fetches of one operand only");
     static_assert(kTiles % kWaves == 0, "every wave fetches the same number of strips");
     static_assert(PARTS == 1 || (!MX && !FLAT), "parts are of bfloat16 tiles");
 
@@ -145,7 +145,8 @@ struct TileProduct {
                 at_flat[i] = row * kRowBytes + (piece ^ place(row)) * 16 + (lane & 1) * 8;
             }
         }
-        // FLAT: the transposing reads are written out, with their wait, as the compiler would have each wait for the requests under way
+        // FLAT: the transposing reads are written out, with their wait, as the compiler would have each wait for the requests under way.  Few of
+        // them to a wave: waves of 64 rows x 128 columns 884 us at 16384 x 8192 x 4096, of 128 x 64 896.
         auto read_flat = [&](const uint8_t* from, auto step, int set) {
             if constexpr (FLAT) {
                 typedef short v4s __attribute__((ext_vector_type(4)));
@@ -155,25 +156,13 @@ struct TileProduct {
                 uint32_t at[RB];
 #pragma unroll
                 for (int i = 0; i < RB; ++i) at[i] = base + (uint32_t)at_flat[i];
-                if constexpr (RB == 4)
-                    asm volatile(
-                        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
-                        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
-                        "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
-                        "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
-                        "s_waitcnt lgkmcnt(0)"
-                        : "=&v"(part[0]), "=&v"(part[1]), "=&v"(part[2]), "=&v"(part[3]), "=&v"(part[2 * RB - 4]), "=&v"(part[2 * RB - 3]),
-                          "=&v"(part[2 * RB - 2]), "=&v"(part[2 * RB - 1])
-                        : "v"(at[0]), "v"(at[1]), "v"(at[RB - 2]), "v"(at[RB - 1]), "n"(kAt), "n"(kAt + 4 * kRowBytes)
-                        : "memory");
-                else
-                    asm volatile(
-                        "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
-                        "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
-                        "s_waitcnt lgkmcnt(0)"
-                        : "=&v"(part[0]), "=&v"(part[1]), "=&v"(part[2]), "=&v"(part[3])
-                        : "v"(at[0]), "v"(at[1]), "n"(kAt), "n"(kAt + 4 * kRowBytes)
-                        : "memory");
+                asm volatile(
+                    "ds_read_b64_tr_b16 %0, %4 offset:%6\n\tds_read_b64_tr_b16 %1, %4 offset:%7\n\t"
+                    "ds_read_b64_tr_b16 %2, %5 offset:%6\n\tds_read_b64_tr_b16 %3, %5 offset:%7\n\t"
+                    "s_waitcnt lgkmcnt(0)"
+                    : "=&v"(part[0]), "=&v"(part[1]), "=&v"(part[2]), "=&v"(part[3])
+                    : "v"(at[0]), "v"(at[1]), "n"(kAt), "n"(kAt + 4 * kRowBytes)
+                    : "memory");
 #pragma unroll
                 for (int i = 0; i < RB; ++i) fr[set][0][i] = __builtin_bit_cast(v4i, __builtin_shufflevector(part[2 * i], part[2 * i + 1], 0, 1, 2, 3, 4, 5, 6, 7));
             }
