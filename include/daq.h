@@ -536,8 +536,8 @@ daq_status daq_clip_search(const daq_conv_desc* desc, const float* dY, float alp
  * alignment of their elements only; packed buffers are 256-byte aligned.  Sizes of zero rows (no tokens)
  * are legal: nothing is read, and what sums over them is zero.  Conventions as above: nothing is allocated
  * or synchronised, arguments are checked before anything is launched.  Sizes: up to 2^31 - 1 rows or
- * columns and 2^40 elements of a matrix, else DAQ_ERR_UNSUPPORTED; the same for launches of more workgroups
- * than a grid holds.
+ * columns and 2^40 elements of a matrix, for products fewer than 2^28 columns K, for weight gradients fewer
+ * than 2^24 tokens, else DAQ_ERR_UNSUPPORTED; the same for launches of more workgroups than a grid holds.
  *
  * Both formats share a power-of-two scale 2^(byte - 127) among 32 neighbours, so that decoding is exact in
  * bfloat16 and fp32 and products of decoded values need no rounding before their fp32 sums.  The byte is at

@@ -321,7 +321,7 @@ static daq_status wgrad_size(int64_t M, int64_t N, int64_t K) {
     if (rc == DAQ_OK) rc = matrix_size(M, N);
     if (rc == DAQ_OK) rc = matrix_size(N, K);
     // a row block's tiles are within 32 bits, with three parts of dY too
-    if (rc == DAQ_OK && ceil_div(M, kStageM) >= (int64_t)1 << 18) rc = DAQ_ERR_UNSUPPORTED;
+    if (rc == DAQ_OK && M >= (int64_t)1 << 24) rc = DAQ_ERR_UNSUPPORTED;
     return rc;
 }
 

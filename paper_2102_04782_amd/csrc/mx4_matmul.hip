@@ -241,7 +241,7 @@ static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, c
     if (rc == DAQ_OK) rc = matrix_size(M, N > 0 ? N : 1);
     if (rc != DAQ_OK) return rc;
     if (N <= 0) return DAQ_ERR_INVALID_ARG;
-    if (ceil_div(K, kMxGroup) >= (int64_t)1 << 20) return DAQ_ERR_UNSUPPORTED;   // a row block's tiles are within 32 bits
+    if (K >= (int64_t)1 << 28) return DAQ_ERR_UNSUPPORTED;   // a row block's tiles are within 32 bits
     if (M > 0 && (!B || !aligned256(B) || !D || !elem_aligned(D, dtype) || ldd < N)) return DAQ_ERR_INVALID_ARG;
     return DAQ_OK;
 }

@@ -101,7 +101,7 @@ def test_refusals_come_before_any_launch():
     assert v(src=None) == v(dst=None) == v(src=a + 16) == v(dst=odd) == v(ld=39) == v(dt=3) == v(r=-1) == v(c=-1) == INV and v(r=0) == v(c=0) == daq.OK
     m = lambda M=4, N=8, K=40, A=a, B=a, D=a, dt=0, ld=8, ws=None, wn=0: L.daq_mx4_matmul(M, N, K, A, B, D, dt, ld, ws, wn, None)
     assert m(A=None) == m(B=None) == m(D=None) == m(A=a + 16) == m(B=a + 16) == m(D=odd) == m(ld=7) == m(N=0) == m(K=0) == m(M=-1) == m(dt=9) == INV
-    assert m(M=0) == daq.OK
+    assert m(K=1 << 28) == UNS and m(M=1 << 31) == UNS and m(M=0) == daq.OK
     assert L.daq_mx4_matmul_workspace(4, 0, 4, C.byref(n)) == L.daq_mx4_matmul_workspace(4, 4, 4, None) == INV
     li = lambda M=64, N=8, K=40, X=a, xd=0, ldx=40, mode=0, W=a, Y=a, yd=0, ldy=8, ws=a, wn=1 << 30: L.daq_mx4_linear(M, N, K, X, xd, ldx, mode, 0, W, Y, yd, ldy, ws, wn, None)
     assert li(X=None) == li(W=None) == li(Y=None) == li(ldx=39) == li(ldy=7) == li(xd=2) == li(yd=2) == li(mode=3) == li(X=odd) == li(N=0) == INV
@@ -120,7 +120,7 @@ def test_refusals_come_before_any_launch():
     assert b(dy=None) == b(dh=None) == b(k=None) == b(dy=odd) == b(dh=odd) == b(k=a + 32) == b(yk=a + 32) == b(ld=39) == b(ldh=79) == b(act=-1) == b(dt=2) == INV
     assert b(r=0) == daq.OK
     g = lambda M=4, N=8, K=40, dy=a, dt=0, ld=8, x=a, dW=a, ldw=40, ws=a, wn=1 << 30: L.daq_ckpt8_weight_grad(M, N, K, dy, dt, ld, x, dW, ldw, 0, ws, wn, None)
-    assert g(dy=None) == g(x=None) == g(dW=None) == g(dy=odd) == g(dW=odd) == g(x=a + 32) == g(ld=7) == g(ldw=39) == g(N=0) == g(K=0) == g(M=-1) == g(dt=2) == INV
+    assert g(dy=None) == g(x=None) == g(dW=None) == g(dy=odd) == g(dW=odd) == g(x=a + 32) == g(ld=7) == g(ldw=39) == g(N=0) == g(K=0) == g(M=-1) == g(dt=2) == INV and g(M=1 << 24) == UNS
     assert L.daq_ckpt8_weight_grad_workspace(4, 4, 4, 5, 4, 0, C.byref(n)) == L.daq_ckpt8_weight_grad_workspace(4, 4, 4, 0, 4, -1, C.byref(n)) == INV
     assert L.daq_ckpt8_weight_grad_workspace(64, 64, 64, 1, 64, 0, C.byref(n)) == daq.OK
     assert g(M=64, N=64, K=64, dt=1, ld=64, ldw=64, ws=None, wn=0) == g(M=64, N=64, K=64, dt=1, ld=64, ldw=64, wn=n.value - 1) == WS
