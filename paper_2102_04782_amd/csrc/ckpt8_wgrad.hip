@@ -257,7 +257,15 @@ __global__ __launch_bounds__(256) void k_ckpt8_wgrad_sum(const float* part, int 
     const int64_t units = (K + 3) / 4, u = (int64_t)blockIdx.x * 256 + threadIdx.x, n = u / units, k = (u - n * units) * 4;
     if (n >= N) return;
     f32x4 sum = {0, 0, 0, 0};
-    for (int s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(part + (s * N + n) * pitch + k);
+    const float* from = part + n * pitch + k;
+    for (int s0 = 0; s0 < splits; s0 += 8) {   // eight parts asked for at a time
+        f32x4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const f32x4*>(from + min(s0 + i, splits - 1) * N * pitch);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (s0 + i < splits) sum += v[i];
+    }
     float* z = dw + n * ldw + k;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
