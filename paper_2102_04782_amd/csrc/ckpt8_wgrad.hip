@@ -28,7 +28,7 @@ struct OrderArgs {
     uint8_t* x_tiles;
     int n_blocks, k_blocks;      // row blocks of 32 of either operand
     int steps;                   // of 16 tokens, a multiple of kGroupSteps
-    int64_t dy_waves, x_waves;
+    uint32_t dy_groups;          // workgroups of dY
 };
 
 // x = hi + mid + lo, each the leading eight bits of what is left (a value that is not finite stays whole).
@@ -68,20 +68,18 @@ __device__ __forceinline__ void store_columns(uint8_t* lds, uint8_t* to, int64_t
     __builtin_amdgcn_wave_barrier();
 }
 
-// A wave takes 128 columns x 16 tokens of either operand, a lane four columns of eight tokens.
+// A workgroup takes 128 columns x 64 tokens of either operand, a wave 16 of the tokens, a lane four columns of eight tokens.
 template <typename T>
 __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
     __shared__ __attribute__((aligned(16))) uint8_t shares[4][4096];
     uint8_t* lds = shares[threadIdx.x / kWave];
     const int lane = threadIdx.x % kWave;
-    int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const bool of_dy = wave < p.dy_waves;
-    if (!of_dy) wave -= p.dy_waves;
-    if (!of_dy && wave >= p.x_waves) return;
+    const bool of_dy = blockIdx.x < p.dy_groups;
+    const uint32_t at = of_dy ? blockIdx.x : blockIdx.x - p.dy_groups;
     const int blocks = of_dy ? p.n_blocks : p.k_blocks;
-    const int wide = (blocks + 3) / 4;
-    const int64_t step = wave / wide;
-    const int b0 = (int)(wave - step * wide) * 4, nb = min(4, blocks - b0);     // row blocks of the tiles
+    const uint32_t wide = (uint32_t)(blocks + 3) / 4, stage = at / wide;
+    const int64_t step = (int64_t)stage * kGroupSteps + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int b0 = (int)(at - stage * wide) * 4, nb = min(4, blocks - b0);     // row blocks of the tiles
     const int64_t col = (int64_t)b0 * 32 + (lane % 32) * 4;
     const int64_t m0 = step * 16 + (lane / 32) * 8;
     const int64_t block_bytes = (int64_t)p.steps * 1024 * (of_dy && sizeof(T) == 4 ? kParts : 1);
@@ -175,12 +173,12 @@ __global__ __launch_bounds__(256) void k_ckpt8_order(OrderArgs p) {
             for (int k = 0; k < kParts; ++k) store_columns(lds, p.dy_tiles + b0 * block_bytes + (step * kParts + k) * 1024, block_bytes, nb, v[k]);
         }
     } else {
-        const int64_t at = col < p.pitch ? col : 0;      // (columns behind the last block are not stored)
+        const int64_t from = col < p.pitch ? col : 0;    // (columns behind the last block are not stored)
         uint32_t w[8], byte[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const uint32_t*>(p.codes + row[j] * p.pitch + at);
+        for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const uint32_t*>(p.codes + row[j] * p.pitch + from);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) byte[j] = p.scales[row[j] * (p.pitch / kMxBlock) + at / kMxBlock];
+        for (int j = 0; j < 8; ++j) byte[j] = p.scales[row[j] * (p.pitch / kMxBlock) + from / kMxBlock];
         u32x2 v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -364,11 +362,10 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     daq_ckpt8_layout L;
     daq_layout_ckpt8(M, K, 1, &L);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    OrderArgs o{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, ws, ws + w.off_x, w.n_blocks, w.k_blocks, w.steps, 0, 0};
-    o.dy_waves = w.flat ? 0 : round_up(ceil_div(w.n_blocks, 4) * w.steps, 4);
-    o.x_waves = ceil_div(w.k_blocks, 4) * w.steps;
-    const int64_t blocks = ceil_div(o.dy_waves + o.x_waves, 4);
+    OrderArgs o{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, ws, ws + w.off_x, w.n_blocks, w.k_blocks, w.steps, 0};
+    const int64_t stages = w.steps / kGroupSteps, dy_groups = w.flat ? 0 : stages * ceil_div(w.n_blocks, 4), blocks = dy_groups + stages * ceil_div(w.k_blocks, 4);
     if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;
+    o.dy_groups = (uint32_t)dy_groups;
     if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, st, o));
     else DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<float>, dim3((unsigned)blocks), dim3(256), 0, st, o));
     WgradArgs p{};
