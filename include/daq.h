@@ -631,7 +631,7 @@ daq_status daq_ckpt8_act_backward(const void* dy, daq_dtype dtype, int64_t rows,
  * bfloat16 values (its 24 bits).  accumulate != 0 adds to dW.
  *   dW         i/o  fp32 [N][K], row stride ldw
  *   workspace  of the bytes daq_ckpt8_weight_grad_workspace reports (dy_misaligned: the address of dY modulo 16; a bfloat16 dY
- *              of 16-byte aligned rows needs less); may be NULL where that is 0
+ *              of 16-byte aligned rows needs less); may be NULL where that is 0, as for no tokens and most small products
  * ------------------------------------------------------------------------------------------- */
 daq_status daq_ckpt8_weight_grad_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, int64_t lddy, int32_t dy_misaligned,
                                            size_t* bytes);

@@ -249,6 +249,178 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_ckpt8_wgrad(WgradArgs p) {
     });
 }
 
+// Small products: 64 x 64 results a workgroup for one part of the tokens, its eight waves sharing these, 16 at a time, everything straight
+// from memory and the next 16 tokens asked for while some are multiplied: one launch (two with several parts) and no tiles.  A lane reads
+// two neighbouring columns of eight tokens of either operand, so the tiles of 32 x 32 it holds are those of even and odd columns.  Its narrow
+// loads bound it, at 1.2 us a wave's step (2.0 from fp32): asking two steps ahead took 10 % longer, the scales of a step in one load the same.
+struct FewGradArgs {
+    const void* dy;
+    int64_t lddy;
+    const uint8_t* codes;
+    const uint8_t* scales;
+    int64_t pitch;
+    int64_t M, N, K;
+    int tiles_k;
+    int steps, per_split;    // of 16 tokens
+    float* out;              // dW, or the parts
+    int64_t ld, split_stride;
+    int accumulate;
+};
+constexpr int kFewWaves = 8, kFewGroups = 256;
+
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves) void k_ckpt8_wgrad_few(FewGradArgs p) {
+    constexpr int kOf = sizeof(T) == 4 ? kParts : 1, kWords = sizeof(T) / 2;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int half = lane / 32, l32 = lane % 32;
+    const uint32_t tile = blockIdx.x, tn = tile / (uint32_t)p.tiles_k, tk = tile - tn * (uint32_t)p.tiles_k;
+    const int64_t n0 = (int64_t)tn * 64, k0 = (int64_t)tk * 64;
+    // (a lane at the last column reads the last two and takes its own; one behind the last is not stored)
+    const int64_t cn = n0 + 2 * l32, cn_from = min(cn, p.N - 2), ck = min(k0 + 2 * l32, p.pitch - 2);
+    const bool second = cn == p.N - 1;
+    const T* dy = static_cast<const T*>(p.dy) + cn_from;
+    const uint8_t* codes = p.codes + ck;
+    const uint8_t* scales = p.scales + ck / kMxBlock;
+    struct Tokens {
+        uint32_t y[8][kWords], c[8], s[8];
+    };
+    auto load = [&](int step, Tokens& o) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t m = min((int64_t)step * 16 + half * 8 + j, p.M - 1);
+            if constexpr (sizeof(T) == 4) {
+                const u32x2_a4 q = *reinterpret_cast<const u32x2_a4*>(dy + m * p.lddy);
+                o.y[j][0] = q[0], o.y[j][1] = q[1];
+            } else {
+                o.y[j][0] = *reinterpret_cast<const u32_a2*>(dy + m * p.lddy);
+            }
+            o.c[j] = *reinterpret_cast<const uint16_t*>(codes + m * p.pitch);
+            o.s[j] = scales[m * (p.pitch / kMxBlock)];
+        }
+    };
+    v16f acc[2][2], small[kOf > 1 ? 2 : 1][kOf > 1 ? 2 : 1];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            acc[a][b] = v16f{};
+            if constexpr (kOf > 1) small[a][b] = v16f{};
+        }
+    const int s0 = blockIdx.y * p.per_split, s1 = min(p.steps, s0 + p.per_split);
+    Tokens cur, next;
+    if (s0 + wave < s1) load(s0 + wave, cur);
+    for (int step = s0 + wave; step < s1; step += kFewWaves) {
+        const bool more = step + kFewWaves < s1;
+        if (more) load(step + kFewWaves, next);
+        const int64_t m0 = (int64_t)step * 16 + half * 8;
+        if (m0 + 8 > p.M) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = m0 + j < p.M;
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) cur.y[j][w] = in ? cur.y[j][w] : 0u;
+                cur.s[j] = in ? cur.s[j] : 1u;
+                cur.c[j] = in ? cur.c[j] : 0u;
+            }
+        }
+        v4i x[2], y[kOf][2];
+        uint32_t xv[2][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float s = scale_of(cur.s[j]);
+            xv[0][j] = __float_as_uint((float)(int8_t)cur.c[j] * s);
+            xv[1][j] = __float_as_uint((float)(int8_t)(cur.c[j] >> 8) * s);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) x[b][i] = (int)__builtin_amdgcn_perm(xv[b][2 * i + 1], xv[b][2 * i], 0x07060302u);   // (exact: upper halves)
+        }
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) cur.y[j][0] = second ? cur.y[j][0] >> 16 : cur.y[j][0];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[0][0][i] = (int)__builtin_amdgcn_perm(cur.y[2 * i + 1][0], cur.y[2 * i][0], 0x05040100u);
+                y[0][1][i] = (int)__builtin_amdgcn_perm(cur.y[2 * i + 1][0], cur.y[2 * i][0], 0x07060302u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t h[2][kParts];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t v = b == 0 && second ? cur.y[2 * i + e][1] : cur.y[2 * i + e][b];
+                        split3(bits_as<float>(v), h[e][0], h[e][1], h[e][2]);
+                    }
+#pragma unroll
+                    for (int q = 0; q < kOf; ++q) y[q][b][i] = (int)(h[0][q] | (h[1][q] << 16));
+                }
+        }
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                acc[a][b] = mfma16(x[a], y[0][b], acc[a][b]);
+                if constexpr (kOf > 1) {
+#pragma unroll
+                    for (int q = kOf - 1; q > 0; --q) small[a][b] = mfma16(x[a], y[q][b], small[a][b]);
+                }
+            }
+        if (more) cur = next;
+    }
+    if constexpr (kOf > 1) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) acc[a][b] += small[a][b];
+    }
+    // The waves' sums meet in LDS, first those of the last four with those of the first four, then these four.  A wave's share: [n][k], 16-byte
+    // pieces of a row in the order piece ^ row / 2 % 16.
+    auto piece = [&](int w, int row, int at) { return reinterpret_cast<f32x4*>(lds + w * 16384 + row * 256 + ((at ^ (row >> 1)) & 15) * 16); };
+    auto each = [&](auto use) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) use(b, q, e, 2 * l32 + b, q * 4 + half * 2 + e);
+    };
+    if (wave >= 4)
+        each([&](int b, int q, int e, int row, int at) {
+            *piece(wave - 4, row, at) = f32x4{acc[0][b][4 * q + 2 * e], acc[1][b][4 * q + 2 * e], acc[0][b][4 * q + 2 * e + 1], acc[1][b][4 * q + 2 * e + 1]};
+        });
+    __syncthreads();
+    if (wave < 4)
+        each([&](int b, int q, int e, int row, int at) {
+            f32x4* z = piece(wave, row, at);
+            *z = f32x4{acc[0][b][4 * q + 2 * e], acc[1][b][4 * q + 2 * e], acc[0][b][4 * q + 2 * e + 1], acc[1][b][4 * q + 2 * e + 1]} + *z;
+        });
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = i * 512 + threadIdx.x, row = at / 16;
+        const int64_t n = n0 + row, k = k0 + (at % 16) * 4;
+        if (n >= p.N || k >= p.K) continue;
+        f32x4 v = *piece(0, row, at % 16);
+#pragma unroll
+        for (int w = 1; w < 4; ++w) v += *piece(w, row, at % 16);
+        float* z = p.out + blockIdx.y * p.split_stride + n * p.ld + k;
+        if (k + 4 <= p.K) {
+            u32x4_a4* q = reinterpret_cast<u32x4_a4*>(z);
+            if (p.accumulate) v += __builtin_bit_cast(f32x4, (u32x4)*q);
+            *q = __builtin_bit_cast(u32x4, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (k + e < p.K) z[e] = p.accumulate ? z[e] + v[e] : v[e];
+        }
+    }
+}
+
 // Sums of the parts, in their order; no parts: zeros.
 __global__ __launch_bounds__(256) void k_ckpt8_wgrad_sum(const float* part, int splits, int64_t N, int64_t K, int64_t pitch, float* dw, int64_t ldw,
                                                          int accumulate) {
@@ -292,10 +464,23 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, i
     w.k_blocks = (int)ceil_div(K, 32);
     w.steps = (int)(ceil_div(M, kStageM) * kGroupSteps);
     w.parts = dtype == DAQ_BF16 ? 1 : kParts;
+    w.pitch = round_up(K, 4);
+    // Small products go without tiles while a workgroup to a CU leaves a wave eight steps at most; a part of the tokens has two steps a wave
+    // or more, as its sum is a launch (4 us).  us without tiles and with: 64 x 64 x 64 4.5 and 7.9 (fp32 5.1 and 10.2), 1000 x 800 x 600 13.9
+    // and 17.6 (20.3 and 25.9), 4096 x 256 x 256 11.7 and 16.1 (13.8 and 26.1), 16384 x 64 x 512 15.6 and 25.1 (20.6 and 30.8); past the
+    // rule 1531 x 607 x 1100 30.9 and 29.0 from fp32, 2048 x 1024 x 1024 25.7 and 24.6, 100 x 4000 x 4000 56 and 21.  Two columns are read at a time.
+    const int64_t few_tiles = ceil_div(N, 64) * ceil_div(K, 64), few_steps = ceil_div(M, 16);
+    if (N >= 2 && few_tiles <= kFewGroups && few_tiles * few_steps <= kFewGroups * kFewWaves * 8) {
+        w.few = true;
+        w.per_split = (int)ceil_div(few_steps, std::max<int64_t>(1, std::min<int64_t>(kFewGroups / few_tiles, few_steps / (2 * kFewWaves))));
+        w.splits = (int)ceil_div(few_steps, w.per_split);
+        w.bytes = w.splits > 1 ? round_up((int64_t)w.splits * N * w.pitch * 4, 256) : 0;
+        return w;
+    }
     // The form and the parts of the tokens that take the least time by what was measured of them (us): a workgroup to a CU, 6 + 1.7 a
     // stage of 64 tokens for tiles of 256 x 256, 3.2 + 0.65 for tiles of 128 x 128 (1.3 with three parts of dY, which have that form
     // only); several parts of the tokens: 3 for their sum, and each part's results written and read at 4 TB/s.  E.g. 2048 x 2048 x 2048
-    // 31.5 us on small tiles, 62 on large ones, 52 on small ones in two parts; 16384 x 256 x 256 from fp32 345 us in one part, 43 in 32.
+    // 31.5 us on small tiles, 62 on large ones, 52 on small ones in two parts; 16384 x 256 x 256 from fp32 345 us in one part, 34 in 32.
     const int stages = w.steps / kGroupSteps;
     const double t_part = (double)N * K * 8 / 4e6;
     SplitModel small{stages, ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4), stages, w.parts > 1 ? 1.3 : 0.65, 3.2, 0.0, 3.0, t_part};
@@ -310,7 +495,6 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, i
     w.flat = dtype == DAQ_BF16 && dy_misaligned == 0 && lddy % 8 == 0 && N % 8 == 0 && lddy < ((int64_t)1 << 24) && K <= (w.big ? 8192 : 1024);
     w.per_split = (int)ceil_div(stages, w.splits);
     w.splits = (int)ceil_div(stages, w.per_split);
-    w.pitch = round_up(K, 4);
     w.off_x = w.flat ? 0 : (int64_t)w.n_blocks * w.steps * w.parts * 1024;
     w.off_part = w.off_x + (int64_t)w.k_blocks * w.steps * 1024;
     w.bytes = w.off_part + (w.splits > 1 ? round_up((int64_t)w.splits * N * w.pitch * 4, 256) : 0);
@@ -358,10 +542,26 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
         return DAQ_OK;
     }
     const WgradPlan w = wgrad_plan(M, N, K, dtype, lddy, (int)((uintptr_t)dY & 15u));
-    if (!workspace || workspace_bytes < (size_t)w.bytes || !aligned256(workspace)) return DAQ_ERR_WORKSPACE;
+    if (w.bytes > 0 && (!workspace || workspace_bytes < (size_t)w.bytes || !aligned256(workspace))) return DAQ_ERR_WORKSPACE;
     daq_ckpt8_layout L;
     daq_layout_ckpt8(M, K, 1, &L);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
+    if (w.few) {
+        const int64_t tiles_k = ceil_div(K, 64), tiles = ceil_div(N, 64) * tiles_k;
+        if (!grid_ok(tiles)) return DAQ_ERR_UNSUPPORTED;
+        const bool parts = w.splits > 1;
+        const FewGradArgs f{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, K, (int)tiles_k, (int)ceil_div(M, 16), w.per_split,
+                            parts ? reinterpret_cast<float*>(ws) : dW, parts ? w.pitch : ldw, N * w.pitch, parts ? 0 : accumulate};
+        const dim3 grid((unsigned)tiles, (unsigned)w.splits);
+        constexpr int kLds = 4 * 16384;
+        if (!allow_lds(dtype == DAQ_BF16 ? (const void*)k_ckpt8_wgrad_few<uint16_t> : (const void*)k_ckpt8_wgrad_few<float>, kLds)) return DAQ_ERR_HIP;
+        if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_wgrad_few", st, hipLaunchKernelGGL(k_ckpt8_wgrad_few<uint16_t>, grid, dim3(64 * kFewWaves), kLds, st, f));
+        else DAQ_LAUNCH("ckpt8_wgrad_few", st, hipLaunchKernelGGL(k_ckpt8_wgrad_few<float>, grid, dim3(64 * kFewWaves), kLds, st, f));
+        if (parts)
+            DAQ_LAUNCH("ckpt8_wgrad_sum", st,
+                       hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, f.out, w.splits, N, K, w.pitch, dW, ldw, accumulate));
+        return DAQ_OK;
+    }
     OrderArgs o{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, ws, ws + w.off_x, w.n_blocks, w.k_blocks, w.steps, 0};
     const int64_t stages = w.steps / kGroupSteps, dy_groups = w.flat ? 0 : stages * ceil_div(w.n_blocks, 4), blocks = dy_groups + stages * ceil_div(w.k_blocks, 4);
     if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;

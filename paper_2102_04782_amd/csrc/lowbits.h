@@ -36,6 +36,7 @@ bool raw_rows(int64_t M, int64_t K, int dtype, int mode);
 // ckpt8_wgrad.hip: sizes of a weight gradient and where its workspace holds what
 struct WgradPlan {
     int n_blocks, k_blocks, steps, parts;   // parts: of a value of dY
+    bool few;                               // small products, no tiles: per_split is of 16 tokens then
     bool flat;                              // dY as it is, not in tiles
     bool big;                               // tiles of 256 x 256 instead of 128 x 128
     int splits, per_split;                  // parts of the tokens, and stages of one

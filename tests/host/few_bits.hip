@@ -32,12 +32,19 @@ static void weight_gradients() {
     EXPECT(!c.big && c.splits > 8 && !c.flat && c.parts == 3);
     EXPECT(!plan(16384, 8191, 4096, DAQ_BF16).flat && !wgrad_plan(16384, 8192, 4096, DAQ_BF16, 8193, 0).flat && !wgrad_plan(16384, 8192, 4096, DAQ_BF16, 8192, 2).flat &&
            !plan(16384, 8192, 4096, DAQ_FP32).flat);
-    // every stage belongs to a part, none of which is empty, and the workspace's pieces follow one another
+    EXPECT(c.few && !a.few && !b.few && plan(1, 2, 1, DAQ_FP32).few && !plan(1, 1, 1, DAQ_FP32).few && !plan(100, 4000, 4000, DAQ_BF16).few);
+    // every stage (step, without tiles) belongs to a part, none of which is empty, and the workspace's pieces follow one another
     for (int64_t M : {1, 63, 64, 65, 1000, 16384, 100000})
         for (int64_t N : {1, 40, 607, 4096})
             for (int64_t K : {1, 33, 1100, 4096})
                 for (int dtype : {DAQ_FP32, DAQ_BF16}) {
                     const WgradPlan w = plan(M, N, K, dtype);
+                    if (w.few) {
+                        const int64_t steps = (M + 15) / 16, tiles = ((N + 63) / 64) * ((K + 63) / 64);
+                        EXPECT((int64_t)w.splits * w.per_split >= steps && (int64_t)(w.splits - 1) * w.per_split < steps && w.splits * tiles <= 256);
+                        EXPECT(w.bytes >= (w.splits > 1 ? (int64_t)w.splits * N * w.pitch * 4 : 0) && w.pitch >= K && w.pitch % 4 == 0);
+                        continue;
+                    }
                     const int64_t stages = w.steps / 4;
                     EXPECT(w.steps % 4 == 0 && stages * 64 >= M && (int64_t)w.splits * w.per_split >= stages && (int64_t)(w.splits - 1) * w.per_split < stages);
                     EXPECT(w.off_x == (w.flat ? 0 : (int64_t)w.n_blocks * w.steps * w.parts * 1024) && w.off_part == w.off_x + (int64_t)w.k_blocks * w.steps * 1024);

@@ -347,6 +347,24 @@ def test_weight_grad_large(M, N, K, pad, dtype):
     assert torch.equal(got, daq.ckpt8_weight_grad(dy, kept))
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K,pad", [(300, 1, 70, 0), (9001, 70, 33, 0), (4100, 65, 129, 2), (17, 1030, 1000, 1), (271, 2, 2, 0), (3001, 610, 1101, 2), (5001, 520, 400, 8),
+                                       (40, 1500, 1400, 0), (300, 1101, 1090, 1), (2050, 1032, 1000, 0)])
+def test_weight_grad_forms(M, N, K, pad, dtype):
+    """Both sides of the sizes at which the products stop reading their operands as they are, and added to what is there."""
+    wide = _x(M, N + pad, dtype, 11).cuda()
+    dy, kept = wide[:, pad:], daq.ckpt8_save(_x(M, K, torch.bfloat16, 12).cuda())
+    xs = daq.ckpt8_restore(kept).double()
+    d = dy.double().t().contiguous()
+    exact, absolute = d @ xs, d.abs() @ xs.abs()
+    got = daq.ckpt8_weight_grad(dy, kept)
+    steps = (3 if dtype == torch.float32 else 1) * -(-M // 16)
+    assert bool(((got.double() - exact).abs() <= (steps + 10) * 2.0 ** -23 * absolute + 1e-40).all())
+    kept_out = torch.full((N, K + 3), 2.0, device="cuda")
+    daq.ckpt8_weight_grad(dy, kept, out=kept_out[:, 1:1 + K], accumulate=True)
+    assert torch.equal(kept_out[:, 1:1 + K], got + 2) and bool((kept_out[:, 0] == 2).all()) and bool((kept_out[:, 1 + K:] == 2).all())
+
+
 def test_offsets_beyond_32_bits():
     """More than 2^31 elements, twice as many bytes: the last rows are what they are alone."""
     rows, cols, tail = 66000, 32800, 40

@@ -122,5 +122,6 @@ def test_refusals_come_before_any_launch():
     g = lambda M=4, N=8, K=40, dy=a, dt=0, ld=8, x=a, dW=a, ldw=40, ws=a, wn=1 << 30: L.daq_ckpt8_weight_grad(M, N, K, dy, dt, ld, x, dW, ldw, 0, ws, wn, None)
     assert g(dy=None) == g(x=None) == g(dW=None) == g(dy=odd) == g(dW=odd) == g(x=a + 32) == g(ld=7) == g(ldw=39) == g(N=0) == g(K=0) == g(M=-1) == g(dt=2) == INV and g(M=1 << 24) == UNS
     assert L.daq_ckpt8_weight_grad_workspace(4, 4, 4, 5, 4, 0, C.byref(n)) == L.daq_ckpt8_weight_grad_workspace(4, 4, 4, 0, 4, -1, C.byref(n)) == INV
-    assert L.daq_ckpt8_weight_grad_workspace(64, 64, 64, 1, 64, 0, C.byref(n)) == daq.OK
-    assert g(M=64, N=64, K=64, dt=1, ld=64, ldw=64, ws=None, wn=0) == g(M=64, N=64, K=64, dt=1, ld=64, ldw=64, wn=n.value - 1) == WS
+    assert L.daq_ckpt8_weight_grad_workspace(64, 64, 64, 1, 64, 0, C.byref(n)) == daq.OK and n.value == 0
+    assert L.daq_ckpt8_weight_grad_workspace(2048, 2048, 64, 1, 2048, 0, C.byref(n)) == daq.OK and n.value > 0
+    assert g(M=2048, N=2048, K=64, dt=1, ld=2048, ldw=64, ws=None, wn=0) == g(M=2048, N=2048, K=64, dt=1, ld=2048, ldw=64, wn=n.value - 1) == WS
