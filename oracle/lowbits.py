@@ -116,7 +116,7 @@ def ckpt8_buffer(codes, byte):
     return buf
 
 
-_erf = np.vectorize(math.erf, otypes=[np.float64])
+_erfc = np.vectorize(math.erfc, otypes=[np.float64])
 
 
 def act(x, name):
@@ -125,5 +125,5 @@ def act(x, name):
     if name == "silu":
         s = 1 / (1 + np.exp(-x))
         return x * s, s + x * s * (1 - s)
-    cdf = 0.5 * (1 + _erf(x / math.sqrt(2)))
+    cdf = 0.5 * _erfc(-x / math.sqrt(2))   # (1 + erf cancels far below zero)
     return x * cdf, cdf + x * np.exp(-x * x / 2) / math.sqrt(2 * math.pi)

@@ -475,3 +475,36 @@ def test_results_and_workspaces_of_another_stream():
             torch.empty(n, dtype=torch.uint8, device="cuda").fill_(0xEE)
         side.synchronize()
         assert all(torch.equal(p, q) for p, q in zip((a, b, c, d), want))
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_gelu_keeps_its_tail(gated):
+    """Relative to the value itself where Phi(x) is far below one.  With u = 2^-24: x / sqrt 2 is off by 1.5 u (its constant and its rounding), which
+    the complementary error function makes x^2 + 1 times as much of, its own error is 32 u at most, and six products and sums follow; the
+    exponential's argument is off by 1.5 u of x^2 / 2.  Where the function leaves the normal range, by one of the smallest normal values."""
+    u = 2.0 ** -24
+    x = torch.cat((torch.linspace(-9, -3, 40 * 64), -torch.tensor([9.5, 10, 11, 12, 12.5, 13, 14, 20, 40, 1e4] * 6 + [9.0] * 4))).view(41, 64)
+    parts = 2 if gated else 1
+    h = torch.cat([x, torch.linspace(0.5, 3, x.numel()).view_as(x)][:parts], 1)
+    dy = torch.linspace(-2, 1, x.numel()).view_as(x)
+    y, kept = daq.ckpt8_act_forward(h.cuda(), daq.ACT_GELU, gated=gated)
+    hv, hs, d = _np(h), _saved(h, parts), _np(dy)
+    up, us = (hv[:, 64:], hs[:, 64:]) if gated else (1.0, 1.0)
+
+    def bound(x, size):
+        with np.errstate(over="ignore"):
+            return (1.5 * x * x + 40) * u * size
+
+    want = ref.act(hv[:, :64], "gelu")[0] * up
+    assert np.all(np.abs(_np(y) - want) <= bound(hv[:, :64], np.abs(want)) + np.abs(hv[:, :64] * up) * 2.0 ** -126)
+    yk = daq.alloc_ckpt8(41, 64)
+    dh = _np(daq.ckpt8_act_backward(dy.cuda(), kept, daq.ACT_GELU, y_ckpt=yk))
+    g = hs[:, :64]
+    f, slope = ref.act(g, "gelu")
+    density = np.exp(-g * g / 2) / np.sqrt(2 * np.pi)
+    terms = np.abs(slope - g * density) + np.abs(g) * density
+    assert np.all(np.abs(dh[:, :64] - d * us * slope) <= np.abs(d * us) * (bound(g, terms) + (1 + np.abs(g)) * 2.0 ** -126) + 2.0 ** -126)
+    if gated:
+        assert np.all(np.abs(dh[:, 64:] - d * f) <= bound(g, np.abs(d * f)) + np.abs(d * g) * 2.0 ** -126 + 2.0 ** -126)
+    step = np.repeat(np.exp2(ref.ckpt8_codes(f * us)[1] - 127.0), 32, axis=1)
+    assert np.all(np.abs(_np(daq.ckpt8_restore(yk)) - f * us) <= 1.01 * step)

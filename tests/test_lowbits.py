@@ -125,3 +125,18 @@ def test_refusals_come_before_any_launch():
     assert L.daq_ckpt8_weight_grad_workspace(64, 64, 64, 1, 64, 0, C.byref(n)) == daq.OK and n.value == 0
     assert L.daq_ckpt8_weight_grad_workspace(2048, 2048, 64, 1, 2048, 0, C.byref(n)) == daq.OK and n.value > 0
     assert g(M=2048, N=2048, K=64, dt=1, ld=2048, ldw=64, ws=None, wn=0) == g(M=2048, N=2048, K=64, dt=1, ld=2048, ldw=64, wn=n.value - 1) == WS
+
+
+def test_oracle_gelu_keeps_its_tail():
+    """Far below zero against the continued fraction Phi(-t) = phi(t) / (t + 1 / (t + 2 / (t + 3 / ...))).  With u = 2^-53: t / sqrt 2 is off by two
+    units, which erfc makes t^2 + 1 times as many of; t^2 / 2 by one, which the exponential makes t^2 / 2 times as many of; the functions and the
+    fraction are good to 16 units together.  The slope is a difference whose terms are at most 5/4 of it."""
+    t = np.linspace(3, 30, 271)
+    f = t.copy()
+    for k in range(400, 0, -1):
+        f = t + k / f
+    phi = np.exp(-t * t / 2) / np.sqrt(2 * np.pi)
+    y, slope = ref.act(-t, "gelu")
+    rel = (3 * t * t + 18) * 2.0 ** -53
+    assert np.all(np.abs(y + t * phi / f) <= rel * t * phi / f)
+    assert np.all(np.abs(slope - (phi / f - t * phi)) <= 2 * rel * t * phi)
