@@ -225,10 +225,13 @@ daq_status launch_few(const FewArgs& f, hipStream_t st) {
 //   256 x 256 tiles  6 + 1.7 a group for every 256
 // e.g. 512 x 512 x 8192: 5.3, 18, 41; 128 x 8192 x 8192: 18.6, 20, 44; 1777 x 2080 x 4096: 28, 12.4, 26; 2048 x 4096 x 4096: -, 22, 29;
 // 4096 x 4096 x 4096: -, 42, 35.5; 16384 x 8192 x 8192: -, 563, 484.
+// Tiles end where a descriptor does: one group more, and the last columns of a row block would read as zeros.
 MatmulForm matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups) {
     const double g = (double)groups, small = (double)(ceil_div(a_blocks, 4) * ceil_div(b_blocks, 4)), big = (double)(ceil_div(a_blocks, 8) * ceil_div(b_blocks, 8));
     const double few = a_blocks > 65535 ? 1e30 : 2.0 + std::max({0.55 * std::ceil(g / kFewWaves), (double)a_blocks * b_blocks * g * 8704 / 19e6, b_blocks * g * 4352 / 5e6});
-    const double tiles = small <= 256 ? 3.2 + 0.55 * g : std::ceil(small / 512) * (3.0 + 1.17 * g), wide = std::ceil(big / 256) * (6.0 + 1.7 * g);
+    const bool reached = groups * kGroupSteps * 1024 <= (int64_t)kTileReach;
+    const double tiles = !reached ? 1e30 : small <= 256 ? 3.2 + 0.55 * g : std::ceil(small / 512) * (3.0 + 1.17 * g);
+    const double wide = !reached ? 1e30 : std::ceil(big / 256) * (6.0 + 1.7 * g);
     const double least = std::min({few, tiles, wide});
     return few == least ? MatmulForm::kFew : tiles == least ? MatmulForm::kSmall : MatmulForm::kBig;
 }
@@ -241,7 +244,7 @@ static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, c
     if (rc == DAQ_OK) rc = matrix_size(M, N > 0 ? N : 1);
     if (rc != DAQ_OK) return rc;
     if (N <= 0) return DAQ_ERR_INVALID_ARG;
-    if (K >= (int64_t)1 << 28) return DAQ_ERR_UNSUPPORTED;   // a row block's tiles are within 32 bits
+    if (K >= (int64_t)1 << 28) return DAQ_ERR_UNSUPPORTED;   // what is counted along k is within 32 bits
     if (M > 0 && (!B || !aligned256(B) || !D || !elem_aligned(D, dtype) || ldd < N)) return DAQ_ERR_INVALID_ARG;
     return DAQ_OK;
 }

@@ -21,6 +21,7 @@ struct TileOperand {
     int64_t pitch, width, depth;
 };
 constexpr int kGroupSteps = 4;
+constexpr uint32_t kTileReach = 0xFFFFFF00u;   // bytes that one descriptor reaches: of a row block's tiles, or of a stage's rows
 
 namespace {
 
@@ -40,7 +41,7 @@ __device__ __forceinline__ v16f mfma16(v4i x, v4i y, v16f c) {
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_from(const uint8_t* base) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)0xFFFFFF00u, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)kTileReach, 0x00020000);
 }
 // 16 or 4 bytes of every lane to consecutive places of LDS, without registers in between.
 __device__ __forceinline__ void tile_to_lds(__amdgpu_buffer_rsrc_t src, uint32_t lane_off, uint32_t off, uint8_t* dst) {
@@ -117,7 +118,7 @@ struct TileProduct {
                 // rows behind the last one are beyond the descriptor's end and read as zeros
                 const int64_t first = (int64_t)s * kSteps * 16 * r.pitch + (int64_t)rb * 64;
                 const int64_t bytes = max((r.depth - 1) * r.pitch + r.width - first, (int64_t)0);
-                const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc((void*)(r.tiles + first), 0, (int)(uint32_t)min(bytes, (int64_t)0xFFFFFF00u), 0x00020000);
+                const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc((void*)(r.tiles + first), 0, (int)(uint32_t)min(bytes, (int64_t)kTileReach), 0x00020000);
 #pragma unroll
                 for (int k = 0; k < kShare * kSteps; ++k) tile_to_lds(rows, flat_off[k], 0, to + (wave * kShare * kSteps + k) * 1024);
                 return;

@@ -9,3 +9,8 @@ from test_host_logic import _run_host_program
 @pytest.mark.skipif(shutil.which("hipcc") is None, reason="no hipcc")
 def test_forms_of_few_bit_products(tmp_path):
     _run_host_program("few_bits.hip", tmp_path, "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops")
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None, reason="no hipcc")
+def test_limits_of_few_bit_products(tmp_path):
+    _run_host_program("few_bits_limits.hip", tmp_path, "--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops")
