@@ -41,7 +41,7 @@ bool rows_grid(int64_t rows, int64_t pitch, Rows& r, dim3& grid) {
     r.shift = 2;
     while (r.shift < 8 && ((int64_t)1 << r.shift) < r.units) ++r.shift;
     const int64_t x = ceil_div(rows, (int64_t)1 << (8 - r.shift)), y = ceil_div(r.units, (int64_t)1 << r.shift);
-    if (!grid_ok(x) || y > 65535) return false;
+    if (!grid_ok(x, kBlock) || y > 65535) return false;
     grid = dim3((unsigned)x, (unsigned)y);
     return true;
 }

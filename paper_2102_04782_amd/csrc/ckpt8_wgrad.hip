@@ -448,7 +448,6 @@ daq_status launch_wgrad(WgradArgs p, hipStream_t st) {
     p.tiles_n = (int)ceil_div(p.dy.blocks, WR * RB);
     p.tiles_k = (int)ceil_div(p.x.blocks, WC * CB);
     const int64_t per = ceil_div((int64_t)p.tiles_n * p.tiles_k * p.splits, kXcd);
-    if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
     p.per_xcd = (int)per;
     const auto kernel = k_ckpt8_wgrad<WR, WC, RB, CB, FLAT, PARTS>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
@@ -535,10 +534,11 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     if (M > 0 && (!dY || !elem_aligned(dY, dtype) || lddy < N || !x_ckpt || !aligned256(x_ckpt))) return DAQ_ERR_INVALID_ARG;
     hipStream_t st = (hipStream_t)stream;
     const int64_t sum_blocks = ceil_div(N * ceil_div(K, 4), 256);
-    if (!grid_ok(sum_blocks)) return DAQ_ERR_UNSUPPORTED;
+    const bool sum_fits = grid_ok(sum_blocks, 256);
     if (M == 0) {   // a sum of nothing
-        if (!accumulate)
-            DAQ_LAUNCH("ckpt8_wgrad_sum", st, hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, nullptr, 0, N, K, 0, dW, ldw, 0));
+        if (accumulate) return DAQ_OK;
+        if (!sum_fits) return DAQ_ERR_UNSUPPORTED;
+        DAQ_LAUNCH("ckpt8_wgrad_sum", st, hipLaunchKernelGGL(k_ckpt8_wgrad_sum, dim3((unsigned)sum_blocks), dim3(256), 0, st, nullptr, 0, N, K, 0, dW, ldw, 0));
         return DAQ_OK;
     }
     const WgradPlan w = wgrad_plan(M, N, K, dtype, lddy, (int)((uintptr_t)dY & 15u));
@@ -548,7 +548,6 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (w.few) {
         const int64_t tiles_k = ceil_div(K, 64), tiles = ceil_div(N, 64) * tiles_k;
-        if (!grid_ok(tiles)) return DAQ_ERR_UNSUPPORTED;
         const bool parts = w.splits > 1;
         const FewGradArgs f{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, K, (int)tiles_k, (int)ceil_div(M, 16), w.per_split,
                             parts ? reinterpret_cast<float*>(ws) : dW, parts ? w.pitch : ldw, N * w.pitch, parts ? 0 : accumulate};
@@ -564,7 +563,8 @@ extern "C" daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, con
     }
     OrderArgs o{dY, lddy, x_ckpt, x_ckpt + L.off_scales, L.pitch, M, N, ws, ws + w.off_x, w.n_blocks, w.k_blocks, w.steps, 0};
     const int64_t stages = w.steps / kGroupSteps, dy_groups = w.flat ? 0 : stages * ceil_div(w.n_blocks, 4), blocks = dy_groups + stages * ceil_div(w.k_blocks, 4);
-    if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;
+    const int64_t edge = w.big ? 8 : 4, tiles = round_up(ceil_div(w.n_blocks, edge) * ceil_div(w.k_blocks, edge) * w.splits, kXcd);
+    if (!grid_ok(blocks, 256) || !grid_ok(tiles, w.big ? 512 : 256) || (w.splits > 1 && !sum_fits)) return DAQ_ERR_UNSUPPORTED;
     o.dy_groups = (uint32_t)dy_groups;
     if (dtype == DAQ_BF16) DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, st, o));
     else DAQ_LAUNCH("ckpt8_order", st, hipLaunchKernelGGL(k_ckpt8_order<float>, dim3((unsigned)blocks), dim3(256), 0, st, o));

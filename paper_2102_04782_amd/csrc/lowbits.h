@@ -20,8 +20,8 @@ inline daq_status matrix_size(int64_t rows, int64_t cols) {
     if (rows > most || cols > most || rows * cols > kMaxElems) return DAQ_ERR_UNSUPPORTED;
     return DAQ_OK;
 }
-// Workgroups along the first axis of a grid.
-inline bool grid_ok(int64_t blocks) { return blocks < ((int64_t)1 << 31); }
+// Workgroups along the first axis of a grid: a launch takes fewer than 2^32 threads along one.
+inline bool grid_ok(int64_t blocks, int threads) { return blocks * threads < ((int64_t)1 << 32); }
 
 // mx4.hip: src to its packed form, and what its arguments have to be
 daq_status mx4_quantize_check(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, int mode);

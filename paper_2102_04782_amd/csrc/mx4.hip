@@ -213,7 +213,7 @@ daq_status mx4_quantize(const void* src, int dtype, int64_t rows, int64_t cols, 
     if (L.bytes == 0) return DAQ_OK;
     PackArgs p{src, ld, rows, cols, dst, dst + L.off_scales, L.row_blocks, L.groups, (uint32_t)round_keys(seed), (uint32_t)((cols + 1) / 2)};
     const int64_t blocks = transpose ? ceil_div(L.row_blocks, 2) * L.groups : (int64_t)L.row_blocks * L.groups;
-    if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;
+    if (!grid_ok(blocks, 256)) return DAQ_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)blocks), block(256);
 #define DAQ_MX4_PACK(KERNEL, NAME)                                                                                          \
     do {                                                                                                                    \
@@ -279,7 +279,7 @@ extern "C" daq_status daq_mx4_dequantize(const uint8_t* src, int64_t rows, int64
     daq_mx4_layout L;
     daq_layout_mx4(rows, cols, &L);
     const int64_t blocks = (int64_t)L.row_blocks * L.groups;
-    if (!grid_ok(blocks)) return DAQ_ERR_UNSUPPORTED;
+    if (!grid_ok(blocks, 256)) return DAQ_ERR_UNSUPPORTED;
     const ValuesArgs p{src, src + L.off_scales, rows, cols, L.row_blocks, L.groups, dst, ld};
     hipStream_t st = (hipStream_t)stream;
     if (dtype == DAQ_BF16) DAQ_LAUNCH("mx4_values", st, hipLaunchKernelGGL(k_mx4_values<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, st, p));

@@ -95,7 +95,6 @@ template <int WR, int WC, int RB, int CB>
 daq_status launch_tiles(const MatmulArgs& p, hipStream_t st) {
     using Product = TileProduct<WR, WC, RB, CB, true>;
     const int64_t tm = ceil_div(p.a_blocks, WR * RB), tn = ceil_div(p.b_blocks, WC * CB), per = ceil_div(tm * tn, kXcd);
-    if (!grid_ok(per * kXcd)) return DAQ_ERR_UNSUPPORTED;
     const auto kernel = k_mx4_tiles<WR, WC, RB, CB>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("mx4_tiles", st,
@@ -219,6 +218,9 @@ daq_status launch_few(const FewArgs& f, hipStream_t st) {
 
 }  // namespace
 
+// Whether the grid of a small product holds its workgroups.
+static bool few_fits(int64_t a_blocks, int64_t b_blocks) { return a_blocks <= 65535 && grid_ok(b_blocks, 64 * kFewWaves); }
+
 // Which form a product takes: the one of the least time by what was measured of each (us, launch included).
 //   small products   2 + the longest of: 0.55 a group that a wave goes through; what the workgroups read at 19 TB/s (L2); B at 5 TB/s
 //   128 x 128 tiles  up to a tile for each CU 3.2 + 0.55 a group; more, two to a CU: 3 + 1.17 a group for every 512
@@ -228,7 +230,7 @@ daq_status launch_few(const FewArgs& f, hipStream_t st) {
 // Tiles end where a descriptor does: one group more, and the last columns of a row block would read as zeros.
 MatmulForm matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups) {
     const double g = (double)groups, small = (double)(ceil_div(a_blocks, 4) * ceil_div(b_blocks, 4)), big = (double)(ceil_div(a_blocks, 8) * ceil_div(b_blocks, 8));
-    const double few = a_blocks > 65535 ? 1e30 : 2.0 + std::max({0.55 * std::ceil(g / kFewWaves), (double)a_blocks * b_blocks * g * 8704 / 19e6, b_blocks * g * 4352 / 5e6});
+    const double few = !few_fits(a_blocks, b_blocks) ? 1e30 : 2.0 + std::max({0.55 * std::ceil(g / kFewWaves), (double)a_blocks * b_blocks * g * 8704 / 19e6, b_blocks * g * 4352 / 5e6});
     const bool reached = groups * kGroupSteps * 1024 <= (int64_t)kTileReach;
     const double tiles = !reached ? 1e30 : small <= 256 ? 3.2 + 0.55 * g : std::ceil(small / 512) * (3.0 + 1.17 * g);
     const double wide = !reached ? 1e30 : std::ceil(big / 256) * (6.0 + 1.7 * g);
@@ -236,8 +238,8 @@ MatmulForm matmul_form(int64_t a_blocks, int64_t b_blocks, int64_t groups) {
     return few == least ? MatmulForm::kFew : tiles == least ? MatmulForm::kSmall : MatmulForm::kBig;
 }
 
-// What the packed operands, the sizes and the result have to be.
-static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, const void* D, int dtype, int64_t ldd) {
+// What the packed operands, the sizes and the result have to be, and the form of the product.
+static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, const void* D, int dtype, int64_t ldd, MatmulForm& form) {
     if (!dtype_ok(dtype)) return DAQ_ERR_INVALID_ARG;
     daq_status rc = matrix_size(M, K);
     if (rc == DAQ_OK) rc = matrix_size(N, K);
@@ -245,7 +247,12 @@ static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, c
     if (rc != DAQ_OK) return rc;
     if (N <= 0) return DAQ_ERR_INVALID_ARG;
     if (K >= (int64_t)1 << 28) return DAQ_ERR_UNSUPPORTED;   // what is counted along k is within 32 bits
-    if (M > 0 && (!B || !aligned256(B) || !D || !elem_aligned(D, dtype) || ldd < N)) return DAQ_ERR_INVALID_ARG;
+    if (M == 0) return DAQ_OK;
+    if (!B || !aligned256(B) || !D || !elem_aligned(D, dtype) || ldd < N) return DAQ_ERR_INVALID_ARG;
+    const int64_t a_blocks = ceil_div(M, 32), b_blocks = ceil_div(N, 32);
+    form = matmul_form(a_blocks, b_blocks, ceil_div(K, kMxGroup));
+    const int64_t edge = form == MatmulForm::kBig ? 8 : 4, tiles = round_up(ceil_div(a_blocks, edge) * ceil_div(b_blocks, edge), kXcd);
+    if (form == MatmulForm::kFew ? !few_fits(a_blocks, b_blocks) : !grid_ok(tiles, form == MatmulForm::kBig ? 512 : 256)) return DAQ_ERR_UNSUPPORTED;
     return DAQ_OK;
 }
 
@@ -255,15 +262,16 @@ static daq_status matmul_check(int64_t M, int64_t N, int64_t K, const void* B, c
 bool raw_rows(int64_t M, int64_t K, int dtype, int mode) {
     return M <= 32 && mode == DAQ_ROUND_NEAREST && M * ceil_div(K, kMxGroup) * 8 * dtype_size(dtype) <= 2048;
 }
+static bool one_launch(int64_t M, int64_t N, int64_t K, int dtype, int mode) { return raw_rows(M, K, dtype, mode) && few_fits(1, ceil_div(N, 32)); }
 
-static daq_status mx4_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, int dtype, int64_t ldd,
+static daq_status mx4_matmul(MatmulForm form, int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, int dtype, int64_t ldd,
                              hipStream_t st) {
     daq_mx4_layout la, lb;
     daq_layout_mx4(M, K, &la);
     daq_layout_mx4(N, K, &lb);
     const MatmulArgs p{A, A + la.off_scales, B, B + lb.off_scales, M, N, la.row_blocks, lb.row_blocks, la.groups,
                        D, ldd, dtype == DAQ_BF16};
-    switch (matmul_form(la.row_blocks, lb.row_blocks, la.groups)) {
+    switch (form) {
         case MatmulForm::kFew: return launch_few<void>(FewArgs{p, nullptr, 0, K}, st);
         case MatmulForm::kSmall: return launch_tiles<2, 2, 2, 2>(p, st);
         case MatmulForm::kBig: break;
@@ -285,11 +293,12 @@ extern "C" daq_status daq_mx4_matmul_workspace(int64_t M, int64_t N, int64_t K, 
 
 extern "C" daq_status daq_mx4_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, daq_dtype dtype,
                                      int64_t ldd, void* workspace, size_t workspace_bytes, void* stream) {
-    const daq_status rc = matmul_check(M, N, K, B, D, dtype, ldd);
+    MatmulForm form = MatmulForm::kFew;
+    const daq_status rc = matmul_check(M, N, K, B, D, dtype, ldd, form);
     if (rc != DAQ_OK) return rc;
     if (M == 0) return DAQ_OK;
     if (!A || !aligned256(A)) return DAQ_ERR_INVALID_ARG;
-    return mx4_matmul(M, N, K, A, B, D, dtype, ldd, (hipStream_t)stream);
+    return mx4_matmul(form, M, N, K, A, B, D, dtype, ldd, (hipStream_t)stream);
 }
 
 extern "C" daq_status daq_mx4_linear_workspace(int64_t M, int64_t N, int64_t K, daq_dtype x_dtype, daq_round mode, size_t* bytes) {
@@ -298,7 +307,7 @@ extern "C" daq_status daq_mx4_linear_workspace(int64_t M, int64_t N, int64_t K, 
     const daq_status rc = daq_mx4_matmul_workspace(M, N, K, &product);
     if (!bytes) return DAQ_ERR_INVALID_ARG;
     *bytes = 0;
-    if (rc != DAQ_OK || raw_rows(M, K, x_dtype, mode)) return rc;
+    if (rc != DAQ_OK || one_launch(M, N, K, x_dtype, mode)) return rc;
     daq_mx4_layout L;
     daq_layout_mx4(M, K, &L);
     *bytes = (size_t)L.bytes + product;
@@ -308,11 +317,12 @@ extern "C" daq_status daq_mx4_linear_workspace(int64_t M, int64_t N, int64_t K, 
 extern "C" daq_status daq_mx4_linear(int64_t M, int64_t N, int64_t K, const void* X, daq_dtype x_dtype, int64_t ldx, daq_round mode,
                                      uint64_t seed, const uint8_t* W, void* Y, daq_dtype y_dtype, int64_t ldy, void* workspace,
                                      size_t workspace_bytes, void* stream) {
-    daq_status rc = matmul_check(M, N, K, W, Y, y_dtype, ldy);
+    MatmulForm form = MatmulForm::kFew;
+    daq_status rc = matmul_check(M, N, K, W, Y, y_dtype, ldy, form);
     if (rc == DAQ_OK) rc = mx4_quantize_check(X, x_dtype, M, K, ldx, mode);
     if (rc != DAQ_OK) return rc;
     if (M == 0) return DAQ_OK;
-    if (raw_rows(M, K, x_dtype, mode)) {
+    if (one_launch(M, N, K, x_dtype, mode)) {
         daq_mx4_layout lb;
         daq_layout_mx4(N, K, &lb);
         const FewArgs f{{nullptr, nullptr, W, W + lb.off_scales, M, N, 1, lb.row_blocks, lb.groups, Y, ldy, y_dtype == DAQ_BF16}, X, ldx, K};
@@ -325,5 +335,5 @@ extern "C" daq_status daq_mx4_linear(int64_t M, int64_t N, int64_t K, const void
     uint8_t* xq = static_cast<uint8_t*>(workspace);
     rc = mx4_quantize(X, x_dtype, M, K, ldx, false, mode == DAQ_ROUND_STOCHASTIC, seed, xq, (hipStream_t)stream);
     if (rc != DAQ_OK) return rc;
-    return mx4_matmul(M, N, K, xq, W, Y, y_dtype, ldy, (hipStream_t)stream);
+    return mx4_matmul(form, M, N, K, xq, W, Y, y_dtype, ldy, (hipStream_t)stream);
 }

@@ -20,8 +20,15 @@ static void reach_of_a_descriptor() {
     }
 }
 
+// A launch takes fewer than 2^32 threads along an axis: 2^23 workgroups of 512 are too many, where tiles of 128 x 128 are not.
+static void threads_of_a_launch() {
+    const int64_t most = ((int64_t)1 << 23) - 1;   // column blocks
+    EXPECT(matmul_form(1, most, 1) == MatmulForm::kFew && matmul_form(1, most + 1, 1) == MatmulForm::kSmall);
+}
+
 int main() {
     reach_of_a_descriptor();
+    threads_of_a_launch();
     if (!fails) std::printf("ok\n");
     return fails != 0;
 }

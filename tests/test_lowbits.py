@@ -140,3 +140,23 @@ def test_oracle_gelu_keeps_its_tail():
     rel = (3 * t * t + 18) * 2.0 ** -53
     assert np.all(np.abs(y + t * phi / f) <= rel * t * phi / f)
     assert np.all(np.abs(slope - (phi / f - t * phi)) <= 2 * rel * t * phi)
+
+
+def test_launches_of_too_many_threads_are_refused_before_the_first():
+    """A launch takes fewer than 2^32 threads along an axis.  Where a call makes several, none is made: there is no GPU here to make one."""
+    L, a, n, UNS = daq.lib(), 1 << 20, C.c_size_t(0), daq.ERR_UNSUPPORTED
+    assert L.daq_mx4_quantize(a, 0, 1 << 29, 1, 1, 0, 0, 0, a, None) == L.daq_mx4_quantize(a, 1, 1, 1 << 30, 1 << 30, 1, 1, 0, a, None) == UNS
+    assert L.daq_mx4_dequantize(a, 1 << 29, 1, a, 0, 1, None) == UNS
+    for rows, parts in ((1 << 30, 1), (1 << 29, 2)):
+        assert L.daq_ckpt8_save(a, 1, rows, 1, parts, parts, a, None) == L.daq_ckpt8_restore(a, rows, 1, parts, a, 0, parts, None) == UNS
+    assert L.daq_ckpt8_act_forward(a, 0, 1 << 30, 1, 1, 0, 0, a, 1, a, None) == L.daq_ckpt8_act_backward(a, 0, 1 << 30, 1, 1, a, 1, 0, a, 1, None, None) == UNS
+    M = N = 1 << 20
+    assert L.daq_mx4_matmul(M, N, 4096, a, a, a, 0, N, None, 0, None) == UNS
+    assert L.daq_mx4_linear(M, N, 4096, a, 0, 4096, 0, 0, a, a, 0, N, a, 1 << 40, None) == UNS
+    for dtype in (0, 1):
+        assert L.daq_ckpt8_weight_grad(1, N, M, a, dtype, N, a, a, M, 0, a, 1 << 60, None) == UNS
+    assert L.daq_ckpt8_weight_grad(0, 1 << 17, 1 << 17, None, 0, 0, None, a, 1 << 17, 0, None, 0, None) == UNS
+    assert L.daq_ckpt8_weight_grad(0, 1 << 17, 1 << 17, None, 0, 0, None, a, 1 << 17, 1, None, 0, None) == daq.OK      # nothing to launch
+    # one row: a launch whose workgroups quantize it, while there are few enough of them
+    for N, one_launch in (((1 << 28) - 32, True), (1 << 28, False)):
+        assert L.daq_mx4_linear_workspace(1, N, 64, 1, 0, C.byref(n)) == daq.OK and (n.value == 0) == one_launch
