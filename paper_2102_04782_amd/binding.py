@@ -688,18 +688,27 @@ class Ckpt8:
     parts: int = 1
 
 
-@functools.lru_cache(maxsize=4096)
 def layout_mx4(rows: int, cols: int) -> Mx4Layout:
     L = Mx4Layout()
     _check(lib().daq_layout_mx4(rows, cols, C.byref(L)), "daq_layout_mx4")
     return L
 
 
-@functools.lru_cache(maxsize=4096)
 def layout_ckpt8(rows: int, cols: int, parts: int = 1) -> Ckpt8Layout:
     L = Ckpt8Layout()
     _check(lib().daq_layout_ckpt8(rows, cols, parts, C.byref(L)), "daq_layout_ckpt8")
     return L
+
+
+# what calls ask of the layouts: numbers, which are kept, while a layout is its caller's to change
+@functools.lru_cache(maxsize=4096)
+def _mx4_bytes(rows: int, cols: int) -> int:
+    return layout_mx4(rows, cols).bytes
+
+
+@functools.lru_cache(maxsize=4096)
+def _ckpt8_bytes(rows: int, cols: int, parts: int) -> int:
+    return layout_ckpt8(rows, cols, parts).bytes
 
 
 def _matrix(t: torch.Tensor):
@@ -734,11 +743,11 @@ def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype, like: torc
 
 
 def alloc_mx4(rows: int, cols: int, device="cuda", stream=None) -> Mx4:
-    return Mx4(_bytes_on(stream, layout_mx4(rows, cols).bytes, device), rows, cols)
+    return Mx4(_bytes_on(stream, _mx4_bytes(rows, cols), device), rows, cols)
 
 
 def alloc_ckpt8(rows: int, cols: int, parts: int = 1, device="cuda", stream=None) -> Ckpt8:
-    return Ckpt8(_bytes_on(stream, layout_ckpt8(rows, cols, parts).bytes, device), rows, cols, parts)
+    return Ckpt8(_bytes_on(stream, _ckpt8_bytes(rows, cols, parts), device), rows, cols, parts)
 
 
 def mx4_quantize(x: torch.Tensor, transpose: bool = False, mode=ROUND_NEAREST, seed=0, out: Optional[Mx4] = None, stream=None) -> Mx4:

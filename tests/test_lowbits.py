@@ -160,3 +160,13 @@ def test_launches_of_too_many_threads_are_refused_before_the_first():
     # one row: a launch whose workgroups quantize it, while there are few enough of them
     for N, one_launch in (((1 << 28) - 32, True), (1 << 28, False)):
         assert L.daq_mx4_linear_workspace(1, N, 64, 1, 0, C.byref(n)) == daq.OK and (n.value == 0) == one_launch
+
+
+def test_a_layout_belongs_to_its_caller():
+    for fn, sizes in ((daq.layout_mx4, (70, 300)), (daq.layout_ckpt8, (70, 300, 2))):
+        first = fn(*sizes)
+        want, first.bytes, first.off_scales = (first.bytes, first.off_scales), 256, 0
+        again = fn(*sizes)
+        assert (again.bytes, again.off_scales) == want
+    assert daq.alloc_mx4(70, 300, device="cpu").buf.numel() == daq.layout_mx4(70, 300).bytes
+    assert daq.alloc_ckpt8(70, 300, 2, device="cpu").buf.numel() == daq.layout_ckpt8(70, 300, 2).bytes
