@@ -315,9 +315,12 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _stream(stream) -> int:
     if stream is None:   # the handle of the current stream, without a Stream object around it (2.9 against 0.2 us)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return _raw_stream(_current_device())
     return stream.cuda_stream
 
 
@@ -711,13 +714,26 @@ def _ckpt8_bytes(rows: int, cols: int, parts: int) -> int:
     return layout_ckpt8(rows, cols, parts).bytes
 
 
+# The address of a packed matrix, of a checkpoint: as many bytes in a row on the GPU as its sizes need.  (Asked of the caller's buffers only.)
+def _packed(q: Mx4) -> int:
+    b = q.buf
+    assert b.is_cuda and b.nbytes >= _mx4_bytes(q.rows, q.cols) and b.is_contiguous()
+    return b.data_ptr()
+
+
+def _kept(c: Ckpt8) -> int:
+    b = c.buf
+    assert b.is_cuda and b.nbytes >= _ckpt8_bytes(c.rows, c.cols, c.parts) and b.is_contiguous()
+    return b.data_ptr()
+
+
 def _matrix(t: torch.Tensor):
     """(rows, cols, row stride, dtype code) of a matrix on the GPU: fp32 or bfloat16, elements of a row next to each other, rows that do
     not overlap."""
     assert t.is_cuda and t.dim() == 2
     (rows, cols), (ld, one) = t.shape, t.stride()
     assert (one == 1 or cols <= 1) and (ld >= cols or rows <= 1)
-    return rows, cols, ld if rows > 1 else max(cols, 1), _DTYPES[t.dtype]
+    return rows, cols, ld if rows > 1 else cols or 1, _DTYPES[t.dtype]
 
 
 def _bytes_on(stream, n: int, device) -> torch.Tensor:
@@ -736,7 +752,7 @@ def _result(out: Optional[torch.Tensor], rows: int, cols: int, dtype, like: torc
         else:
             with torch.cuda.stream(stream):
                 out = torch.empty(rows, cols, dtype=dtype, device=like.device)
-        return out, max(cols, 1), _DTYPES[dtype]
+        return out, cols or 1, _DTYPES[dtype]
     r, c, ld, code = _matrix(out)
     assert (r, c) == (rows, cols) and (dtype is None or out.dtype == dtype)
     return out, ld, code
@@ -756,16 +772,18 @@ def mx4_quantize(x: torch.Tensor, transpose: bool = False, mode=ROUND_NEAREST, s
     r, c = (cols, rows) if transpose else (rows, cols)
     if out is None:
         out = alloc_mx4(r, c, x.device, stream)
-    assert out.rows == r and out.cols == c
-    _check(lib().daq_mx4_quantize(x.data_ptr(), code, rows, cols, ld, int(transpose), mode, seed, out.buf.data_ptr(), _stream(stream)),
-           "daq_mx4_quantize")
+        to = out.buf.data_ptr()
+    else:
+        assert out.rows == r and out.cols == c
+        to = _packed(out)
+    _check(lib().daq_mx4_quantize(x.data_ptr(), code, rows, cols, ld, int(transpose), mode, seed, to, _stream(stream)), "daq_mx4_quantize")
     return out
 
 
 def mx4_dequantize(q: Mx4, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """daq_mx4_dequantize: the values that ``q`` holds, exact in either type (that of ``out`` where it is given)."""
     out, ld, code = _result(out, q.rows, q.cols, dtype if out is None else None, q.buf, stream)
-    _check(lib().daq_mx4_dequantize(q.buf.data_ptr(), q.rows, q.cols, out.data_ptr(), code, ld, _stream(stream)), "daq_mx4_dequantize")
+    _check(lib().daq_mx4_dequantize(_packed(q), q.rows, q.cols, out.data_ptr(), code, ld, _stream(stream)), "daq_mx4_dequantize")
     return out
 
 
@@ -776,7 +794,9 @@ def mx4_matmul(a: Mx4, b: Mx4, dtype=torch.bfloat16, out: Optional[torch.Tensor]
     out, ld, code = _result(out, a.rows, b.rows, dtype if out is None else None, b.buf, stream)
     if workspace is None:
         workspace = _few_ws("daq_mx4_matmul_workspace", stream, b.buf.device, a.rows, b.rows, a.cols)
-    _check(lib().daq_mx4_matmul(a.rows, b.rows, a.cols, a.buf.data_ptr(), b.buf.data_ptr(), out.data_ptr(), code, ld, _ptr(workspace),
+    else:
+        assert workspace.is_cuda and workspace.is_contiguous()
+    _check(lib().daq_mx4_matmul(a.rows, b.rows, a.cols, _packed(a), _packed(b), out.data_ptr(), code, ld, _ptr(workspace),
                                 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_matmul")
     return out
 
@@ -790,7 +810,9 @@ def mx4_linear(x: torch.Tensor, w: Mx4, mode=ROUND_NEAREST, seed=0, dtype=None, 
     out, ldy, y_code = _result(out, M, N, (dtype or x.dtype) if out is None else dtype, x, stream)
     if workspace is None:
         workspace = _few_ws("daq_mx4_linear_workspace", stream, x.device, M, N, K, x_code, mode)
-    _check(lib().daq_mx4_linear(M, N, K, x.data_ptr(), x_code, ldx, mode, seed, w.buf.data_ptr(), out.data_ptr(), y_code, ldy, _ptr(workspace),
+    else:
+        assert workspace.is_cuda and workspace.is_contiguous()
+    _check(lib().daq_mx4_linear(M, N, K, x.data_ptr(), x_code, ldx, mode, seed, _packed(w), out.data_ptr(), y_code, ldy, _ptr(workspace),
                                 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_mx4_linear")
     return out
 
@@ -815,15 +837,18 @@ def ckpt8_save(x: torch.Tensor, parts: int = 1, out: Optional[Ckpt8] = None, str
     cols = width // parts
     if out is None:
         out = alloc_ckpt8(rows, cols, parts, x.device, stream)
-    assert out.rows == rows and out.cols == cols and out.parts == parts
-    _check(lib().daq_ckpt8_save(x.data_ptr(), code, rows, cols, parts, ld, out.buf.data_ptr(), _stream(stream)), "daq_ckpt8_save")
+        to = out.buf.data_ptr()
+    else:
+        assert out.rows == rows and out.cols == cols and out.parts == parts
+        to = _kept(out)
+    _check(lib().daq_ckpt8_save(x.data_ptr(), code, rows, cols, parts, ld, to, _stream(stream)), "daq_ckpt8_save")
     return out
 
 
 def ckpt8_restore(c: Ckpt8, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """daq_ckpt8_restore: the values that ``c`` holds, exact in either type (that of ``out`` where it is given)."""
     out, ld, code = _result(out, c.rows, c.parts * c.cols, dtype if out is None else None, c.buf, stream)
-    _check(lib().daq_ckpt8_restore(c.buf.data_ptr(), c.rows, c.cols, c.parts, out.data_ptr(), code, ld, _stream(stream)), "daq_ckpt8_restore")
+    _check(lib().daq_ckpt8_restore(_kept(c), c.rows, c.cols, c.parts, out.data_ptr(), code, ld, _stream(stream)), "daq_ckpt8_restore")
     return out
 
 
@@ -837,9 +862,12 @@ def ckpt8_act_forward(h: torch.Tensor, act: int, gated: bool = False, out: Optio
     out, ldy, _ = _result(out, rows, cols, h.dtype, h, stream)
     if ckpt is None:
         ckpt = alloc_ckpt8(rows, cols, parts, h.device, stream)
-    assert ckpt.rows == rows and ckpt.cols == cols and ckpt.parts == parts
-    _check(lib().daq_ckpt8_act_forward(h.data_ptr(), code, rows, cols, ldh, act, int(gated), out.data_ptr(), ldy, ckpt.buf.data_ptr(),
-                                       _stream(stream)), "daq_ckpt8_act_forward")
+        to = ckpt.buf.data_ptr()
+    else:
+        assert ckpt.rows == rows and ckpt.cols == cols and ckpt.parts == parts
+        to = _kept(ckpt)
+    _check(lib().daq_ckpt8_act_forward(h.data_ptr(), code, rows, cols, ldh, act, int(gated), out.data_ptr(), ldy, to, _stream(stream)),
+           "daq_ckpt8_act_forward")
     return out, ckpt
 
 
@@ -851,8 +879,8 @@ def ckpt8_act_backward(dy: torch.Tensor, ckpt: Ckpt8, act: int, out: Optional[to
     assert rows == ckpt.rows and cols == ckpt.cols
     out, lddh, _ = _result(out, rows, ckpt.parts * cols, dy.dtype, dy, stream)
     assert y_ckpt is None or (y_ckpt.rows, y_ckpt.cols, y_ckpt.parts) == (rows, cols, 1)
-    _check(lib().daq_ckpt8_act_backward(dy.data_ptr(), code, rows, cols, lddy, ckpt.buf.data_ptr(), act, int(ckpt.parts == 2), out.data_ptr(), lddh,
-                                        None if y_ckpt is None else y_ckpt.buf.data_ptr(), _stream(stream)), "daq_ckpt8_act_backward")
+    _check(lib().daq_ckpt8_act_backward(dy.data_ptr(), code, rows, cols, lddy, _kept(ckpt), act, int(ckpt.parts == 2), out.data_ptr(), lddh,
+                                        None if y_ckpt is None else _kept(y_ckpt), _stream(stream)), "daq_ckpt8_act_backward")
     return out
 
 
@@ -864,7 +892,9 @@ def ckpt8_weight_grad(dy: torch.Tensor, x: Ckpt8, out: Optional[torch.Tensor] = 
     out, ldw, _ = _result(out, N, x.cols, torch.float32, dy, stream)
     if workspace is None:
         workspace = _few_ws("daq_ckpt8_weight_grad_workspace", stream, dy.device, M, N, x.cols, code, lddy, dy.data_ptr() % 16)
-    _check(lib().daq_ckpt8_weight_grad(M, N, x.cols, dy.data_ptr(), code, lddy, x.buf.data_ptr(), out.data_ptr(), ldw, int(accumulate),
+    else:
+        assert workspace.is_cuda and workspace.is_contiguous()
+    _check(lib().daq_ckpt8_weight_grad(M, N, x.cols, dy.data_ptr(), code, lddy, _kept(x), out.data_ptr(), ldw, int(accumulate),
                                        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_ckpt8_weight_grad")
     return out
 

@@ -508,3 +508,28 @@ def test_gelu_keeps_its_tail(gated):
         assert np.all(np.abs(dh[:, 64:] - d * f) <= bound(g, np.abs(d * f)) + np.abs(d * g) * 2.0 ** -126 + 2.0 ** -126)
     step = np.repeat(np.exp2(ref.ckpt8_codes(f * us)[1] - 127.0), 32, axis=1)
     assert np.all(np.abs(_np(daq.ckpt8_restore(yk)) - f * us) <= 1.01 * step)
+
+
+def test_packed_buffers_are_looked_at_before_a_launch():
+    """A buffer on the host, one of fewer bytes than its sizes need, one whose bytes are not in a row; a workspace on the host or not in a row."""
+    x, dy = _x(40, 300, torch.bfloat16, 1).cuda(), _x(40, 50, torch.bfloat16, 2).cuda()
+    w, h, kept = daq.mx4_quantize(_x(50, 300, torch.bfloat16, 3).cuda()), daq.ckpt8_save(dy), daq.ckpt8_save(x)
+
+    def broken(q):
+        for buf in (q.buf.cpu(), q.buf[:-1], q.buf[:1].expand(q.buf.numel()), torch.empty(2 * q.buf.numel(), dtype=torch.uint8, device="cuda")[::2]):
+            yield type(q)(buf, *[getattr(q, f) for f in ("rows", "cols", "parts") if hasattr(q, f)])
+
+    calls = [(w, lambda q: daq.mx4_dequantize(q)), (w, lambda q: daq.mx4_linear(x, q)), (w, lambda q: daq.mx4_matmul(q, w)), (w, lambda q: daq.mx4_matmul(w, q)),
+             (w, lambda q: daq.mx4_quantize(_x(50, 300, torch.bfloat16, 3).cuda(), out=q)), (h, lambda q: daq.ckpt8_restore(q)), (h, lambda q: daq.ckpt8_save(dy, out=q)),
+             (h, lambda q: daq.ckpt8_act_forward(dy, daq.ACT_SILU, ckpt=q)), (h, lambda q: daq.ckpt8_act_backward(dy, q, daq.ACT_SILU)),
+             (h, lambda q: daq.ckpt8_act_backward(dy, h, daq.ACT_SILU, y_ckpt=q)), (kept, lambda q: daq.ckpt8_weight_grad(dy, q))]
+    for good, call in calls:
+        call(good)
+        for q in broken(good):
+            with pytest.raises(AssertionError):
+                call(q)
+    for ws in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8, device="cuda").expand(1 << 20)):
+        for call in (lambda: daq.mx4_linear(x, w, workspace=ws), lambda: daq.mx4_matmul(w, w, workspace=ws), lambda: daq.ckpt8_weight_grad(dy, kept, workspace=ws)):
+            with pytest.raises(AssertionError):
+                call()
+    torch.cuda.synchronize()

@@ -170,3 +170,15 @@ def test_a_layout_belongs_to_its_caller():
         assert (again.bytes, again.off_scales) == want
     assert daq.alloc_mx4(70, 300, device="cpu").buf.numel() == daq.layout_mx4(70, 300).bytes
     assert daq.alloc_ckpt8(70, 300, 2, device="cpu").buf.numel() == daq.layout_ckpt8(70, 300, 2).bytes
+
+
+def test_packed_buffers_off_the_gpu_are_refused(monkeypatch):
+    """As weights read from a file are: their host addresses must not get to a kernel."""
+    def reached(stream):
+        raise RuntimeError("reached the call")
+
+    monkeypatch.setattr(daq, "_stream", reached)
+    q, c = daq.alloc_mx4(40, 70, device="cpu"), daq.alloc_ckpt8(40, 70, device="cpu")
+    for call in (lambda: daq.mx4_dequantize(q), lambda: daq.mx4_matmul(q, q), lambda: daq.ckpt8_restore(c)):
+        with pytest.raises(AssertionError):
+            call()
