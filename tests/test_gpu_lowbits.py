@@ -533,3 +533,37 @@ def test_packed_buffers_are_looked_at_before_a_launch():
             with pytest.raises(AssertionError):
                 call()
     torch.cuda.synchronize()
+
+
+# weight gradients on tiles, by form (few_bits_plans.hip holds that they are of it); first: the column of a wider matrix at which dY begins
+LARGE_TILES = [(700, 4103, 4100, 0, 0), (700, 4104, 4100, 1, 8), (600, 4096, 8200, 0, 0), (9000, 2049, 2100, 0, 0), (6000, 1536, 1300, 0, 0), (1111, 3000, 900, 0, 0)]
+
+
+@pytest.mark.parametrize("M,N,K,first,pad", LARGE_TILES)
+def test_weight_grad_on_tiles(M, N, K, first, pad):
+    wide = _x(M, N + pad, torch.bfloat16, 21).cuda()
+    dy, kept = wide[:, first:first + N], daq.ckpt8_save(_x(M, K, torch.bfloat16, 22).cuda())
+    xs = daq.ckpt8_restore(kept).double()
+    d = dy.double().t().contiguous()
+    exact, absolute = d @ xs, d.abs() @ xs.abs()
+    got = daq.ckpt8_weight_grad(dy, kept)
+    assert bool(((got.double() - exact).abs() <= (-(-M // 16) + 10) * 2.0 ** -23 * absolute + 1e-40).all())
+    out = torch.full((N, K + 3), 2.0, device="cuda")
+    daq.ckpt8_weight_grad(dy, kept, out=out[:, 1:1 + K], accumulate=True)
+    assert torch.equal(out[:, 1:1 + K], got + 2) and bool((out[:, 0] == 2).all()) and bool((out[:, 1 + K:] == 2).all())
+
+
+@pytest.mark.parametrize("dtype,M,N,K", [(torch.float32, 300, 1101, 1090), (torch.float32, 3001, 610, 1101), (torch.float32, 700, 4103, 4100),
+                                         (torch.bfloat16, 300, 1101, 1090), (torch.bfloat16, 3001, 610, 1101), (torch.bfloat16, 1111, 3000, 900),
+                                         (torch.bfloat16, 2050, 1032, 1000), (torch.bfloat16, 700, 4103, 4100), (torch.bfloat16, 700, 4104, 4100),
+                                         (torch.bfloat16, 9000, 2049, 2100), (torch.bfloat16, 6000, 1536, 1300)])
+def test_weight_grad_on_tiles_keeps_what_is_not_finite_to_itself(dtype, M, N, K):
+    """In the first and last columns, where reads pass a row's end, and in the first and last tokens, where they pass the last row's."""
+    dy, x = _x(M, N, dtype, 31), _x(M, K, torch.bfloat16, 32)
+    dy[0, 0], dy[M - 1, N - 1], dy[M // 2, N // 2], x[M - 1, K - 1] = float("nan"), float("inf"), float("-inf"), float("inf")
+    got = daq.ckpt8_weight_grad(dy.cuda(), daq.ckpt8_save(x.cuda()))
+    k0 = (K - 1) // 32 * 32
+    bad = torch.zeros(N, K, dtype=torch.bool, device="cuda")
+    bad[[0, N // 2, N - 1]] = True
+    bad[:, k0:] = True
+    assert bool(got[0].isnan().all()) and bool(got[:, k0:].isnan().all()) and not bool(got[bad].isfinite().any()) and bool(got[~bad].isfinite().all())
