@@ -567,3 +567,34 @@ def test_weight_grad_on_tiles_keeps_what_is_not_finite_to_itself(dtype, M, N, K)
     bad[[0, N // 2, N - 1]] = True
     bad[:, k0:] = True
     assert bool(got[0].isnan().all()) and bool(got[:, k0:].isnan().all()) and not bool(got[bad].isfinite().any()) and bool(got[~bad].isfinite().all())
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("name,act", ACTS)
+def test_large_activations_are_their_parts(name, act, dtype, gated):
+    """From 48 MiB on the kernels pass the caches by: every value and every code as of the two halves, which do not (and are compared with
+    the oracle at their small sizes).  Rows of any length that begin at any element."""
+    parts, cols = (2, 1003) if gated else (1, 1003)
+    rows = (51 << 20) // (parts * cols * (2 if dtype == torch.bfloat16 else 4)) + 1
+    half = rows // 2 + 3
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    h = torch.randn(rows, parts * cols + 3, generator=g, device="cuda").mul_(3).to(dtype)[:, 1:1 + parts * cols]
+    dy = torch.randn(rows, cols + 1, generator=g, device="cuda").to(dtype)[:, :cols]
+
+    def run(rs):
+        y, kept = daq.ckpt8_act_forward(h[rs], act, gated=gated)
+        yk = daq.alloc_ckpt8(*y.shape)
+        dh = daq.ckpt8_act_backward(dy[rs], kept, act, y_ckpt=yk)
+        assert torch.equal(daq.ckpt8_act_backward(dy[rs], kept, act), dh)
+        return y, dh, daq.ckpt8_restore(kept), daq.ckpt8_restore(yk), daq.ckpt8_restore(kept, dtype=torch.bfloat16)
+
+    whole = run(slice(None))
+    for rs in (slice(0, half), slice(half, rows)):
+        for a, b in zip(whole, run(rs)):
+            assert bool(b.isfinite().all()) and torch.equal(a[rs], b)
+    saved = daq.ckpt8_save(h, parts)
+    assert torch.equal(daq.ckpt8_restore(saved), whole[2])
+    for rs in (slice(0, half), slice(half, rows)):
+        assert torch.equal(daq.ckpt8_restore(daq.ckpt8_save(h[rs], parts)), whole[2][rs])
