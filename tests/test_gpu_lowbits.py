@@ -598,3 +598,49 @@ def test_large_activations_are_their_parts(name, act, dtype, gated):
     assert torch.equal(daq.ckpt8_restore(saved), whole[2])
     for rs in (slice(0, half), slice(half, rows)):
         assert torch.equal(daq.ckpt8_restore(daq.ckpt8_save(h[rs], parts)), whole[2][rs])
+
+
+def test_feed_forward_block_product_by_product(monkeypatch):
+    """Every call of a training step against the oracle on the values that the block passes to it: products elementwise from their own operands, in
+    the rounding and with the draws that each is meant to have, and both gradients of the weights."""
+    from paper_2102_04782_amd import feed_forward as ff
+
+    products, grads = [], []
+    linear, weight_grad = daq.mx4_linear, daq.ckpt8_weight_grad
+
+    def recording_linear(x, w, mode=daq.ROUND_NEAREST, seed=0, **kw):
+        out = linear(x, w, mode=mode, seed=seed, **kw)
+        products.append((x.clone(), w, mode, seed, out.clone()))
+        return out
+
+    def recording_grad(dy, x, **kw):
+        out = weight_grad(dy, x, **kw)
+        grads.append((dy.clone(), daq.ckpt8_restore(x), out.clone()))
+        return out
+
+    monkeypatch.setattr(ff.daq, "mx4_linear", recording_linear)
+    monkeypatch.setattr(ff.daq, "ckpt8_weight_grad", recording_grad)
+    block = ff.FeedForward(160, 224, seed=6)
+    x, dy = _x(90, 160, torch.bfloat16, 3, 1).cuda(), _x(90, 160, torch.bfloat16, 4, 1).cuda()
+    y, saved = block.forward(x)
+    dx, dw_in, dw_out = block.backward(dy, saved, seed=7)
+
+    w_in, w_out = block.w_in.cpu(), block.w_out.cpu()
+    by = [(block.q_in, _values(w_in)), (block.q_out, _values(w_out)), (block.q_out_t, _values(w_out, transpose=True)), (block.q_in_t, _values(w_in, transpose=True))]
+    assert len(products) == 4 and len(grads) == 2
+    for i, ((a, w, mode, seed, out), (packed, vw)) in enumerate(zip(products, by)):
+        assert w is packed and mode == (daq.ROUND_NEAREST if i < 2 else daq.ROUND_STOCHASTIC)
+        va = _values(a.cpu(), stochastic=i >= 2, seed=seed)
+        exact, absolute = va @ vw.T, np.abs(va) @ np.abs(vw).T
+        assert out.dtype == torch.bfloat16 and np.all(np.abs(_np(out) - exact) <= _bound(-(-a.shape[1] // 64), absolute, exact, torch.bfloat16))
+    assert products[2][3] != products[3][3]                                  # draws of their own
+    (x0, *_, h), (a, *_, y0), (dy0, *_, da), (dh, *_, dx0) = products
+    assert all(torch.equal(p, q) for p, q in ((x0, x), (y0, y), (dy0, dy), (dx0, dx)))
+    want_a, kept = daq.ckpt8_act_forward(h, daq.ACT_SILU, gated=True)        # (compared with the oracle above)
+    a8 = daq.alloc_ckpt8(90, 224)
+    want_dh = daq.ckpt8_act_backward(da, kept, daq.ACT_SILU, y_ckpt=a8)
+    assert torch.equal(a, want_a) and torch.equal(dh, want_dh)
+    for (d, xs, out), (want_d, want_x, want_out) in zip(grads, ((dh, _saved(x.cpu()), dw_in), (dy, _np(daq.ckpt8_restore(a8)), dw_out))):
+        assert torch.equal(d, want_d) and np.array_equal(_np(xs), want_x) and torch.equal(out, want_out)
+        exact, absolute = _np(d).T @ want_x, np.abs(_np(d)).T @ np.abs(want_x)
+        assert np.all(np.abs(_np(out) - exact) <= _bound(-(-90 // 16), absolute, exact, torch.float32))
