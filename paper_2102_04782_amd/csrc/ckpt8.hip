@@ -2,8 +2,8 @@
 //
 // All of it is bound by memory: a thread takes 8 elements, 16 bytes of a bfloat16 row, and four neighbours share a block's largest
 // magnitude by lane exchanges.  Measured (us; TB/s of what is read and written, the Infinity Cache keeping part of it): 32768 x 8192 saved
-// 135 (6.0) and restored 116 (7.0); gated, 16384 x 8192, forward 159 (6.8: h read, y and the codes written), backward 167 (6.5).  Small
-// matrices 3 to 5 us.  Exponentials and Phi are fp32; f' shares them with f.
+// 134 (6.1) and restored 116 (7.0); gated, 16384 x 8192, forward 157 (6.9: h read, y and the codes written), backward 175 (6.2), 10 more with
+// y saved again (0.14 GB).  Small matrices 3 to 5 us.  Exponentials and Phi are fp32; f' shares them with f.
 #include <type_traits>
 
 #include "lowbits.h"

@@ -6,7 +6,7 @@
 // Both operands have their summed axis, the tokens, outermost.  A first launch brings X^, and dY where the products do not read it as it is,
 // into the order of the matrix instructions (eight tokens of a column in 16 bytes), decoding the one and splitting an fp32 dY on
 // the way: each is read and written once, at 5.4 TB/s (X^ of 16384 x 4096 35 us, with a dY of 8192 columns 137).  The products then run on
-// whole KiB tiles: 16384 x 8192 x 4096 840-930 us, 1.2 to 1.3 PFLOP/s, against 1.85 of the same instructions on registers alone, both at
+// whole KiB tiles: 16384 x 8192 x 4096 884-988 us, medians of traces 939 and 943, 1.17 PFLOP/s, against 1.85 of the same instructions on registers alone, both at
 // what clock the power limit leaves; torch's bfloat16 product of 8192 x 8192 x 8192 makes 1.2.
 #include "tile_product.h"
 
@@ -479,7 +479,8 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, i
     // The form and the parts of the tokens that take the least time by what was measured of them (us): a workgroup to a CU, 6 + 1.7 a
     // stage of 64 tokens for tiles of 256 x 256, 3.2 + 0.65 for tiles of 128 x 128 (1.3 with three parts of dY, which have that form
     // only); several parts of the tokens: 3 for their sum, and each part's results written and read at 4 TB/s.  E.g. 2048 x 2048 x 2048
-    // 31.5 us on small tiles, 62 on large ones, 52 on small ones in two parts; 16384 x 256 x 256 from fp32 345 us in one part, 34 in 32.
+    // 32 us on small tiles, 62 on large ones, 52 on small ones in two parts; 16384 x 8192 x 4096 918 on large ones, 1190 on small ones; 16384 x 4096 x 512
+    // 346 in one part, 88 in eight; from fp32 1531 x 607 x 1100 39 in one part, 28.3 in four, 3001 x 610 x 1101 58.5, 33.4 in five.
     const int stages = w.steps / kGroupSteps;
     const double t_part = (double)N * K * 8 / 4e6;
     SplitModel small{stages, ceil_div(w.n_blocks, 4) * ceil_div(w.k_blocks, 4), stages, w.parts > 1 ? 1.3 : 0.65, 3.2, 0.0, 3.0, t_part};
@@ -488,9 +489,10 @@ WgradPlan wgrad_plan(int64_t M, int64_t N, int64_t K, int dtype, int64_t lddy, i
     w.big = w.parts == 1 && big.cost(s_big) < small.cost(s_small);
     w.splits = w.big ? s_big : s_small;
     // A bfloat16 dY of whole 16-byte pieces can be read by the products as it is (what they reach of it at a time is within 31 bits): that
-    // spares its way into tiles, and the fragments' transposing reads cost the products some.  us with it and without: 16384 x 8192 x 4096
-    // 941 and 976, 4096 x 4096 x 4096 133 and 133, 16384 x 4096 x 512 103 and 141; on small tiles 2048 x 2048 x 2048 37.3 and 35.1,
-    // 8192 x 1024 x 1024 42.2 and 42.3, 16384 x 256 x 256 29.9 and 31.6.
+    // spares its way into tiles, and the fragments' transposing reads cost the products some, the more the more columns X has.  us with it and
+    // without: 16384 x 4096 x 512 88 and 155, 16384 x 8192 x 4096 918 and 919, 4096 x 4096 x 4096 129 and 128, 16384 x 512 x 8192 211 and 213,
+    // 16384 x 4096 x 8192 944 and 900; on small tiles 20000 x 704 x 704 51.5 and 59.7, 8192 x 1024 x 1024 38.1 and 41, 2048 x 2048 x 2048 33.3 and
+    // 31.9, but 8192 x 512 x 2048 41.8 and 48.3.
     w.flat = dtype == DAQ_BF16 && dy_misaligned == 0 && lddy % 8 == 0 && N % 8 == 0 && lddy < ((int64_t)1 << 24) && K <= (w.big ? 8192 : 1024);
     w.per_split = (int)ceil_div(stages, w.splits);
     w.splits = (int)ceil_div(stages, w.per_split);

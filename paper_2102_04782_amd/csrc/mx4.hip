@@ -2,8 +2,8 @@
 //
 // A block of 32 elements becomes 16 bytes of codes and a scale byte, so a bfloat16 matrix of 2 bytes an element is read once and 17/32
 // of one are written.  Measured (us, and TB/s of what is read and written): 16384 x 8192 by rows 62-69 (5.2); 16384 x 4096 by rows 24.4,
-// by columns 26.9 (6.4), stochastically 38.5 and 39 - there the vector instructions bound it, 17 an element, 5 of them the random word's;
-// back to bfloat16 25.7.  Small matrices take the 3 us of a launch whose lanes wait for memory once: a lane has one block, and asks for
+// by columns 26.9 (6.4), stochastically 38.5 and 41 - there the vector instructions bound it, 17 an element, 5 of them the random word's;
+// back to bfloat16 26.4.  Small matrices take the 3 us of a launch whose lanes wait for memory once: a lane has one block, and asks for
 // all of it at a time (77 x 1000 3.3; with four blocks a lane, one after the other, 4.7).
 #include <type_traits>
 

@@ -45,9 +45,9 @@ __device__ __forceinline__ void store4(const MatmulArgs& p, int64_t row, int64_t
 
 // Tiles of 32 RB WR x 32 CB WC results, a workgroup each.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles, in bands
 // of four row tiles, so that the 32 it holds at a time share twelve panels of the operands in its L2.
-// 16384 x 8192 x 8192 470-530 us, 4.2-4.7 PFLOP/s: the matrix cores are busy 72 % of the cycles, at the 1.45 to 1.6 GHz that the power limit
-// leaves; a loop of the same instructions on registers alone makes 5.4-6.2.  128 x 128 tiles read twice as much LDS for the same
-// products: 1777 x 2080 x 4096, 238 tiles, 12.4-14.3 us, 2.2 PFLOP/s.  Results that left as 8 bytes a lane took 554 us at the first size.
+// 16384 x 8192 x 8192 464-564 us, medians of traces 503 and 524, 4.3 PFLOP/s: the matrix cores are busy 72 % of the cycles, at the 1.3 to 1.6 GHz
+// that the power limit leaves; a loop of the same instructions on registers alone makes 5.4-6.2.  128 x 128 tiles read twice as much LDS for the same
+// products: 1777 x 2080 x 4096, 238 tiles, 12.7-16.1 us, median 14, 2.2 PFLOP/s.  Results that left as 8 bytes a lane took 554 us at the first size.
 template <int WR, int WC, int RB, int CB>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_mx4_tiles(MatmulArgs p, int tiles_m, int tiles_n, int per_xcd) {
     using Product = TileProduct<WR, WC, RB, CB, true>;

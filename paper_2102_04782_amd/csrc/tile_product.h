@@ -146,8 +146,8 @@ struct TileProduct {
                 at_flat[i] = row * kRowBytes + (piece ^ place(row)) * 16 + (lane & 1) * 8;
             }
         }
-        // FLAT: the transposing reads are written out, with their wait, as the compiler would have each wait for the requests under way.  Few of
-        // them to a wave: waves of 64 rows x 128 columns 884 us at 16384 x 8192 x 4096, of 128 x 64 896.
+        // FLAT: the transposing reads are written out, with their wait, as the compiler would have each wait for the requests under way.  Waves
+        // of 64 rows x 128 columns make few of them; 16384 x 8192 x 4096 takes as long with waves of 128 x 64, within what two runs differ by.
         auto read_flat = [&](const uint8_t* from, auto step, int set) {
             if constexpr (FLAT) {
                 typedef short v4s __attribute__((ext_vector_type(4)));
