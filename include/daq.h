@@ -538,7 +538,8 @@ daq_status daq_clip_search(const daq_conv_desc* desc, const float* dY, float alp
  * or synchronised, arguments are checked before anything is launched.  Sizes: up to 2^31 - 1 rows or
  * columns and 2^40 elements of a matrix, for products fewer than 2^28 columns K, for weight gradients fewer
  * than 2^24 tokens, else DAQ_ERR_UNSUPPORTED; the same for launches of 2^32 threads or more (256 to a workgroup, 512 for 4-bit
- * products), e.g. 2^30 rows of a checkpoint of up to 32 columns, 2^29 rows of a 4-bit matrix of up to 256.
+ * products), e.g. 2^30 rows of a checkpoint of up to 32 columns, 2^29 rows of a 4-bit matrix of up to 256, and for checkpoints
+ * of more than 65535 * 2048 columns.
  *
  * Both formats share a power-of-two scale 2^(byte - 127) among 32 neighbours, so that decoding is exact in
  * bfloat16 and fp32 and products of decoded values need no rounding before their fp32 sums.  The byte is at

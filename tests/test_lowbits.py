@@ -150,6 +150,9 @@ def test_launches_of_too_many_threads_are_refused_before_the_first():
     for rows, parts in ((1 << 30, 1), (1 << 29, 2)):
         assert L.daq_ckpt8_save(a, 1, rows, 1, parts, parts, a, None) == L.daq_ckpt8_restore(a, rows, 1, parts, a, 0, parts, None) == UNS
     assert L.daq_ckpt8_act_forward(a, 0, 1 << 30, 1, 1, 0, 0, a, 1, a, None) == L.daq_ckpt8_act_backward(a, 0, 1 << 30, 1, 1, a, 1, 0, a, 1, None, None) == UNS
+    wide = 65535 * 2048 + 1                                       # along the other axis workgroups are counted
+    assert L.daq_ckpt8_save(a, 1, 1, wide, 1, wide, a, None) == L.daq_ckpt8_restore(a, 1, wide, 1, a, 1, wide, None) == UNS
+    assert L.daq_ckpt8_act_forward(a, 1, 1, wide, wide, 0, 0, a, wide, a, None) == UNS
     M = N = 1 << 20
     assert L.daq_mx4_matmul(M, N, 4096, a, a, a, 0, N, None, 0, None) == UNS
     assert L.daq_mx4_linear(M, N, 4096, a, 0, 4096, 0, 0, a, a, 0, N, a, 1 << 40, None) == UNS
