@@ -5,7 +5,7 @@ Five kinds of cases, each one pass of what a training or serving program does:
 linear   Y = X W^T, both operands in 8-bit floating point (a sign, four exponent and three mantissa bits, largest value 448), a power-of-two
          scale for every block of 128 along the summed axis; a tile of 128 x 128 of the weights shares one.  W laid out once,
          X quantized in the call.
-train    the same layer's forward pass and both gradients: dX = dY W, dW = dY^T X, the latter in blocks of 128 tokens.
+train    the same layer's forward pass and both gradients: dX = dY W, dW = dY^T X, the latter in blocks of 128 tokens; all of the type of X.
 route    a router: softmax or sigmoid scores of the logits, a bias that counts for the choice only, groups of experts of which the best
          (by the sum of their two best) stay, the k best experts, their scores as weights, renormalised or not; the order of the rows
          by expert; with "train" the gradient of the logits.
@@ -266,7 +266,7 @@ def _experts_plain(s):
                 by_dy, by_x = _row_values(s["dy"][here].t()), _row_values(s["x"][token[here]].t())
                 dw[e] = torch.matmul(by_dy, by_x.t())
         at += n
-    return {"y": y.to(to), "dx": dx.to(to), "dw": dw} if train else y.to(to)
+    return {"y": y.to(to), "dx": dx.to(to), "dw": dw.to(to)} if train else y.to(to)
 
 
 def _combine_plain(s):
@@ -292,7 +292,7 @@ def _run_plain(s):
         x, dy, w = s["x"], s["dy"], s["w"][0]
         y, dx = torch.matmul(_row_values(x), w.t()), torch.matmul(_row_values(dy), w)
         dw = torch.matmul(_row_values(dy.t()), _row_values(x.t()).t())
-        return {"y": y.to(x.dtype), "dx": dx.to(x.dtype), "dw": dw}
+        return {"y": y.to(x.dtype), "dx": dx.to(x.dtype), "dw": dw.to(x.dtype)}
     return {"route": _route_plain, "experts": _experts_plain, "combine": _combine_plain}[k](s)
 
 
@@ -307,7 +307,7 @@ def run(s):
         y = daq.fp8_matmul(x, s["w"], dtype=s["x"].dtype)
         dy, dy_c = daq.fp8_quantize_both(s["dy"])
         dx = daq.fp8_matmul(dy, s["w_t"], dtype=s["x"].dtype)
-        return {"y": y, "dx": dx, "dw": daq.fp8_matmul(dy_c, x_c, dtype=torch.float32)}
+        return {"y": y, "dx": dx, "dw": daq.fp8_matmul(dy_c, x_c, dtype=s["x"].dtype)}
     if k == "route":
         form = {"scores": s["scores"], "renormalize": case["renormalize"], "scale": case["scale"]}
         weights, experts = daq.route(s["logits"], case["k"], bias=s["bias"], groups=case["groups"], top_groups=case["top_groups"], **form)
@@ -325,7 +325,7 @@ def run(s):
         y = daq.experts_matmul(x, s["w"], plan, dtype=to)
         dy, dy_c = daq.experts_quantize(s["dy"], plan, sorted_rows=True)
         dx = daq.experts_matmul(dy, s["w_t"], plan, sorted_rows=True, dtype=to)
-        return {"y": y, "dx": dx, "dw": daq.experts_weight_grad(dy_c, x_c, plan)}
+        return {"y": y, "dx": dx, "dw": daq.experts_weight_grad(dy_c, x_c, plan, dtype=to)}
     out = daq.experts_combine(s["y"], plan, s["weights"])
     if not case["train"]:
         return out
@@ -342,7 +342,7 @@ def work(case):
         return {"bytes": size * M * K + codes(N, K) + (2 if case["out"] == "bf16" else 4) * M * N, "flops": 2 * M * N * K}
     if k == "train":                     # x, dy and w; y, dx and dw
         M, N, K = case["M"], case["N"], case["K"]
-        return {"bytes": 2 * size * M * (K + N) + codes(N, K) + 4 * N * K, "flops": 6 * M * N * K}
+        return {"bytes": 2 * size * M * (K + N) + codes(N, K) + size * N * K, "flops": 6 * M * N * K}
     T, E, picks = case["T"], case["E"], case["T"] * case["k"]
     if k == "route":                     # logits in; weights, experts, order and place out; backwards logits, gradients and choices in, logits' gradients out
         n = size * T * E + 16 * picks + 4 * E
@@ -351,7 +351,7 @@ def work(case):
         N, K, used = case["N"], case["K"], min(E, picks)
         n = size * T * K + codes(used * N, K) + size * picks * N
         if case["train"]:
-            return {"bytes": n + size * picks * (N + K) + 4 * E * N * K, "flops": 6 * picks * N * K}
+            return {"bytes": n + size * picks * (N + K) + size * E * N * K, "flops": 6 * picks * N * K}
         return {"bytes": n, "flops": 2 * picks * N * K}
     D = case["D"]
     n = size * D * (picks + T) + 8 * picks
