@@ -642,6 +642,153 @@ daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, const void* dY
                                  size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Linear layers in 8-bit floating point
+ *
+ * Elements of 1 sign, 4 exponent and 3 mantissa bits (up to 448, steps of 2^-9 below 2^-6), a power-of-two scale 2^(byte - 127) for
+ * every block of 128 along the axis that a product sums over.  Per block, with a = max |x|: e = the smallest integer >= -126 with
+ * a <= 448 * 2^e (nothing is cut off), code = x / 2^e to the nearest element, ties to the even code, byte = e + 127.  A block with a
+ * NaN or an infinity gets the byte 255 and the codes of NaN; every sum it enters is NaN.
+ * Products: a result in bfloat16 comes from the matrix cores' 8-bit floating point, which take codes and scales as they are and add
+ * eight neighbouring products (of a block: 8 i .. 8 i + 7) with 2^-13 of the largest of them cut off of each other one, these sums in fp32;
+ * on bell-shaped values 2^-16 of the result, against the 2^-9 of its rounding.  A result in fp32 comes from their bfloat16, in which
+ * the values are exact (those within its range: scales of 2^-117 .. 2^119 at least), with fp32 sums of exact products, at half the rate.
+ * Conventions as of the layers above.  Sizes: as above, and fewer than 2^23
+ * columns K of a product; launches of 2^32 threads or more are DAQ_ERR_UNSUPPORTED.
+ *
+ * Matrix: codes of element (r, c) at byte r * pitch + c, pitch = columns rounded up to 128; the scale byte of block (r, c / 128) at
+ * off_scales + ((c/512) * rows + r) * 4 + (c/128) % 4.  Padding is quantized as zeros: codes of zero (in a block of byte 255 of NaN, as all
+ * of that block's), scale bytes of blocks behind the last column zero.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    int64_t bytes, off_scales;
+    int64_t pitch;
+} daq_fp8_layout;
+daq_status daq_layout_fp8(int64_t rows, int64_t cols, daq_fp8_layout* out);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_fp8_quantize -- src [rows][cols], read once, to
+ *   by_rows     the matrix [rows][cols], blocks along its rows, and / or
+ *   by_columns  its transpose [cols][rows], blocks along the columns of src: what a weight gradient sums over
+ * (either may be NULL, not both; layouts of daq_layout_fp8(rows, cols) and (cols, rows), 256-byte aligned, written whole).
+ * daq_fp8_quantize_weights -- `count` matrices src [rows][cols], `stride` elements apart, where a tile of 128 x 128 shares a scale, so that
+ *   dst    [count * rows][cols]  (the matrices one below the other) and
+ *   dst_t  [count * cols][rows]  (their transposes)   hold the same values; either may be NULL, not both.
+ * daq_fp8_dequantize -- the values of a matrix, exact in fp32, in bfloat16 but for those below its smallest (and 2^128, which rounding can
+ * make of magnitudes above 1.9 * 2^127, is an infinity).
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_fp8_quantize(const void* src, daq_dtype dtype, int64_t rows, int64_t cols, int64_t ld, uint8_t* by_rows,
+                            uint8_t* by_columns, void* stream);
+daq_status daq_fp8_quantize_weights(const void* src, daq_dtype dtype, int64_t count, int64_t rows, int64_t cols, int64_t ld,
+                                    int64_t stride, uint8_t* dst, uint8_t* dst_t, void* stream);
+daq_status daq_fp8_dequantize(const uint8_t* src, int64_t rows, int64_t cols, void* dst, daq_dtype dtype, int64_t ld, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_fp8_matmul -- D[m][n] = sum over k of A[m][k] * B[n][k], D rounded once to its type; accumulate != 0 (fp32 only) adds to D.
+ *   a layer   Y = X W^T:  A = X by rows, B = W;     dX = dY W:  A = dY by rows, B = W transposed;
+ *             dW = dY^T X:  A = dY by columns, B = X by columns (K counts tokens; K = 0, no tokens, is a sum of nothing)
+ * daq_fp8_linear -- the same with A quantized in the call from X [M][K].
+ *   workspace  of the bytes daq_fp8_matmul_workspace / daq_fp8_linear_workspace report; may be NULL where that is 0
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_fp8_matmul_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, size_t* bytes);
+daq_status daq_fp8_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, daq_dtype dtype,
+                          int64_t ldd, int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+daq_status daq_fp8_linear_workspace(int64_t M, int64_t N, int64_t K, daq_dtype x_dtype, daq_dtype y_dtype, size_t* bytes);
+daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void* X, daq_dtype x_dtype, int64_t ldx, const uint8_t* W, void* Y,
+                          daq_dtype y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Sparse feed-forward layers: a router, and the products of the experts that it chooses
+ *
+ * daq_route -- per token (row of logits [tokens][experts]), in 64 bits where 32 do not decide:
+ *   s = softmax(l) or sigmoid(l);  c = s + bias (bias may be NULL; it counts for the choice only)
+ *   groups > 1: the experts are `groups` runs of neighbours; a group counts the sum of its two best c (its best one where it has no
+ *   more); the `top_groups` best groups stay
+ *   the `picks` best c of those, in descending order, ties to the lowest index (of groups too)
+ *   weight = scale * s / (renormalize ? sum of s over the chosen : 1), 0 where that sum is 0
+ * An expert whose logit or bias is -infinity is never chosen: such places hold the expert -1 and the weight 0, as all of a token
+ * do whose logits are all -infinity (a padded one).  A token with a NaN, or with an infinity that makes one (softmax), has the expert -1 and the
+ * weight NaN in all its places.
+ *   logits   in   fp32 or bfloat16, row stride ld;  bias  in  fp32 [experts] or NULL
+ *   weights  out  fp32 [tokens][picks];  chosen  out  int32 [tokens][picks]
+ * daq_route_backward -- the gradient of the logits from that of the weights, the choice being what it was; in fp32, rounded once to the
+ * type of the logits.  Places of expert -1 count for nothing, and dweights is not read there.
+ * Limits: experts <= 1024, picks <= 32, groups <= 64, tokens < 2^28.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { DAQ_SCORES_SOFTMAX = 0, DAQ_SCORES_SIGMOID = 1 } daq_scores;
+typedef struct {
+    int32_t scores;               /* daq_scores */
+    int32_t picks;                /* experts of a token, 1 .. experts of the groups that stay */
+    int32_t groups, top_groups;   /* 1 and 1: no groups */
+    int32_t renormalize;
+    float scale;
+} daq_route_opts;
+daq_status daq_route(int64_t tokens, int32_t experts, const void* logits, daq_dtype dtype, int64_t ld, const float* bias,
+                     const daq_route_opts* opts, float* weights, int32_t* chosen, void* stream);
+daq_status daq_route_backward(int64_t tokens, int32_t experts, const float* dweights, const void* logits, daq_dtype dtype, int64_t ld,
+                              const int32_t* chosen, const daq_route_opts* opts, void* dlogits, int64_t ldd, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_experts_plan -- the order of a batch's rows by expert.  A slot is token * picks + place; the slots with an expert in 0 .. experts - 1
+ * are put in the order of their experts, and in their own order within one; all others (expert -1) are left out.
+ *   counts  out  int32 [experts]            rows of every expert
+ *   table   out  int32 [4][experts + 1]     rows, and row tiles of 256, 128 and 64 (of one expert each), before every expert and in all
+ *   rows    out  int32 [tokens * picks]     the slot of every row, -1 behind the last
+ *   place   out  int32 [tokens * picks]     the row of every slot, -1 for slots left out
+ * tokens * picks < 2^28, experts <= 1024.  The other calls take the plan as a daq_experts and read these on the device.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    int64_t tokens;
+    int32_t picks, experts;
+    const int32_t* table;
+    const int32_t* rows;
+    const int32_t* place;
+} daq_experts;
+daq_status daq_experts_plan_workspace(int64_t tokens, int32_t picks, int32_t experts, size_t* bytes);
+daq_status daq_experts_plan(int64_t tokens, int32_t picks, int32_t experts, const int32_t* chosen, int32_t* counts, int32_t* table,
+                            int32_t* rows, int32_t* place, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Experts' products, W of `experts` matrices [N][K] by daq_fp8_quantize_weights.  Row p of the order has the expert e(p) and the
+ * token rows[p] / picks.
+ * daq_experts_matmul -- Y[p][n] = sum over k of A[a(p)][k] * W[e(p)][n][k];  A by rows: sorted == 0: [tokens][K], a(p) the token of
+ *   row p;  sorted != 0: [tokens * picks][K], a(p) = p.  Rows of Y behind the last of the order are left as they were.
+ * daq_experts_linear -- the same with A quantized in the call from X ([tokens][K] or, sorted, [tokens * picks][K]).
+ * daq_experts_quantize -- src [tokens][cols] or, sorted, [tokens * picks][cols] to
+ *   by_rows     blocks along its rows (all of them, as daq_fp8_quantize), and / or
+ *   by_columns  [cols][daq_experts_columns(...)]: the rows in the order of the experts, each expert's beginning a new block of 128 (padding
+ *               is zero, also behind an expert's last row), blocks along the columns.  Blocks behind the last expert's are left as they were.
+ * daq_experts_weight_grad -- dW[e][n][k] = sum over the rows p of e of dY[p][n] * X[a(p)][k], both by_columns of the same plan;
+ *   [experts][N][K], row stride ldw, experts `stride` elements apart; accumulate != 0 (fp32 only) adds.  An expert without rows has
+ *   the gradient zero.
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_experts_columns(int64_t tokens, int32_t picks, int32_t experts, int64_t* columns);
+daq_status daq_experts_quantize(const daq_experts* plan, const void* src, daq_dtype dtype, int64_t cols, int64_t ld, int32_t sorted,
+                                uint8_t* by_rows, uint8_t* by_columns, void* stream);
+daq_status daq_experts_matmul(const daq_experts* plan, int64_t N, int64_t K, const uint8_t* A, int32_t sorted, const uint8_t* W, void* Y,
+                              daq_dtype dtype, int64_t ldy, void* stream);
+daq_status daq_experts_linear_workspace(const daq_experts* plan, int64_t N, int64_t K, daq_dtype x_dtype, int32_t sorted, size_t* bytes);
+daq_status daq_experts_linear(const daq_experts* plan, int64_t N, int64_t K, const void* X, daq_dtype x_dtype, int64_t ldx, int32_t sorted,
+                              const uint8_t* W, void* Y, daq_dtype y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes,
+                              void* stream);
+daq_status daq_experts_weight_grad(const daq_experts* plan, int64_t N, int64_t K, const uint8_t* dY, const uint8_t* X, void* dW,
+                                   daq_dtype dtype, int64_t ldw, int64_t stride, int32_t accumulate, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * daq_experts_combine -- out[t] = sum over the places j of token t of weights[t][j] * y[place[t][j]], in fp32, in the order of the places,
+ *   rounded once.  weights NULL: all 1 (the gradient of rows that several experts read).  A place left out of the order adds
+ *   weight * 0 (nothing, or NaN where the weight is NaN).
+ * daq_experts_combine_backward -- dy[place[t][j]] = weights[t][j] * dout[t] (rounded once to its type; rows behind the last of the
+ *   order are left as they were) and dweights[t][j] = sum over d of dout[t][d] * y[place[t][j]][d] (0 for places left out).
+ *   dy and y, out and dout: [tokens * picks][cols] and [tokens][cols], one type;  weights, dweights  fp32 [tokens][picks], dense;
+ *   dweights may be NULL, then y is not read and may be NULL
+ * ------------------------------------------------------------------------------------------- */
+daq_status daq_experts_combine(const daq_experts* plan, const void* y, daq_dtype dtype, int64_t cols, int64_t ldy, const float* weights,
+                               void* out, int64_t ldo, void* stream);
+daq_status daq_experts_combine_backward(const daq_experts* plan, const void* dout, daq_dtype dtype, int64_t cols, int64_t ldo,
+                                        const void* y, int64_t ldy, const float* weights, void* dy, int64_t lddy, float* dweights,
+                                        void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Measurement aid (not part of the method).  Between daq_prof_begin() and daq_prof_end() every
  * kernel the library launches is bracketed by a HIP event pair on its stream.  daq_prof_end()
  * waits for those events and fills one row per distinct kernel name.  The list of pending event

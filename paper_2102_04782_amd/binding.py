@@ -26,6 +26,7 @@ OP_QUANTIZE_GRAD, OP_CONV_FWD, OP_CONV_BWD_DATA, OP_CONV_BWD_FILTER, OP_CONV_BWD
 LAYOUT_NHWC, LAYOUT_CNHW = 0, 1
 FP32, BF16 = 0, 1
 ACT_SILU, ACT_GELU = 0, 1
+SCORES_SOFTMAX, SCORES_SIGMOID = 0, 1
 SCHEDULE_AUTO, SCHEDULE_THREE_SWEEPS, SCHEDULE_EARLY_COPY, SCHEDULE_CHANNEL_RESIDENT = range(4)
 
 EXPORTS = [
@@ -37,6 +38,10 @@ EXPORTS = [
     "daq_mx4_linear_workspace", "daq_mx4_linear", "daq_ckpt8_save", "daq_ckpt8_restore", "daq_ckpt8_act_forward", "daq_ckpt8_act_backward",
     "daq_ckpt8_weight_grad_workspace", "daq_ckpt8_weight_grad",
     "daq_prof_begin", "daq_prof_end", "daq_status_string", "daq_ceiling_mfma_i8", "daq_ceiling_stream",
+    "daq_layout_fp8", "daq_fp8_quantize", "daq_fp8_quantize_weights", "daq_fp8_dequantize", "daq_fp8_matmul_workspace", "daq_fp8_matmul",
+    "daq_fp8_linear_workspace", "daq_fp8_linear", "daq_route", "daq_route_backward", "daq_experts_plan_workspace", "daq_experts_plan",
+    "daq_experts_columns", "daq_experts_quantize", "daq_experts_matmul", "daq_experts_linear_workspace", "daq_experts_linear",
+    "daq_experts_weight_grad", "daq_experts_combine", "daq_experts_combine_backward",
 ]
 
 
@@ -203,6 +208,20 @@ class Ckpt8Layout(C.Structure):
     _fields_ = [("bytes", C.c_int64), ("off_scales", C.c_int64), ("pitch", C.c_int64)]
 
 
+class Fp8Layout(C.Structure):
+    _fields_ = [("bytes", C.c_int64), ("off_scales", C.c_int64), ("pitch", C.c_int64)]
+
+
+class RouteOpts(C.Structure):
+    _fields_ = [("scores", C.c_int32), ("picks", C.c_int32), ("groups", C.c_int32), ("top_groups", C.c_int32), ("renormalize", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class Experts(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("picks", C.c_int32), ("experts", C.c_int32), ("table", C.c_void_p), ("rows", C.c_void_p),
+                ("place", C.c_void_p)]
+
+
 class ProfRow(C.Structure):
     _fields_ = [("name", C.c_char * 64), ("total_ms", C.c_double), ("launches", C.c_int32)]
 
@@ -271,6 +290,27 @@ def lib():
         L.daq_ckpt8_act_backward.argtypes = [vp, C.c_int, i64, i64, i64, vp, C.c_int, i32, vp, i64, vp, vp]
         L.daq_ckpt8_weight_grad_workspace.argtypes = [i64, i64, i64, C.c_int, i64, i32, psz]
         L.daq_ckpt8_weight_grad.argtypes = [i64, i64, i64, vp, C.c_int, i64, vp, vp, i64, i32, vp, sz, vp]
+        pe, po = C.POINTER(Experts), C.POINTER(RouteOpts)
+        L.daq_layout_fp8.argtypes = [i64, i64, C.POINTER(Fp8Layout)]
+        L.daq_fp8_quantize.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, vp]
+        L.daq_fp8_quantize_weights.argtypes = [vp, C.c_int, i64, i64, i64, i64, i64, vp, vp, vp]
+        L.daq_fp8_dequantize.argtypes = [vp, i64, i64, vp, C.c_int, i64, vp]
+        L.daq_fp8_matmul_workspace.argtypes = [i64, i64, i64, C.c_int, psz]
+        L.daq_fp8_matmul.argtypes = [i64, i64, i64, vp, vp, vp, C.c_int, i64, i32, vp, sz, vp]
+        L.daq_fp8_linear_workspace.argtypes = [i64, i64, i64, C.c_int, C.c_int, psz]
+        L.daq_fp8_linear.argtypes = [i64, i64, i64, vp, C.c_int, i64, vp, vp, C.c_int, i64, vp, sz, vp]
+        L.daq_route.argtypes = [i64, i32, vp, C.c_int, i64, vp, po, vp, vp, vp]
+        L.daq_route_backward.argtypes = [i64, i32, vp, vp, C.c_int, i64, vp, po, vp, i64, vp]
+        L.daq_experts_plan_workspace.argtypes = [i64, i32, i32, psz]
+        L.daq_experts_plan.argtypes = [i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.daq_experts_columns.argtypes = [i64, i32, i32, C.POINTER(i64)]
+        L.daq_experts_quantize.argtypes = [pe, vp, C.c_int, i64, i64, i32, vp, vp, vp]
+        L.daq_experts_matmul.argtypes = [pe, i64, i64, vp, i32, vp, vp, C.c_int, i64, vp]
+        L.daq_experts_linear_workspace.argtypes = [pe, i64, i64, C.c_int, i32, psz]
+        L.daq_experts_linear.argtypes = [pe, i64, i64, vp, C.c_int, i64, i32, vp, vp, C.c_int, i64, vp, sz, vp]
+        L.daq_experts_weight_grad.argtypes = [pe, i64, i64, vp, vp, vp, C.c_int, i64, i64, i32, vp]
+        L.daq_experts_combine.argtypes = [pe, vp, C.c_int, i64, i64, vp, vp, i64, vp]
+        L.daq_experts_combine_backward.argtypes = [pe, vp, C.c_int, i64, i64, vp, i64, vp, vp, i64, vp, vp]
         L.daq_prof_end.argtypes = [C.POINTER(ProfRow), C.c_int32, C.POINTER(C.c_int32)]
         L.daq_ceiling_mfma_i8.argtypes = [C.c_int32, C.c_int32, vp, C.POINTER(C.c_double), vp]
         L.daq_ceiling_stream.argtypes = [C.c_int32, vp, vp, sz, C.c_int32, vp, vp]
@@ -897,6 +937,339 @@ def ckpt8_weight_grad(dy: torch.Tensor, x: Ckpt8, out: Optional[torch.Tensor] = 
     _check(lib().daq_ckpt8_weight_grad(M, N, x.cols, dy.data_ptr(), code, lddy, _kept(x), out.data_ptr(), ldw, int(accumulate),
                                        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "daq_ckpt8_weight_grad")
     return out
+
+
+# ------------------------------------------------------------------------------------------------
+# linear layers in 8-bit floating point, sparse feed-forward layers
+# ------------------------------------------------------------------------------------------------
+@dataclass
+class Fp8:
+    """A [rows, cols] matrix in 8-bit floating point (daq_layout_fp8)."""
+    buf: torch.Tensor       # u8
+    rows: int
+    cols: int
+
+
+@dataclass
+class Plan:
+    """The order of a batch's rows by expert (daq_experts_plan)."""
+    counts: torch.Tensor    # int32 [experts]
+    table: torch.Tensor     # int32 [4, experts + 1]
+    rows: torch.Tensor      # int32 [tokens * picks]: the slot of every row, -1 behind the last
+    place: torch.Tensor     # int32 [tokens, picks]: the row of every slot, -1 for those left out
+    tokens: int
+    picks: int
+    experts: int
+
+
+def layout_fp8(rows: int, cols: int) -> Fp8Layout:
+    L = Fp8Layout()
+    _check(lib().daq_layout_fp8(rows, cols, C.byref(L)), "daq_layout_fp8")
+    return L
+
+
+@functools.lru_cache(maxsize=4096)
+def _fp8_bytes(rows: int, cols: int) -> int:
+    return layout_fp8(rows, cols).bytes
+
+
+def _here(*tensors):
+    """On the device that the call runs on: all of them the current one."""
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.get_device() == _current_device())
+
+
+def _codes(q: Fp8) -> int:
+    b = q.buf
+    _here(b)
+    assert b.dtype == torch.uint8 and b.numel() >= _fp8_bytes(q.rows, q.cols) and b.is_contiguous()
+    return b.data_ptr()
+
+
+def _dense(t: torch.Tensor, dtype, *shape) -> int:
+    _here(t)
+    assert t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _matrix_here(t: torch.Tensor):
+    _here(t)
+    return _matrix(t)
+
+
+def _new(stream, shape, dtype, like: torch.Tensor) -> torch.Tensor:
+    """A tensor of the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _given_ws(workspace: Optional[torch.Tensor], fn_name: str, stream, device, *sizes):
+    """(the workspace, its address, its bytes): the caller's, or one for the call."""
+    if workspace is None:
+        workspace = _few_ws(fn_name, stream, device, *sizes)
+        return workspace, _ptr(workspace), 0 if workspace is None else workspace.numel()
+    _here(workspace)
+    assert workspace.is_contiguous()
+    return workspace, workspace.data_ptr(), workspace.nbytes
+
+
+def alloc_fp8(rows: int, cols: int, device="cuda", stream=None) -> Fp8:
+    return Fp8(_bytes_on(stream, _fp8_bytes(rows, cols), device), rows, cols)
+
+
+def _fp8_out(out: Optional[Fp8], rows: int, cols: int, like: torch.Tensor, stream) -> Fp8:
+    if out is None:
+        return alloc_fp8(rows, cols, like.device, stream)
+    assert out.rows == rows and out.cols == cols
+    return out
+
+
+def fp8_quantize(x: torch.Tensor, columns: bool = False, out: Optional[Fp8] = None, stream=None) -> Fp8:
+    """daq_fp8_quantize: ``x`` [rows, cols] with blocks along its rows, or (``columns``) its transpose, with blocks along its columns."""
+    rows, cols, ld, code = _matrix_here(x)
+    out = _fp8_out(out, *((cols, rows) if columns else (rows, cols)), x, stream)
+    to = _codes(out)
+    _check(lib().daq_fp8_quantize(x.data_ptr(), code, rows, cols, ld, None if columns else to, to if columns else None, _stream(stream)),
+           "daq_fp8_quantize")
+    return out
+
+
+def fp8_quantize_both(x: torch.Tensor, by_rows: Optional[Fp8] = None, by_columns: Optional[Fp8] = None, stream=None):
+    """daq_fp8_quantize: (``x`` [rows, cols] with blocks along its rows, its transpose with blocks along its columns), ``x`` read once."""
+    rows, cols, ld, code = _matrix_here(x)
+    by_rows, by_columns = _fp8_out(by_rows, rows, cols, x, stream), _fp8_out(by_columns, cols, rows, x, stream)
+    _check(lib().daq_fp8_quantize(x.data_ptr(), code, rows, cols, ld, _codes(by_rows), _codes(by_columns), _stream(stream)), "daq_fp8_quantize")
+    return by_rows, by_columns
+
+
+def fp8_quantize_weights(w: torch.Tensor, out: Optional[Fp8] = None, out_t: Optional[Fp8] = None, transposed: bool = True, stream=None):
+    """daq_fp8_quantize_weights: ``w`` [N, K] or [experts, N, K] in tiles of 128 x 128, as (matrices, transposed matrices), the latter None
+    unless ``transposed``."""
+    _here(w)
+    assert w.dim() in (2, 3)
+    count, (rows, cols) = (1 if w.dim() == 2 else w.shape[0]), w.shape[-2:]
+    ld, one = w.stride()[-2:]
+    if rows <= 1:
+        ld = cols
+    stride = w.stride(0) if w.dim() == 3 and count > 1 else 0
+    assert (one == 1 or cols <= 1) and ld >= cols
+    out = _fp8_out(out, count * rows, cols, w, stream)
+    if transposed or out_t is not None:
+        out_t = _fp8_out(out_t, count * cols, rows, w, stream)
+    _check(lib().daq_fp8_quantize_weights(w.data_ptr(), _DTYPES[w.dtype], count, rows, cols, ld, stride, _codes(out),
+                                          None if out_t is None else _codes(out_t), _stream(stream)), "daq_fp8_quantize_weights")
+    return out, out_t
+
+
+def fp8_dequantize(q: Fp8, dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_fp8_dequantize: the values that ``q`` holds, of ``dtype`` (that of ``out`` where it is given)."""
+    codes = _codes(q)
+    out, ld, code = _result(out, q.rows, q.cols, dtype if out is None else None, q.buf, stream)
+    _here(out)
+    _check(lib().daq_fp8_dequantize(codes, q.rows, q.cols, out.data_ptr(), code, ld, _stream(stream)), "daq_fp8_dequantize")
+    return out
+
+
+def fp8_matmul(a: Fp8, b: Fp8, dtype=None, out: Optional[torch.Tensor] = None, accumulate: bool = False,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_fp8_matmul: a b^T, [a.rows, b.rows], of ``dtype`` (that of ``out``, or bfloat16); ``accumulate`` adds it to ``out`` (fp32)."""
+    assert a.cols == b.cols and (out is not None or not accumulate)
+    pa, pb = _codes(a), _codes(b)
+    out, ld, code = _result(out, a.rows, b.rows, (dtype or torch.bfloat16) if out is None else dtype, b.buf, stream)
+    _here(out)
+    ws, at, n = _given_ws(workspace, "daq_fp8_matmul_workspace", stream, b.buf.device, a.rows, b.rows, a.cols, code)
+    _check(lib().daq_fp8_matmul(a.rows, b.rows, a.cols, pa, pb, out.data_ptr(), code, ld, int(accumulate), at, n, _stream(stream)),
+           "daq_fp8_matmul")
+    return out
+
+
+def fp8_linear(x: torch.Tensor, w: Fp8, dtype=None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """daq_fp8_linear: x w^T with ``x`` [M, w.cols] quantized in the call; the result is of ``dtype`` (that of ``out``, or of ``x``)."""
+    M, K, ldx, x_code = _matrix_here(x)
+    N, pw = w.rows, _codes(w)
+    assert K == w.cols
+    out, ldy, y_code = _result(out, M, N, (dtype or x.dtype) if out is None else dtype, x, stream)
+    _here(out)
+    ws, at, n = _given_ws(workspace, "daq_fp8_linear_workspace", stream, x.device, M, N, K, x_code, y_code)
+    _check(lib().daq_fp8_linear(M, N, K, x.data_ptr(), x_code, ldx, pw, out.data_ptr(), y_code, ldy, at, n, _stream(stream)), "daq_fp8_linear")
+    return out
+
+
+def route(logits: torch.Tensor, picks: int, scores=SCORES_SOFTMAX, bias: Optional[torch.Tensor] = None, groups: int = 1, top_groups: int = 1,
+          renormalize: bool = True, scale: float = 1.0, out=None, stream=None):
+    """daq_route: (weights fp32 [tokens, picks], experts int32 [tokens, picks]) for ``logits`` [tokens, experts]; ``out``: such a pair."""
+    tokens, experts, ld, code = _matrix_here(logits)
+    pb = None if bias is None else _dense(bias, torch.float32, experts)
+    if out is None:
+        out = _new(stream, (tokens, picks), torch.float32, logits), _new(stream, (tokens, picks), torch.int32, logits)
+    weights, chosen = out
+    opts = RouteOpts(scores, picks, groups, top_groups, int(renormalize), scale)
+    _check(lib().daq_route(tokens, experts, logits.data_ptr(), code, ld, pb, C.byref(opts), _dense(weights, torch.float32, tokens, picks),
+                           _dense(chosen, torch.int32, tokens, picks), _stream(stream)), "daq_route")
+    return out
+
+
+def route_backward(dweights: torch.Tensor, logits: torch.Tensor, chosen: torch.Tensor, scores=SCORES_SOFTMAX, renormalize: bool = True,
+                   scale: float = 1.0, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_route_backward: the gradient of ``logits``, of their type, from that of the weights; ``chosen``, ``scores``, ``renormalize`` and
+    ``scale`` as of the forward pass."""
+    tokens, experts, ld, code = _matrix_here(logits)
+    picks = chosen.shape[1]
+    out, ldd, _ = _result(out, tokens, experts, logits.dtype, logits, stream)
+    _here(out)
+    opts = RouteOpts(scores, picks, 1, 1, int(renormalize), scale)
+    _check(lib().daq_route_backward(tokens, experts, _dense(dweights, torch.float32, tokens, picks), logits.data_ptr(), code, ld,
+                                    _dense(chosen, torch.int32, tokens, picks), C.byref(opts), out.data_ptr(), ldd, _stream(stream)),
+           "daq_route_backward")
+    return out
+
+
+def alloc_plan(tokens: int, picks: int, experts: int, device="cuda", stream=None) -> Plan:
+    """Memory of a plan: of ``stream``, or of the current one."""
+    def ints(*shape):
+        if stream is None:
+            return torch.empty(shape, dtype=torch.int32, device=device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=torch.int32, device=device)
+
+    return Plan(ints(experts), ints(4, experts + 1), ints(tokens * picks), ints(tokens, picks), tokens, picks, experts)
+
+
+def experts_plan(chosen: torch.Tensor, experts: int, out: Optional[Plan] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> Plan:
+    """daq_experts_plan: the order of the rows of ``chosen`` int32 [tokens, picks] (-1: none) by expert."""
+    assert chosen.dim() == 2
+    tokens, picks = chosen.shape
+    at = _dense(chosen, torch.int32, tokens, picks)
+    if out is None:
+        out = alloc_plan(tokens, picks, experts, chosen.device, stream)
+    assert (out.tokens, out.picks, out.experts) == (tokens, picks, experts)
+    c, t = _dense(out.counts, torch.int32, experts), _dense(out.table, torch.int32, 4, experts + 1)
+    r, p = _dense(out.rows, torch.int32, tokens * picks), _dense(out.place, torch.int32, tokens, picks)
+    ws, wa, n = _given_ws(workspace, "daq_experts_plan_workspace", stream, chosen.device, tokens, picks, experts)
+    _check(lib().daq_experts_plan(tokens, picks, experts, at, c, t, r, p, wa, n, _stream(stream)), "daq_experts_plan")
+    return out
+
+
+def _plan(p: Plan) -> Experts:
+    slots = p.tokens * p.picks
+    return Experts(p.tokens, p.picks, p.experts, _dense(p.table, torch.int32, 4, p.experts + 1), _dense(p.rows, torch.int32, slots),
+                   _dense(p.place, torch.int32, p.tokens, p.picks))
+
+
+@functools.lru_cache(maxsize=4096)
+def experts_columns(tokens: int, picks: int, experts: int) -> int:
+    """daq_experts_columns: columns of what ``experts_quantize`` makes by columns."""
+    n = C.c_int64(0)
+    _check(lib().daq_experts_columns(tokens, picks, experts, C.byref(n)), "daq_experts_columns")
+    return n.value
+
+
+def experts_quantize(x: torch.Tensor, plan: Plan, sorted_rows: bool = False, by_rows: Optional[Fp8] = None, by_columns: Optional[Fp8] = None,
+                     stream=None):
+    """daq_experts_quantize: (``x`` [tokens, cols], or [tokens * picks, cols] in the order of the plan, with blocks along its rows, and its rows in
+    the order of the plan with blocks along the columns, each expert's beginning a new one)."""
+    rows, cols, ld, code = _matrix_here(x)
+    assert rows == plan.tokens * (plan.picks if sorted_rows else 1)
+    e = _plan(plan)
+    by_rows = _fp8_out(by_rows, rows, cols, x, stream)
+    by_columns = _fp8_out(by_columns, cols, experts_columns(plan.tokens, plan.picks, plan.experts), x, stream)
+    _check(lib().daq_experts_quantize(C.byref(e), x.data_ptr(), code, cols, ld, int(sorted_rows), _codes(by_rows), _codes(by_columns),
+                                      _stream(stream)), "daq_experts_quantize")
+    return by_rows, by_columns
+
+
+def experts_matmul(a: Fp8, w: Fp8, plan: Plan, sorted_rows: bool = False, dtype=None, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """daq_experts_matmul: row p of the plan times its expert's matrix, [tokens * picks, N], of ``dtype`` (that of ``out``, or bfloat16)."""
+    slots = plan.tokens * plan.picks
+    N = w.rows // plan.experts
+    assert a.cols == w.cols and w.rows == N * plan.experts and a.rows == (slots if sorted_rows else plan.tokens)
+    e, pa, pw = _plan(plan), _codes(a), _codes(w)
+    out, ld, code = _result(out, slots, N, (dtype or torch.bfloat16) if out is None else dtype, w.buf, stream)
+    _here(out)
+    _check(lib().daq_experts_matmul(C.byref(e), N, a.cols, pa, int(sorted_rows), pw, out.data_ptr(), code, ld, _stream(stream)),
+           "daq_experts_matmul")
+    return out
+
+
+def experts_linear(x: torch.Tensor, w: Fp8, plan: Plan, sorted_rows: bool = False, dtype=None, out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """daq_experts_linear: the same with ``x`` quantized in the call; the result is of ``dtype`` (that of ``out``, or of ``x``)."""
+    rows, K, ldx, x_code = _matrix_here(x)
+    slots = plan.tokens * plan.picks
+    N = w.rows // plan.experts
+    assert K == w.cols and w.rows == N * plan.experts and rows == (slots if sorted_rows else plan.tokens)
+    e, pw = _plan(plan), _codes(w)
+    out, ldy, y_code = _result(out, slots, N, (dtype or x.dtype) if out is None else dtype, x, stream)
+    _here(out)
+    if workspace is None:
+        need = C.c_size_t(0)
+        _check(lib().daq_experts_linear_workspace(C.byref(e), N, K, x_code, int(sorted_rows), C.byref(need)), "daq_experts_linear_workspace")
+        workspace = _bytes_on(stream, need.value, x.device) if need.value else None
+    else:
+        _here(workspace)
+        assert workspace.is_contiguous()
+    _check(lib().daq_experts_linear(C.byref(e), N, K, x.data_ptr(), x_code, ldx, int(sorted_rows), pw, out.data_ptr(), y_code, ldy,
+                                    _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream(stream)), "daq_experts_linear")
+    return out
+
+
+def experts_weight_grad(dy: Fp8, x: Fp8, plan: Plan, dtype=None, out: Optional[torch.Tensor] = None, accumulate: bool = False,
+                        stream=None) -> torch.Tensor:
+    """daq_experts_weight_grad: every expert's dy^T x, [experts, N, K] of ``dtype`` (that of ``out``, or fp32), of what ``experts_quantize`` made by
+    columns; ``accumulate`` adds it to ``out`` (fp32)."""
+    columns = experts_columns(plan.tokens, plan.picks, plan.experts)
+    assert dy.cols == columns and x.cols == columns and (out is not None or not accumulate)
+    N, K = dy.rows, x.rows
+    e, pd, px = _plan(plan), _codes(dy), _codes(x)
+    if out is None:
+        out = _new(stream, (plan.experts, N, K), dtype or torch.float32, dy.buf)
+    _here(out)
+    assert tuple(out.shape) == (plan.experts, N, K) and (dtype is None or out.dtype == dtype) and (out.stride(2) == 1 or K <= 1)
+    ldw = out.stride(1) if N > 1 else K
+    stride = out.stride(0) if plan.experts > 1 else (N - 1) * ldw + K
+    _check(lib().daq_experts_weight_grad(C.byref(e), N, K, pd, px, out.data_ptr(), _DTYPES[out.dtype], ldw, stride, int(accumulate),
+                                         _stream(stream)), "daq_experts_weight_grad")
+    return out
+
+
+def experts_combine(y: torch.Tensor, plan: Plan, weights: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """daq_experts_combine: the sum of each token's rows of ``y`` [tokens * picks, cols], times ``weights`` [tokens, picks]; of the type of ``y``."""
+    rows, cols, ldy, code = _matrix_here(y)
+    assert rows == plan.tokens * plan.picks
+    e = _plan(plan)
+    w = None if weights is None else _dense(weights, torch.float32, plan.tokens, plan.picks)
+    out, ldo, _ = _result(out, plan.tokens, cols, y.dtype, y, stream)
+    _here(out)
+    _check(lib().daq_experts_combine(C.byref(e), y.data_ptr(), code, cols, ldy, w, out.data_ptr(), ldo, _stream(stream)), "daq_experts_combine")
+    return out
+
+
+def experts_combine_backward(dout: torch.Tensor, y: Optional[torch.Tensor], plan: Plan, weights: Optional[torch.Tensor] = None,
+                             out: Optional[torch.Tensor] = None, dweights: Optional[torch.Tensor] = None, stream=None):
+    """daq_experts_combine_backward: (the gradient of ``y``, that of the weights; None without ``y``)."""
+    rows, cols, ldo, code = _matrix_here(dout)
+    slots = plan.tokens * plan.picks
+    assert rows == plan.tokens and (y is not None or dweights is None)
+    e = _plan(plan)
+    w = None if weights is None else _dense(weights, torch.float32, plan.tokens, plan.picks)
+    out, lddy, _ = _result(out, slots, cols, dout.dtype, dout, stream)
+    _here(out)
+    py, ldy, dw = None, 0, None
+    if y is not None:
+        y_rows, y_cols, ldy, y_code = _matrix_here(y)
+        assert (y_rows, y_cols, y_code) == (slots, cols, code)
+        py = y.data_ptr()
+        if dweights is None:
+            dweights = _new(stream, (plan.tokens, plan.picks), torch.float32, dout)
+        dw = _dense(dweights, torch.float32, plan.tokens, plan.picks)
+    _check(lib().daq_experts_combine_backward(C.byref(e), dout.data_ptr(), code, cols, ldo, py, ldy, w, out.data_ptr(), lddy, dw,
+                                              _stream(stream)), "daq_experts_combine_backward")
+    return out, dweights
 
 
 # ------------------------------------------------------------------------------------------------

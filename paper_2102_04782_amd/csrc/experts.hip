@@ -1,0 +1,148 @@
+// The weighted sum of the rows that a token's experts made, and its gradients.
+#include "fp8_block.h"
+
+namespace daq {
+
+namespace {
+
+struct CombineArgs {
+    int64_t tokens, cols, ldy, ldo, lddy;
+    int picks, chunks;        // of columns, of a workgroup each
+    const int32_t* place;
+    const float* weights;
+    float* dweights;
+};
+
+__device__ __forceinline__ float element(const Eight<float>& v, int i) { return bits_as<float>(v.w[i]); }
+__device__ __forceinline__ float element(const Eight<uint16_t>& v, int i) { return (i & 1) ? bf16_hi(v.w[i / 2]) : bf16_lo(v.w[i / 2]); }
+// Eight results of a row, or the first `left` of them.
+__device__ __forceinline__ void store8(float* z, int left, const float (&v)[8]) {
+    if (left >= 8) {
+        *reinterpret_cast<u32x4_a4*>(z) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+        *reinterpret_cast<u32x4_a4*>(z + 4) = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) z[i] = v[i];
+    }
+}
+__device__ __forceinline__ void store8(uint16_t* z, int left, const float (&v)[8]) {
+    if (left >= 8) {
+        *reinterpret_cast<u32x4_a2*>(z) = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) z[i] = (uint16_t)(pack_bf16(v[i], 0.f) & 0xFFFFu);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load_some(const T* p, int64_t left, Eight<T>& v) {
+    if (left >= 8) load8(p, v);
+    else load8(p, (int)max(left, (int64_t)0), v);
+}
+
+// Eight columns of a token a lane; the rows of four places are asked for before the first is added.
+template <typename T>
+__global__ __launch_bounds__(256) void k_combine(const T* y, T* out, CombineArgs p) {
+    const int64_t t = blockIdx.x / p.chunks, c = (int64_t)(blockIdx.x - t * p.chunks) * 2048 + threadIdx.x * 8, left = p.cols - c;
+    if (left <= 0) return;
+    const int32_t* place = p.place + t * p.picks;
+    const float* weights = p.weights ? p.weights + t * p.picks : nullptr;
+    float sum[8] = {};
+    for (int j0 = 0; j0 < p.picks; j0 += 4) {
+        Eight<T> v[4];
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = j0 + i, row = j < p.picks ? place[j] : -1;
+            w[i] = j < p.picks ? weights ? weights[j] : 1.f : 0.f;
+            load_some(y + (int64_t)max(row, 0) * p.ldy + c, row >= 0 ? left : 0, v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = fmaf(w[i], element(v[i], e), sum[e]);
+    }
+    store8(out + t * p.ldo + c, (int)min(left, (int64_t)8), sum);
+}
+
+// A wave a place of a token: the row's gradient, and the dot product that is its weight's.
+template <typename T, bool DW>
+__global__ __launch_bounds__(256) void k_combine_back(const T* dout, const T* y, T* dy, CombineArgs p) {
+    const int lane = threadIdx.x % kWave;
+    const int64_t slot = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    if (slot >= p.tokens * p.picks) return;
+    const int64_t t = slot / p.picks;
+    const int row = p.place[slot];
+    if (row < 0) {
+        if (DW && lane == 0) p.dweights[slot] = 0.f;
+        return;
+    }
+    const float w = p.weights ? p.weights[slot] : 1.f;
+    float dot = 0.f;
+    for (int64_t c = lane * 8; c < p.cols; c += 512) {
+        Eight<T> d, v;
+        load_some(dout + t * p.ldo + c, p.cols - c, d);
+        if (DW) load_some(y + (int64_t)row * p.ldy + c, p.cols - c, v);
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = element(d, e);
+            z[e] = w * x;
+            if (DW) dot = fmaf(x, element(v, e), dot);
+        }
+        store8(dy + (int64_t)row * p.lddy + c, (int)min(p.cols - c, (int64_t)8), z);
+    }
+    if (DW) {
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) dot += __shfl_xor(dot, d);
+        if (lane == 0) p.dweights[slot] = dot;
+    }
+}
+
+template <typename T>
+daq_status launch_combine(const void* y, void* out, const CombineArgs& p, hipStream_t st) {
+    DAQ_LAUNCH("combine", st, hipLaunchKernelGGL(k_combine<T>, dim3((unsigned)(p.tokens * p.chunks)), dim3(256), 0, st, static_cast<const T*>(y), static_cast<T*>(out), p));
+    return DAQ_OK;
+}
+template <typename T>
+daq_status launch_combine_back(const void* dout, const void* y, void* dy, const CombineArgs& p, hipStream_t st) {
+    const auto kernel = p.dweights ? k_combine_back<T, true> : k_combine_back<T, false>;
+    DAQ_LAUNCH("combine_back", st, hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(p.tokens * p.picks, 4)), dim3(256), 0, st, static_cast<const T*>(dout), static_cast<const T*>(y), static_cast<T*>(dy), p));
+    return DAQ_OK;
+}
+daq_status combine_check(const daq_experts* plan, int dtype, int64_t cols) {
+    if (!plan_ok(plan) || !dtype_ok(dtype) || cols <= 0) return DAQ_ERR_INVALID_ARG;
+    return matrix_size(plan_slots(*plan), cols);
+}
+bool a4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+}  // namespace
+
+}  // namespace daq
+
+using namespace daq;
+
+extern "C" daq_status daq_experts_combine(const daq_experts* plan, const void* y, daq_dtype dtype, int64_t cols, int64_t ldy, const float* weights,
+                                          void* out, int64_t ldo, void* stream) {
+    const daq_status rc = combine_check(plan, dtype, cols);
+    if (rc != DAQ_OK || plan->tokens == 0) return rc;
+    if (!y || !elem_aligned(y, dtype) || !out || !elem_aligned(out, dtype) || ldy < cols || ldo < cols || !a4(weights)) return DAQ_ERR_INVALID_ARG;
+    const int64_t chunks = ceil_div(cols, 2048);
+    if (!grid_ok(plan->tokens * chunks, 256)) return DAQ_ERR_UNSUPPORTED;
+    const CombineArgs p{plan->tokens, cols, ldy, ldo, 0, plan->picks, (int)chunks, plan->place, weights, nullptr};
+    return dtype == DAQ_BF16 ? launch_combine<uint16_t>(y, out, p, (hipStream_t)stream) : launch_combine<float>(y, out, p, (hipStream_t)stream);
+}
+
+extern "C" daq_status daq_experts_combine_backward(const daq_experts* plan, const void* dout, daq_dtype dtype, int64_t cols, int64_t ldo,
+                                                   const void* y, int64_t ldy, const float* weights, void* dy, int64_t lddy, float* dweights,
+                                                   void* stream) {
+    const daq_status rc = combine_check(plan, dtype, cols);
+    if (rc != DAQ_OK || plan->tokens == 0) return rc;
+    if (!dout || !elem_aligned(dout, dtype) || !dy || !elem_aligned(dy, dtype) || ldo < cols || lddy < cols || !a4(weights) || !a4(dweights)) return DAQ_ERR_INVALID_ARG;
+    if (dweights && (!y || !elem_aligned(y, dtype) || ldy < cols)) return DAQ_ERR_INVALID_ARG;
+    if (!grid_ok(ceil_div(plan_slots(*plan), 4), 256)) return DAQ_ERR_UNSUPPORTED;
+    const CombineArgs p{plan->tokens, cols, ldy, ldo, lddy, plan->picks, 0, plan->place, weights, dweights};
+    return dtype == DAQ_BF16 ? launch_combine_back<uint16_t>(dout, y, dy, p, (hipStream_t)stream)
+                             : launch_combine_back<float>(dout, y, dy, p, (hipStream_t)stream);
+}

@@ -1,0 +1,606 @@
+// Products of 8-bit floating point matrices with a scale for every 128 elements, D[m][n] = sum over k of A[m][k] * B[n][k], whole ones and those of
+// experts, whose rows, or whose share of the summed axis, a plan on the device tells.
+//
+// The matrix instructions take codes and scale bytes as they are: 32 x 32 x 64 (tiles) or 16 x 16 x 128 (few rows), 32 bytes a lane of each operand
+// and one scale for 32 of the summed axis.  As a block is 128 long and both operands are cut alike, which of a block's elements a
+// lane holds does not matter, as long as it is the same of both.  B goes in as the first operand, so that a lane holds
+// neighbouring columns of a row of D.
+#include <cmath>
+
+#include "fp8_block.h"
+#include "tile_product.h"
+
+namespace daq {
+
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+struct Fp8Operand {
+    const uint8_t* codes;
+    const uint8_t* scales;
+    int64_t rows, pitch;
+};
+Fp8Operand operand(const uint8_t* buf, int64_t rows, int64_t cols) {
+    daq_fp8_layout L;
+    daq_layout_fp8(rows, cols, &L);
+    return {buf, buf + L.off_scales, rows, L.pitch};
+}
+
+struct ProductArgs {
+    Fp8Operand a, b;
+    int64_t M, N;             // of one product
+    int stages;               // blocks of 128 of the summed axis
+    void* d;
+    int64_t ldd;
+    int bf16, accumulate;
+    int tiles_m, tiles_n;     // (experts' rows: tiles_m is the most there can be)
+    int splits, per_split;    // of the summed axis: part z, of per_split stages, goes to d + z * M * ldd
+    // experts
+    const int32_t* table;
+    const int32_t* order;
+    int experts, picks;       // picks: row p of the order is row order[p] / picks of A, 0: row p
+    int64_t stride;           // from one expert's gradient to the next
+};
+enum class Of { kWhole, kExpertRows, kExpertWeights };
+
+// 32 x 32 x 64; the scale is the lowest byte of its word.
+__device__ __forceinline__ v16f mfma8(v8i x, v8i y, v16f c, int sx, int sy) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 0, 0, 0, sx, 0, sy);
+}
+
+// Eight codes to bfloat16, times the scale: exact, but what the scale takes beyond bfloat16's range.
+__device__ __forceinline__ v4i in_bf16(int lo, int hi, float s) {
+    const bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true)};
+    return v4i{__builtin_bit_cast(int, v[0]), __builtin_bit_cast(int, v[1]), __builtin_bit_cast(int, v[2]), __builtin_bit_cast(int, v[3])};
+}
+
+// The results of a workgroup of WR x WC waves, each RB x CB tiles of 32 x 32, summed over the stages s0 .. s1 - 1 of 128.  A stage of both operands,
+// 128 bytes of every row, goes straight to LDS, where the 16-byte piece j of a row lies at j ^ row % 8: eight lanes ask for a row's line in that
+// order, and the fragment reads of eight rows share no bank.  SLOTS stages are under way or being read.  Fragments are read a step
+// (64 of a stage's 128) ahead into the registers that the products have just done with; the barrier stands behind the first products of a stage's
+// second step, when this stage is read out and the next has landed.
+template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT>
+struct Fp8Product {
+    static constexpr int kWaves = WR * WC, kRows = WR * RB * 32, kCols = WC * CB * 32;
+    static constexpr int kCodes = (kRows + kCols) * 128, kStage = kCodes + (kRows + kCols) * 4;   // bytes of a stage, its scale words behind the codes
+    static constexpr int kLdsBytes = SLOTS * kStage;
+    static constexpr int kAsks = 9;                       // requests of a wave for a stage: 64 rows, eight at a time, and their scale words
+    static_assert(kRows + kCols == kWaves * 64 && kRows % 64 == 0, "a wave asks for 64 rows of one operand");
+    static_assert(SLOTS == 2 || SLOTS == 4, "the loop is written out for these");
+    static_assert(kLdsBytes / kWaves >= RB * 32 * 128, "a wave's share holds its rows of results");
+
+    v16f acc[CB][RB];
+
+    // Rows a0 .. of A (a_end: the first that is not the tile's; rows behind it repeat the last) and b0 .. of B; `order`: of A's rows.
+    __device__ __forceinline__ void run(const Fp8Operand& a, const Fp8Operand& b, int64_t a0, int64_t a_end, int64_t b0, int64_t b_end,
+                                        const int32_t* order, int picks, int s0, int s1, uint8_t* lds) {
+        run_on(a, b, a0, a_end, b0, b_end, order, picks, s0, s1, lds, lds + kStage, lds + 2 % SLOTS * kStage, lds + 3 % SLOTS * kStage);
+    }
+    // lds0 ..: the stages' places, as arguments so that the compiler knows them apart, and does not let a read of one wait for the requests
+    // into the others.
+    __device__ __forceinline__ void run_on(const Fp8Operand& a, const Fp8Operand& b, int64_t a0, int64_t a_end, int64_t b0, int64_t b_end,
+                                           const int32_t* order, int picks, int s0, int s1, uint8_t* __restrict__ lds0, uint8_t* __restrict__ lds1,
+                                           uint8_t* __restrict__ lds2, uint8_t* __restrict__ lds3) {
+        const int lane = threadIdx.x % kWave;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const int wr = wave / WC, wc = wave % WC;
+        // what this wave asks for
+        const bool of_b = wave >= kRows / 64;
+        const Fp8Operand& o = of_b ? b : a;
+        const bool gather = !of_b && order != nullptr;
+        const int64_t first = of_b ? b0 + (wave - kRows / 64) * 64 : a0 + wave * 64, end = of_b ? b_end : a_end;
+        const int64_t base = gather ? 0 : min(first, end - 1);
+        uint32_t off[8], soff;
+        auto row_of = [&](int i) {
+            const int64_t r = min(first + i, end - 1);
+            return (uint32_t)(gather ? (picks ? order[r] / picks : (int)r) : r - base);
+        };
+#pragma unroll
+        for (int i = 0; i < 8; ++i) off[i] = row_of(i * 8 + lane / 8) * (uint32_t)o.pitch + (uint32_t)((lane % 8) ^ (lane / 8)) * 16u;
+        soff = row_of(lane) * 4u;
+        auto bytes = [](const uint8_t* from, int64_t n) {
+            return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(n < (int64_t)kTileReach ? (uint32_t)n : kTileReach), 0x00020000);
+        };
+        const __amdgpu_buffer_rsrc_t src = bytes(o.codes + base * o.pitch, (o.rows - base) * o.pitch);
+        auto ask = [&](int s, uint8_t* to) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) tile_to_lds(src, off[i], (uint32_t)s * 128u, to + (wave * 8 + i) * 1024);
+            words_to_lds(bytes(o.scales + ((int64_t)(s / 4) * o.rows + base) * 4, (o.rows - base) * 4), soff, 0, to + kCodes + wave * 256);
+        };
+        v8i fr[RB], fc[2][CB];
+        int sr[RB], sc[CB];
+        int at[2][2];     // of a lane in 32 rows: step and half of its 32 bytes
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) at[k][t] = (lane % 32) * 128 + ((k * 4 + lane / 32 * 2 + t) ^ (lane & 7)) * 16;
+        auto fragment = [&](const uint8_t* from, int block, int k) {
+            const v4i lo = *reinterpret_cast<const v4i*>(from + block * 4096 + at[k][0]), hi = *reinterpret_cast<const v4i*>(from + block * 4096 + at[k][1]);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        const int block_r = wr * RB, block_c = WR * RB + wc * CB;
+        auto read_c = [&](const uint8_t* from, int k) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) fc[k][j] = fragment(from, block_c + j, k);
+        };
+        int wr_next[RB], wc_next[CB];
+        auto read_words = [&](const uint8_t* from) {
+#pragma unroll
+            for (int i = 0; i < RB; ++i) wr_next[i] = *reinterpret_cast<const int*>(from + kCodes + (block_r + i) * 128 + (lane % 32) * 4);
+#pragma unroll
+            for (int j = 0; j < CB; ++j) wc_next[j] = *reinterpret_cast<const int*>(from + kCodes + (block_c + j) * 128 + (lane % 32) * 4);
+        };
+        auto take_words = [&](int s) {      // the byte of stage s; EXACT: the scale itself
+            auto of = [&](int w) { return EXACT ? __float_as_int(scale_of((uint32_t)w >> (s % 4 * 8) & 255u)) : w >> (s % 4 * 8); };
+#pragma unroll
+            for (int i = 0; i < RB; ++i) sr[i] = of(wr_next[i]);
+#pragma unroll
+            for (int j = 0; j < CB; ++j) sc[j] = of(wc_next[j]);
+        };
+        auto multiply = [&](int i, int k) {
+            if constexpr (!EXACT) {
+#pragma unroll
+                for (int j = 0; j < CB; ++j) acc[j][i] = mfma8(fc[k][j], fr[i], acc[j][i], sc[j], sr[i]);
+            }
+        };
+        // EXACT: a step in bfloat16, eight of a lane's 32 elements at a time
+        auto multiply_all = [&](int k) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                v4i x[CB];
+#pragma unroll
+                for (int j = 0; j < CB; ++j) x[j] = in_bf16(fc[k][j][2 * q], fc[k][j][2 * q + 1], __int_as_float(sc[j]));
+#pragma unroll
+                for (int i = 0; i < RB; ++i) {
+                    const v4i y = in_bf16(fr[i][2 * q], fr[i][2 * q + 1], __int_as_float(sr[i]));
+#pragma unroll
+                    for (int j = 0; j < CB; ++j) acc[j][i] = mfma16(x[j], y, acc[j][i]);
+                }
+            }
+        };
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int i = 0; i < RB; ++i) acc[j][i] = v16f{};
+        if (s0 >= s1) return;
+        const int last = s1 - 1;
+        ask(s0, lds0);
+        ask(min(s0 + 1, last), lds1);
+        if constexpr (SLOTS == 4) {
+            ask(min(s0 + 2, last), lds2);
+            ask(min(s0 + 3, last), lds3);
+        }
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * kAsks) : "memory");
+        __builtin_amdgcn_s_barrier();
+        read_words(lds0);
+        read_c(lds0, 0);
+#pragma unroll
+        for (int i = 0; i < RB; ++i) fr[i] = fragment(lds0, block_r + i, 0);
+        take_words(s0);
+        auto stage = [&](int s, uint8_t* here, uint8_t* next) {
+            if constexpr (EXACT) {
+                // (the conversions leave the compiler enough to put between reads and products)
+                read_c(here, 1);
+                v8i fr1[RB];
+#pragma unroll
+                for (int i = 0; i < RB; ++i) fr1[i] = fragment(here, block_r + i, 1);
+                multiply_all(0);
+#pragma unroll
+                for (int i = 0; i < RB; ++i) fr[i] = fr1[i];
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");
+                __builtin_amdgcn_s_barrier();
+                ask(min(s + SLOTS, last), here);
+                read_words(next);
+                read_c(next, 0);
+                v8i fr0[RB];
+#pragma unroll
+                for (int i = 0; i < RB; ++i) fr0[i] = fragment(next, block_r + i, 0);
+                multiply_all(1);
+#pragma unroll
+                for (int i = 0; i < RB; ++i) fr[i] = fr0[i];
+                __builtin_amdgcn_sched_barrier(0);
+                take_words(s + 1);
+                return;
+            }
+            read_c(here, 1);
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                multiply(i, 0);
+                fr[i] = fragment(here, block_r + i, 1);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * CB, 0);      // LDS reads
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, CB, 0);      // matrix instructions
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(0, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            // the next stage has landed, this one is read out
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");
+            __builtin_amdgcn_s_barrier();
+            read_words(next);
+            read_c(next, 0);
+            fr[0] = fragment(next, block_r, 0);
+            ask(min(s + SLOTS, last), here);
+#pragma unroll
+            for (int i = 1; i < RB; ++i) {
+                multiply(i, 1);
+                fr[i] = fragment(next, block_r + i, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x100, RB + CB + 2 * CB + 2, 0);
+#pragma unroll
+            for (int i = 1; i < RB; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, CB, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            take_words(s + 1);
+        };
+        int s = s0;
+        if constexpr (SLOTS == 4) {
+            for (; s + 3 < s1; s += 4) {
+                stage(s, lds0, lds1);
+                stage(s + 1, lds1, lds2);
+                stage(s + 2, lds2, lds3);
+                stage(s + 3, lds3, lds0);
+            }
+            if (s < s1) stage(s, lds0, lds1);
+            if (s + 1 < s1) stage(s + 1, lds1, lds2);
+            if (s + 2 < s1) stage(s + 2, lds2, lds3);
+        } else {
+            for (; s + 1 < s1; s += 2) {
+                stage(s, lds0, lds1);
+                stage(s + 1, lds1, lds0);
+            }
+            if (s < s1) stage(s, lds0, lds1);
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the requests past the end have landed before LDS is put to other use
+    }
+};
+
+// Tiles of kRows x kCols results, a workgroup each.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles, in bands of four row
+// tiles, whose panels its L2 holds.
+template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
+__global__ __launch_bounds__(64 * WR * WC, 1) void k_fp8_product(ProductArgs p) {
+    using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
+    constexpr int kTable = Product::kRows == 256 ? kTable256 : Product::kRows == 128 ? kTable128 : kTable64;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int32_t* tiles = OF == Of::kExpertRows ? p.table + kTable * (p.experts + 1) : nullptr;
+    const int tiles_m = OF == Of::kExpertRows ? tiles[p.experts] : p.tiles_m;
+    const int64_t all = (int64_t)tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1), per = (all + kXcd - 1) / kXcd;
+    const int64_t index = blockIdx.x / kXcd;
+    int64_t t = (int64_t)(blockIdx.x % kXcd) * per + index;
+    if (index >= per || t >= all) return;
+    int e = 0;
+    if constexpr (OF == Of::kExpertWeights) {
+        const int each = tiles_m * p.tiles_n;
+        e = (int)(t / each);
+        t -= (int64_t)e * each;
+    }
+    const int64_t band = t / (4 * p.tiles_n);
+    const int rest = (int)(t - band * 4 * p.tiles_n), high = min(4, tiles_m - (int)band * 4);
+    const int tm = (int)band * 4 + rest % high, tn = rest / high;
+
+    int64_t a0 = (int64_t)tm * Product::kRows, a_end = p.M, b0 = (int64_t)tn * Product::kCols, b_end = p.N;
+    int s0 = 0, s1 = p.stages;
+    uint8_t* d = static_cast<uint8_t*>(p.d);
+    int64_t b_first = 0;
+    if constexpr (OF == Of::kExpertRows) {
+        e = expert_of_tile(tiles, p.experts, tm, threadIdx.x % kWave);
+        a0 = p.table[e] + (int64_t)(tm - tiles[e]) * Product::kRows;
+        a_end = p.table[e + 1];
+        b_first = (int64_t)e * p.N;
+    } else if constexpr (OF == Of::kExpertWeights) {
+        const int32_t* blocks = p.table + kTable128 * (p.experts + 1);
+        s0 = blocks[e];
+        s1 = blocks[e + 1];
+        if (s0 == s1 && p.accumulate) return;
+        d += (int64_t)e * p.stride * (p.bf16 ? 2 : 4);
+    } else {
+        s0 = (int)blockIdx.y * p.per_split;
+        s1 = min(s0 + p.per_split, p.stages);
+        d += (int64_t)blockIdx.y * p.M * p.ldd * 4;      // (parts are fp32)
+    }
+    Product prod;
+    prod.run(p.a, p.b, a0, a_end, b_first + b0, b_first + b_end, OF == Of::kExpertRows && p.picks ? p.order : nullptr, p.picks, s0, s1, lds);
+    const int wave = threadIdx.x / kWave;
+    const int64_t m0 = a0 + wave / WC * RB * 32, c0 = b0 + wave % WC * CB * 32;
+    if (p.bf16) {
+        store_tiles<RB, CB>(prod.acc, true, lds, [&](int row, int col, u32x4 v) {
+            const int64_t m = m0 + row, n = c0 + col;
+            if (m >= a_end || n >= p.N) return;
+            uint16_t* z = reinterpret_cast<uint16_t*>(d) + m * p.ldd + n;
+            if (n + 8 <= p.N) {
+                *reinterpret_cast<u32x4_a2*>(z) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 7; ++i)
+                    if (n + i < p.N) z[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+            }
+        });
+    } else {
+        store_tiles<RB, CB>(prod.acc, false, lds, [&](int row, int col, u32x4 v) {
+            const int64_t m = m0 + row, n = c0 + col;
+            if (m >= a_end || n >= p.N) return;
+            float* z = reinterpret_cast<float*>(d) + m * p.ldd + n;
+            if (n + 4 <= p.N) {
+                u32x4_a4* q = reinterpret_cast<u32x4_a4*>(z);
+                if (p.accumulate) *q = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, (u32x4)*q) + __builtin_bit_cast(f32x4, v));
+                else *q = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (n + i < p.N) z[i] = p.accumulate ? z[i] + bits_as<float>(v[i]) : bits_as<float>(v[i]);
+            }
+        });
+    }
+}
+
+// The parts of a product that was split along the summed axis, added in their order.
+__global__ __launch_bounds__(256) void k_fp8_sum(const float* parts, int splits, int64_t M, int64_t N, void* d, int64_t ldd, int bf16, int accumulate) {
+    const int64_t pieces = (N + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / pieces, n = (i - m * pieces) * 4;
+    if (m >= M) return;
+    const int64_t pitch = pieces * 4;
+    f32x4 v = {0, 0, 0, 0};
+    for (int z = 0; z < splits; ++z) v += *reinterpret_cast<const f32x4*>(parts + (z * M + m) * pitch + n);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (n + j >= N) break;
+        if (bf16) static_cast<uint16_t*>(d)[m * ldd + n + j] = (uint16_t)(pack_bf16(v[j], 0.f) & 0xFFFFu);
+        else static_cast<float*>(d)[m * ldd + n + j] = accumulate ? static_cast<float*>(d)[m * ldd + n + j] + v[j] : v[j];
+    }
+}
+
+template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
+daq_status launch_product(ProductArgs p, hipStream_t st) {
+    using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
+    const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, Product::kRows), tn = ceil_div(p.N, Product::kCols);
+    const int64_t tiles = round_up(tm * tn * (OF == Of::kExpertWeights ? p.experts : 1), kXcd);
+    if (tm > 0x7FFFFFFF / std::max<int64_t>(1, 4 * tn) || !grid_ok(tiles, Product::kWaves * 64)) return DAQ_ERR_UNSUPPORTED;
+    p.tiles_m = (int)tm;
+    p.tiles_n = (int)tn;
+    const auto kernel = k_fp8_product<WR, WC, RB, CB, SLOTS, EXACT, OF>;
+    if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
+    DAQ_LAUNCH("fp8_product", st, hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)p.splits), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
+    return DAQ_OK;
+}
+template <Of OF>
+daq_status launch_form(Fp8Form form, bool exact, const ProductArgs& p, hipStream_t st) {
+    if (exact) return form == Fp8Form::k64 ? launch_product<2, 1, 1, 2, 4, true, OF>(p, st) : launch_product<2, 2, 2, 2, 2, true, OF>(p, st);
+    switch (form) {
+        case Fp8Form::k64: return launch_product<2, 1, 1, 2, 4, false, OF>(p, st);
+        case Fp8Form::k128: return launch_product<2, 2, 2, 2, 2, false, OF>(p, st);
+        default: return launch_product<2, 4, 4, 2, 2, false, OF>(p, st);
+    }
+}
+
+}  // namespace
+
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
+    Fp8Plan pl{};
+    const int64_t stages = ceil_div(K, kFp8Block);
+    auto tiles = [&](int64_t n) { return ceil_div(M, n) * ceil_div(N, n); };
+    pl.form = tiles(256) >= 192 && !exact ? Fp8Form::k256 : tiles(128) >= 256 ? Fp8Form::k128 : Fp8Form::k64;
+    pl.splits = 1;
+    pl.per_split = (int)stages;
+    return pl;
+}
+
+static daq_status product_sizes(int64_t M, int64_t N, int64_t K) {
+    if (M < 0 || N <= 0 || K < 0) return DAQ_ERR_INVALID_ARG;
+    daq_status rc = matrix_size(M, K > 0 ? K : 1);
+    if (rc == DAQ_OK) rc = matrix_size(N, K > 0 ? K : 1);
+    if (rc == DAQ_OK) rc = matrix_size(M, N);
+    if (rc != DAQ_OK) return rc;
+    return K > kFp8MaxK ? DAQ_ERR_UNSUPPORTED : DAQ_OK;
+}
+static daq_status result_check(const void* D, int dtype, int64_t N, int64_t ldd, int accumulate) {
+    return !dtype_ok(dtype) || !D || !elem_aligned(D, dtype) || ldd < N || (accumulate && dtype != DAQ_FP32) ? DAQ_ERR_INVALID_ARG : DAQ_OK;
+}
+
+static daq_status fp8_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, int dtype, int64_t ldd, int accumulate,
+                             void* ws, hipStream_t st) {
+    const bool exact = dtype == DAQ_FP32;
+    const Fp8Plan pl = fp8_plan(M, N, K, exact);
+    ProductArgs p{};
+    p.a = operand(A, M, K);
+    p.b = operand(B, N, K);
+    p.M = M;
+    p.N = N;
+    p.stages = (int)ceil_div(K, kFp8Block);
+    p.splits = pl.splits;
+    p.per_split = pl.per_split;
+    if (pl.splits == 1) {
+        p.d = D;
+        p.ldd = ldd;
+        p.bf16 = dtype == DAQ_BF16;
+        p.accumulate = accumulate;
+        return launch_form<Of::kWhole>(pl.form, exact, p, st);
+    }
+    p.d = ws;
+    p.ldd = round_up(N, 4);
+    const int64_t blocks = ceil_div(M * ceil_div(N, 4), 256);
+    if (!grid_ok(blocks, 256)) return DAQ_ERR_UNSUPPORTED;
+    const daq_status rc = launch_form<Of::kWhole>(pl.form, exact, p, st);
+    if (rc != DAQ_OK) return rc;
+    DAQ_LAUNCH("fp8_sum", st, hipLaunchKernelGGL(k_fp8_sum, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const float*>(ws), pl.splits, M, N, D, ldd, dtype == DAQ_BF16, accumulate));
+    return DAQ_OK;
+}
+
+}  // namespace daq
+
+using namespace daq;
+
+extern "C" daq_status daq_fp8_matmul_workspace(int64_t M, int64_t N, int64_t K, daq_dtype dtype, size_t* bytes) {
+    if (!bytes || !dtype_ok(dtype)) return DAQ_ERR_INVALID_ARG;
+    *bytes = 0;
+    const daq_status rc = product_sizes(M, N, K);
+    if (rc != DAQ_OK || M == 0 || K == 0) return rc;
+    const Fp8Plan pl = fp8_plan(M, N, K, dtype == DAQ_FP32);
+    if (pl.splits > 1) *bytes = (size_t)round_up(pl.splits * M * round_up(N, 4) * 4, 256);
+    return DAQ_OK;
+}
+
+extern "C" daq_status daq_fp8_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, daq_dtype dtype,
+                                     int64_t ldd, int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream) {
+    size_t need = 0;
+    daq_status rc = daq_fp8_matmul_workspace(M, N, K, dtype, &need);
+    if (rc != DAQ_OK) return rc;
+    if (accumulate && dtype != DAQ_FP32) return DAQ_ERR_INVALID_ARG;
+    if (M == 0) return DAQ_OK;
+    rc = result_check(D, dtype, N, ldd, accumulate);
+    if (rc != DAQ_OK) return rc;
+    if (K > 0 && (!A || !aligned256(A) || !B || !aligned256(B))) return DAQ_ERR_INVALID_ARG;
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned256(workspace))) return DAQ_ERR_WORKSPACE;
+    return fp8_matmul(M, N, K, A, B, D, dtype, ldd, accumulate, workspace, (hipStream_t)stream);
+}
+
+extern "C" daq_status daq_fp8_linear_workspace(int64_t M, int64_t N, int64_t K, daq_dtype x_dtype, daq_dtype y_dtype, size_t* bytes) {
+    if (!dtype_ok(x_dtype) || K <= 0) return DAQ_ERR_INVALID_ARG;
+    size_t product = 0;
+    const daq_status rc = daq_fp8_matmul_workspace(M, N, K, y_dtype, &product);
+    if (!bytes) return DAQ_ERR_INVALID_ARG;
+    *bytes = 0;
+    if (rc != DAQ_OK || M == 0) return rc;
+    daq_fp8_layout L;
+    daq_layout_fp8(M, K, &L);
+    *bytes = (size_t)L.bytes + product;
+    return DAQ_OK;
+}
+
+extern "C" daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void* X, daq_dtype x_dtype, int64_t ldx, const uint8_t* W, void* Y,
+                                     daq_dtype y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    size_t need = 0;
+    daq_status rc = daq_fp8_linear_workspace(M, N, K, x_dtype, y_dtype, &need);
+    if (rc != DAQ_OK) return rc;
+    if (M == 0) return DAQ_OK;
+    rc = result_check(Y, y_dtype, N, ldy, 0);
+    if (rc != DAQ_OK) return rc;
+    if (!X || !elem_aligned(X, x_dtype) || ldx < K || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
+    if (!fp8_rows_grid_ok(M, K)) return DAQ_ERR_UNSUPPORTED;
+    if (!workspace || workspace_bytes < need || !aligned256(workspace)) return DAQ_ERR_WORKSPACE;
+    uint8_t* xq = static_cast<uint8_t*>(workspace);
+    daq_fp8_layout L;
+    daq_layout_fp8(M, K, &L);
+    rc = fp8_quantize_rows(X, x_dtype, M, K, ldx, xq, (hipStream_t)stream);
+    if (rc != DAQ_OK) return rc;
+    return fp8_matmul(M, N, K, xq, W, Y, y_dtype, ldy, 0, xq + L.bytes, (hipStream_t)stream);
+}
+
+static daq_status experts_product(const daq_experts& plan, int64_t N, int64_t K, const uint8_t* A, int sorted, const uint8_t* W, void* Y, int dtype,
+                                  int64_t ldy, hipStream_t st) {
+    const int64_t slots = plan_slots(plan);
+    ProductArgs p{};
+    p.a = operand(A, sorted ? slots : plan.tokens, K);
+    p.b = operand(W, plan.experts * N, K);
+    p.M = slots;
+    p.N = N;
+    p.stages = (int)ceil_div(K, kFp8Block);
+    p.d = Y;
+    p.ldd = ldy;
+    p.bf16 = dtype == DAQ_BF16;
+    p.splits = 1;
+    p.table = plan.table;
+    p.order = plan.rows;
+    p.experts = plan.experts;
+    p.picks = sorted ? 0 : plan.picks;
+    const bool exact = dtype == DAQ_FP32;
+    const Fp8Form form = experts_form(plan, N, exact);
+    p.tiles_m = (int)most_tiles(plan, form == Fp8Form::k256 ? 256 : form == Fp8Form::k128 ? 128 : 64);
+    return launch_form<Of::kExpertRows>(form, exact, p, st);
+}
+
+Fp8Form daq::experts_form(const daq_experts& plan, int64_t N, bool exact) {
+    const int64_t slots = plan_slots(plan), each = slots / std::min<int64_t>(slots, plan.experts);
+    auto tiles = [&](int64_t n) { return std::max<int64_t>(1, slots / n) * ceil_div(N, n); };
+    return each >= 256 && tiles(256) >= 192 && !exact ? Fp8Form::k256 : each >= 96 && tiles(128) >= 256 ? Fp8Form::k128 : Fp8Form::k64;
+}
+
+// What the plan, the sizes, the weights and the result have to be.
+static daq_status experts_check(const daq_experts* plan, int64_t N, int64_t K, int sorted) {
+    if (!plan_ok(plan) || N <= 0 || K <= 0) return DAQ_ERR_INVALID_ARG;
+    const int64_t slots = plan_slots(*plan), rows = sorted ? slots : plan->tokens;
+    daq_status rc = matrix_size(rows, K);
+    if (rc == DAQ_OK) rc = matrix_size(slots, N);
+    if (rc == DAQ_OK) rc = N > (((int64_t)1 << 31) - 1) / plan->experts ? DAQ_ERR_UNSUPPORTED : matrix_size(plan->experts * N, K);
+    if (rc != DAQ_OK) return rc;
+    // rows that are taken in another order are read through one descriptor
+    if (K > kFp8MaxK || (!sorted && rows * round_up(K, kFp8Block) > (int64_t)kTileReach)) return DAQ_ERR_UNSUPPORTED;
+    return DAQ_OK;
+}
+
+extern "C" daq_status daq_experts_matmul(const daq_experts* plan, int64_t N, int64_t K, const uint8_t* A, int32_t sorted, const uint8_t* W, void* Y,
+                                         daq_dtype dtype, int64_t ldy, void* stream) {
+    daq_status rc = experts_check(plan, N, K, sorted);
+    if (rc != DAQ_OK) return rc;
+    if (!dtype_ok(dtype)) return DAQ_ERR_INVALID_ARG;
+    if (plan->tokens == 0) return DAQ_OK;
+    rc = result_check(Y, dtype, N, ldy, 0);
+    if (rc != DAQ_OK) return rc;
+    if (!A || !aligned256(A) || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
+    return experts_product(*plan, N, K, A, sorted, W, Y, dtype, ldy, (hipStream_t)stream);
+}
+
+extern "C" daq_status daq_experts_linear_workspace(const daq_experts* plan, int64_t N, int64_t K, daq_dtype x_dtype, int32_t sorted, size_t* bytes) {
+    if (!bytes || !dtype_ok(x_dtype)) return DAQ_ERR_INVALID_ARG;
+    *bytes = 0;
+    const daq_status rc = experts_check(plan, N, K, sorted);
+    if (rc != DAQ_OK || plan->tokens == 0) return rc;
+    daq_fp8_layout L;
+    daq_layout_fp8(sorted ? plan_slots(*plan) : plan->tokens, K, &L);
+    *bytes = (size_t)L.bytes;
+    return DAQ_OK;
+}
+
+extern "C" daq_status daq_experts_linear(const daq_experts* plan, int64_t N, int64_t K, const void* X, daq_dtype x_dtype, int64_t ldx, int32_t sorted,
+                                         const uint8_t* W, void* Y, daq_dtype y_dtype, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    size_t need = 0;
+    daq_status rc = daq_experts_linear_workspace(plan, N, K, x_dtype, sorted, &need);
+    if (rc != DAQ_OK) return rc;
+    if (!dtype_ok(y_dtype)) return DAQ_ERR_INVALID_ARG;
+    if (plan->tokens == 0) return DAQ_OK;
+    rc = result_check(Y, y_dtype, N, ldy, 0);
+    if (rc != DAQ_OK) return rc;
+    if (!X || !elem_aligned(X, x_dtype) || ldx < K || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
+    const int64_t rows = sorted ? plan_slots(*plan) : plan->tokens;
+    if (!fp8_rows_grid_ok(rows, K)) return DAQ_ERR_UNSUPPORTED;
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned256(workspace))) return DAQ_ERR_WORKSPACE;
+    rc = fp8_quantize_rows(X, x_dtype, rows, K, ldx, static_cast<uint8_t*>(workspace), (hipStream_t)stream);
+    if (rc != DAQ_OK) return rc;
+    return experts_product(*plan, N, K, static_cast<const uint8_t*>(workspace), sorted, W, Y, y_dtype, ldy, (hipStream_t)stream);
+}
+
+extern "C" daq_status daq_experts_weight_grad(const daq_experts* plan, int64_t N, int64_t K, const uint8_t* dY, const uint8_t* X, void* dW,
+                                              daq_dtype dtype, int64_t ldw, int64_t stride, int32_t accumulate, void* stream) {
+    if (!plan_ok(plan) || N <= 0 || K <= 0 || !dtype_ok(dtype) || (accumulate && dtype != DAQ_FP32)) return DAQ_ERR_INVALID_ARG;
+    const int64_t columns = most_tiles(*plan, 128) * 128;
+    daq_status rc = matrix_size(N, std::max<int64_t>(columns, 1));
+    if (rc == DAQ_OK) rc = matrix_size(K, std::max<int64_t>(columns, 1));
+    if (rc == DAQ_OK) rc = matrix_size(N, K);
+    if (rc != DAQ_OK) return rc;
+    if (columns > kFp8MaxK || N * K > kMaxElems / plan->experts) return DAQ_ERR_UNSUPPORTED;
+    if (!dW || !elem_aligned(dW, dtype) || ldw < K || stride < 0 || (plan->experts > 1 && stride < (N - 1) * ldw + K)) return DAQ_ERR_INVALID_ARG;
+    if (plan->tokens == 0 && accumulate) return DAQ_OK;
+    if (plan->tokens > 0 && (!dY || !aligned256(dY) || !X || !aligned256(X))) return DAQ_ERR_INVALID_ARG;
+    ProductArgs p{};
+    p.a = operand(dY, N, columns);
+    p.b = operand(X, K, columns);
+    p.M = N;
+    p.N = K;
+    p.d = dW;
+    p.ldd = ldw;
+    p.accumulate = accumulate;
+    p.bf16 = dtype == DAQ_BF16;
+    p.splits = 1;
+    p.table = plan->table;
+    p.experts = plan->experts;
+    p.stride = stride;
+    const int64_t big = ceil_div(N, 256) * ceil_div(K, 256) * plan->experts, mid = ceil_div(N, 128) * ceil_div(K, 128) * plan->experts;
+    const bool exact = dtype == DAQ_FP32;
+    return launch_form<Of::kExpertWeights>(big >= 192 && !exact ? Fp8Form::k256 : mid >= 256 ? Fp8Form::k128 : Fp8Form::k64, exact, p, (hipStream_t)stream);
+}

@@ -51,6 +51,56 @@ __device__ __forceinline__ void words_to_lds(__amdgpu_buffer_rsrc_t src, uint32_
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (__attribute__((address_space(3))) void*)dst, 4, (int)lane_off, (int)off, 0, 0);
 }
 
+// Results leave in rows of 128 bytes (64 bfloat16 or 32 fp32 columns) so that whole lines are written: through the wave's share of
+// LDS, 16-byte pieces of a row in the order piece ^ row % 8, which keeps both sides off one another's banks.  put(row, column,
+// piece): row and column of the wave's tile.  LDS holds RB * 4 KiB for every wave.
+template <int RB, int CB, typename Put>
+__device__ __forceinline__ void store_tiles(const v16f (&acc)[CB][RB], bool bf16, uint8_t* lds, Put put) {
+    static_assert(CB % 2 == 0, "pairs of column blocks");
+    const int lane = threadIdx.x % kWave;
+    uint8_t* mine = lds + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (RB * 32 * 128);
+    __builtin_amdgcn_s_barrier();   // everybody has read the last stage
+    auto out = [&](int col0, int per) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int k = 0; k < RB * 4; ++k) {
+            const int row = k * 8 + lane / 8;
+            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * 128 + ((lane ^ row) & 7) * 16);
+            put(row, col0 + (lane & 7) * per, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+    };
+    const int m = lane % 32, h = lane / 32;
+    if (bf16) {
+#pragma unroll
+        for (int j0 = 0; j0 < CB; j0 += 2) {
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const v16f& a = acc[j0 + j][i];
+                        *reinterpret_cast<u32x2*>(mine + (i * 32 + m) * 128 + (((j * 4 + q) ^ m) & 7) * 16 + h * 8) =
+                            u32x2{pack_bf16(a[4 * q], a[4 * q + 1]), pack_bf16(a[4 * q + 2], a[4 * q + 3])};
+                    }
+            out(j0 * 32, 8);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < CB; ++j) {
+#pragma unroll
+            for (int i = 0; i < RB; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const v16f& a = acc[j][i];
+                    *reinterpret_cast<f32x4*>(mine + (i * 32 + m) * 128 + (((q * 2 + h) ^ m) & 7) * 16) = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                }
+            out(j * 32, 4);
+        }
+    }
+}
+
 // The results of a workgroup of WR x WC waves, each RB x CB tiles of 32 x 32: rows from row block `rb` of `r` on, columns from row block
 // `cb` of `c` on, summed over the stages s0 .. s1 - 1.  A stage, two steps of both operands, is asked for while the three before it are multiplied,
 // straight into LDS, and the fragments of a step while the step before is multiplied, the first step of a stage among them:
@@ -267,54 +317,10 @@ struct TileProduct {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the requests past the end have landed before LDS is put to other use
     }
 
-    // Results leave in rows of 128 bytes (64 bfloat16 or 32 fp32 columns) so that whole lines are written: through the wave's share of
-    // LDS, 16-byte pieces of a row in the order piece ^ row % 8, which keeps both sides off one another's banks.  put(row, column,
-    // piece): row and column of the wave's tile.
-    static_assert(kLdsBytes / kWaves >= RB * 32 * 128 && (CB % 2 == 0), "a wave's share holds its rows");
+    static_assert(kLdsBytes / kWaves >= RB * 32 * 128, "a wave's share holds its rows");
     template <typename Put>
     __device__ __forceinline__ void store(bool bf16, uint8_t* lds, Put put) const {
-        const int lane = threadIdx.x % kWave;
-        uint8_t* mine = lds + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (RB * 32 * 128);
-        __builtin_amdgcn_s_barrier();   // everybody has read the last stage
-        auto out = [&](int col0, int per) {
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int k = 0; k < RB * 4; ++k) {
-                const int row = k * 8 + lane / 8;
-                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * 128 + ((lane ^ row) & 7) * 16);
-                put(row, col0 + (lane & 7) * per, v);
-            }
-            __builtin_amdgcn_wave_barrier();
-        };
-        const int m = lane % 32, h = lane / 32;
-        if (bf16) {
-#pragma unroll
-            for (int j0 = 0; j0 < CB; j0 += 2) {
-#pragma unroll
-                for (int i = 0; i < RB; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const v16f& a = acc[j0 + j][i];
-                            *reinterpret_cast<u32x2*>(mine + (i * 32 + m) * 128 + (((j * 4 + q) ^ m) & 7) * 16 + h * 8) =
-                                u32x2{pack_bf16(a[4 * q], a[4 * q + 1]), pack_bf16(a[4 * q + 2], a[4 * q + 3])};
-                        }
-                out(j0 * 32, 8);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < CB; ++j) {
-#pragma unroll
-                for (int i = 0; i < RB; ++i)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const v16f& a = acc[j][i];
-                        *reinterpret_cast<f32x4*>(mine + (i * 32 + m) * 128 + (((q * 2 + h) ^ m) & 7) * 16) = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
-                    }
-                out(j * 32, 4);
-            }
-        }
+        store_tiles<RB, CB>(acc, bf16, lds, put);
     }
 };
 

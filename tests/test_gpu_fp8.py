@@ -1,0 +1,216 @@
+"""8-bit floating point matrices and their products on the GPU, through the binding, against the oracle in 64 bits.
+
+Codes, scales and whole buffers are compared byte for byte.  Sums in fp32 (results in fp32, through bfloat16): every product is exact, each addition is
+off by at most 2^-23 of the magnitudes added so far (to nearest or cut off), so a sum of n terms by at most n * 2^-23 * sum |products|; the matrix
+instructions add 16 products as trees, so n counts these, with ten additions inside and behind them.  Results in bfloat16: the 8-bit instructions add
+eight products at a time, each cut off at a multiple of 2^-13 of a power of two that the largest does not fall below, so seven of them lose at most
+7 * 2^-13 of it; with the additions that follow as above, and 2^-8 of itself for the rounding."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import fp8 as ref
+from paper_2102_04782_amd import binding as daq
+
+pytestmark = pytest.mark.gpu
+
+DT = [torch.float32, torch.bfloat16]
+SIZES = [(1, 1), (1, 127), (3, 128), (2, 129), (17, 511), (16, 512), (33, 513), (127, 64), (128, 130), (129, 255), (7, 1000), (300, 130), (257, 1029)]
+
+
+def _x(rows, cols, dtype, seed, spread=6):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g) * torch.exp2(torch.randint(-spread, spread + 1, (rows, cols), generator=g).float())
+    if rows > 2 and cols > 130:
+        x[1, :128] = 0                                            # a block of zeros
+        x[0, :128] = 0
+        x[0, :64] = (torch.arange(64) + 0.5) * 0.5                # ties, once the block's scale is a power of two
+        x[0, 64] = 256.0
+        x[2, :32] = torch.arange(32) * 2.0 ** -10                 # below the codes' normal range
+        x[2, 32:128] = 0
+        x[2, 33] = 448.0
+    return x.to(dtype)
+
+
+def _strided(x, dev="cuda", pad=5, first=3):
+    """x inside a wider matrix of other values: rows start at any element."""
+    wide = torch.full((x.shape[0], x.shape[1] + pad), 7.0, dtype=x.dtype, device=dev)
+    v = wide[:, first:first + x.shape[1]]
+    v.copy_(x)
+    return v
+
+
+def _np(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _filled(rows, cols):
+    q = daq.alloc_fp8(rows, cols)
+    q.buf.fill_(0xA5)
+    return q
+
+
+def _same(q, codes, byte):
+    """Every byte of a packed matrix; a code of zero may carry either sign."""
+    want, known = ref.buffer(codes, byte)
+    got = q.buf.cpu().numpy()
+    assert got.size == want.size
+    off = daq.layout_fp8(q.rows, q.cols).off_scales
+    assert np.array_equal(got[off:][known[off:]], want[off:][known[off:]])
+    g, w = got[:off][known[:off]], want[:off][known[:off]]
+    assert np.all((g == w) | ((g & 127 == 0) & (w & 127 == 0)))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_codes_scales_and_padding(rows, cols, dtype):
+    x = _x(rows, cols, dtype, rows * 1000 + cols)
+    by_rows, by_columns = ref.quantize(_np(x)), ref.quantize(_np(x).T)
+    for src in (x.cuda(), _strided(x)):
+        _same(daq.fp8_quantize(src, out=_filled(rows, cols)), *by_rows)
+        _same(daq.fp8_quantize(src, columns=True, out=_filled(cols, rows)), *by_columns)
+        r, c = daq.fp8_quantize_both(src, _filled(rows, cols), _filled(cols, rows))
+        _same(r, *by_rows)
+        _same(c, *by_columns)
+        for to in DT:
+            assert np.array_equal(_np(daq.fp8_dequantize(r, dtype=to)), ref.values(*by_rows))
+            assert np.array_equal(_np(daq.fp8_dequantize(c, dtype=to)), ref.values(*by_columns))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("count,rows,cols", [(1, 1, 1), (1, 128, 128), (2, 129, 127), (3, 70, 300), (5, 256, 640), (2, 300, 1030)])
+def test_weights_by_tiles_and_their_transposes(count, rows, cols, dtype):
+    w = _x(count * rows, cols, dtype, rows + cols).view(count, rows, cols)
+    parts = [ref.quantize_weights(_np(w[e])) for e in range(count)]
+    turned = [ref.transposed_weights(*p) for p in parts]
+    stack = lambda ps: (np.concatenate([p[0] for p in ps]), np.concatenate([p[1] for p in ps]))
+    wide = torch.full((count, rows + 2, cols + 3), 9.0, dtype=dtype, device="cuda")[:, 1:1 + rows, 2:2 + cols]
+    wide.copy_(w)
+    for src in (w.cuda(), wide):
+        q, t = daq.fp8_quantize_weights(src, _filled(count * rows, cols), _filled(count * cols, rows))
+        _same(q, *stack(parts))
+        _same(t, *stack(turned))
+        alone, none = daq.fp8_quantize_weights(src, transposed=False)
+        assert none is None
+        _same(alone, *stack(parts))
+    if count == 1:
+        _same(daq.fp8_quantize_weights(w[0].cuda())[0], *parts[0])
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_extremes(dtype):
+    x = torch.zeros(12, 300, dtype=dtype)
+    big = torch.finfo(dtype).max
+    x[0, 0], x[0, 200], x[1, 5] = big, -big, 2.0 ** -126
+    x[2, 7], x[2, 40] = 2.0 ** -133, 2.0 ** -128                  # below the normal range
+    x[3, 3], x[4, 150], x[5, 299] = float("nan"), float("inf"), float("-inf")
+    x[6] = torch.tensor([2.0 ** -133 * (i % 13) for i in range(300)])
+    x[7, 31], x[7, 0], x[7, 129] = 448.0, 449.0, 464.0
+    x[8, :8] = torch.tensor([448.0, 450.0, 456.0, 460.0, 464.0, 5.0, 1e-30, -447.9])
+    x[9, 0], x[9, 1], x[10, 140], x[10, 130] = 448 * 2.0 ** -126, 2.0 ** -130, 450 * 2.0 ** -126, 3 * 2.0 ** -133
+    for m, q in ((_np(x), daq.fp8_quantize(x.cuda())), (_np(x).T, daq.fp8_quantize(x.cuda(), columns=True))):
+        codes, byte = ref.quantize(m)
+        _same(q, codes, byte)
+        with np.errstate(over="ignore"):                           # (2^128, which rounding can make of the largest values, is an infinity in either type)
+            v = ref.values(codes, byte).astype(np.float32)
+        assert np.array_equal(_np(daq.fp8_dequantize(q)), v, equal_nan=True)
+        got = _np(daq.fp8_dequantize(q, dtype=torch.bfloat16))
+        with np.errstate(invalid="ignore"):
+            assert np.all((got == v) | (np.isnan(got) & np.isnan(v)) | (np.abs(got - v) <= 2.0 ** -134))   # half a step of the smallest
+    w = x.cuda()
+    q, t = daq.fp8_quantize_weights(w)
+    codes, byte = ref.quantize_weights(_np(x))
+    _same(q, codes, byte)
+    _same(t, *ref.transposed_weights(codes, byte))
+
+
+def test_all_codes_and_all_ties():
+    """Every code, every middle between two codes, and what lies a little beside it."""
+    g = ref.GRID
+    mid = (g[1:] + g[:-1]) / 2
+    v = np.concatenate((g, mid, np.nextafter(mid.astype(np.float32), np.float32(0)), np.nextafter(mid.astype(np.float32), np.float32(1e9))))
+    v = np.concatenate((v, -v)).astype(np.float32)
+    x = np.zeros((-(-v.size // 127), 128), np.float32)
+    x[:, 0] = 448
+    x[:, 1:].flat[:v.size] = v
+    for shift in (-100, 0, 37):
+        t = torch.from_numpy(x * np.float32(2.0) ** shift)
+        codes, byte = ref.quantize(_np(t))
+        assert np.all(byte == 127 + shift)
+        _same(daq.fp8_quantize(t.cuda()), codes, byte)
+        _same(daq.fp8_quantize(t.t().contiguous().cuda(), columns=True), codes, byte)
+
+
+MATMUL = [(1, 1, 1), (1, 33, 130), (1, 512, 2048), (2, 70, 300), (5, 64, 256), (13, 100, 1030), (16, 2049, 512), (17, 256, 513), (32, 256, 512), (33, 129, 64),
+          (40, 2049, 96), (64, 64, 4096), (65, 130, 8200), (100, 260, 700), (255, 257, 513), (256, 256, 256), (300, 600, 320), (513, 511, 1024), (1030, 770, 200),
+          (2050, 2100, 300), (4100, 3900, 129)]
+
+
+def _bound(K, absolute, exact, dtype):
+    return (-(-K // 16) + 10) * 2.0 ** -23 * absolute + (7 * 2.0 ** -13 * absolute + 2.0 ** -8 * np.abs(exact) if dtype == torch.bfloat16 else 0) + 1e-40
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", MATMUL)
+def test_matmul(M, N, K, dtype):
+    a, b = _x(M, K, torch.bfloat16, M + K), _x(N, K, torch.float32, N + 3 * K)
+    va, vb = ref.values(*ref.quantize(_np(a))), ref.values(*ref.quantize(_np(b)))
+    exact, absolute = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    qa, qb = daq.fp8_quantize(a.cuda()), daq.fp8_quantize(b.cuda())
+    wide = torch.full((M, N + 7), 55.0, dtype=dtype, device="cuda")
+    for out in (torch.full((M, N), float("nan"), dtype=dtype, device="cuda"), wide[:, 3:3 + N]):
+        got = _np(daq.fp8_matmul(qa, qb, out=out))
+        assert np.all(np.abs(got - exact) <= _bound(K, absolute, exact, dtype))
+    assert bool((wide[:, :3] == 55).all()) and bool((wide[:, 3 + N:] == 55).all())     # nothing beside the result
+    if dtype == torch.float32:
+        start = torch.randn(M, N, device="cuda")
+        got = _np(daq.fp8_matmul(qa, qb, out=start.clone(), accumulate=True))
+        want = exact + _np(start)
+        assert np.all(np.abs(got - want) <= _bound(K, absolute, exact, dtype) + 2.0 ** -23 * np.abs(want))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", MATMUL)
+def test_linear(M, N, K, dtype):
+    x, w = _x(M, K, dtype, M + 2 * K), _x(N, K, torch.bfloat16, N + 5 * K)
+    vx, vw = ref.values(*ref.quantize(_np(x))), ref.values(*ref.quantize_weights(_np(w)))
+    exact, absolute = vx @ vw.T, np.abs(vx) @ np.abs(vw).T
+    qw, _ = daq.fp8_quantize_weights(w.cuda())
+    for src in (x.cuda(), _strided(x)):
+        for to in DT:
+            got = _np(daq.fp8_linear(src, qw, dtype=to))
+            assert np.all(np.abs(got - exact) <= _bound(K, absolute, exact, to))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", [(1, 40, 70), (129, 200, 330), (600, 513, 257), (1500, 130, 700)])
+def test_gradients_of_a_layer(M, N, K, dtype):
+    x, w, dy = _x(M, K, dtype, 1), _x(N, K, torch.bfloat16, 2), _x(M, N, dtype, 3)
+    qw, qt = daq.fp8_quantize_weights(w.cuda())
+    (_, xc), (dr, dc) = daq.fp8_quantize_both(x.cuda()), daq.fp8_quantize_both(dy.cuda())
+    vw, vd = ref.values(*ref.quantize_weights(_np(w))), ref.values(*ref.quantize(_np(dy)))
+    got, want = _np(daq.fp8_matmul(dr, qt, dtype=torch.float32)), vd @ vw
+    assert np.all(np.abs(got - want) <= _bound(N, np.abs(vd) @ np.abs(vw), want, torch.float32))
+    cd, cx = ref.values(*ref.quantize(_np(dy).T)), ref.values(*ref.quantize(_np(x).T))
+    got, want = _np(daq.fp8_matmul(dc, xc, dtype=torch.float32)), cd @ cx.T
+    assert np.all(np.abs(got - want) <= _bound(M, np.abs(cd) @ np.abs(cx).T, want, torch.float32))
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (20, 130, 700), (200, 300, 600), (600, 300, 513), (2100, 2050, 513)])
+def test_what_is_not_finite_reaches_its_sums_only(M, N, K):
+    x, w = torch.randn(M, K), torch.randn(N, K)
+    x[M // 2, 140], w[N - 2, 5], w[1, K - 1] = float("nan"), float("inf"), float("-inf")
+    got = daq.fp8_matmul(daq.fp8_quantize(x.cuda()), daq.fp8_quantize(w.cuda())).float().cpu()
+    bad = torch.zeros(M, N, dtype=torch.bool)
+    bad[M // 2], bad[:, N - 2], bad[:, 1] = True, True, True
+    assert torch.equal(torch.isnan(got), bad) and bool(torch.isfinite(got[~bad]).all())
+
+
+def test_nothing_to_do_and_nothing_to_sum():
+    w, _ = daq.fp8_quantize_weights(torch.randn(40, 70, device="cuda"))
+    assert daq.fp8_linear(torch.empty(0, 70, device="cuda"), w).shape == (0, 40)
+    a, b = daq.fp8_quantize(torch.empty(0, 40, device="cuda"), columns=True), daq.fp8_quantize(torch.empty(0, 70, device="cuda"), columns=True)
+    assert (a.rows, a.cols, b.rows, b.cols) == (40, 0, 70, 0)
+    out = torch.full((40, 70), 3.0, device="cuda")
+    assert bool((daq.fp8_matmul(a, b, out=out, accumulate=True) == 3).all())
+    assert bool((daq.fp8_matmul(a, b, out=out) == 0).all())
