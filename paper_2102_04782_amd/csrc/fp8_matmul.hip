@@ -7,46 +7,16 @@
 // neighbouring columns of a row of D.
 #include <cmath>
 
-#include "fp8_block.h"
-#include "tile_product.h"
+#include "fp8_product.h"
 
 namespace daq {
 
 namespace {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
-
-struct Fp8Operand {
-    const uint8_t* codes;
-    const uint8_t* scales;
-    int64_t rows, pitch;
-};
 Fp8Operand operand(const uint8_t* buf, int64_t rows, int64_t cols) {
     daq_fp8_layout L;
     daq_layout_fp8(rows, cols, &L);
     return {buf, buf + L.off_scales, rows, L.pitch};
-}
-
-struct ProductArgs {
-    Fp8Operand a, b;
-    int64_t M, N;             // of one product
-    int stages;               // blocks of 128 of the summed axis
-    void* d;
-    int64_t ldd;
-    int bf16, accumulate;
-    int tiles_m, tiles_n;     // (experts' rows: tiles_m is the most there can be)
-    int splits, per_split;    // of the summed axis: part z, of per_split stages, goes to d + z * M * ldd
-    // experts
-    const int32_t* table;
-    const int32_t* order;
-    int experts, picks;       // picks: row p of the order is row order[p] / picks of A, 0: row p
-    int64_t stride;           // from one expert's gradient to the next
-};
-enum class Of { kWhole, kExpertRows, kExpertWeights };
-
-// 32 x 32 x 64; the scale is the lowest byte of its word.
-__device__ __forceinline__ v16f mfma8(v8i x, v8i y, v16f c, int sx, int sy) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 0, 0, 0, sx, 0, sy);
 }
 
 // Eight codes to bfloat16, times the scale: exact, but what the scale takes beyond bfloat16's range.
@@ -57,8 +27,8 @@ __device__ __forceinline__ v4i in_bf16(int lo, int hi, float s) {
 }
 
 // The results of a workgroup of WR x WC waves, each RB x CB tiles of 32 x 32, summed over the stages s0 .. s1 - 1 of 128.  A stage of both operands,
-// 128 bytes of every row, goes straight to LDS, where the 16-byte piece j of a row lies at j ^ row % 8: eight lanes ask for a row's line in that
-// order, and the fragment reads of eight rows share no bank.  SLOTS stages are under way or being read.  Fragments are read a step
+// 128 bytes of every row, goes straight to LDS, where the 16-byte piece j of a row lies at j ^ (row / 2 % 8): eight lanes ask for a row's line in
+// that order, and the fragment reads of sixteen rows share no bank.  SLOTS stages are under way or being read.  Fragments are read a step
 // (64 of a stage's 128) ahead into the registers that the products have just done with; the barrier stands behind the first products of a stage's
 // second step, when this stage is read out and the next has landed.
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT>
@@ -66,8 +36,9 @@ struct Fp8Product {
     static constexpr int kWaves = WR * WC, kRows = WR * RB * 32, kCols = WC * CB * 32;
     static constexpr int kCodes = (kRows + kCols) * 128, kStage = kCodes + (kRows + kCols) * 4;   // bytes of a stage, its scale words behind the codes
     static constexpr int kLdsBytes = SLOTS * kStage;
-    static constexpr int kAsks = 9;                       // requests of a wave for a stage: 64 rows, eight at a time, and their scale words
-    static_assert(kRows + kCols == kWaves * 64 && kRows % 64 == 0, "a wave asks for 64 rows of one operand");
+    static constexpr int kUnits = (kRows + kCols) / 64 / kWaves;   // of 64 rows, that a wave asks for
+    static constexpr int kAsks = 9 * kUnits;              // requests of a wave for a stage: eight rows at a time, and the scale words of a unit
+    static_assert((kRows + kCols) % (kWaves * 64) == 0 && kRows % (64 * kUnits) == 0, "a wave asks for rows of one operand");
     static_assert(SLOTS == 2 || SLOTS == 4, "the loop is written out for these");
     static_assert(kLdsBytes / kWaves >= RB * 32 * 128, "a wave's share holds its rows of results");
 
@@ -87,43 +58,50 @@ struct Fp8Product {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const int wr = wave / WC, wc = wave % WC;
         // what this wave asks for
-        const bool of_b = wave >= kRows / 64;
+        const bool of_b = wave >= kRows / 64 / kUnits;
         const Fp8Operand& o = of_b ? b : a;
         const bool gather = !of_b && order != nullptr;
-        const int64_t first = of_b ? b0 + (wave - kRows / 64) * 64 : a0 + wave * 64, end = of_b ? b_end : a_end;
+        const int64_t first = of_b ? b0 + wave * kUnits * 64 - kRows : a0 + wave * kUnits * 64, end = of_b ? b_end : a_end;
         const int64_t base = gather ? 0 : min(first, end - 1);
-        uint32_t off[8], soff;
+        uint32_t off[8 * kUnits], soff[kUnits];
         auto row_of = [&](int i) {
             const int64_t r = min(first + i, end - 1);
             return (uint32_t)(gather ? (picks ? order[r] / picks : (int)r) : r - base);
         };
 #pragma unroll
-        for (int i = 0; i < 8; ++i) off[i] = row_of(i * 8 + lane / 8) * (uint32_t)o.pitch + (uint32_t)((lane % 8) ^ (lane / 8)) * 16u;
-        soff = row_of(lane) * 4u;
-        auto bytes = [](const uint8_t* from, int64_t n) {
-            return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(n < (int64_t)kTileReach ? (uint32_t)n : kTileReach), 0x00020000);
-        };
-        const __amdgpu_buffer_rsrc_t src = bytes(o.codes + base * o.pitch, (o.rows - base) * o.pitch);
-        auto ask = [&](int s, uint8_t* to) {
+        for (int i = 0; i < 8 * kUnits; ++i) off[i] = row_of(i * 8 + lane / 8) * (uint32_t)o.pitch + (uint32_t)((lane % 8) ^ ((i * 4 + lane / 16) & 7)) * 16u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) tile_to_lds(src, off[i], (uint32_t)s * 128u, to + (wave * 8 + i) * 1024);
-            words_to_lds(bytes(o.scales + ((int64_t)(s / 4) * o.rows + base) * 4, (o.rows - base) * 4), soff, 0, to + kCodes + wave * 256);
+        for (int u = 0; u < kUnits; ++u) soff[u] = row_of(u * 64 + lane) * 4u;
+        // (a stage behind the last one is asked for through descriptors without an extent: LDS receives zeros)
+        auto codes_of = [&](int s) { return bytes_of(o.codes + base * o.pitch, s < s1 ? (o.rows - base) * o.pitch : 0); };
+        auto words_of = [&](int s) { return bytes_of(o.scales + ((int64_t)(s / 4) * o.rows + base) * 4, s < s1 ? (o.rows - base) * 4 : 0); };
+        // request n of a stage: eight rows, or the words of a unit
+        auto request = [&](int n, int s, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t words, uint8_t* to) {
+            if (n < 8 * kUnits) tile_to_lds(codes, off[n], (uint32_t)s * 128u, to + (wave * 8 * kUnits + n) * 1024);
+            else words_to_lds(words, soff[n - 8 * kUnits], 0, to + kCodes + (wave * kUnits + n - 8 * kUnits) * 256);
         };
-        v8i fr[RB], fc[2][CB];
+        auto ask = [&](int s, uint8_t* to) {
+            const __amdgpu_buffer_rsrc_t codes = codes_of(s), words = words_of(s);
+#pragma unroll
+            for (int n = 0; n < kAsks; ++n) request(n, s, codes, words, to);
+        };
+        v8i fr[2][RB], fc[2][CB];
         int sr[RB], sc[CB];
         int at[2][2];     // of a lane in 32 rows: step and half of its 32 bytes
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) at[k][t] = (lane % 32) * 128 + ((k * 4 + lane / 32 * 2 + t) ^ (lane & 7)) * 16;
+            for (int t = 0; t < 2; ++t) at[k][t] = (lane % 32) * 128 + ((k * 4 + lane / 32 * 2 + t) ^ (lane / 2 & 7)) * 16;
         auto fragment = [&](const uint8_t* from, int block, int k) {
             const v4i lo = *reinterpret_cast<const v4i*>(from + block * 4096 + at[k][0]), hi = *reinterpret_cast<const v4i*>(from + block * 4096 + at[k][1]);
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
         const int block_r = wr * RB, block_c = WR * RB + wc * CB;
-        auto read_c = [&](const uint8_t* from, int k) {
+        auto read = [&](const uint8_t* from, int k) {
 #pragma unroll
             for (int j = 0; j < CB; ++j) fc[k][j] = fragment(from, block_c + j, k);
+#pragma unroll
+            for (int i = 0; i < RB; ++i) fr[k][i] = fragment(from, block_r + i, k);
         };
         int wr_next[RB], wc_next[CB];
         auto read_words = [&](const uint8_t* from) {
@@ -139,25 +117,25 @@ struct Fp8Product {
 #pragma unroll
             for (int j = 0; j < CB; ++j) sc[j] = of(wc_next[j]);
         };
-        auto multiply = [&](int i, int k) {
-            if constexpr (!EXACT) {
+        auto multiply = [&](int k) {
+            if constexpr (EXACT) {             // in bfloat16, eight of a lane's 32 elements at a time
 #pragma unroll
-                for (int j = 0; j < CB; ++j) acc[j][i] = mfma8(fc[k][j], fr[i], acc[j][i], sc[j], sr[i]);
-            }
-        };
-        // EXACT: a step in bfloat16, eight of a lane's 32 elements at a time
-        auto multiply_all = [&](int k) {
+                for (int q = 0; q < 4; ++q) {
+                    v4i x[CB];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                v4i x[CB];
+                    for (int j = 0; j < CB; ++j) x[j] = in_bf16(fc[k][j][2 * q], fc[k][j][2 * q + 1], __int_as_float(sc[j]));
 #pragma unroll
-                for (int j = 0; j < CB; ++j) x[j] = in_bf16(fc[k][j][2 * q], fc[k][j][2 * q + 1], __int_as_float(sc[j]));
+                    for (int i = 0; i < RB; ++i) {
+                        const v4i y = in_bf16(fr[k][i][2 * q], fr[k][i][2 * q + 1], __int_as_float(sr[i]));
 #pragma unroll
-                for (int i = 0; i < RB; ++i) {
-                    const v4i y = in_bf16(fr[i][2 * q], fr[i][2 * q + 1], __int_as_float(sr[i]));
-#pragma unroll
-                    for (int j = 0; j < CB; ++j) acc[j][i] = mfma16(x[j], y, acc[j][i]);
+                        for (int j = 0; j < CB; ++j) acc[j][i] = mfma16(x[j], y, acc[j][i]);
+                    }
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int j = 0; j < CB; ++j) acc[j][i] = mfma8(fc[k][j], fr[k][i], acc[j][i], sc[j], sr[i]);
             }
         };
 #pragma unroll
@@ -165,80 +143,42 @@ struct Fp8Product {
 #pragma unroll
             for (int i = 0; i < RB; ++i) acc[j][i] = v16f{};
         if (s0 >= s1) return;
-        const int last = s1 - 1;
         ask(s0, lds0);
-        ask(min(s0 + 1, last), lds1);
+        ask(s0 + 1, lds1);
         if constexpr (SLOTS == 4) {
-            ask(min(s0 + 2, last), lds2);
-            ask(min(s0 + 3, last), lds3);
+            ask(s0 + 2, lds2);
+            ask(s0 + 3, lds3);
         }
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SLOTS - 1) * kAsks) : "memory");
         __builtin_amdgcn_s_barrier();
         read_words(lds0);
-        read_c(lds0, 0);
-#pragma unroll
-        for (int i = 0; i < RB; ++i) fr[i] = fragment(lds0, block_r + i, 0);
+        read(lds0, 0);
         take_words(s0);
+        // Reads and requests stand between the products, one each: left to itself the compiler moves them together, and they are waited for.
+        auto between = [&](auto reads, auto requests) {
+            if constexpr (!EXACT) {
+#pragma unroll
+                for (int i = 0; i < RB * CB; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                          // a matrix instruction
+                    __builtin_amdgcn_sched_group_barrier(0x100, decltype(reads)::value, 0);     // LDS reads
+                    if constexpr (decltype(requests)::value > 0) __builtin_amdgcn_sched_group_barrier(0x020, decltype(requests)::value, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        constexpr int kReads = (2 * (RB + CB) + RB * CB - 1) / (RB * CB), kReadsAll = (3 * (RB + CB) + RB * CB - 1) / (RB * CB);
         auto stage = [&](int s, uint8_t* here, uint8_t* next) {
-            if constexpr (EXACT) {
-                // (the conversions leave the compiler enough to put between reads and products)
-                read_c(here, 1);
-                v8i fr1[RB];
-#pragma unroll
-                for (int i = 0; i < RB; ++i) fr1[i] = fragment(here, block_r + i, 1);
-                multiply_all(0);
-#pragma unroll
-                for (int i = 0; i < RB; ++i) fr[i] = fr1[i];
-                __builtin_amdgcn_sched_barrier(0);
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");
-                __builtin_amdgcn_s_barrier();
-                ask(min(s + SLOTS, last), here);
-                read_words(next);
-                read_c(next, 0);
-                v8i fr0[RB];
-#pragma unroll
-                for (int i = 0; i < RB; ++i) fr0[i] = fragment(next, block_r + i, 0);
-                multiply_all(1);
-#pragma unroll
-                for (int i = 0; i < RB; ++i) fr[i] = fr0[i];
-                __builtin_amdgcn_sched_barrier(0);
-                take_words(s + 1);
-                return;
-            }
-            read_c(here, 1);
-#pragma unroll
-            for (int i = 0; i < RB; ++i) {
-                multiply(i, 0);
-                fr[i] = fragment(here, block_r + i, 1);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x100, 2 * CB, 0);      // LDS reads
-#pragma unroll
-            for (int i = 0; i < RB; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, CB, 0);      // matrix instructions
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(0, 1);
-            __builtin_amdgcn_sched_barrier(0);
+            read(here, 1);
+            multiply(0);
+            between(std::integral_constant<int, kReads>{}, std::integral_constant<int, 0>{});
             // the next stage has landed, this one is read out
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * kAsks) : "memory");
             __builtin_amdgcn_s_barrier();
+            read(next, 0);
             read_words(next);
-            read_c(next, 0);
-            fr[0] = fragment(next, block_r, 0);
-            ask(min(s + SLOTS, last), here);
-#pragma unroll
-            for (int i = 1; i < RB; ++i) {
-                multiply(i, 1);
-                fr[i] = fragment(next, block_r + i, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x100, RB + CB + 2 * CB + 2, 0);
-#pragma unroll
-            for (int i = 1; i < RB; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, CB, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            ask(s + SLOTS, here);
+            multiply(1);
+            between(std::integral_constant<int, kReadsAll>{}, std::integral_constant<int, (kAsks + RB * CB - 1) / (RB * CB)>{});
             take_words(s + 1);
         };
         int s = s0;
@@ -268,66 +208,27 @@ struct Fp8Product {
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_fp8_product(ProductArgs p) {
     using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
-    constexpr int kTable = Product::kRows == 256 ? kTable256 : Product::kRows == 128 ? kTable128 : kTable64;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    const int32_t* tiles = OF == Of::kExpertRows ? p.table + kTable * (p.experts + 1) : nullptr;
-    const int tiles_m = OF == Of::kExpertRows ? tiles[p.experts] : p.tiles_m;
-    const int64_t all = (int64_t)tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1), per = (all + kXcd - 1) / kXcd;
-    const int64_t index = blockIdx.x / kXcd;
-    int64_t t = (int64_t)(blockIdx.x % kXcd) * per + index;
-    if (index >= per || t >= all) return;
-    int e = 0;
-    if constexpr (OF == Of::kExpertWeights) {
-        const int each = tiles_m * p.tiles_n;
-        e = (int)(t / each);
-        t -= (int64_t)e * each;
-    }
-    const int64_t band = t / (4 * p.tiles_n);
-    const int rest = (int)(t - band * 4 * p.tiles_n), high = min(4, tiles_m - (int)band * 4);
-    const int tm = (int)band * 4 + rest % high, tn = rest / high;
-
-    int64_t a0 = (int64_t)tm * Product::kRows, a_end = p.M, b0 = (int64_t)tn * Product::kCols, b_end = p.N;
-    int s0 = 0, s1 = p.stages;
-    uint8_t* d = static_cast<uint8_t*>(p.d);
-    int64_t b_first = 0;
-    if constexpr (OF == Of::kExpertRows) {
-        e = expert_of_tile(tiles, p.experts, tm, threadIdx.x % kWave);
-        a0 = p.table[e] + (int64_t)(tm - tiles[e]) * Product::kRows;
-        a_end = p.table[e + 1];
-        b_first = (int64_t)e * p.N;
-    } else if constexpr (OF == Of::kExpertWeights) {
-        const int32_t* blocks = p.table + kTable128 * (p.experts + 1);
-        s0 = blocks[e];
-        s1 = blocks[e + 1];
-        if (s0 == s1 && p.accumulate) return;
-        d += (int64_t)e * p.stride * (p.bf16 ? 2 : 4);
-    } else {
-        s0 = (int)blockIdx.y * p.per_split;
-        s1 = min(s0 + p.per_split, p.stages);
-        d += (int64_t)blockIdx.y * p.M * p.ldd * 4;      // (parts are fp32)
-    }
+    const TileCount<Product::kRows, OF> count(p);
+    const int64_t index = blockIdx.x / kXcd, t = (int64_t)(blockIdx.x % kXcd) * count.per_xcd + index;
+    if (index >= count.per_xcd || t >= count.all) return;
+    const Tile tile = tile_at<Product::kRows, Product::kCols, OF>(p, count, t, blockIdx.y);
+    if (OF == Of::kExpertWeights && tile.s0 == tile.s1 && p.accumulate) return;
     Product prod;
-    prod.run(p.a, p.b, a0, a_end, b_first + b0, b_first + b_end, OF == Of::kExpertRows && p.picks ? p.order : nullptr, p.picks, s0, s1, lds);
+    prod.run(p.a, p.b, tile.a0, tile.a_end, tile.b0, tile.b_end, OF == Of::kExpertRows && p.picks ? p.order : nullptr, p.picks, tile.s0, tile.s1, lds);
     const int wave = threadIdx.x / kWave;
-    const int64_t m0 = a0 + wave / WC * RB * 32, c0 = b0 + wave % WC * CB * 32;
+    const int64_t m0 = tile.a0 + wave / WC * RB * 32, c0 = tile.c0 + wave % WC * CB * 32;
     if (p.bf16) {
         store_tiles<RB, CB>(prod.acc, true, lds, [&](int row, int col, u32x4 v) {
             const int64_t m = m0 + row, n = c0 + col;
-            if (m >= a_end || n >= p.N) return;
-            uint16_t* z = reinterpret_cast<uint16_t*>(d) + m * p.ldd + n;
-            if (n + 8 <= p.N) {
-                *reinterpret_cast<u32x4_a2*>(z) = v;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 7; ++i)
-                    if (n + i < p.N) z[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
-            }
+            if (m >= tile.a_end || n >= p.N) return;
+            put8(reinterpret_cast<uint16_t*>(tile.d) + m * p.ldd + n, v, p.N - n);
         });
     } else {
         store_tiles<RB, CB>(prod.acc, false, lds, [&](int row, int col, u32x4 v) {
             const int64_t m = m0 + row, n = c0 + col;
-            if (m >= a_end || n >= p.N) return;
-            float* z = reinterpret_cast<float*>(d) + m * p.ldd + n;
+            if (m >= tile.a_end || n >= p.N) return;
+            float* z = reinterpret_cast<float*>(tile.d) + m * p.ldd + n;
             if (n + 4 <= p.N) {
                 u32x4_a4* q = reinterpret_cast<u32x4_a4*>(z);
                 if (p.accumulate) *q = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, (u32x4)*q) + __builtin_bit_cast(f32x4, v));
@@ -370,13 +271,15 @@ daq_status launch_product(ProductArgs p, hipStream_t st) {
     return DAQ_OK;
 }
 template <Of OF>
-daq_status launch_form(Fp8Form form, bool exact, const ProductArgs& p, hipStream_t st) {
+daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) {
     if (exact) return form == Fp8Form::k64 ? launch_product<2, 1, 1, 2, 4, true, OF>(p, st) : launch_product<2, 2, 2, 2, 2, true, OF>(p, st);
-    switch (form) {
-        case Fp8Form::k64: return launch_product<2, 1, 1, 2, 4, false, OF>(p, st);
-        case Fp8Form::k128: return launch_product<2, 2, 2, 2, 2, false, OF>(p, st);
-        default: return launch_product<2, 4, 4, 2, 2, false, OF>(p, st);
-    }
+    if (form == Fp8Form::k64) return launch_product<2, 1, 1, 2, 4, false, OF>(p, st);
+    if (form == Fp8Form::k128) return launch_product<2, 2, 2, 2, 2, false, OF>(p, st);
+    const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, 256), tn = ceil_div(p.N, 256);
+    if (tm > 0x7FFFFFFF / (4 * tn) || tm * tn > (int64_t)1 << 40) return DAQ_ERR_UNSUPPORTED;
+    p.tiles_m = (int)tm;
+    p.tiles_n = (int)tn;
+    return fp8_large(OF, p, st);
 }
 
 }  // namespace
