@@ -17,6 +17,14 @@ constexpr int kPlaces = kB * kB;                            // products of a ste
 // every place between two products is given what it can take: two reads, or a request, as the way into LDS takes 16 cycles of each of the four waves' and
 // a product 64.  A stage is read out in the first half of its first step, then the stage after the next is asked for in its place, while
 // the next one has until the second step to land.  Behind a tile's last stage the first two of the next tile are asked for before its results leave.
+// The lane, as a value that the compiler works on where it stands: places of lanes that it kept from tile to tile would cost the registers that
+// the sums need.
+__device__ __forceinline__ int lane_now() {
+    int lane = threadIdx.x % kWave;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+
 struct Source {              // what a wave asks for: 128 rows of A (waves 0 and 1) or B
     uint32_t off[16], word_off[2];
     const uint8_t* codes;
@@ -24,8 +32,7 @@ struct Source {              // what a wave asks for: 128 rows of A (waves 0 and
     int64_t codes_left, words_left, pitch_words;
     int s1;
 
-    __device__ __forceinline__ void set(const ProductArgs& p, const Tile& t, bool gather) {
-        const int lane = threadIdx.x % kWave;
+    __device__ __forceinline__ void set(const ProductArgs& p, const Tile& t, bool gather, int lane) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
         const bool of_b = wave >= kWaves / 2;
         const Fp8Operand& o = of_b ? p.b : p.a;
@@ -63,8 +70,8 @@ struct Source {              // what a wave asks for: 128 rows of A (waves 0 and
 // The results of a wave, through its 4 KiB of LDS so that whole lines are written: 32 rows of 64 columns at a time, 16-byte pieces of a row in the order
 // piece ^ row % 8.  put(row block, pair of column blocks, rows 8 k .., pieces)
 template <typename Put>
-__device__ __forceinline__ void results_out(const v16f (&acc)[kB][kB], uint8_t* mine, Put put) {
-    const int lane = threadIdx.x % kWave, m = lane % 32, h = lane / 32;
+__device__ __forceinline__ void results_out(const v16f (&acc)[kB][kB], uint8_t* mine, int lane, Put put) {
+    const int m = lane % 32, h = lane / 32;
 #pragma unroll
     for (int i = 0; i < kB; ++i)
 #pragma unroll
@@ -87,29 +94,26 @@ __device__ __forceinline__ void results_out(const v16f (&acc)[kB][kB], uint8_t* 
 }
 
 // lds0, lds1: the stages' places, as arguments so that the compiler knows them apart, and does not let a read of one wait for the requests into the other.
-template <Of OF>
+// FLUSH: rows of results are whole 16-byte pieces, and leave through one descriptor, which ends with the product's last row: every tile has the same
+// number of stores, so that what is waited for is known here.
+template <Of OF, bool FLUSH>
 __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restrict__ lds0, uint8_t* __restrict__ lds1, uint8_t* __restrict__ out) {
-    const int lane = threadIdx.x % kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wr = wave / 2, wc = wave % 2;
     const bool gather = OF == Of::kExpertRows && p.picks != 0;
     const TileCount<kEdge, OF> count(p);
-    const int64_t first = (int64_t)(blockIdx.x % kXcd) * count.per_xcd, end = min(first + count.per_xcd, count.all);
-    int64_t t = first + blockIdx.x / kXcd;
+    const int first = (int)(blockIdx.x % kXcd) * count.per_xcd, end = min(first + count.per_xcd, count.all);
+    int t = first + (int)(blockIdx.x / kXcd);
     if (t >= end) return;
     Tile tile = tile_at<kEdge, kEdge, OF>(p, count, t, 0);
     Source from;
-    from.set(p, tile, gather);
+    from.set(p, tile, gather, lane_now());
     from.ask(wave, tile.s0, lds0);
     from.ask(wave, tile.s0 + 1, lds1);
-    bool stored = false;               // the stores of a whole tile are under way behind the first two stages' requests
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
     v8i fr[2][kB], fc[2][kB];
-    int sr[kB], sc[kB], wr_next[kB], wc_next[kB], at[2][2];     // at: of a lane in 32 rows, step and half of its 32 bytes
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) at[k][u] = (lane % 32) * 128 + ((k * 4 + lane / 32 * 2 + u) ^ (lane / 2 & 7)) * 16;
+    int sr[kB], sc[kB], wr_next[kB], wc_next[kB], at[2][2], at_word;     // at: of a lane in 32 rows, step and half of its 32 bytes
     auto fragment = [&](const uint8_t* p0, int block, int k) {
         const v4i lo = *reinterpret_cast<const v4i*>(p0 + block * 4096 + at[k][0]), hi = *reinterpret_cast<const v4i*>(p0 + block * 4096 + at[k][1]);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -121,8 +125,8 @@ __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restr
     auto read_words = [&](const uint8_t* p0) {
 #pragma unroll
         for (int i = 0; i < kB; ++i) {
-            wr_next[i] = *reinterpret_cast<const int*>(p0 + kCodes + (wr * kB + i) * 128 + (lane % 32) * 4);
-            wc_next[i] = *reinterpret_cast<const int*>(p0 + kCodes + (2 * kB + wc * kB + i) * 128 + (lane % 32) * 4);
+            wr_next[i] = *reinterpret_cast<const int*>(p0 + kCodes + (wr * kB + i) * 128 + at_word);
+            wc_next[i] = *reinterpret_cast<const int*>(p0 + kCodes + (2 * kB + wc * kB + i) * 128 + at_word);
         }
     };
     auto take_words = [&](int s) {      // the byte of stage s
@@ -134,16 +138,22 @@ __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restr
     static_assert(2 * kB + 2 < kPlaces && kAsks <= kDone + kPlaces, "everything has its place");
 
     for (;;) {
-        if (stored) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAsks + kStores) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAsks) : "memory");
+        // the first stage has landed; the stores of the tile before follow the requests for the first two
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(FLUSH ? kAsks + kStores : 0) : "memory");
         __builtin_amdgcn_s_barrier();
+        const int lane = lane_now();
+        at_word = (lane % 32) * 4;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) at[k][u] = (lane % 32) * 128 + ((k * 4 + lane / 32 * 2 + u) ^ (lane / 2 & 7)) * 16;
         v16f acc[kB][kB];
 #pragma unroll
         for (int j = 0; j < kB; ++j)
 #pragma unroll
             for (int i = 0; i < kB; ++i) acc[j][i] = v16f{};
         auto product = [&](int n, int k) { acc[n % kB][n / kB] = mfma8(fc[k][n % kB], fr[k][n / kB], acc[n % kB][n / kB], sc[n % kB], sr[n / kB]); };
-        auto stage = [&](int s, uint8_t* here, uint8_t* next) {
+        auto stage = [&](int s, uint8_t* here, uint8_t* next, auto stores) {
             const int later = s + 2;
             const __amdgpu_buffer_rsrc_t codes = from.codes_of(later), words = from.words_of(later);
 #pragma unroll
@@ -160,9 +170,7 @@ __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restr
 #pragma unroll
             for (int n = 0; n < kPlaces; ++n) {
                 if (n == 2) {
-                    // the next stage has landed
-                    if (stored && s == tile.s0) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kDone + 2 + kStores) : "memory");
-                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kDone + 2) : "memory");
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kDone + 2 + decltype(stores)::value) : "memory");      // the next stage has landed
                     __builtin_amdgcn_s_barrier();
                 }
                 product(n, 1);
@@ -177,52 +185,57 @@ __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restr
 #pragma unroll
         for (int n = 0; n < 2 * kB; ++n) fetch(lds0, n, 0);
         take_words(tile.s0);
-        for (int s = tile.s0; s < tile.s1; s += 2) {            // (an odd count has a stage of zeros behind it)
-            stage(s, lds0, lds1);
-            stage(s + 1, lds1, lds0);
+        // (an odd count has a stage of zeros behind it, a count of zero two)
+        constexpr std::integral_constant<int, 0> kNone{};
+        stage(tile.s0, lds0, lds1, std::integral_constant<int, FLUSH ? kStores : 0>{});
+        stage(tile.s0 + 1, lds1, lds0, kNone);
+#pragma nounroll
+        for (int s = tile.s0 + 2; s < tile.s1; s += 2) {
+            stage(s, lds0, lds1, kNone);
+            stage(s + 1, lds1, lds0, kNone);
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // the requests past the end have landed
         __builtin_amdgcn_s_barrier();
         const Tile done = tile;
-        t += gridDim.x / kXcd;
+        t += (int)(gridDim.x / kXcd);
         const bool more = t < end;
         if (more) {
             tile = tile_at<kEdge, kEdge, OF>(p, count, t, 0);
-            from.set(p, tile, gather);
+            from.set(p, tile, gather, lane_now());
             from.ask(wave, tile.s0, lds0);
             from.ask(wave, tile.s0 + 1, lds1);
         }
-        const int64_t row0 = done.a0 + wr * 128 + lane / 8, col0 = done.c0 + wc * 128 + (lane & 7) * 8;
-        uint16_t* const d = reinterpret_cast<uint16_t*>(done.d);
-        const bool whole = done.a0 + kEdge <= done.a_end && done.c0 + kEdge <= p.N && p.ldd % 8 == 0 && p.ldd < (1 << 22) && ((uintptr_t)d & 15) == 0;
-        if (whole) {
-            const __amdgpu_buffer_rsrc_t to = bytes_of(reinterpret_cast<const uint8_t*>(d + done.a0 * p.ldd + done.c0), (int64_t)kTileReach);
-            const uint32_t lane_off = (uint32_t)((wr * 128 + lane / 8) * p.ldd + wc * 128 + (lane & 7) * 8) * 2u;
-            results_out(acc, out + wave * 4096, [&](int i, int jp, int k, u32x4 v) {
-                __builtin_amdgcn_raw_buffer_store_b128(v, to, lane_off, (uint32_t)((i * 32 + k * 8) * p.ldd + jp * 64) * 2u, 0);
+        uint16_t* const d = reinterpret_cast<uint16_t*>(done.d) + done.a0 * p.ldd + done.c0;
+        const int rows = (int)min(done.a_end - done.a0, (int64_t)kEdge), cols = (int)min(p.N - done.c0, (int64_t)kEdge);
+        const int now = lane_now(), row0 = wr * 128 + now / 8, col0 = wc * 128 + (now & 7) * 8;
+        if constexpr (FLUSH) {
+            const __amdgpu_buffer_rsrc_t to = bytes_of(reinterpret_cast<const uint8_t*>(d), ((rows - 1) * p.ldd + cols) * 2);
+            const uint32_t off0 = (uint32_t)(row0 * (int)p.ldd + col0) * 2u;
+            results_out(acc, out + wave * 4096, now, [&](int i, int jp, int k, u32x4 v) {
+                const uint32_t off = off0 + (uint32_t)((i * 32 + k * 8) * (int)p.ldd + jp * 64) * 2u;
+                __builtin_amdgcn_raw_buffer_store_b128(v, to, (int)(col0 + jp * 64 < cols ? off : kTileReach), 0, 0);
             });
+            static_assert(kStores == kB * (kB / 2) * 4, "as many as results_out puts");
         } else {
-            results_out(acc, out + wave * 4096, [&](int i, int jp, int k, u32x4 v) {
-                const int64_t m = row0 + i * 32 + k * 8, n = col0 + jp * 64;
-                if (m < done.a_end && n < p.N) put8(d + m * p.ldd + n, v, p.N - n);
+            results_out(acc, out + wave * 4096, now, [&](int i, int jp, int k, u32x4 v) {
+                const int m = row0 + i * 32 + k * 8, n = col0 + jp * 64;
+                if (m < rows && n < cols) put8(d + m * p.ldd + n, v, cols - n);
             });
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         }
         if (!more) return;
-        stored = whole;
     }
 }
 
-template <Of OF>
+template <Of OF, bool FLUSH>
 __global__ __launch_bounds__(64 * kWaves, 1) void k_fp8_large(ProductArgs p) {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    run_tiles<OF>(p, lds, lds + kStage, lds + 2 * kStage);
+    run_tiles<OF, FLUSH>(p, lds, lds + kStage, lds + 2 * kStage);
 }
 
-template <Of OF>
+template <Of OF, bool FLUSH>
 daq_status launch(const ProductArgs& p, hipStream_t st) {
     const int64_t tiles = round_up((int64_t)p.tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1), kXcd);
-    const auto kernel = k_fp8_large<OF>;
+    const auto kernel = k_fp8_large<OF, FLUSH>;
     if (!allow_lds((const void*)kernel, kLds)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("fp8_large", st, hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(tiles, 256)), dim3(64 * kWaves), kLds, st, p));
     return DAQ_OK;
@@ -231,10 +244,11 @@ daq_status launch(const ProductArgs& p, hipStream_t st) {
 }  // namespace
 
 daq_status fp8_large(Of of, const ProductArgs& p, hipStream_t st) {
+    const bool flush = p.N % 8 == 0 && p.ldd % 8 == 0 && p.ldd < (1 << 22) && ((uintptr_t)p.d & 15) == 0 && p.stride % 8 == 0;
     switch (of) {
-        case Of::kWhole: return launch<Of::kWhole>(p, st);
-        case Of::kExpertRows: return launch<Of::kExpertRows>(p, st);
-        default: return launch<Of::kExpertWeights>(p, st);
+        case Of::kWhole: return flush ? launch<Of::kWhole, true>(p, st) : launch<Of::kWhole, false>(p, st);
+        case Of::kExpertRows: return flush ? launch<Of::kExpertRows, true>(p, st) : launch<Of::kExpertRows, false>(p, st);
+        default: return flush ? launch<Of::kExpertWeights, true>(p, st) : launch<Of::kExpertWeights, false>(p, st);
     }
 }
 

@@ -210,7 +210,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_fp8_product(ProductArgs p) 
     using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const TileCount<Product::kRows, OF> count(p);
-    const int64_t index = blockIdx.x / kXcd, t = (int64_t)(blockIdx.x % kXcd) * count.per_xcd + index;
+    const int index = (int)(blockIdx.x / kXcd), t = (int)(blockIdx.x % kXcd) * count.per_xcd + index;
     if (index >= count.per_xcd || t >= count.all) return;
     const Tile tile = tile_at<Product::kRows, Product::kCols, OF>(p, count, t, blockIdx.y);
     if (OF == Of::kExpertWeights && tile.s0 == tile.s1 && p.accumulate) return;
@@ -257,12 +257,16 @@ __global__ __launch_bounds__(256) void k_fp8_sum(const float* parts, int splits,
     }
 }
 
+// Tiles are counted, and eight more of them and four bands, within 31 bits.
+bool tiles_ok(int64_t tm, int64_t tn, int64_t experts) { return tm <= (0x7FFFFFFF - 64) / (4 * tn) && tm * tn <= (0x7FFFFFFF - 64) / experts; }
+
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
 daq_status launch_product(ProductArgs p, hipStream_t st) {
     using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
     const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, Product::kRows), tn = ceil_div(p.N, Product::kCols);
+    if (!tiles_ok(tm, tn, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
     const int64_t tiles = round_up(tm * tn * (OF == Of::kExpertWeights ? p.experts : 1), kXcd);
-    if (tm > 0x7FFFFFFF / std::max<int64_t>(1, 4 * tn) || !grid_ok(tiles, Product::kWaves * 64)) return DAQ_ERR_UNSUPPORTED;
+    if (!grid_ok(tiles, Product::kWaves * 64)) return DAQ_ERR_UNSUPPORTED;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
     const auto kernel = k_fp8_product<WR, WC, RB, CB, SLOTS, EXACT, OF>;
@@ -276,7 +280,7 @@ daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) 
     if (form == Fp8Form::k64) return launch_product<2, 1, 1, 2, 4, false, OF>(p, st);
     if (form == Fp8Form::k128) return launch_product<2, 2, 2, 2, 2, false, OF>(p, st);
     const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, 256), tn = ceil_div(p.N, 256);
-    if (tm > 0x7FFFFFFF / (4 * tn) || tm * tn > (int64_t)1 << 40) return DAQ_ERR_UNSUPPORTED;
+    if (!tiles_ok(tm, tn, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
     return fp8_large(OF, p, st);

@@ -46,13 +46,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_of(const uint8_t* from, 
 template <int ROWS, Of OF>
 struct TileCount {
     const int32_t* before;    // experts' rows: tiles before every expert
-    int tiles_m;
-    int64_t all, per_xcd;
+    int tiles_m, all, per_xcd;    // (host: all of a launch's are within 31 bits)
     __device__ __forceinline__ explicit TileCount(const ProductArgs& p) {
         constexpr int kTable = ROWS == 256 ? kTable256 : ROWS == 128 ? kTable128 : kTable64;
         before = OF == Of::kExpertRows ? p.table + kTable * (p.experts + 1) : nullptr;
-        tiles_m = OF == Of::kExpertRows ? before[p.experts] : p.tiles_m;
-        all = (int64_t)tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1);
+        tiles_m = OF == Of::kExpertRows ? __builtin_amdgcn_readfirstlane(before[p.experts]) : p.tiles_m;
+        all = tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1);
         per_xcd = (all + kXcd - 1) / kXcd;
     }
 };
@@ -66,16 +65,17 @@ struct Tile {
 };
 // Tile t, in bands of four row tiles, whose panels the L2 of an XCD holds.  The whole wave asks.
 template <int ROWS, int COLS, Of OF>
-__device__ __forceinline__ Tile tile_at(const ProductArgs& p, const TileCount<ROWS, OF>& n, int64_t t, int part) {
+__device__ __forceinline__ Tile tile_at(const ProductArgs& p, const TileCount<ROWS, OF>& n, int t, int part) {
+    auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     int e = 0;
     if constexpr (OF == Of::kExpertWeights) {
         const int each = n.tiles_m * p.tiles_n;
-        e = (int)(t / each);
-        t -= (int64_t)e * each;
+        e = uniform((int)((uint32_t)t / (uint32_t)each));
+        t -= e * each;
     }
-    const int64_t band = t / (4 * p.tiles_n);
-    const int rest = (int)(t - band * 4 * p.tiles_n), high = min(4, n.tiles_m - (int)band * 4);
-    const int tm = (int)band * 4 + rest % high, tn = rest / high;
+    const int band = uniform((int)((uint32_t)t / (4u * (uint32_t)p.tiles_n)));
+    const int rest = t - band * 4 * p.tiles_n, high = min(4, n.tiles_m - band * 4);
+    const int col = uniform((int)((uint32_t)rest / (uint32_t)high)), tm = band * 4 + rest - col * high, tn = col;
     Tile w;
     w.a0 = (int64_t)tm * ROWS;
     w.a_end = p.M;
@@ -86,14 +86,14 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs& p, const TileCount<RO
     w.d = static_cast<uint8_t*>(p.d);
     if constexpr (OF == Of::kExpertRows) {
         e = expert_of_tile(n.before, p.experts, tm, threadIdx.x % kWave);
-        w.a0 = p.table[e] + (int64_t)(tm - n.before[e]) * ROWS;
-        w.a_end = p.table[e + 1];
+        w.a0 = uniform(p.table[e] + (tm - n.before[e]) * ROWS);
+        w.a_end = uniform(p.table[e + 1]);
         w.b0 += (int64_t)e * p.N;
         w.b_end += (int64_t)e * p.N;
     } else if constexpr (OF == Of::kExpertWeights) {
         const int32_t* blocks = p.table + kTable128 * (p.experts + 1);
-        w.s0 = blocks[e];
-        w.s1 = blocks[e + 1];
+        w.s0 = uniform(blocks[e]);
+        w.s1 = uniform(blocks[e + 1]);
         w.d += (int64_t)e * p.stride * (p.bf16 ? 2 : 4);
     } else {
         w.s0 = part * p.per_split;
