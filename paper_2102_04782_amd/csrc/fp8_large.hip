@@ -102,10 +102,9 @@ __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restr
     const int wr = wave / 2, wc = wave % 2;
     const bool gather = OF == Of::kExpertRows && p.picks != 0;
     const TileCount<kEdge, OF> count(p);
-    const int first = (int)(blockIdx.x % kXcd) * count.per_xcd, end = min(first + count.per_xcd, count.all);
-    int t = first + (int)(blockIdx.x / kXcd);
-    if (t >= end) return;
-    Tile tile = tile_at<kEdge, kEdge, OF>(p, count, t, 0);
+    int t = (int)(blockIdx.x / kXcd);
+    Tile tile;
+    if (!tile_at<kEdge, kEdge, OF>(p, count, t, 0, tile)) return;      // (an expert's last tiles: one workgroup, one tile)
     Source from;
     from.set(p, tile, gather, lane_now());
     from.ask(wave, tile.s0, lds0);
@@ -198,9 +197,8 @@ __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restr
         __builtin_amdgcn_s_barrier();
         const Tile done = tile;
         t += (int)(gridDim.x / kXcd);
-        const bool more = t < end;
+        const bool more = tile_at<kEdge, kEdge, OF>(p, count, t, 0, tile);
         if (more) {
-            tile = tile_at<kEdge, kEdge, OF>(p, count, t, 0);
             from.set(p, tile, gather, lane_now());
             from.ask(wave, tile.s0, lds0);
             from.ask(wave, tile.s0 + 1, lds1);
@@ -234,10 +232,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void k_fp8_large(ProductArgs p) {
 
 template <Of OF, bool FLUSH>
 daq_status launch(const ProductArgs& p, hipStream_t st) {
-    const int64_t tiles = round_up((int64_t)p.tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1), kXcd);
+    // (gradients of experts take times of their own: a workgroup for each tile, which the CUs take as they get free)
+    const int64_t tiles = OF == Of::kExpertWeights ? tile_groups<OF>(p) : std::min<int64_t>(tile_groups<OF>(p), 256);
     const auto kernel = k_fp8_large<OF, FLUSH>;
     if (!allow_lds((const void*)kernel, kLds)) return DAQ_ERR_HIP;
-    DAQ_LAUNCH("fp8_large", st, hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(tiles, 256)), dim3(64 * kWaves), kLds, st, p));
+    DAQ_LAUNCH("fp8_large", st, hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(64 * kWaves), kLds, st, p));
     return DAQ_OK;
 }
 

@@ -210,9 +210,8 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_fp8_product(ProductArgs p) 
     using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const TileCount<Product::kRows, OF> count(p);
-    const int index = (int)(blockIdx.x / kXcd), t = (int)(blockIdx.x % kXcd) * count.per_xcd + index;
-    if (index >= count.per_xcd || t >= count.all) return;
-    const Tile tile = tile_at<Product::kRows, Product::kCols, OF>(p, count, t, blockIdx.y);
+    Tile tile;
+    if (!tile_at<Product::kRows, Product::kCols, OF>(p, count, (int)(blockIdx.x / kXcd), blockIdx.y, tile)) return;
     if (OF == Of::kExpertWeights && tile.s0 == tile.s1 && p.accumulate) return;
     Product prod;
     prod.run(p.a, p.b, tile.a0, tile.a_end, tile.b0, tile.b_end, OF == Of::kExpertRows && p.picks ? p.order : nullptr, p.picks, tile.s0, tile.s1, lds);
@@ -258,17 +257,17 @@ __global__ __launch_bounds__(256) void k_fp8_sum(const float* parts, int splits,
 }
 
 // Tiles are counted, and eight more of them and four bands, within 31 bits.
-bool tiles_ok(int64_t tm, int64_t tn, int64_t experts) { return tm <= (0x7FFFFFFF - 64) / (4 * tn) && tm * tn <= (0x7FFFFFFF - 64) / experts; }
+bool tiles_ok(int64_t tm, int64_t tn, int64_t experts) { return tm <= (0x7FFFFFFF - 64) / (4 * tn) && tm * tn + kXcd <= (0x7FFFFFFF - 64) / experts; }
 
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
 daq_status launch_product(ProductArgs p, hipStream_t st) {
     using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
     const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, Product::kRows), tn = ceil_div(p.N, Product::kCols);
     if (!tiles_ok(tm, tn, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
-    const int64_t tiles = round_up(tm * tn * (OF == Of::kExpertWeights ? p.experts : 1), kXcd);
-    if (!grid_ok(tiles, Product::kWaves * 64)) return DAQ_ERR_UNSUPPORTED;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
+    const int64_t tiles = tile_groups<OF>(p);
+    if (!grid_ok(tiles, Product::kWaves * 64)) return DAQ_ERR_UNSUPPORTED;
     const auto kernel = k_fp8_product<WR, WC, RB, CB, SLOTS, EXACT, OF>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("fp8_product", st, hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)p.splits), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
@@ -283,6 +282,7 @@ daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) 
     if (!tiles_ok(tm, tn, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
+    if (!grid_ok(tile_groups<OF>(p), 256)) return DAQ_ERR_UNSUPPORTED;
     return fp8_large(OF, p, st);
 }
 

@@ -42,19 +42,25 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_of(const uint8_t* from, 
     return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(n < (int64_t)kTileReach ? (uint32_t)n : kTileReach), 0x00020000);
 }
 
-// Tiles of ROWS x COLS results that a launch has, and how many an XCD takes.
+// The tiles of ROWS x COLS results that an XCD takes, numbered from 0: a run of them all; of experts' gradients, whose lengths differ, a run of every
+// expert's, another XCD's for every expert.
 template <int ROWS, Of OF>
 struct TileCount {
     const int32_t* before;    // experts' rows: tiles before every expert
-    int tiles_m, all, per_xcd;    // (host: all of a launch's are within 31 bits)
+    int tiles_m, all, per_xcd, mine;    // all: of an expert's gradient; mine: of this XCD (host: all of a launch's are within 31 bits)
     __device__ __forceinline__ explicit TileCount(const ProductArgs& p) {
         constexpr int kTable = ROWS == 256 ? kTable256 : ROWS == 128 ? kTable128 : kTable64;
         before = OF == Of::kExpertRows ? p.table + kTable * (p.experts + 1) : nullptr;
         tiles_m = OF == Of::kExpertRows ? __builtin_amdgcn_readfirstlane(before[p.experts]) : p.tiles_m;
-        all = tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1);
+        all = tiles_m * p.tiles_n;
         per_xcd = (all + kXcd - 1) / kXcd;
+        mine = OF == Of::kExpertWeights ? p.experts * per_xcd : max(0, min(per_xcd, all - xcd() * per_xcd));
     }
+    static __device__ __forceinline__ int xcd() { return (int)(blockIdx.x % kXcd); }
 };
+// Workgroups of a launch with one for every tile.
+template <Of OF>
+int64_t tile_groups(const ProductArgs& p) { return round_up((int64_t)p.tiles_m * p.tiles_n, kXcd) * (OF == Of::kExpertWeights ? p.experts : 1); }
 
 // A tile: rows a0 .. of A (a_end: the first that is not its product's), rows b0 .. of B, stages s0 .. s1 - 1, and its results, of which row
 // a0, column c0 are the first.
@@ -63,20 +69,20 @@ struct Tile {
     int s0, s1;
     uint8_t* d;
 };
-// Tile t, in bands of four row tiles, whose panels the L2 of an XCD holds.  The whole wave asks.
+// The XCD's tile i, in bands of four row tiles, whose panels its L2 holds; false: there is none.  The whole wave asks.
 template <int ROWS, int COLS, Of OF>
-__device__ __forceinline__ Tile tile_at(const ProductArgs& p, const TileCount<ROWS, OF>& n, int t, int part) {
+__device__ __forceinline__ bool tile_at(const ProductArgs& p, const TileCount<ROWS, OF>& n, int i, int part, Tile& w) {
     auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    int e = 0;
+    if (i >= n.mine) return false;
+    int e = 0, t = n.xcd() * n.per_xcd + i;
     if constexpr (OF == Of::kExpertWeights) {
-        const int each = n.tiles_m * p.tiles_n;
-        e = uniform((int)((uint32_t)t / (uint32_t)each));
-        t -= e * each;
+        e = uniform((int)((uint32_t)i / (uint32_t)n.per_xcd));
+        t = ((n.xcd() + e) % kXcd) * n.per_xcd + i - e * n.per_xcd;
+        if (t >= n.all) return false;
     }
     const int band = uniform((int)((uint32_t)t / (4u * (uint32_t)p.tiles_n)));
     const int rest = t - band * 4 * p.tiles_n, high = min(4, n.tiles_m - band * 4);
     const int col = uniform((int)((uint32_t)rest / (uint32_t)high)), tm = band * 4 + rest - col * high, tn = col;
-    Tile w;
     w.a0 = (int64_t)tm * ROWS;
     w.a_end = p.M;
     w.c0 = w.b0 = (int64_t)tn * COLS;
@@ -100,7 +106,7 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs& p, const TileCount<RO
         w.s1 = min(w.s0 + p.per_split, p.stages);
         w.d += (int64_t)part * p.M * p.ldd * 4;      // (parts are fp32)
     }
-    return w;
+    return true;
 }
 
 // Eight neighbouring bfloat16 results, of which `left` are within the row.
