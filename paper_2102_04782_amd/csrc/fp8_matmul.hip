@@ -19,13 +19,6 @@ Fp8Operand operand(const uint8_t* buf, int64_t rows, int64_t cols) {
     return {buf, buf + L.off_scales, rows, L.pitch};
 }
 
-// Eight codes to bfloat16, times the scale: exact, but what the scale takes beyond bfloat16's range.
-__device__ __forceinline__ v4i in_bf16(int lo, int hi, float s) {
-    const bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true)};
-    return v4i{__builtin_bit_cast(int, v[0]), __builtin_bit_cast(int, v[1]), __builtin_bit_cast(int, v[2]), __builtin_bit_cast(int, v[3])};
-}
-
 // The results of a workgroup of WR x WC waves, each RB x CB tiles of 32 x 32, summed over the stages s0 .. s1 - 1 of 128.  A stage of both operands,
 // 128 bytes of every row, goes straight to LDS, where the 16-byte piece j of a row lies at j ^ (row / 2 % 8): eight lanes ask for a row's line in
 // that order, and the fragment reads of sixteen rows share no bank.  SLOTS stages are under way or being read.  Fragments are read a step
@@ -277,7 +270,11 @@ template <Of OF>
 daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) {
     if (exact) return form == Fp8Form::k64 ? launch_product<2, 1, 1, 2, 4, true, OF>(p, st) : launch_product<2, 2, 2, 2, 2, true, OF>(p, st);
     if (form == Fp8Form::k64) return launch_product<2, 1, 1, 2, 4, false, OF>(p, st);
-    if (form == Fp8Form::k128) return launch_product<2, 2, 2, 2, 2, false, OF>(p, st);
+    if (form == Fp8Form::k128) {
+        // a workgroup to a CU: four stages in LDS (512 x 8192 x 8192 39.4 us instead of 48); two to a CU: two each (2048 x 4096 x 4096 32.8 instead of 38)
+        const int64_t tiles = (OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, 128)) * ceil_div(p.N, 128) * (OF == Of::kExpertWeights ? p.experts : 1);
+        return tiles <= 256 ? launch_product<2, 2, 2, 2, 4, false, OF>(p, st) : launch_product<2, 2, 2, 2, 2, false, OF>(p, st);
+    }
     const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, 256), tn = ceil_div(p.N, 256);
     if (!tiles_ok(tm, tn, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
     p.tiles_m = (int)tm;
@@ -288,14 +285,39 @@ daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) 
 
 }  // namespace
 
+static bool few_fits(int64_t tiles, int64_t N) { return tiles <= 65535 && grid_ok(ceil_div(N, 16), 512); }
+// Whether the workgroups of a product of few rows quantize these themselves: 16384 elements are 4 a thread.  us with it and in two launches: 1 x 8192 x 4096
+// 7.7 and 10.7, 4 x 8192 x 8192 18.3 and 18.5, 8 x 8192 x 8192 24 and 19.3.
+bool fp8_raw_rows(int64_t rows, int64_t K) { return rows <= 64 && rows * round_up(K, kFp8Block) <= 16384; }
+
+// us that a product of so many tiles of a form takes, by what was measured of each: a fixed time, and one for a stage, longer where more workgroups than one are
+// on a CU.  E.g., bfloat16, 64, 128 and 256: 1111 x 1500 x 2030 9.7, 12.7, -; 1777 x 2080 x 4096 28.5, 21.1, 36.5; 2048 x 4096 x 4096 -, 32.8, 38.7;
+// 2100 x 6000 x 3000 -, 51, 35.5; 512 x 8192 x 8192 -, 39.4, 66.9; fp32, 64 and 128: 1111 x 1500 x 2030 16.8, 18.8; 1777 x 2080 x 4096 53.5, 35.2.
+static double fp8_cost(Fp8Form form, double tiles, double stages, bool exact) {
+    switch (form) {
+        case Fp8Form::k64: return std::ceil(tiles / 512) * (3 + stages * (exact ? (tiles <= 256 ? 0.53 : 0.8) : tiles <= 256 ? 0.24 : 0.4));
+        case Fp8Form::k128: return tiles <= 256 ? 3 + stages * (exact ? 1.02 : 0.57) : std::ceil(tiles / 512) * (3 + stages * (exact ? 1.74 : 0.94));
+        default: return exact ? 1e30 : std::ceil(tiles / 256) * (4 + stages * (tiles <= 128 ? 1.04 : 1.36));
+    }
+}
+static Fp8Form least_cost(double t64, double t128, double t256, double stages, bool exact) {
+    const double a = fp8_cost(Fp8Form::k64, t64, stages, exact), b = fp8_cost(Fp8Form::k128, t128, stages, exact), c = fp8_cost(Fp8Form::k256, t256, stages, exact);
+    return a <= b && a <= c ? Fp8Form::k64 : b <= c ? Fp8Form::k128 : Fp8Form::k256;
+}
+
+// Few rows: up to 32, while their tiles of 64 would not fill the CUs.  8192 columns of K = 8192, 1 to 16 rows 16.6 us, 32 rows 26.8, 64 rows 42.5; tiles 18.
 Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
     Fp8Plan pl{};
     const int64_t stages = ceil_div(K, kFp8Block);
-    auto tiles = [&](int64_t n) { return ceil_div(M, n) * ceil_div(N, n); };
-    pl.form = tiles(256) >= 192 && !exact ? Fp8Form::k256 : tiles(128) >= 256 ? Fp8Form::k128 : Fp8Form::k64;
+    auto tiles = [&](int64_t n) { return (double)ceil_div(M, n) * (double)ceil_div(N, n); };
+    pl.form = M <= 32 && few_fits(1, N) && ceil_div(N, 64) < 256 ? Fp8Form::kFew : least_cost(tiles(64), tiles(128), tiles(256), (double)stages, exact);
     pl.splits = 1;
     pl.per_split = (int)stages;
     return pl;
+}
+
+static bool one_launch(int64_t M, int64_t N, int64_t K, int y_dtype) {
+    return fp8_raw_rows(M, K) && fp8_plan(M, N, K, y_dtype == DAQ_FP32).form == Fp8Form::kFew;
 }
 
 static daq_status product_sizes(int64_t M, int64_t N, int64_t K) {
@@ -310,8 +332,9 @@ static daq_status result_check(const void* D, int dtype, int64_t N, int64_t ldd,
     return !dtype_ok(dtype) || !D || !elem_aligned(D, dtype) || ldd < N || (accumulate && dtype != DAQ_FP32) ? DAQ_ERR_INVALID_ARG : DAQ_OK;
 }
 
-static daq_status fp8_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const uint8_t* B, void* D, int dtype, int64_t ldd, int accumulate,
-                             void* ws, hipStream_t st) {
+// X not NULL: A from X, in the call.
+static daq_status fp8_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, const void* X, int x_dtype, int64_t ldx, const uint8_t* B, void* D, int dtype,
+                             int64_t ldd, int accumulate, void* ws, hipStream_t st) {
     const bool exact = dtype == DAQ_FP32;
     const Fp8Plan pl = fp8_plan(M, N, K, exact);
     ProductArgs p{};
@@ -327,6 +350,7 @@ static daq_status fp8_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, 
         p.ldd = ldd;
         p.bf16 = dtype == DAQ_BF16;
         p.accumulate = accumulate;
+        if (pl.form == Fp8Form::kFew) return fp8_few(Of::kWhole, p, ceil_div(M, 64), std::min<int64_t>(M, 64), X, x_dtype, ldx, K, st);
         return launch_form<Of::kWhole>(pl.form, exact, p, st);
     }
     p.d = ws;
@@ -364,7 +388,7 @@ extern "C" daq_status daq_fp8_matmul(int64_t M, int64_t N, int64_t K, const uint
     if (rc != DAQ_OK) return rc;
     if (K > 0 && (!A || !aligned256(A) || !B || !aligned256(B))) return DAQ_ERR_INVALID_ARG;
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned256(workspace))) return DAQ_ERR_WORKSPACE;
-    return fp8_matmul(M, N, K, A, B, D, dtype, ldd, accumulate, workspace, (hipStream_t)stream);
+    return fp8_matmul(M, N, K, A, nullptr, 0, 0, B, D, dtype, ldd, accumulate, workspace, (hipStream_t)stream);
 }
 
 extern "C" daq_status daq_fp8_linear_workspace(int64_t M, int64_t N, int64_t K, daq_dtype x_dtype, daq_dtype y_dtype, size_t* bytes) {
@@ -373,7 +397,7 @@ extern "C" daq_status daq_fp8_linear_workspace(int64_t M, int64_t N, int64_t K, 
     const daq_status rc = daq_fp8_matmul_workspace(M, N, K, y_dtype, &product);
     if (!bytes) return DAQ_ERR_INVALID_ARG;
     *bytes = 0;
-    if (rc != DAQ_OK || M == 0) return rc;
+    if (rc != DAQ_OK || M == 0 || one_launch(M, N, K, y_dtype)) return rc;
     daq_fp8_layout L;
     daq_layout_fp8(M, K, &L);
     *bytes = (size_t)L.bytes + product;
@@ -389,6 +413,7 @@ extern "C" daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void
     rc = result_check(Y, y_dtype, N, ldy, 0);
     if (rc != DAQ_OK) return rc;
     if (!X || !elem_aligned(X, x_dtype) || ldx < K || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
+    if (one_launch(M, N, K, y_dtype)) return fp8_matmul(M, N, K, nullptr, X, x_dtype, ldx, W, Y, y_dtype, ldy, 0, nullptr, (hipStream_t)stream);
     if (!fp8_rows_grid_ok(M, K)) return DAQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < need || !aligned256(workspace)) return DAQ_ERR_WORKSPACE;
     uint8_t* xq = static_cast<uint8_t*>(workspace);
@@ -396,11 +421,26 @@ extern "C" daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void
     daq_layout_fp8(M, K, &L);
     rc = fp8_quantize_rows(X, x_dtype, M, K, ldx, xq, (hipStream_t)stream);
     if (rc != DAQ_OK) return rc;
-    return fp8_matmul(M, N, K, xq, W, Y, y_dtype, ldy, 0, xq + L.bytes, (hipStream_t)stream);
+    return fp8_matmul(M, N, K, xq, nullptr, 0, 0, W, Y, y_dtype, ldy, 0, xq + L.bytes, (hipStream_t)stream);
 }
 
-static daq_status experts_product(const daq_experts& plan, int64_t N, int64_t K, const uint8_t* A, int sorted, const uint8_t* W, void* Y, int dtype,
-                                  int64_t ldy, hipStream_t st) {
+// An expert has at most so many rows: a token may name one several times.
+static int64_t most_rows(const daq_experts& plan) { return plan_slots(plan); }
+
+Fp8Form daq::experts_form(const daq_experts& plan, int64_t N, int64_t K, bool exact) {
+    const int64_t slots = plan_slots(plan), each = slots / std::min<int64_t>(slots, plan.experts);
+    if (each <= 32 && ceil_div(N, 64) * std::min<int64_t>(slots, plan.experts) < 256 && most_tiles(plan, 64) <= 65535) return Fp8Form::kFew;
+    const double active = (double)std::min<int64_t>(slots, plan.experts);
+    auto tiles = [&](int64_t n) { return active * (double)ceil_div(each, n) * (double)ceil_div(N, n); };
+    return least_cost(tiles(64), tiles(128), tiles(256), (double)ceil_div(K, kFp8Block), exact);
+}
+static bool experts_one_launch(const daq_experts& plan, int64_t N, int64_t K, int y_dtype) {
+    return experts_form(plan, N, K, y_dtype == DAQ_FP32) == Fp8Form::kFew && fp8_raw_rows(most_rows(plan), K);
+}
+
+// X not NULL: A from X, in the call.
+static daq_status experts_product(const daq_experts& plan, int64_t N, int64_t K, const uint8_t* A, const void* X, int x_dtype, int64_t ldx, int sorted,
+                                  const uint8_t* W, void* Y, int dtype, int64_t ldy, hipStream_t st) {
     const int64_t slots = plan_slots(plan);
     ProductArgs p{};
     p.a = operand(A, sorted ? slots : plan.tokens, K);
@@ -417,15 +457,10 @@ static daq_status experts_product(const daq_experts& plan, int64_t N, int64_t K,
     p.experts = plan.experts;
     p.picks = sorted ? 0 : plan.picks;
     const bool exact = dtype == DAQ_FP32;
-    const Fp8Form form = experts_form(plan, N, exact);
+    const Fp8Form form = experts_form(plan, N, K, exact);
+    if (form == Fp8Form::kFew) return fp8_few(Of::kExpertRows, p, most_tiles(plan, 64), std::min<int64_t>(most_rows(plan), 64), X, x_dtype, ldx, K, st);
     p.tiles_m = (int)most_tiles(plan, form == Fp8Form::k256 ? 256 : form == Fp8Form::k128 ? 128 : 64);
     return launch_form<Of::kExpertRows>(form, exact, p, st);
-}
-
-Fp8Form daq::experts_form(const daq_experts& plan, int64_t N, bool exact) {
-    const int64_t slots = plan_slots(plan), each = slots / std::min<int64_t>(slots, plan.experts);
-    auto tiles = [&](int64_t n) { return std::max<int64_t>(1, slots / n) * ceil_div(N, n); };
-    return each >= 256 && tiles(256) >= 192 && !exact ? Fp8Form::k256 : each >= 96 && tiles(128) >= 256 ? Fp8Form::k128 : Fp8Form::k64;
 }
 
 // What the plan, the sizes, the weights and the result have to be.
@@ -450,7 +485,7 @@ extern "C" daq_status daq_experts_matmul(const daq_experts* plan, int64_t N, int
     rc = result_check(Y, dtype, N, ldy, 0);
     if (rc != DAQ_OK) return rc;
     if (!A || !aligned256(A) || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
-    return experts_product(*plan, N, K, A, sorted, W, Y, dtype, ldy, (hipStream_t)stream);
+    return experts_product(*plan, N, K, A, nullptr, 0, 0, sorted, W, Y, dtype, ldy, (hipStream_t)stream);
 }
 
 extern "C" daq_status daq_experts_linear_workspace(const daq_experts* plan, int64_t N, int64_t K, daq_dtype x_dtype, int32_t sorted, size_t* bytes) {
@@ -475,11 +510,12 @@ extern "C" daq_status daq_experts_linear(const daq_experts* plan, int64_t N, int
     if (rc != DAQ_OK) return rc;
     if (!X || !elem_aligned(X, x_dtype) || ldx < K || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
     const int64_t rows = sorted ? plan_slots(*plan) : plan->tokens;
+    if (experts_one_launch(*plan, N, K, y_dtype)) return experts_product(*plan, N, K, nullptr, X, x_dtype, ldx, sorted, W, Y, y_dtype, ldy, (hipStream_t)stream);
     if (!fp8_rows_grid_ok(rows, K)) return DAQ_ERR_UNSUPPORTED;
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned256(workspace))) return DAQ_ERR_WORKSPACE;
     rc = fp8_quantize_rows(X, x_dtype, rows, K, ldx, static_cast<uint8_t*>(workspace), (hipStream_t)stream);
     if (rc != DAQ_OK) return rc;
-    return experts_product(*plan, N, K, static_cast<const uint8_t*>(workspace), sorted, W, Y, y_dtype, ldy, (hipStream_t)stream);
+    return experts_product(*plan, N, K, static_cast<const uint8_t*>(workspace), nullptr, 0, 0, sorted, W, Y, y_dtype, ldy, (hipStream_t)stream);
 }
 
 extern "C" daq_status daq_experts_weight_grad(const daq_experts* plan, int64_t N, int64_t K, const uint8_t* dY, const uint8_t* X, void* dW,
@@ -507,7 +543,8 @@ extern "C" daq_status daq_experts_weight_grad(const daq_experts* plan, int64_t N
     p.table = plan->table;
     p.experts = plan->experts;
     p.stride = stride;
-    const int64_t big = ceil_div(N, 256) * ceil_div(K, 256) * plan->experts, mid = ceil_div(N, 128) * ceil_div(K, 128) * plan->experts;
     const bool exact = dtype == DAQ_FP32;
-    return launch_form<Of::kExpertWeights>(big >= 192 && !exact ? Fp8Form::k256 : mid >= 256 ? Fp8Form::k128 : Fp8Form::k64, exact, p, (hipStream_t)stream);
+    auto tiles = [&](int64_t n) { return (double)plan->experts * (double)ceil_div(N, n) * (double)ceil_div(K, n); };
+    const Fp8Form form = least_cost(tiles(64), tiles(128), tiles(256), (double)ceil_div(plan_slots(*plan), kFp8Block * (int64_t)plan->experts), exact);
+    return launch_form<Of::kExpertWeights>(form, exact, p, (hipStream_t)stream);
 }

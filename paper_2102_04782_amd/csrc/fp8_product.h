@@ -38,6 +38,13 @@ __device__ __forceinline__ v16f mfma8(v8i x, v8i y, v16f c, int sx, int sy) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 0, 0, 0, sx, 0, sy);
 }
 
+// Eight codes to bfloat16, times the scale: exact, but what the scale takes beyond bfloat16's range.
+__device__ __forceinline__ v4i in_bf16(int lo, int hi, float s) {
+    const bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true)};
+    return v4i{__builtin_bit_cast(int, v[0]), __builtin_bit_cast(int, v[1]), __builtin_bit_cast(int, v[2]), __builtin_bit_cast(int, v[3])};
+}
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_of(const uint8_t* from, int64_t n) {
     return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)(n < (int64_t)kTileReach ? (uint32_t)n : kTileReach), 0x00020000);
 }
@@ -124,5 +131,8 @@ __device__ __forceinline__ void put8(uint16_t* z, u32x4 v, int64_t left) {
 
 // fp8_large.hip: results in bfloat16 on tiles of 256 x 256; operands and sizes are checked, p.tiles_m and p.tiles_n set
 daq_status fp8_large(Of of, const ProductArgs& p, hipStream_t st);
+// fp8_few.hip: whole products or experts' rows in `tiles` row tiles of 64 (experts: at most so many), none of more than most_rows rows; x not NULL: A from X
+// [..][K], quantized on the way
+daq_status fp8_few(Of of, const ProductArgs& p, int64_t tiles, int64_t most_rows, const void* x, int x_dtype, int64_t ldx, int64_t K, hipStream_t st);
 
 }  // namespace daq
