@@ -35,57 +35,94 @@ __device__ __forceinline__ void best_of_wave(double& c, int& at) {
     }
 }
 
-// A wave a token; lane l has the experts l, l + 64, ..
-template <typename T, int PER>
-__global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
-    constexpr double kNone = -__builtin_inf();
-    const int lane = threadIdx.x % kWave;
-    const int64_t t = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    if (t >= p.tokens) return;
-    double s[PER], c[PER];
-    float l[PER];
-    bool bad = false;
-    float most = -__builtin_inff();
+// The largest of the wave, to all lanes: six exchanges in registers.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_with(float v) {
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, ROWS, 0xF, false)));
+}
+__device__ __forceinline__ float top_of_wave(float v) {
+    v = max_with<0x111, 0xF>(v);      // from 1, 2, 4 and 8 lanes before, within 16
+    v = max_with<0x112, 0xF>(v);
+    v = max_with<0x114, 0xF>(v);
+    v = max_with<0x118, 0xF>(v);
+    v = max_with<0x142, 0xA>(v);      // from the last lane of the 16, and of the 32, before
+    v = max_with<0x143, 0xC>(v);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// The two largest of a lane and of the one that it exchanges with.
+template <typename Swap>
+__device__ __forceinline__ void merge_two(float& one, float& two, Swap swap) {
+    const float o1 = swap(one), o2 = swap(two);
+    two = fmaxf(fmaxf(two, o2), fminf(one, o1));
+    one = fmaxf(one, o1);
+}
+template <int CTRL>
+__device__ __forceinline__ float swapped(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
+
+// Neighbouring logits, -infinity behind the last.
+template <int PER>
+__device__ __forceinline__ void load_logits(const float* p, int left, float (&l)[PER]) {
+    if (PER >= 4 && left >= PER) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = i * kWave + lane;
-        l[i] = e < p.experts ? logit_at(logits + t * p.ld + e) : -__builtin_inff();
-        bad |= l[i] != l[i] || (!p.sigmoid && l[i] == __builtin_inff());
-        most = fmaxf(most, l[i]);
-    }
-    if (p.sigmoid) {
+        for (int i = 0; i < PER; i += 4) {
+            const u32x4 v = *reinterpret_cast<const u32x4_a4*>(p + i);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) s[i] = 1.0 / (1.0 + exp(-(double)l[i]));
+            for (int j = 0; j < 4 && i + j < PER; ++j) l[i + j] = bits_as<float>(v[j]);
+        }
     } else {
 #pragma unroll
-        for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        for (int i = 0; i < PER; ++i) l[i] = i < left ? p[i] : -__builtin_inff();
+    }
+}
+template <int PER>
+__device__ __forceinline__ void load_logits(const uint16_t* p, int left, float (&l)[PER]) {
+    if (PER >= 4 && left >= PER) {
+#pragma unroll
+        for (int i = 0; i < PER; i += 4) {
+            const u32x2 v = *reinterpret_cast<const u32x2_a2*>(p + i);
+#pragma unroll
+            for (int j = 0; j < 4 && i + j < PER; ++j) l[i + j] = (j & 1) ? bf16_hi(v[j / 2]) : bf16_lo(v[j / 2]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) l[i] = i < left ? logit_at(p + i) : -__builtin_inff();
+    }
+}
+
+// The choice in 64 bits: lane j has the expert of place j, -1 where there is none.
+template <int PER>
+__device__ __forceinline__ int choose_exactly(const RouteArgs& p, const float (&l)[PER], float most, const float* bias, int lane) {
+    constexpr double kNone = -__builtin_inf();
+    double c[PER];
+    if (p.sigmoid) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = 1.0 / (1.0 + exp(-(double)l[i]));
+    } else {
         double sum = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            s[i] = l[i] > -__builtin_inff() ? exp((double)l[i] - (double)most) : 0.0;
-            sum += s[i];
+            c[i] = l[i] > -__builtin_inff() ? exp((double)l[i] - (double)most) : 0.0;
+            sum += c[i];
         }
 #pragma unroll
         for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) s[i] = sum > 0 ? s[i] / sum : 0.0;
+        for (int i = 0; i < PER; ++i) c[i] = sum > 0 ? c[i] / sum : 0.0;
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int e = i * kWave + lane;
-        c[i] = kNone;
-        if (e < p.experts && l[i] > -__builtin_inff()) c[i] = p.bias ? s[i] + (double)p.bias[e] : s[i];
-        if (c[i] != c[i]) bad = true;
+        const int e = lane * PER + i;
+        if (!(e < p.experts && l[i] > -__builtin_inff())) c[i] = kNone;
+        else if (bias) c[i] += (double)bias[e];
     }
-    bad = __any(bad);
-    if (p.groups > 1 && !bad) {
+    if (p.groups > 1) {
         double total = kNone;                 // of group `lane`
         for (int g = 0; g < p.groups; ++g) {
             double one = kNone, two = kNone;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int e = i * kWave + lane;
-                if (e / p.per_group != g) continue;
+                if ((lane * PER + i) / p.per_group != g) continue;
                 two = fmax(two, fmin(one, c[i]));
                 one = fmax(one, c[i]);
             }
@@ -106,11 +143,10 @@ __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int g = (i * kWave + lane) / p.per_group;
+            const int g = (lane * PER + i) / p.per_group;
             if (g >= p.groups || !(stay >> g & 1)) c[i] = kNone;
         }
     }
-    double mine = 0;                          // lane j: the score of place j
     int expert = -1;
     for (int j = 0; j < p.picks; ++j) {
         double best = kNone;
@@ -119,30 +155,158 @@ __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
         for (int i = 0; i < PER; ++i)
             if (c[i] > best) {
                 best = c[i];
-                at = i * kWave + lane;
+                at = lane * PER + i;
             }
         best_of_wave(best, at);
-        double score = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (i * kWave + lane == at) {
-                score = s[i];
-                c[i] = kNone;
+            if (lane * PER + i == at) c[i] = kNone;
+        if (lane == j && best > kNone) expert = at;
+    }
+    return expert;
+}
+
+// A wave a token; lane l has the experts l * PER .. of it.  The choice is made in 32 bits, by the logits themselves where no bias counts (the scores rise with
+// them), otherwise by scores that are off by less than 2^-19 (of 1, or of the largest c).  Wherever two c that decide are nearer to one another than that, or logits
+// than 64 bits keep their scores apart, the wave chooses again in 64 bits.  What bounds it are vector instructions, some 25 for a place.
+template <typename T, int PER>
+__global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
+    constexpr float kNone = -__builtin_inff();
+    const int lane = threadIdx.x % kWave;
+    const int64_t t = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    if (t >= p.tokens) return;
+    const T* row = logits + t * p.ld;
+    const int first = lane * PER;
+    float l[PER], c[PER];
+    load_logits<PER>(row + first, p.experts - first, l);
+    bool bad = false;
+    float most = kNone;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        bad |= l[i] != l[i] || (!p.sigmoid && l[i] == __builtin_inff());
+        most = fmaxf(most, l[i]);
+    }
+    most = top_of_wave(most);
+    const bool by_score = p.bias || p.groups > 1;
+    if (by_score) {
+        if (p.sigmoid) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
+        } else {
+            float sum = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                c[i] = l[i] > kNone ? __expf(l[i] - most) : 0.f;
+                sum += c[i];
             }
-        const bool any = best > kNone;
-        score = __shfl(score, at % kWave);
-        if (lane == j && any) {
-            mine = score;
-            expert = at;
+#pragma unroll
+            for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+            const float over = sum > 0 ? __builtin_amdgcn_rcpf(sum) : 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] *= over;
         }
     }
-    double sum = mine;
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
+    for (int i = 0; i < PER; ++i) {
+        if (p.bias && first + i < p.experts) c[i] += p.bias[first + i];
+        bad |= by_score && first + i < p.experts && l[i] > kNone && c[i] != c[i];
+        if (!by_score || !(l[i] > kNone)) c[i] = l[i] > kNone ? l[i] : kNone;
+    }
+    bad = __any(bad);
+    // what c may be off by, and whether the wave has to choose again
+    float top = kNone;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) top = fmaxf(top, fabsf(c[i]) < __builtin_inff() ? fabsf(c[i]) : 0.f);
+    const float off = by_score ? fmaxf(1.f, top_of_wave(top)) * 0x1p-19f : 0.f;
+    bool again = false;
+    if (p.groups > 1) {
+        float one = kNone, two = kNone, total;
+        const int lanes = p.per_group / PER;
+        uint64_t mine = ~(uint64_t)0;         // lanes of this lane's group
+        if (lanes * PER == p.per_group && (lanes & (lanes - 1)) == 0) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                two = fmaxf(two, fminf(one, c[i]));
+                one = fmaxf(one, c[i]);
+            }
+            if (lanes >= 2) merge_two(one, two, swapped<0xB1>);
+            if (lanes >= 4) merge_two(one, two, swapped<0x4E>);
+            if (lanes >= 8) merge_two(one, two, swapped<0x141>);
+            if (lanes >= 16) merge_two(one, two, swapped<0x140>);
+            if (lanes >= 32) merge_two(one, two, [](float v) { return __shfl_xor(v, 16); });
+            total = two == kNone ? one : one + two;
+            float before = __builtin_inff();
+            uint64_t stay = 0;
+            for (int n = 0; n <= p.top_groups && n < p.groups; ++n) {
+                const bool left = first < p.experts && !(stay >> lane & 1);
+                const float best = top_of_wave(left ? total : kNone);
+                const uint64_t at = __ballot(left && total == best);
+                if (n == p.top_groups) {
+                    again |= best > kNone && !(before - best > 4 * off);
+                    break;
+                }
+                if (at) stay |= (lanes == kWave ? ~(uint64_t)0 : ((uint64_t)1 << lanes) - 1) << (__builtin_ctzll(at) / lanes * lanes);
+                before = best;
+            }
+            if (!(stay >> lane & 1)) mine = 0;
+        } else {
+            again = true;                     // groups that do not lie in whole lanes
+        }
+        if (!mine) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = kNone;
+        }
+        if (!p.bias) {                        // the logits of those that stay
+#pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = c[i] > kNone ? l[i] : kNone;
+        }
+    }
+    int expert = -1;
+    float before = __builtin_inff();
+    for (int j = 0; j <= p.picks && !again; ++j) {
+        float m = kNone;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) m = fmaxf(m, c[i]);
+        const float best = top_of_wave(m);
+        if (best == kNone) break;
+        if (p.bias) again = !(before - best > 2 * off);
+        else again = (before > best && before - best < 0x1p-36f) || best < (p.sigmoid ? -600.f : most - 600.f) || (p.sigmoid && best > 10.f);
+        before = best;
+        if (j == p.picks) break;
+        const int owner = __builtin_ctzll(__ballot(m == best));
+        int at = 0;
+#pragma unroll
+        for (int i = PER - 1; i >= 0; --i) at = c[i] == best ? i : at;
+        at = __builtin_amdgcn_readlane(at, owner);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = lane == owner && i == at ? kNone : c[i];
+        expert = lane == j ? owner * PER + at : expert;
+    }
+    if (again && !bad) expert = choose_exactly<PER>(p, l, most, p.bias, lane);
+    // the weights of the places in 64 bits
+    const bool there = expert >= 0;
+    const double x = there ? (double)logit_at(row + expert) : 0.0;
+    double s = 0, total = 1;
+    if (p.sigmoid) {
+        s = 1.0 / (1.0 + exp(-x));
+    } else {
+        s = exp(x - (there ? (double)most : 0.0));
+        if (!p.renormalize) {
+            total = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) total += l[i] > kNone ? exp((double)l[i] - (double)most) : 0.0;
+#pragma unroll
+            for (int d = 1; d < kWave; d *= 2) total += __shfl_xor(total, d);
+        }
+    }
+    if (!there) s = 0;
+    if (p.renormalize) {                      // (places are lanes 0 .. 31)
+        total = s;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) total += __shfl_xor(total, d);
+    }
     if (lane < p.picks) {
-        double w = mine * p.scale;
-        if (p.renormalize) w = sum > 0 ? mine / sum * p.scale : 0.0;
-        p.weights[t * p.picks + lane] = bad ? __builtin_nanf("") : (float)w;
+        p.weights[t * p.picks + lane] = bad ? __builtin_nanf("") : (float)(total > 0 ? s / total * p.scale : 0.0);
         p.chosen[t * p.picks + lane] = bad ? -1 : expert;
     }
 }
