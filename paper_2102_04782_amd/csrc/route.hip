@@ -35,30 +35,38 @@ __device__ __forceinline__ void best_of_wave(double& c, int& at) {
     }
 }
 
+// Values as whole numbers of the same order, for one instruction a comparison; kNoKey is below all of them (it is a NaN's).
+constexpr int kNoKey = (int)0x80000000;
+__device__ __forceinline__ int key_of(float v) {
+    const int b = __float_as_int(v);
+    return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float of_key(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF)); }
+
 // The largest of the wave, to all lanes: six exchanges in registers.
 template <int CTRL, int ROWS>
-__device__ __forceinline__ float max_with(float v) {
-    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, ROWS, 0xF, false)));
+__device__ __forceinline__ int max_with(int v) {
+    return max(v, __builtin_amdgcn_update_dpp(kNoKey, v, CTRL, ROWS, 0xF, false));
 }
-__device__ __forceinline__ float top_of_wave(float v) {
+__device__ __forceinline__ int top_of_wave(int v) {
     v = max_with<0x111, 0xF>(v);      // from 1, 2, 4 and 8 lanes before, within 16
     v = max_with<0x112, 0xF>(v);
     v = max_with<0x114, 0xF>(v);
     v = max_with<0x118, 0xF>(v);
     v = max_with<0x142, 0xA>(v);      // from the last lane of the 16, and of the 32, before
     v = max_with<0x143, 0xC>(v);
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+    return __builtin_amdgcn_readlane(v, 63);
 }
 
 // The two largest of a lane and of the one that it exchanges with.
 template <typename Swap>
-__device__ __forceinline__ void merge_two(float& one, float& two, Swap swap) {
-    const float o1 = swap(one), o2 = swap(two);
-    two = fmaxf(fmaxf(two, o2), fminf(one, o1));
-    one = fmaxf(one, o1);
+__device__ __forceinline__ void merge_two(int& one, int& two, Swap swap) {
+    const int o1 = swap(one), o2 = swap(two);
+    two = max(max(two, o2), min(one, o1));
+    one = max(one, o1);
 }
 template <int CTRL>
-__device__ __forceinline__ float swapped(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ int swapped(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true); }
 
 // Neighbouring logits, -infinity behind the last.
 template <int PER>
@@ -177,7 +185,7 @@ __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
     if (t >= p.tokens) return;
     const T* row = logits + t * p.ld;
     const int first = lane * PER;
-    float l[PER], c[PER];
+    float l[PER];
     load_logits<PER>(row + first, p.experts - first, l);
     bool bad = false;
     float most = kNone;
@@ -186,101 +194,142 @@ __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
         bad |= l[i] != l[i] || (!p.sigmoid && l[i] == __builtin_inff());
         most = fmaxf(most, l[i]);
     }
-    most = top_of_wave(most);
+    most = of_key(top_of_wave(key_of(most)));
     const bool by_score = p.bias || p.groups > 1;
+    int c[PER];                               // as keys
+    float off = 0.f;                          // what a c may be off by
     if (by_score) {
+        float v[PER], top = 1.f;
         if (p.sigmoid) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) c[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
+            for (int i = 0; i < PER; ++i) v[i] = __builtin_amdgcn_rcpf(1.f + __expf(-l[i]));
         } else {
             float sum = 0;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                c[i] = l[i] > kNone ? __expf(l[i] - most) : 0.f;
-                sum += c[i];
+                v[i] = l[i] > kNone ? __expf(l[i] - most) : 0.f;
+                sum += v[i];
             }
 #pragma unroll
             for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d);
             const float over = sum > 0 ? __builtin_amdgcn_rcpf(sum) : 0.f;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) c[i] *= over;
+            for (int i = 0; i < PER; ++i) v[i] *= over;
         }
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (p.bias && first + i < p.experts) c[i] += p.bias[first + i];
-        bad |= by_score && first + i < p.experts && l[i] > kNone && c[i] != c[i];
-        if (!by_score || !(l[i] > kNone)) c[i] = l[i] > kNone ? l[i] : kNone;
-    }
-    bad = __any(bad);
-    // what c may be off by, and whether the wave has to choose again
-    float top = kNone;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) top = fmaxf(top, fabsf(c[i]) < __builtin_inff() ? fabsf(c[i]) : 0.f);
-    const float off = by_score ? fmaxf(1.f, top_of_wave(top)) * 0x1p-19f : 0.f;
-    bool again = false;
-    if (p.groups > 1) {
-        float one = kNone, two = kNone, total;
-        const int lanes = p.per_group / PER;
-        uint64_t mine = ~(uint64_t)0;         // lanes of this lane's group
-        if (lanes * PER == p.per_group && (lanes & (lanes - 1)) == 0) {
+        if (p.bias) {
+            float b[PER];
+            load_logits<PER>(p.bias + first, p.experts - first, b);
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                two = fmaxf(two, fminf(one, c[i]));
-                one = fmaxf(one, c[i]);
+                v[i] += b[i];
+                top = fmaxf(top, fabsf(v[i]) < __builtin_inff() ? fabsf(v[i]) : 0.f);
+                bad |= l[i] > kNone && v[i] != v[i];
+            }
+            top = of_key(top_of_wave(key_of(top)));
+        }
+        off = top * 0x1p-19f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = l[i] > kNone && v[i] > kNone ? key_of(v[i]) : kNoKey;
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = l[i] > kNone ? key_of(l[i]) : kNoKey;
+    }
+    bad = __any(bad);
+    bool again = false;                       // whether the wave has to choose again
+    if (p.groups > 1) {
+        const int lanes = p.per_group / PER;
+        if (lanes * PER == p.per_group && (lanes & (lanes - 1)) == 0) {
+            int one = kNoKey, two = kNoKey;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                two = max(two, min(one, c[i]));
+                one = max(one, c[i]);
             }
             if (lanes >= 2) merge_two(one, two, swapped<0xB1>);
             if (lanes >= 4) merge_two(one, two, swapped<0x4E>);
             if (lanes >= 8) merge_two(one, two, swapped<0x141>);
             if (lanes >= 16) merge_two(one, two, swapped<0x140>);
-            if (lanes >= 32) merge_two(one, two, [](float v) { return __shfl_xor(v, 16); });
-            total = two == kNone ? one : one + two;
+            if (lanes >= 32) merge_two(one, two, [](int v) { return __shfl_xor(v, 16); });
+            int total = two == kNoKey ? one : key_of(of_key(one) + of_key(two));
             float before = __builtin_inff();
             uint64_t stay = 0;
             for (int n = 0; n <= p.top_groups && n < p.groups; ++n) {
-                const bool left = first < p.experts && !(stay >> lane & 1);
-                const float best = top_of_wave(left ? total : kNone);
-                const uint64_t at = __ballot(left && total == best);
+                const int best = top_of_wave(total);
                 if (n == p.top_groups) {
-                    again |= best > kNone && !(before - best > 4 * off);
+                    again |= best != kNoKey && !(before - of_key(best) > 4 * off);
                     break;
                 }
-                if (at) stay |= (lanes == kWave ? ~(uint64_t)0 : ((uint64_t)1 << lanes) - 1) << (__builtin_ctzll(at) / lanes * lanes);
-                before = best;
+                const uint64_t at = __ballot(total == best);
+                if (best != kNoKey) {
+                    const uint64_t these = (lanes == kWave ? ~(uint64_t)0 : ((uint64_t)1 << lanes) - 1) << (__builtin_ctzll(at) / lanes * lanes);
+                    stay |= these;
+                    if (these >> lane & 1) total = kNoKey;
+                    before = of_key(best);
+                }
             }
-            if (!(stay >> lane & 1)) mine = 0;
+            const bool in = stay >> lane & 1;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = in ? (p.bias || c[i] == kNoKey) ? c[i] : key_of(l[i]) : kNoKey;      // (no bias: the logits of those that stay)
         } else {
             again = true;                     // groups that do not lie in whole lanes
         }
-        if (!mine) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i) c[i] = kNone;
-        }
-        if (!p.bias) {                        // the logits of those that stay
-#pragma unroll
-            for (int i = 0; i < PER; ++i) c[i] = c[i] > kNone ? l[i] : kNone;
-        }
     }
     int expert = -1;
-    float before = __builtin_inff();
-    for (int j = 0; j <= p.picks && !again; ++j) {
-        float m = kNone;
+    if (!again) {
+        // a lane's own in descending order, equals in the order of their indices, which are four bits each of `at`
+        constexpr bool kSorted = PER <= 4;
+        uint32_t at = 0x3210u;
+        if constexpr (kSorted) {
+            int ix[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) m = fmaxf(m, c[i]);
-        const float best = top_of_wave(m);
-        if (best == kNone) break;
-        if (p.bias) again = !(before - best > 2 * off);
-        else again = (before > best && before - best < 0x1p-36f) || best < (p.sigmoid ? -600.f : most - 600.f) || (p.sigmoid && best > 10.f);
-        before = best;
-        if (j == p.picks) break;
-        const int owner = __builtin_ctzll(__ballot(m == best));
-        int at = 0;
+            for (int i = 0; i < PER; ++i) ix[i] = i;
 #pragma unroll
-        for (int i = PER - 1; i >= 0; --i) at = c[i] == best ? i : at;
-        at = __builtin_amdgcn_readlane(at, owner);
+            for (int n = 0; n < PER - 1; ++n)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) c[i] = lane == owner && i == at ? kNone : c[i];
-        expert = lane == j ? owner * PER + at : expert;
+                for (int i = 0; i < PER - 1 - n; ++i) {
+                    const bool swap = c[i] < c[i + 1];
+                    const int ci = c[i], xi = ix[i];
+                    c[i] = swap ? c[i + 1] : ci;
+                    ix[i] = swap ? ix[i + 1] : xi;
+                    c[i + 1] = swap ? ci : c[i + 1];
+                    ix[i + 1] = swap ? xi : ix[i + 1];
+                }
+            at = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) at |= (uint32_t)ix[i] << (4 * i);
+        }
+        float before = __builtin_inff();
+        for (int j = 0; j <= p.picks; ++j) {
+            int m = c[0];
+            if constexpr (!kSorted) {
+#pragma unroll
+                for (int i = 1; i < PER; ++i) m = max(m, c[i]);
+            }
+            const int key = top_of_wave(m);
+            if (key == kNoKey) break;
+            const float best = of_key(key);
+            if (p.bias) again |= !(before - best > 2 * off);
+            else again |= (before > best && before - best < 0x1p-36f) || best < (p.sigmoid ? -600.f : most - 600.f) || (p.sigmoid && best > 10.f);
+            before = best;
+            if (j == p.picks) break;
+            const int owner = __builtin_ctzll(__ballot(m == key));
+            const bool mine = lane == owner;
+            int which;
+            if constexpr (kSorted) {
+                which = __builtin_amdgcn_readlane((int)at, owner) & 15;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) c[i] = mine ? (i + 1 < PER ? c[i + 1 < PER ? i + 1 : i] : kNoKey) : c[i];
+                at = mine ? at >> 4 : at;
+            } else {
+                int first_of = 0;
+#pragma unroll
+                for (int i = PER - 1; i >= 0; --i) first_of = c[i] == key ? i : first_of;
+                which = __builtin_amdgcn_readlane(first_of, owner);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) c[i] = mine && i == which ? kNoKey : c[i];
+            }
+            expert = lane == j ? owner * PER + which : expert;
+        }
     }
     if (again && !bad) expert = choose_exactly<PER>(p, l, most, p.bias, lane);
     // the weights of the places in 64 bits
@@ -433,33 +482,38 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_count(PlanArgs p) {
     for (int e = threadIdx.x; e < p.experts; e += kPlanThreads) p.per_block[(int64_t)blockIdx.x * p.experts + e] = n[e];
 }
 
-// Sums over 1024 threads of what stands before each of them; the total to all.
-__device__ __forceinline__ int before_me(int v, int* per_wave, int& total) {
+// Of four values of each of 1024 threads: the sums of what stands before each thread, and the totals, to all.
+__device__ __forceinline__ void before_me(const int (&v)[4], int (*per_wave)[kPlanWaves], int (&first)[4], int (&total)[4]) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    int sum = v;
+    int sum[4];
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const int o = __shfl_up(sum, d);
-        if (lane >= d) sum += o;
-    }
-    if (lane == kWave - 1) per_wave[wave] = sum;
-    __syncthreads();
-    int first = 0;
-    total = 0;
+    for (int k = 0; k < 4; ++k) {
+        sum[k] = v[k];
 #pragma unroll
-    for (int w = 0; w < kPlanWaves; ++w) {
-        const int n = per_wave[w];
-        first += w < wave ? n : 0;
-        total += n;
+        for (int d = 1; d < kWave; d *= 2) {
+            const int o = __shfl_up(sum[k], d);
+            if (lane >= d) sum[k] += o;
+        }
+        if (lane == kWave - 1) per_wave[k][wave] = sum[k];
     }
     __syncthreads();
-    return first + sum - v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        first[k] = sum[k] - v[k];
+        total[k] = 0;
+#pragma unroll
+        for (int w = 0; w < kPlanWaves; ++w) {
+            const int n = per_wave[k][w];
+            first[k] += w < wave ? n : 0;
+            total[k] += n;
+        }
+    }
 }
 
 __global__ __launch_bounds__(kPlanThreads) void k_plan_place(PlanArgs p) {
     __shared__ int next[kMaxExperts];                       // the row of an expert's next slot
-    __shared__ uint16_t ranks[kPlanWaves][kMaxExperts];     // slots of an expert in a wave of this round
-    __shared__ int per_wave[kPlanWaves];
+    __shared__ __attribute__((aligned(16))) uint16_t ranks[kPlanWaves][kMaxExperts];     // slots of an expert in a wave of this round
+    __shared__ int per_wave[4][kPlanWaves];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, e0 = threadIdx.x;
     int before = 0, all = 0;                                // slots of expert e0 in the runs before this one, and in all
     if (p.blocks == 1) {
@@ -472,37 +526,50 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_place(PlanArgs p) {
         }
         __syncthreads();
         all = next[e0];
-    } else if (e0 < p.experts) {
-        for (int b = 0; b < p.blocks; ++b) {
-            const int n = p.per_block[(int64_t)b * p.experts + e0];
-            all += n;
-            before += b < (int)blockIdx.x ? n : 0;
+    } else {
+        // the runs shared among as many threads of an expert as there are, sixteen asked for at a time
+        int* sums = reinterpret_cast<int*>(&ranks[0][0]);   // [part][all, before][expert]
+        const int wide = (p.experts + kWave - 1) / kWave * kWave, parts = kPlanThreads / wide, part = threadIdx.x / wide, e = threadIdx.x - part * wide;
+        if (part < parts && e < p.experts) {
+            int a = 0, f = 0;
+            for (int b0 = part; b0 < p.blocks; b0 += 16 * parts) {
+                int n[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) n[i] = b0 + i * parts < p.blocks ? p.per_block[(int64_t)(b0 + i * parts) * p.experts + e] : 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    a += n[i];
+                    f += b0 + i * parts < (int)blockIdx.x ? n[i] : 0;
+                }
+            }
+            sums[(part * 2) * wide + e] = a;
+            sums[(part * 2 + 1) * wide + e] = f;
         }
-    }
-    int total;
-    const int first = before_me(all, per_wave, total);
-    if (e0 < p.experts) next[e0] = first + before;
-    if (blockIdx.x == 0) {
-        int t256, t128, t64;
-        const int b256 = before_me((all + 255) / 256, per_wave, t256), b128 = before_me((all + 127) / 128, per_wave, t128),
-                  b64 = before_me((all + 63) / 64, per_wave, t64);
-        const int pitch = p.experts + 1;
+        __syncthreads();
         if (e0 < p.experts) {
-            p.counts[e0] = all;
-            p.table[kTableRows * pitch + e0] = first;
-            p.table[kTable256 * pitch + e0] = b256;
-            p.table[kTable128 * pitch + e0] = b128;
-            p.table[kTable64 * pitch + e0] = b64;
+            for (int i = 0; i < parts; ++i) {
+                all += sums[(i * 2) * wide + e0];
+                before += sums[(i * 2 + 1) * wide + e0];
+            }
         }
-        if (e0 == 0) {
-            p.table[kTableRows * pitch + p.experts] = total;
-            p.table[kTable256 * pitch + p.experts] = t256;
-            p.table[kTable128 * pitch + p.experts] = t128;
-            p.table[kTable64 * pitch + p.experts] = t64;
+        __syncthreads();
+    }
+    int first[4], totals[4];
+    before_me({all, (all + 255) / 256, (all + 127) / 128, (all + 63) / 64}, per_wave, first, totals);
+    static_assert(kTableRows == 0 && kTable256 == 1 && kTable128 == 2 && kTable64 == 3, "in this order");
+    const int total = totals[0];
+    if (e0 < p.experts) next[e0] = first[0] + before;
+    if (blockIdx.x == 0) {
+        if (e0 < p.experts) p.counts[e0] = all;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (e0 < p.experts) p.table[k * (p.experts + 1) + e0] = first[k];
+            if (e0 == 0) p.table[k * (p.experts + 1) + p.experts] = totals[k];
         }
     }
     for (int r = 0; r < p.rounds; ++r) {
-        for (int i = threadIdx.x; i < kPlanWaves * p.experts; i += kPlanThreads) ranks[i / p.experts][i % p.experts] = 0;
+        for (int w = threadIdx.x / 128; w < kPlanWaves; w += kPlanThreads / 128)          // 16 bytes a thread
+            if (threadIdx.x % 128 * 8 < (unsigned)p.experts) *reinterpret_cast<u32x4*>(&ranks[w][threadIdx.x % 128 * 8]) = u32x4{0, 0, 0, 0};
         __syncthreads();
         const int64_t slot = ((int64_t)blockIdx.x * p.rounds + r) * kPlanThreads + threadIdx.x;
         const int e = slot_expert(p, slot);
