@@ -74,12 +74,18 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
     const int64_t mat = kWeights ? rt / p.row_tiles : 0, rb = kWeights ? rt - mat * p.row_tiles : rt;   // rb: block along the columns
     int64_t r0 = rb * 128;
     int64_t rows = p.rows;                                // rows of src, or of the order, that this tile may take, from 0 on
+    bool ordered = true;
     if constexpr (kExperts) {
         const int32_t* tiles = p.table + kTable128 * (p.experts + 1);
-        if (rt >= tiles[p.experts]) return;
-        const int e = expert_of_tile(tiles, p.experts, (int)rt, lane);
-        r0 = p.table[e] + (rt - tiles[e]) * 128;
-        rows = p.table[e + 1];
+        if (rt < tiles[p.experts]) {
+            const int e = expert_of_tile(tiles, p.experts, (int)rt, lane);
+            r0 = p.table[e] + (rt - tiles[e]) * 128;
+            rows = p.table[e + 1];
+        } else {                                          // by rows only: those behind the last of the order
+            r0 = p.table[p.experts] + (rt - tiles[p.experts]) * 128;
+            if (!BYROWS || r0 >= rows) return;
+            ordered = false;
+        }
     }
     Eight<T> v[4];
 #pragma unroll
@@ -130,9 +136,9 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
     if constexpr (BYROWS) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t r = rb * 128 + quad * 4 + i, at = mat * p.rows + r;
+            const int64_t r = r0 + quad * 4 + i, at = mat * p.rows + r;
             const uint32_t byte = kWeights ? whole : fp8_scale_byte(max16(top_of(v[i])));
-            if (r >= p.rows) continue;
+            if (r >= rows) continue;
             *reinterpret_cast<u32x2*>(p.r.codes + at * p.r.pitch + c) = codes8(v[i], byte);
             if (piece == 0) {
                 const int64_t cb = c0 / 128;
@@ -144,6 +150,7 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
         }
     }
     if constexpr (BYCOLS) {
+        if (!ordered) return;
         uint32_t bytes[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -178,7 +185,7 @@ template <typename T, Tiles KIND>
 daq_status launch_tiles(const T* src, TileArgs p, int64_t tiles, hipStream_t st) {
     const dim3 grid((unsigned)(tiles * p.col_tiles));
     const bool r = p.r.codes != nullptr, c = p.c.codes != nullptr;
-    const auto kernel = KIND == Tiles::kExperts || !r ? k_fp8_tiles<T, KIND, false, true> : c ? k_fp8_tiles<T, KIND == Tiles::kExperts ? Tiles::kBlocks : KIND, true, true> : k_fp8_tiles<T, KIND == Tiles::kExperts ? Tiles::kBlocks : KIND, true, false>;
+    const auto kernel = !r ? k_fp8_tiles<T, KIND, false, true> : c || KIND == Tiles::kExperts ? k_fp8_tiles<T, KIND, true, true> : k_fp8_tiles<T, KIND == Tiles::kExperts ? Tiles::kBlocks : KIND, true, false>;
     DAQ_LAUNCH("fp8_tiles", st, hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, src, p));
     return DAQ_OK;
 }
@@ -299,11 +306,14 @@ extern "C" daq_status daq_experts_quantize(const daq_experts* plan, const void* 
     rc = source_check(src, dtype, cols, ld);
     if (rc != DAQ_OK) return rc;
     const int64_t tiles = columns / 128, col_tiles = ceil_div(cols, 128);
-    if ((by_rows && !fp8_rows_grid_ok(rows, cols)) || (by_columns && !grid_ok(tiles * col_tiles, 512))) return DAQ_ERR_UNSUPPORTED;
+    if ((by_rows && !fp8_rows_grid_ok(rows, cols)) || (by_columns && !grid_ok((tiles + 1) * col_tiles, 512))) return DAQ_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
-    if (by_rows) rc = fp8_quantize_rows(src, dtype, rows, cols, ld, by_rows, st);
+    // rows in their order are read once for both; those that several experts take are quantized by rows on their own.  (One tile more than the order needs at
+    // the most: with those that it leaves over they hold the rows behind its last.)
+    const bool both = by_rows && by_columns && sorted;
+    if (by_rows && !both) rc = fp8_quantize_rows(src, dtype, rows, cols, ld, by_rows, st);
     if (rc != DAQ_OK || !by_columns) return rc;
-    TileArgs p{ld, 0, rows, cols, (int)col_tiles, tiles, {}, packed(by_columns, cols, columns), plan->table, plan->rows, plan->experts, sorted ? 0 : plan->picks};
-    return dtype == DAQ_BF16 ? launch_tiles<uint16_t, Tiles::kExperts>(static_cast<const uint16_t*>(src), p, tiles, st)
-                             : launch_tiles<float, Tiles::kExperts>(static_cast<const float*>(src), p, tiles, st);
+    TileArgs p{ld, 0, rows, cols, (int)col_tiles, tiles, packed(both ? by_rows : nullptr, rows, cols), packed(by_columns, cols, columns), plan->table, plan->rows, plan->experts, sorted ? 0 : plan->picks};
+    return dtype == DAQ_BF16 ? launch_tiles<uint16_t, Tiles::kExperts>(static_cast<const uint16_t*>(src), p, tiles + both, st)
+                             : launch_tiles<float, Tiles::kExperts>(static_cast<const float*>(src), p, tiles + both, st);
 }
