@@ -1,7 +1,7 @@
 // Products of 8-bit floating point matrices for few rows of A: what counts is the way of the weights.
 //
 // A workgroup's eight waves share the blocks of 128 of the summed axis among 1, 2, 4 or 8 of them, four blocks or more each where there are so many, and
-// take 16 columns of D with each such set of waves, and up to 64 rows; what a wave needs of four blocks is asked for at once, and their sums meet in LDS.
+// take 16 columns of D with each such set of waves, and up to 64 rows; what a wave needs of four blocks (three, in bfloat16) is asked for at once, and their sums meet in LDS.
 // The matrix instruction is that of 16 x 16 x 128 (a block), in bfloat16 four of 16 x 16 x 32: lane l has row l % 16 and the 16-byte pieces l / 16 and
 // l / 16 + 4 of a block, so that a load takes 64 bytes in a row of every row.  Where the rows are few they are quantized by every workgroup itself, into
 // LDS, while its first weights are on their way: a launch less.
@@ -12,11 +12,12 @@ namespace daq {
 namespace {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
-constexpr int kFewWaves = 8, kAhead = 4;
+constexpr int kFewWaves = 8;
 
 template <typename X, bool EXACT, Of OF>
 __global__ __launch_bounds__(64 * kFewWaves, 4) void k_fp8_few(ProductArgs p, const X* x, int64_t ldx, int64_t K, int share) {
     constexpr bool kRaw = !std::is_void_v<X>;
+    constexpr int kAhead = EXACT ? 3 : 4;                // (conversions take registers)
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     __shared__ int taken[64];                            // rows of A of this tile
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r = lane % 16, q = lane / 16;
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void k_fp8_few(ProductArgs p, co
 // Waves that share the summed axis: four blocks each, but more of them where the columns do not fill the CUs.
 int few_share(const ProductArgs& p, int64_t tiles) {
     int share = 8;
-    while (share > 1 && p.stages <= share * kAhead / 2 && ceil_div(p.N, 16 * (kFewWaves / share)) * tiles >= 512) share /= 2;
+    while (share > 1 && p.stages <= share * 2 && ceil_div(p.N, 16 * (kFewWaves / share)) * tiles >= 512) share /= 2;
     return share;
 }
 
