@@ -950,7 +950,7 @@ class Fp8:
     cols: int
 
 
-@dataclass
+@dataclass(frozen=True)
 class Plan:
     """The order of a batch's rows by expert (daq_experts_plan)."""
     counts: torch.Tensor    # int32 [experts]
@@ -960,6 +960,13 @@ class Plan:
     tokens: int
     picks: int
     experts: int
+
+    def __post_init__(self):
+        shapes = ((self.experts,), (4, self.experts + 1), (self.tokens * self.picks,), (self.tokens, self.picks))
+        for t, shape in zip((self.counts, self.table, self.rows, self.place), shapes):
+            assert t.dtype == torch.int32 and t.shape == shape and t.is_contiguous() and t.device == self.table.device
+        # what the calls hand on, made once: the tensors of a plan are not exchanged
+        object.__setattr__(self, "handed_on", Experts(self.tokens, self.picks, self.experts, self.table.data_ptr(), self.rows.data_ptr(), self.place.data_ptr()))
 
 
 def layout_fp8(rows: int, cols: int) -> Fp8Layout:
@@ -988,7 +995,7 @@ def _codes(q: Fp8) -> int:
 
 def _dense(t: torch.Tensor, dtype, *shape) -> int:
     _here(t)
-    assert t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous()
+    assert t.dtype == dtype and t.shape == shape and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -1098,6 +1105,11 @@ def fp8_linear(x: torch.Tensor, w: Fp8, dtype=None, out: Optional[torch.Tensor] 
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _route_opts(*fields):      # (read only)
+    return RouteOpts(*fields)
+
+
 def route(logits: torch.Tensor, picks: int, scores=SCORES_SOFTMAX, bias: Optional[torch.Tensor] = None, groups: int = 1, top_groups: int = 1,
           renormalize: bool = True, scale: float = 1.0, out=None, stream=None):
     """daq_route: (weights fp32 [tokens, picks], experts int32 [tokens, picks]) for ``logits`` [tokens, experts]; ``out``: such a pair."""
@@ -1106,7 +1118,7 @@ def route(logits: torch.Tensor, picks: int, scores=SCORES_SOFTMAX, bias: Optiona
     if out is None:
         out = _new(stream, (tokens, picks), torch.float32, logits), _new(stream, (tokens, picks), torch.int32, logits)
     weights, chosen = out
-    opts = RouteOpts(scores, picks, groups, top_groups, int(renormalize), scale)
+    opts = _route_opts(scores, picks, groups, top_groups, bool(renormalize), scale)
     _check(lib().daq_route(tokens, experts, logits.data_ptr(), code, ld, pb, C.byref(opts), _dense(weights, torch.float32, tokens, picks),
                            _dense(chosen, torch.int32, tokens, picks), _stream(stream)), "daq_route")
     return out
@@ -1120,7 +1132,7 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, chosen: torch.T
     picks = chosen.shape[1]
     out, ldd, _ = _result(out, tokens, experts, logits.dtype, logits, stream)
     _here(out)
-    opts = RouteOpts(scores, picks, 1, 1, int(renormalize), scale)
+    opts = _route_opts(scores, picks, 1, 1, bool(renormalize), scale)
     _check(lib().daq_route_backward(tokens, experts, _dense(dweights, torch.float32, tokens, picks), logits.data_ptr(), code, ld,
                                     _dense(chosen, torch.int32, tokens, picks), C.byref(opts), out.data_ptr(), ldd, _stream(stream)),
            "daq_route_backward")
@@ -1129,13 +1141,15 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, chosen: torch.T
 
 def alloc_plan(tokens: int, picks: int, experts: int, device="cuda", stream=None) -> Plan:
     """Memory of a plan: of ``stream``, or of the current one."""
-    def ints(*shape):
-        if stream is None:
-            return torch.empty(shape, dtype=torch.int32, device=device)
+    slots = tokens * picks
+    sizes = [experts, 4 * (experts + 1), slots, slots]
+    if stream is None:
+        buf = torch.empty(sum(sizes), dtype=torch.int32, device=device)
+    else:
         with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=torch.int32, device=device)
-
-    return Plan(ints(experts), ints(4, experts + 1), ints(tokens * picks), ints(tokens, picks), tokens, picks, experts)
+            buf = torch.empty(sum(sizes), dtype=torch.int32, device=device)
+    counts, table, rows, place = buf.split_with_sizes(sizes)
+    return Plan(counts, table.view(4, experts + 1), rows, place.view(tokens, picks), tokens, picks, experts)
 
 
 def experts_plan(chosen: torch.Tensor, experts: int, out: Optional[Plan] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> Plan:
@@ -1146,17 +1160,16 @@ def experts_plan(chosen: torch.Tensor, experts: int, out: Optional[Plan] = None,
     if out is None:
         out = alloc_plan(tokens, picks, experts, chosen.device, stream)
     assert (out.tokens, out.picks, out.experts) == (tokens, picks, experts)
-    c, t = _dense(out.counts, torch.int32, experts), _dense(out.table, torch.int32, 4, experts + 1)
-    r, p = _dense(out.rows, torch.int32, tokens * picks), _dense(out.place, torch.int32, tokens, picks)
+    _here(out.table)
+    e = out.handed_on
     ws, wa, n = _given_ws(workspace, "daq_experts_plan_workspace", stream, chosen.device, tokens, picks, experts)
-    _check(lib().daq_experts_plan(tokens, picks, experts, at, c, t, r, p, wa, n, _stream(stream)), "daq_experts_plan")
+    _check(lib().daq_experts_plan(tokens, picks, experts, at, out.counts.data_ptr(), e.table, e.rows, e.place, wa, n, _stream(stream)), "daq_experts_plan")
     return out
 
 
 def _plan(p: Plan) -> Experts:
-    slots = p.tokens * p.picks
-    return Experts(p.tokens, p.picks, p.experts, _dense(p.table, torch.int32, 4, p.experts + 1), _dense(p.rows, torch.int32, slots),
-                   _dense(p.place, torch.int32, p.tokens, p.picks))
+    _here(p.table)
+    return p.handed_on
 
 
 @functools.lru_cache(maxsize=4096)
