@@ -211,7 +211,9 @@ __device__ __forceinline__ void run_tiles(const ProductArgs& p, uint8_t* __restr
             const uint32_t off0 = (uint32_t)(row0 * (int)p.ldd + col0) * 2u;
             results_out(acc, out + wave * 4096, now, [&](int i, int jp, int k, u32x4 v) {
                 const uint32_t off = off0 + (uint32_t)((i * 32 + k * 8) * (int)p.ldd + jp * 64) * 2u;
-                __builtin_amdgcn_raw_buffer_store_b128(v, to, (int)(col0 + jp * 64 < cols ? off : kTileReach), 0, 0);
+                const int where = (int)(col0 + jp * 64 < cols ? off : kTileReach);
+                if (p.stream) __builtin_amdgcn_raw_buffer_store_b128(v, to, where, 0, 2);      // (non-temporal)
+                else __builtin_amdgcn_raw_buffer_store_b128(v, to, where, 0, 0);
             });
             static_assert(kStores == kB * (kB / 2) * 4, "as many as results_out puts");
         } else {
@@ -242,7 +244,12 @@ daq_status launch(const ProductArgs& p, hipStream_t st) {
 
 }  // namespace
 
-daq_status fp8_large(Of of, const ProductArgs& p, hipStream_t st) {
+// Results of more than the caches behind L2 keep (256 MiB) pass them by: 65536 x 2048 x 2048 (256 MiB of results) 215 us instead of 251, 16384 x 8192 x 8192 721
+// instead of 737; of half as much they stay, 8192 x 8192 x 4096 193 instead of 196.
+constexpr int64_t kStreamProduct = (int64_t)192 << 20;
+
+daq_status fp8_large(Of of, ProductArgs p, hipStream_t st) {
+    p.stream = p.M * p.N * 2 * (of == Of::kExpertWeights ? p.experts : 1) >= kStreamProduct;
     const bool flush = p.N % 8 == 0 && p.ldd % 8 == 0 && p.ldd < (1 << 22) && ((uintptr_t)p.d & 15) == 0 && p.stride % 8 == 0;
     switch (of) {
         case Of::kWhole: return flush ? launch<Of::kWhole, true>(p, st) : launch<Of::kWhole, false>(p, st);

@@ -20,7 +20,7 @@ struct ProductArgs {
     int stages;               // blocks of 128 of the summed axis
     void* d;
     int64_t ldd;
-    int bf16, accumulate;
+    int bf16, accumulate, stream;   // stream: results pass the caches by
     int tiles_m, tiles_n;     // (experts' rows: tiles_m is the most there can be)
     int splits, per_split;    // of the summed axis: part z, of per_split stages, goes to d + z * M * ldd
     // experts
@@ -130,7 +130,7 @@ __device__ __forceinline__ void put8(uint16_t* z, u32x4 v, int64_t left) {
 }  // namespace
 
 // fp8_large.hip: results in bfloat16 on tiles of 256 x 256; operands and sizes are checked, p.tiles_m and p.tiles_n set
-daq_status fp8_large(Of of, const ProductArgs& p, hipStream_t st);
+daq_status fp8_large(Of of, ProductArgs p, hipStream_t st);
 // fp8_few.hip: whole products or experts' rows in `tiles` row tiles of 64 (experts: at most so many), none of more than most_rows rows; x not NULL: A from X
 // [..][K], quantized on the way
 daq_status fp8_few(Of of, const ProductArgs& p, int64_t tiles, int64_t most_rows, const void* x, int x_dtype, int64_t ldx, int64_t K, hipStream_t st);
