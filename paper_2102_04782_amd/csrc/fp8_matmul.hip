@@ -313,6 +313,19 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
     pl.form = M <= 32 && few_fits(1, N) && ceil_div(N, 64) < 256 ? Fp8Form::kFew : least_cost(tiles(64), tiles(128), tiles(256), (double)stages, exact);
     pl.splits = 1;
     pl.per_split = (int)stages;
+    if (pl.form == Fp8Form::kFew) return pl;
+    // parts of the summed axis, of four stages or more, for what they and the launch that adds them up (at 3 TB/s) take less
+    const int64_t edge = pl.form == Fp8Form::k256 ? 256 : pl.form == Fp8Form::k128 ? 128 : 64;
+    double least = fp8_cost(pl.form, tiles(edge), (double)stages, exact);
+    for (const Fp8Form form : {Fp8Form::k64, Fp8Form::k128})
+        for (int s = 2; s <= 16 && stages >= 4 * s; s *= 2) {
+            const double cost = fp8_cost(form, tiles(form == Fp8Form::k64 ? 64 : 128) * s, std::ceil((double)stages / s), exact) + 3.5 + s * (double)M * (double)N * 8 / 3e6;
+            if (cost >= least) continue;
+            least = cost;
+            pl.form = form;
+            pl.per_split = (int)ceil_div(stages, s);
+            pl.splits = (int)ceil_div(stages, pl.per_split);
+        }
     return pl;
 }
 
