@@ -364,6 +364,7 @@ struct RouteBackArgs {
     int64_t tokens, ld, ldd;
     int experts, picks;
     int sigmoid, renormalize;
+    int each, slot;           // tokens of a wave; log2 of the lanes for a token's places
     float scale;
     const float* dweights;
     const int32_t* chosen;
@@ -381,23 +382,35 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
-// A wave a token: the chosen ones' part in lane j for place j, then the row, zero or (softmax that is not renormalised) the others' part.
-template <typename T>
+__device__ __forceinline__ void store_logits(float* p, const float* v, int left) {
+    if (left >= 4) *reinterpret_cast<u32x4_a4*>(p) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+    else
+        for (int i = 0; i < left; ++i) p[i] = v[i];
+}
+__device__ __forceinline__ void store_logits(uint16_t* p, const float* v, int left) {
+    if (left >= 4) *reinterpret_cast<u32x2_a2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    else
+        for (int i = 0; i < left; ++i) p[i] = (uint16_t)(pack_bf16(v[i], 0.f) & 0xFFFFu);
+}
+
+// Lane n << slot + j has place j of the wave's token n.  The chosen ones' part goes to its place of the row by way of LDS; the others' is zero or, where the softmax is not
+// renormalised, needs the row.
+template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits, RouteBackArgs p) {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
-    __shared__ float row[4][kMaxExperts];
-    if (t >= p.tokens) return;
-    const T* from = logits + t * p.ld;
-    T* to = dlogits + t * p.ldd;
-    const int e = lane < p.picks ? p.chosen[t * p.picks + lane] : -1;
+    __shared__ __attribute__((aligned(16))) float rows[4][PARTS * 256];
+    const int lane = threadIdx.x % kWave;
+    const int64_t t0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * p.each;
+    if (t0 >= p.tokens) return;
+    float* const row = rows[threadIdx.x / kWave];
+    const int tok = lane >> p.slot, j = lane & ((1 << p.slot) - 1);
+    const int64_t t = t0 + tok;
+    const bool held = tok < p.each && t < p.tokens && j < p.picks;
+    const int e = held ? p.chosen[t * p.picks + j] : -1;
     const bool there = e >= 0 && e < p.experts;
-    const float g = there ? p.dweights[t * p.picks + lane] : 0.f, l = there ? logit_at(from + e) : 0.f;
-    float* mine = row[wave];
-    for (int i = lane; i < p.experts; i += kWave) mine[i] = 0.f;
+    const float g = there ? p.dweights[t * p.picks + j] : 0.f, l = there ? logit_at(logits + t * p.ld + e) : 0.f;
+    const bool dense = !p.sigmoid && !p.renormalize;
     float d = 0.f;                             // of the chosen one's logit
-    float most = 0.f, sum = 1.f, back = 0.f;
-    if (p.sigmoid || p.renormalize) {
+    if (!dense) {
         // s and, where it is renormalised, its share of the chosen ones', which may all be tiny: in 64 bits, as in the forward pass
         double s, rest = 1.0;
         if (p.sigmoid) {
@@ -405,38 +418,76 @@ __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits,
             s = l >= 0 ? one : ex * one;
             rest = l >= 0 ? ex * one : one;
         } else {
-            most = wave_max(there ? l : -__builtin_inff());
+            float most = there ? l : -__builtin_inff();
+            for (int k = 1; k < 1 << p.slot; k *= 2) most = fmaxf(most, __shfl_xor(most, k));
             s = exp((double)l - (double)most);
         }
         if (!there) s = 0;
         double v = g;
         if (p.renormalize) {
-            const double total = wave_sum(s);
-            s = total > 0 ? s / total : 0.0;
-            v -= wave_sum(g * s);
+            double total = s, mean = g * s;
+            for (int k = 1; k < 1 << p.slot; k *= 2) {
+                total += __shfl_xor(total, k);
+                mean += __shfl_xor(mean, k);
+            }
+            const double over = total > 0 ? 1.0 / total : 0.0;
+            s *= over;
+            v -= mean * over;
         }
         d = (float)(p.scale * v * s * rest);
-    } else {
-        float m = -__builtin_inff();
-        for (int i = lane; i < p.experts; i += kWave) m = fmaxf(m, logit_at(from + i));
-        most = wave_max(m);
-        float total = 0.f;
-        for (int i = lane; i < p.experts; i += kWave) total += expf(logit_at(from + i) - most);
-        sum = wave_sum(total);
-        const float s = there ? expf(l - most) / sum : 0.f;
-        back = wave_sum(p.scale * g * s);
-        d = p.scale * g;
     }
-    const bool any = __any(there);
-    for (int j = 0; j < p.picks; ++j) {        // one after the other: an expert that a token names twice has both parts
-        if (lane == j && there) mine[e] += d;
+    // an expert that a token names twice: its places one after the other
+    bool twice = false;
+    for (int k = 1; k < p.picks; ++k) twice |= there && j >= k && __shfl(e, lane - k) == e;
+    const bool any_twice = __any(twice);
+    for (int n = 0; n < p.each && t0 + n < p.tokens; ++n) {
+        const bool mine = there && tok == n;
+        const bool any = __any(mine);
+        float x[PARTS][4], sum = 1.f, back = 0.f;          // dense: the row's exponentials
+        if (dense) {
+            float m = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+                load_logits<4>(logits + (t0 + n) * p.ld + i * 256 + lane * 4, p.experts - i * 256 - lane * 4, x[i]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m = fmaxf(m, x[i][k]);
+            }
+            m = wave_max(m);
+            float total = 0.f;
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    x[i][k] = expf(x[i][k] - m);
+                    total += x[i][k];
+                }
+            sum = wave_sum(total);
+            back = wave_sum(mine ? p.scale * g * (expf(l - m) / sum) : 0.f);
+            if (mine) d = p.scale * g;
+        }
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) *reinterpret_cast<f32x4*>(row + i * 256 + lane * 4) = f32x4{0, 0, 0, 0};
         __builtin_amdgcn_wave_barrier();
-    }
-    for (int i = lane; i < p.experts; i += kWave) {
-        float v = mine[i];
-        if (!p.sigmoid && !p.renormalize) v = any ? expf(logit_at(from + i) - most) / sum * (v - back) : 0.f;
-        if constexpr (sizeof(T) == 4) to[i] = v;
-        else to[i] = (T)(pack_bf16(v, 0.f) & 0xFFFFu);
+        if (!any_twice) {
+            if (mine) row[e] = d;
+        } else {
+            for (int k = 0; k < p.picks; ++k) {
+                if (mine && j == k) row[e] += d;
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            f32x4 z = *reinterpret_cast<const f32x4*>(row + i * 256 + lane * 4);
+            if (dense) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) z[k] = any ? x[i][k] / sum * (z[k] - back) : 0.f;
+            }
+            const float v[4] = {z[0], z[1], z[2], z[3]};
+            store_logits(dlogits + (t0 + n) * p.ldd + i * 256 + lane * 4, v, p.experts - i * 256 - lane * 4);
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -626,7 +677,8 @@ daq_status launch_route(const T* logits, const RouteArgs& p, hipStream_t st) {
 }
 template <typename T>
 daq_status launch_back(const T* logits, T* dlogits, const RouteBackArgs& p, hipStream_t st) {
-    DAQ_LAUNCH("route_back", st, hipLaunchKernelGGL(k_route_back<T>, dim3((unsigned)ceil_div(p.tokens, 4)), dim3(256), 0, st, logits, dlogits, p));
+    const auto kernel = p.experts <= 256 ? k_route_back<T, 1> : p.experts <= 512 ? k_route_back<T, 2> : k_route_back<T, 4>;
+    DAQ_LAUNCH("route_back", st, hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(p.tokens, 4 * p.each)), dim3(256), 0, st, logits, dlogits, p));
     return DAQ_OK;
 }
 
@@ -652,7 +704,10 @@ extern "C" daq_status daq_route_backward(int64_t tokens, int32_t experts, const 
     const daq_status rc = route_check(tokens, experts, logits, dtype, ld, opts);
     if (rc != DAQ_OK || tokens == 0) return rc;
     if (!dweights || !a4(dweights) || !chosen || !a4(chosen) || !dlogits || !elem_aligned(dlogits, dtype) || ldd < experts) return DAQ_ERR_INVALID_ARG;
-    const RouteBackArgs p{tokens, ld, ldd, experts, opts->picks, opts->scores == DAQ_SCORES_SIGMOID, opts->renormalize != 0, opts->scale, dweights, chosen};
+    // what is computed in 64 bits takes a wave as long for one token's places as for several's: four tokens a wave, once there are enough of them (16384 x 256,
+    // 8 places, 7.5 us instead of 12)
+    const int slot = opts->picks <= 8 ? 3 : opts->picks <= 16 ? 4 : 5, each = tokens >= 8192 ? std::min(4, kWave >> slot) : 1;
+    const RouteBackArgs p{tokens, ld, ldd, experts, opts->picks, opts->scores == DAQ_SCORES_SIGMOID, opts->renormalize != 0, each, slot, opts->scale, dweights, chosen};
     return dtype == DAQ_BF16 ? launch_back(static_cast<const uint16_t*>(logits), static_cast<uint16_t*>(dlogits), p, (hipStream_t)stream)
                              : launch_back(static_cast<const float*>(logits), static_cast<float*>(dlogits), p, (hipStream_t)stream);
 }
