@@ -438,7 +438,10 @@ __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits,
     }
     // an expert that a token names twice: its places one after the other
     bool twice = false;
-    for (int k = 1; k < p.picks; ++k) twice |= there && j >= k && __shfl(e, lane - k) == e;
+    for (int k = 1; k < p.picks; ++k) {
+        const int other = __shfl(e, lane - k);      // (of all lanes: a lane that does not take part has nothing to give)
+        twice |= there && j >= k && other == e;
+    }
     const bool any_twice = __any(twice);
     for (int n = 0; n < p.each && t0 + n < p.tokens; ++n) {
         const bool mine = there && tok == n;

@@ -340,3 +340,92 @@ def test_the_same_bits_every_time():
     first = once()
     for _ in range(3):
         assert all(torch.equal(a, b) for a, b in zip(first, once()))
+
+
+@pytest.mark.parametrize("E,k", [(40, 3), (300, 12), (520, 20)])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_router_of_many_tokens(E, k, kind):
+    """Tokens enough for a wave to take several backwards; their number leaves the last wave some."""
+    T = 8197
+    logits = torch.randn(T, E, generator=torch.Generator().manual_seed(E))
+    logits[77] = -torch.inf
+    g = torch.randn(T, k, generator=torch.Generator().manual_seed(k))
+    for renormalize in (True, False):
+        s = ref.scores(_np(logits), kind)
+        chosen = np.argsort(-np.where(np.isneginf(_np(logits)), -np.inf, _np(logits)), axis=1, kind="stable")[:, :k]
+        chosen[77] = -1
+        w, e = daq.route(logits.cuda(), k, KIND[kind], renormalize=renormalize)
+        assert np.array_equal(_np(e), chosen)
+        take = np.where(chosen >= 0, np.take_along_axis(s, np.maximum(chosen, 0), 1), 0)
+        total = np.where(chosen[:, :1] >= 0, take.sum(1, keepdims=True), 1.0) if renormalize else np.ones((T, 1))
+        assert np.all(np.abs(_np(w) - take / total) <= (2.0 ** -24 + 2.0 ** -48) * take / total + 2.0 ** -149)
+        want = ref.route_backward(_np(g), _np(logits), chosen, kind, renormalize)
+        got = _np(daq.route_backward(g.cuda(), logits.cuda(), e, KIND[kind], renormalize))
+        size = np.abs(want) + s * np.abs(_np(g)).sum(1, keepdims=True) * (1.0 if not renormalize else 2.0 ** -20 / total)
+        assert np.all(np.abs(got - want) <= (E / 64 + k + 30) * 2.0 ** -24 * size + 1e-37)
+
+
+@pytest.mark.parametrize("T", [5, 8200])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_a_token_that_names_an_expert_twice(T, kind):
+    """Each place counts, in the gradient, in the order of the rows and in the sum."""
+    logits, g = torch.randn(T, 12, generator=torch.Generator().manual_seed(1)), torch.randn(T, 4, generator=torch.Generator().manual_seed(2))
+    chosen = torch.randint(0, 12, (T, 4), generator=torch.Generator().manual_seed(3)).int()
+    chosen[:, 2], chosen[1] = chosen[:, 0], 7
+    for renormalize in (True, False):
+        want = ref.route_backward(_np(g), _np(logits), _np(chosen).astype(int), kind, renormalize)
+        got = _np(daq.route_backward(g.cuda(), logits.cuda(), chosen.cuda(), KIND[kind], renormalize))
+        # the places of an expert are added in 32 bits: parts of up to its share of the chosen ones' scores, times the weights' gradients
+        s = ref.scores(_np(logits), kind)
+        share = s / np.take_along_axis(s, _np(chosen).astype(int), 1).sum(1, keepdims=True) if renormalize else s
+        assert np.all(np.abs(got - want) <= 50 * 2.0 ** -24 * (np.abs(want) + share * np.abs(_np(g)).sum(1, keepdims=True)) + 1e-37)
+    plan = daq.experts_plan(chosen.cuda(), 12)
+    _, _, rows, place = ref.plan(chosen.numpy(), 12)
+    assert np.array_equal(_np(plan.rows), rows) and np.array_equal(_np(plan.place), place)
+
+
+def test_all_tokens_of_one_expert():
+    """The longest run that a plan can have, among experts without rows; few experts' rows in a wide matrix."""
+    c = torch.full((3000, 1), 5, dtype=torch.int32)
+    plan = daq.experts_plan(c.cuda(), 64)
+    assert plan.counts[5] == 3000 and plan.table[1, -1] == 12 and plan.table[2, -1] == 24
+    x, w = torch.randn(3000, 256), torch.randn(64, 512, 256)
+    qw, _ = daq.fp8_quantize_weights(w.cuda())
+    got = _np(daq.experts_linear(x.cuda(), qw, plan, dtype=torch.float32))
+    vx, vw = ref.values(*ref.quantize(_np(x))), ref.values(*ref.quantize_weights(_np(w[5])))
+    assert np.all(np.abs(got - vx @ vw.T) <= _bound(256, np.abs(vx) @ np.abs(vw).T, vx @ vw.T, torch.float32))
+    few = torch.tensor([[63], [0], [63]], dtype=torch.int32).cuda()
+    got = _np(daq.experts_linear(x[:3].cuda(), qw, daq.experts_plan(few, 64), dtype=torch.float32))
+    for p, (t, e) in enumerate(((1, 0), (0, 63), (2, 63))):
+        vw = ref.values(*ref.quantize_weights(_np(w[e])))
+        assert np.all(np.abs(got[p] - vw @ vx[t]) <= _bound(256, np.abs(vw) @ np.abs(vx[t]), vw @ vx[t], torch.float32))
+
+
+@pytest.mark.parametrize("sorted_rows", [False, True])
+def test_large_products_of_experts(sorted_rows):
+    """Tiles of 256 x 256 of uneven experts, more of them than CUs, rows of whole 16-byte pieces; and their gradients."""
+    T, k, E, N, K = 9000, 2, 9, 2048, 264
+    c = _chosen(T, k, E, 3, none=0.02, skew=0.3)
+    plan = daq.experts_plan(c.cuda(), E)
+    counts, table, rows, place = ref.plan(c.numpy(), E)
+    total, ends = int(counts.sum()), np.cumsum(counts)
+    a = torch.randn(T * k if sorted_rows else T, K, generator=torch.Generator().manual_seed(1)).bfloat16()
+    w = torch.randn(E, N, K, generator=torch.Generator().manual_seed(2)).bfloat16()
+    qw, _ = daq.fp8_quantize_weights(w.cuda())
+    va = ref.values(*ref.quantize(_np(a)))
+    out = torch.full((T * k, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    y = _np(daq.experts_linear(a.cuda(), qw, plan, sorted_rows=sorted_rows, out=out))
+    d = torch.randn(T * k, N, generator=torch.Generator().manual_seed(3)).bfloat16()
+    _, ac = daq.experts_quantize(a.cuda(), plan, sorted_rows=sorted_rows)
+    _, dc = daq.experts_quantize(d.cuda(), plan, sorted_rows=True)
+    grads = {to: _np(daq.experts_weight_grad(dc, ac, plan, dtype=to)) for to in DT}
+    for e in range(E):
+        here = slice(ends[e] - counts[e], ends[e])
+        r = va[here] if sorted_rows else va[rows[here] // k]
+        vw = ref.values(*ref.quantize_weights(_np(w[e])))
+        assert np.all(np.abs(y[here] - r @ vw.T) <= _bound(K, np.abs(r) @ np.abs(vw).T, r @ vw.T, torch.bfloat16))
+        r = _np(a)[here] if sorted_rows else _np(a)[rows[here] // k]
+        vd, vx = ref.values(*ref.quantize(_np(d)[here].T)), ref.values(*ref.quantize(r.T))
+        for to in DT:
+            assert np.all(np.abs(grads[to][e] - vd @ vx.T) <= _bound(int(counts[e]), np.abs(vd) @ np.abs(vx).T, vd @ vx.T, to))
+    assert bool((out[total:] == 7).all())
