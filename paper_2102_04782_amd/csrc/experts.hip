@@ -15,26 +15,6 @@ struct CombineArgs {
 
 __device__ __forceinline__ float element(const Eight<float>& v, int i) { return bits_as<float>(v.w[i]); }
 __device__ __forceinline__ float element(const Eight<uint16_t>& v, int i) { return (i & 1) ? bf16_hi(v.w[i / 2]) : bf16_lo(v.w[i / 2]); }
-// Eight results of a row, or the first `left` of them.
-__device__ __forceinline__ void store8(float* z, int left, const float (&v)[8]) {
-    if (left >= 8) {
-        *reinterpret_cast<u32x4_a4*>(z) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
-        *reinterpret_cast<u32x4_a4*>(z + 4) = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
-    } else {
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < left) z[i] = v[i];
-    }
-}
-__device__ __forceinline__ void store8(uint16_t* z, int left, const float (&v)[8]) {
-    if (left >= 8) {
-        *reinterpret_cast<u32x4_a2*>(z) = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < left) z[i] = (uint16_t)(pack_bf16(v[i], 0.f) & 0xFFFFu);
-    }
-}
 template <typename T>
 __device__ __forceinline__ void load_some(const T* p, int64_t left, Eight<T>& v) {
     if (left >= 8) load8(p, v);

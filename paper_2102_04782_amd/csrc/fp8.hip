@@ -190,15 +190,22 @@ daq_status launch_tiles(const T* src, TileArgs p, int64_t tiles, hipStream_t st)
     return DAQ_OK;
 }
 
-// 64 columns of a row a wave.
+// Eight columns of a row a lane.
 template <typename T>
 __global__ __launch_bounds__(256) void k_fp8_values(const uint8_t* codes, const uint8_t* scales, int64_t pitch, int64_t rows, int64_t cols, T* dst, int64_t ld) {
-    const int64_t strips = (cols + 255) / 256, r = blockIdx.x / strips, c = (blockIdx.x - r * strips) * 256 + threadIdx.x;
+    const int64_t strips = (cols + 2047) / 2048, r = blockIdx.x / strips, c = (blockIdx.x - r * strips) * 2048 + threadIdx.x * 8;
     if (c >= cols) return;
-    const uint32_t byte = scales[((c / kFp8Group) * rows + r) * 4 + (c / kFp8Block) % 4];
-    const float v = __builtin_amdgcn_cvt_f32_fp8((int)codes[r * pitch + c], 0) * scale_of(byte);
-    if constexpr (sizeof(T) == 4) dst[r * ld + c] = v;
-    else dst[r * ld + c] = (T)(pack_bf16(v, 0.f) & 0xFFFFu);
+    const float s = scale_of(scales[((c / kFp8Group) * rows + r) * 4 + (c / kFp8Block) % 4]);
+    const u32x2 q = *reinterpret_cast<const u32x2*>(codes + r * pitch + c);
+    float v[8];
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+        v[4 * d] = __builtin_amdgcn_cvt_f32_fp8((int)q[d], 0) * s;
+        v[4 * d + 1] = __builtin_amdgcn_cvt_f32_fp8((int)q[d], 1) * s;
+        v[4 * d + 2] = __builtin_amdgcn_cvt_f32_fp8((int)q[d], 2) * s;
+        v[4 * d + 3] = __builtin_amdgcn_cvt_f32_fp8((int)q[d], 3) * s;
+    }
+    store8(dst + r * ld + c, (int)min(cols - c, (int64_t)8), v);
 }
 
 daq_status source_check(const void* src, int dtype, int64_t cols, int64_t ld) {
@@ -276,7 +283,7 @@ extern "C" daq_status daq_fp8_dequantize(const uint8_t* src, int64_t rows, int64
     if (rc != DAQ_OK) return rc;
     if (rows == 0 || cols == 0) return DAQ_OK;
     if (!src || !aligned256(src) || !dst || !elem_aligned(dst, dtype) || ld < cols) return DAQ_ERR_INVALID_ARG;
-    const int64_t blocks = rows * ceil_div(cols, 256);
+    const int64_t blocks = rows * ceil_div(cols, 2048);
     if (!grid_ok(blocks, 256)) return DAQ_ERR_UNSUPPORTED;
     const Packed q = packed(const_cast<uint8_t*>(src), rows, cols);
     if (dtype == DAQ_BF16)

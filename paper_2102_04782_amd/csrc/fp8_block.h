@@ -33,6 +33,27 @@ __device__ __forceinline__ void load8(const float* p, int left, Eight<float>& v)
     for (int i = 0; i < 8; ++i) v.w[i] = i < left ? __float_as_uint(p[i]) : 0u;
 }
 
+// Eight results of a row, or the first `left` of them.
+__device__ __forceinline__ void store8(float* z, int left, const float (&v)[8]) {
+    if (left >= 8) {
+        *reinterpret_cast<u32x4_a4*>(z) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+        *reinterpret_cast<u32x4_a4*>(z + 4) = __builtin_bit_cast(u32x4, f32x4{v[4], v[5], v[6], v[7]});
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) z[i] = v[i];
+    }
+}
+__device__ __forceinline__ void store8(uint16_t* z, int left, const float (&v)[8]) {
+    if (left >= 8) {
+        *reinterpret_cast<u32x4_a2*>(z) = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < left) z[i] = (uint16_t)(pack_bf16(v[i], 0.f) & 0xFFFFu);
+    }
+}
+
 // Magnitudes are compared as integers: NaN and infinity are the largest.  Of fp32 one a word, of bfloat16 two.
 __device__ __forceinline__ uint32_t larger(const uint16_t*, uint32_t m, uint32_t w) { return max_pairs(m, w & 0x7FFF7FFFu); }
 __device__ __forceinline__ uint32_t larger(const float*, uint32_t m, uint32_t w) { return max(m, w & 0x7FFFFFFFu); }

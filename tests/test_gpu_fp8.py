@@ -214,3 +214,73 @@ def test_nothing_to_do_and_nothing_to_sum():
     out = torch.full((40, 70), 3.0, device="cuda")
     assert bool((daq.fp8_matmul(a, b, out=out, accumulate=True) == 3).all())
     assert bool((daq.fp8_matmul(a, b, out=out) == 0).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(4352, 4096, 100), (4100, 4104, 200), (4352, 4096, 300), (4097, 4352, 640), (2304, 8192, 1100)])
+def test_large_products_go_from_tile_to_tile(M, N, K):
+    """More tiles than CUs, rows of whole 16-byte pieces, one stage to nine: results whose stores are still under way when the next tile begins."""
+    a, b = _x(M, K, torch.bfloat16, M + K), _x(N, K, torch.bfloat16, N + 3 * K)
+    va, vb = ref.values(*ref.quantize(_np(a))), ref.values(*ref.quantize(_np(b)))
+    exact, absolute = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    qa, qb = daq.fp8_quantize(a.cuda()), daq.fp8_quantize(b.cuda())
+    wide = torch.full((M + 3, N + 16), 55.0, dtype=torch.bfloat16, device="cuda")
+    for out in (torch.full((M, N), float("nan"), dtype=torch.bfloat16, device="cuda"), wide[1:1 + M, 8:8 + N]):
+        got = _np(daq.fp8_matmul(qa, qb, out=out))
+        assert np.all(np.abs(got - exact) <= _bound(K, absolute, exact, torch.bfloat16))
+    assert bool((wide[:, :8] == 55).all()) and bool((wide[:, 8 + N:] == 55).all()) and bool((wide[0] == 55).all()) and bool((wide[1 + M:] == 55).all())
+
+
+def test_results_that_pass_the_caches_by():
+    """192 MiB of results: the same values as of two halves."""
+    a, b = daq.fp8_quantize(torch.randn(12800, 256, device="cuda")), daq.fp8_quantize(torch.randn(8192, 256, device="cuda"))
+    half = daq.fp8_quantize(daq.fp8_dequantize(b)[4096:].contiguous())
+    whole = daq.fp8_matmul(a, b)
+    assert torch.equal(whole[:, 4096:], daq.fp8_matmul(a, half))
+
+
+@pytest.mark.parametrize("M,N,K", [(64, 64, 8192), (130, 70, 5000), (512, 512, 8192), (300, 1000, 4096), (128, 300, 16384)])
+def test_sums_in_parts(M, N, K):
+    """Few tiles and a long axis: parts of it, added up in their order."""
+    a, b = _x(M, K, torch.float32, 1, 2), _x(N, K, torch.float32, 2, 2)
+    va, vb = ref.values(*ref.quantize(_np(a))), ref.values(*ref.quantize(_np(b)))
+    exact, absolute = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    qa, qb = daq.fp8_quantize(a.cuda()), daq.fp8_quantize(b.cuda())
+    assert daq._few_ws_bytes("daq_fp8_matmul_workspace", M, N, K, daq.FP32) > 0
+    for to in DT:
+        first = daq.fp8_matmul(qa, qb, dtype=to)
+        assert np.all(np.abs(_np(first) - exact) <= _bound(K, absolute, exact, to))
+        assert torch.equal(first, daq.fp8_matmul(qa, qb, dtype=to))
+    start = torch.randn(M, N, device="cuda")
+    want = exact + _np(start)
+    assert np.all(np.abs(_np(daq.fp8_matmul(qa, qb, out=start, accumulate=True)) - want) <= _bound(K, absolute, exact, torch.float32) + 2.0 ** -23 * np.abs(want))
+
+
+def test_offsets_beyond_32_bits():
+    """4.4 GB of codes, 8.8 GB of elements, 5 GB of results: the first and the last rows against those of small matrices."""
+    rows, K = 540001, 8192
+    x = torch.empty(rows, K, dtype=torch.bfloat16, device="cuda")
+    x.view(-1)[:1 << 20].normal_()
+    x.view(-1)[1 << 20:] = 0.5
+    ends = torch.cat((torch.arange(40), torch.arange(rows - 40, rows))).cuda()
+    x[ends] = torch.randn(80, K, device="cuda").bfloat16()
+    w, _ = daq.fp8_quantize_weights(torch.randn(72, K, device="cuda"))
+    q, small = daq.fp8_quantize(x), daq.fp8_quantize(x[ends].contiguous())
+    for to in DT:
+        got, want = daq.fp8_matmul(q, w, dtype=to)[ends].double(), daq.fp8_matmul(small, w, dtype=torch.float32).double()
+        assert bool(((got - want).abs() <= 2.0 ** -6 * want.abs() + 1e-2).all())
+        assert torch.equal(got, daq.fp8_linear(x, w, dtype=to)[ends].double())
+    assert torch.equal(daq.fp8_dequantize(q, dtype=torch.bfloat16)[ends], daq.fp8_dequantize(small, dtype=torch.bfloat16))
+    c = daq.fp8_quantize(x, columns=True)
+    assert c.rows == K and c.cols == rows
+    byte = daq.layout_fp8(K, rows)
+    last = c.buf[(K - 1) * byte.pitch:(K - 1) * byte.pitch + rows][ends]
+    tail = daq.fp8_quantize(x[rows - rows % 128:].contiguous(), columns=True)      # the last block of tokens
+    assert torch.equal(last[40:], tail.buf[(K - 1) * 128:(K - 1) * 128 + rows % 128][-40:]) or rows % 128 < 40
+    del x, q, c
+    # results of more than 2^32 bytes
+    a, b = daq.fp8_quantize(torch.randn(70000, 128, device="cuda")), daq.fp8_quantize(torch.randn(36000, 128, device="cuda"))
+    out = daq.fp8_matmul(a, b)
+    ends = torch.cat((torch.arange(40), torch.arange(70000 - 40, 70000))).cuda()
+    part = daq.fp8_quantize(daq.fp8_dequantize(a)[ends].contiguous())
+    want = daq.fp8_matmul(part, b, dtype=torch.float32)
+    assert bool(((out[ends].float() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -5).all())
