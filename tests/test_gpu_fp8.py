@@ -196,14 +196,30 @@ def test_gradients_of_a_layer(M, N, K, dtype):
     assert np.all(np.abs(got - want) <= _bound(M, np.abs(cd) @ np.abs(cx).T, want, torch.float32))
 
 
-@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (20, 130, 700), (200, 300, 600), (600, 300, 513), (2100, 2050, 513)])
-def test_what_is_not_finite_reaches_its_sums_only(M, N, K):
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", [(3, 40, 300), (20, 130, 700), (200, 300, 600), (600, 300, 513), (2100, 2050, 513), (4352, 4096, 300)])
+def test_what_is_not_finite_reaches_its_sums_only(M, N, K, dtype):
     x, w = torch.randn(M, K), torch.randn(N, K)
     x[M // 2, 140], w[N - 2, 5], w[1, K - 1] = float("nan"), float("inf"), float("-inf")
-    got = daq.fp8_matmul(daq.fp8_quantize(x.cuda()), daq.fp8_quantize(w.cuda())).float().cpu()
+    got = daq.fp8_matmul(daq.fp8_quantize(x.cuda()), daq.fp8_quantize(w.cuda()), dtype=dtype).float().cpu()
     bad = torch.zeros(M, N, dtype=torch.bool)
     bad[M // 2], bad[:, N - 2], bad[:, 1] = True, True, True
     assert torch.equal(torch.isnan(got), bad) and bool(torch.isfinite(got[~bad]).all())
+    if M <= 32:                                                           # rows quantized on the way
+        got = daq.fp8_linear(x.cuda(), daq.fp8_quantize(w.cuda()), dtype=dtype).float().cpu()
+        assert torch.equal(torch.isnan(got), bad) and bool(torch.isfinite(got[~bad]).all())
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("M,N,K", [(2, 40, 300), (70, 70, 300), (300, 600, 320)])
+def test_scales_far_apart(M, N, K, dtype):
+    """Operands near the ends of the range that a product in bfloat16 keeps: 2^-117 times 2^110, and 2^60 times 2^60."""
+    for ea, eb in ((-117, 110), (100, -105), (60, 60), (-60, -60)):
+        a, b = torch.randn(M, K) * 2.0 ** ea, torch.randn(N, K) * 2.0 ** eb
+        va, vb = ref.values(*ref.quantize(_np(a))), ref.values(*ref.quantize(_np(b)))
+        exact, absolute = va @ vb.T, np.abs(va) @ np.abs(vb).T
+        got = _np(daq.fp8_matmul(daq.fp8_quantize(a.cuda()), daq.fp8_quantize(b.cuda()), dtype=dtype))
+        assert np.all(np.abs(got - exact) <= _bound(K, absolute, exact, dtype))
 
 
 def test_nothing_to_do_and_nothing_to_sum():
