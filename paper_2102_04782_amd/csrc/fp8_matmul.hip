@@ -542,6 +542,7 @@ extern "C" daq_status daq_experts_weight_grad(const daq_experts* plan, int64_t N
     if (columns > kFp8MaxK || N * K > kMaxElems / plan->experts) return DAQ_ERR_UNSUPPORTED;
     if (!dW || !elem_aligned(dW, dtype) || ldw < K || stride < 0 || (plan->experts > 1 && stride < (N - 1) * ldw + K)) return DAQ_ERR_INVALID_ARG;
     if (plan->tokens == 0 && accumulate) return DAQ_OK;
+    if (!plan->table || ((uintptr_t)plan->table & 3)) return DAQ_ERR_INVALID_ARG;      // (read without tokens too)
     if (plan->tokens > 0 && (!dY || !aligned256(dY) || !X || !aligned256(X))) return DAQ_ERR_INVALID_ARG;
     ProductArgs p{};
     p.a = operand(dY, N, columns);

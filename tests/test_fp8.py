@@ -181,6 +181,14 @@ def test_refusals_come_before_any_launch():
             assert fn() == INV, none
 
 
+def test_weight_gradients_without_tokens_read_the_table():
+    L, a, odd = daq.lib(), 1 << 20, (1 << 20) + 2
+    for table in (None, odd):
+        plan = C.byref(daq.Experts(0, 2, 8, table, None, None))
+        assert L.daq_experts_weight_grad(plan, 8, 40, None, None, a, 0, 40, 320, 0, None) == daq.ERR_INVALID_ARG
+        assert L.daq_experts_weight_grad(plan, 8, 40, None, None, a, 0, 40, 320, 1, None) == daq.OK      # (adds nothing)
+
+
 def test_buffers_off_the_gpu_are_refused(monkeypatch):
     """As weights read from a file are: their host addresses must not get to a kernel."""
     def reached(stream):
