@@ -191,6 +191,7 @@ __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
     float most = kNone;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
+        l[i] += 0.f;                          // (-0 to 0: they are equals, their keys are not)
         bad |= l[i] != l[i] || (!p.sigmoid && l[i] == __builtin_inff());
         most = fmaxf(most, l[i]);
     }
@@ -393,6 +394,12 @@ __device__ __forceinline__ void store_logits(uint16_t* p, const float* v, int le
         for (int i = 0; i < left; ++i) p[i] = (uint16_t)(pack_bf16(v[i], 0.f) & 0xFFFFu);
 }
 
+// What the wave's lanes wrote to LDS before is there for what they read behind (LDS serves a wave in order; the compiler is told to).
+__device__ __forceinline__ void lds_in_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Lane n << slot + j has place j of the wave's token n.  The chosen ones' part goes to its place of the row by way of LDS; the others' is zero or, where the softmax is not
 // renormalised, needs the row.
 template <typename T, int PARTS>
@@ -470,16 +477,16 @@ __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits,
         }
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) *reinterpret_cast<f32x4*>(row + i * 256 + lane * 4) = f32x4{0, 0, 0, 0};
-        __builtin_amdgcn_wave_barrier();
+        lds_in_order();
         if (!any_twice) {
             if (mine) row[e] = d;
         } else {
             for (int k = 0; k < p.picks; ++k) {
                 if (mine && j == k) row[e] += d;
-                __builtin_amdgcn_wave_barrier();
+                lds_in_order();
             }
         }
-        __builtin_amdgcn_wave_barrier();
+        lds_in_order();
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) {
             f32x4 z = *reinterpret_cast<const f32x4*>(row + i * 256 + lane * 4);
@@ -490,7 +497,7 @@ __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits,
             const float v[4] = {z[0], z[1], z[2], z[3]};
             store_logits(dlogits + (t0 + n) * p.ldd + i * 256 + lane * 4, v, p.experts - i * 256 - lane * 4);
         }
-        __builtin_amdgcn_wave_barrier();
+        lds_in_order();
     }
 }
 

@@ -135,6 +135,22 @@ def test_scores_that_32_bits_do_not_tell_apart():
         assert np.array_equal(_np(e), chosen)
 
 
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E", [60, 100, 256, 512, 1000])
+def test_zeros_of_both_signs_are_equals(E, kind, dtype):
+    logits = torch.full((6, E), -1.0)
+    logits[:, 1::7] = -0.0
+    logits[:, 3::7] = 0.0
+    logits[1] = -0.0
+    logits[2] = 0.0
+    logits[2, :8] = -0.0
+    for groups in (1, 4):
+        _, want = ref.route(_np(logits), 8, kind, None, groups, min(groups, 2), True, 1.0)
+        _, e = daq.route(logits.to(dtype).cuda(), 8, KIND[kind], None, groups, min(groups, 2))
+        assert np.array_equal(_np(e), want) and want[2].tolist() == list(range(8))
+
+
 def _chosen(T, k, E, seed, none=0.1, skew=1.0):
     g = torch.Generator().manual_seed(seed)
     score = torch.randn(T, E, generator=g) + skew * torch.randn(E, generator=g)
