@@ -1,6 +1,10 @@
 // Products of 8-bit floating point matrices with a scale for every 128 elements, D[m][n] = sum over k of A[m][k] * B[n][k], whole ones and those of
 // experts, whose rows, or whose share of the summed axis, a plan on the device tells.
 //
+// Results in bfloat16 take the 8-bit matrix instructions.  These add eight neighbouring products with what lies below 2^-13 of the largest cut off (measured), some
+// 2^-16 of a result's magnitude: nothing beside bfloat16's rounding, but 200 times an fp32 sum's error.  Results in fp32 (EXACT) therefore
+// decode to bfloat16, which holds code times scale exactly, and take those instructions at half the rate.
+//
 // The matrix instructions take codes and scale bytes as they are: 32 x 32 x 64 (tiles) or 16 x 16 x 128 (few rows), 32 bytes a lane of each operand
 // and one scale for 32 of the summed axis.  As a block is 128 long and both operands are cut alike, which of a block's elements a
 // lane holds does not matter, as long as it is the same of both.  B goes in as the first operand, so that a lane holds
@@ -22,8 +26,8 @@ Fp8Operand operand(const uint8_t* buf, int64_t rows, int64_t cols) {
 // The results of a workgroup of WR x WC waves, each RB x CB tiles of 32 x 32, summed over the stages s0 .. s1 - 1 of 128.  A stage of both operands,
 // 128 bytes of every row, goes straight to LDS, where the 16-byte piece j of a row lies at j ^ (row / 2 % 8): eight lanes ask for a row's line in
 // that order, and the fragment reads of sixteen rows share no bank.  SLOTS stages are under way or being read.  Fragments are read a step
-// (64 of a stage's 128) ahead into the registers that the products have just done with; the barrier stands behind the first products of a stage's
-// second step, when this stage is read out and the next has landed.
+// (64 of a stage's 128) ahead into the registers that the products have just done with; the barrier stands between a stage's two steps, when this
+// stage is read out and the next has landed.
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT>
 struct Fp8Product {
     static constexpr int kWaves = WR * WC, kRows = WR * RB * 32, kCols = WC * CB * 32;
@@ -197,7 +201,8 @@ struct Fp8Product {
 };
 
 // Tiles of kRows x kCols results, a workgroup each.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles, in bands of four row
-// tiles, whose panels its L2 holds.
+// tiles, whose panels its L2 holds.  Bound: too few tiles for the CUs (1111 x 1500 x 2030, fp32: 432 of 64 x 64, 19.7 us, where the bytes take 2 and the
+// matrix cores 4), and LDS reads: a wave of a tile of 128 makes 32 products of a byte, of 64 21, of 256 64 (2048 x 4096 x 4096, bfloat16, 32.8 us, 2.1 PFLOP/s).
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_fp8_product(ProductArgs p) {
     using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
