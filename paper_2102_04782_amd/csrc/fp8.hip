@@ -68,7 +68,8 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
     constexpr int W = Eight<T>::kWords;
     constexpr bool kWeights = KIND == Tiles::kWeights, kExperts = KIND == Tiles::kExperts;
     __shared__ uint32_t turned[BYCOLS ? 128 * 32 : 1];
-    __shared__ uint32_t tops[8][16][W];
+    __shared__ __attribute__((aligned(16))) uint32_t tops[8][16][W];
+    __shared__ __attribute__((aligned(16))) uint8_t column_bytes[128];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, piece = lane % 16, quad = wave * 4 + lane / 16;
     const int64_t rt = blockIdx.x / p.col_tiles;
     const int64_t c0 = (int64_t)(blockIdx.x - rt * p.col_tiles) * 128, c = c0 + piece * 8;
@@ -129,10 +130,21 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
             if (lane < 16) tops[wave][piece][j] = m[j];
         }
         __syncthreads();
+        // a thread a column: its scale byte
+        if (threadIdx.x < 128) {
+            const int col = threadIdx.x;
+            uint32_t t = 0;
 #pragma unroll
-        for (int j = 0; j < W; ++j)
-#pragma unroll
-            for (int w = 0; w < 8; ++w) m[j] = larger((const T*)nullptr, m[j], tops[w][piece][j]);
+            for (int w = 0; w < 8; ++w) t = larger((const T*)nullptr, t, tops[w][col / 8][col % 8 * W / 8]);
+            const uint32_t byte = fp8_scale_byte(sizeof(T) == 4 ? t : (col & 1) ? t & 0xFFFF0000u : t << 16);
+            column_bytes[col] = (uint8_t)byte;
+            if (ordered && c0 + col < p.cols) {
+                uint8_t* s = p.c.scales + ((rb / 4) * p.c.rows + mat * p.cols + c0 + col) * 4;
+                s[rb % 4] = (uint8_t)byte;
+                if (!kExperts && (rb + 1) * 128 >= p.rows)
+                    for (int b = (int)(rb % 4) + 1; b < 4; ++b) s[b] = 0;
+            }
+        }
     }
     if constexpr (BYROWS) {
 #pragma unroll
@@ -152,25 +164,19 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
     }
     if constexpr (BYCOLS) {
         if (!ordered) return;
-        uint32_t bytes[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (kWeights) bytes[j] = whole;
-            else if constexpr (sizeof(T) == 4) bytes[j] = fp8_scale_byte(m[j]);
-            else bytes[j] = fp8_scale_byte((j & 1) ? m[j / 2] & 0xFFFF0000u : m[j / 2] << 16);
-            turned[(piece * 8 + j) * 32 + (quad ^ ((piece & 7) * 4))] = codes_down(v, j, bytes[j]);
+        u32x2 bytes = {whole * 0x01010101u, whole * 0x01010101u};      // of the lane's columns
+        if constexpr (!kWeights) {
+            __syncthreads();
+            bytes = *reinterpret_cast<const u32x2*>(column_bytes + piece * 8);
+        } else if (threadIdx.x < 128 && c0 + threadIdx.x < p.cols) {
+            uint8_t* s = p.c.scales + ((rb / 4) * p.c.rows + mat * p.cols + c0 + threadIdx.x) * 4;
+            s[rb % 4] = (uint8_t)whole;
+            if ((rb + 1) * 128 >= p.rows)
+                for (int b = (int)(rb % 4) + 1; b < 4; ++b) s[b] = 0;
         }
-        const bool last = !kExperts && (rb + 1) * 128 >= p.rows;
-        if (wave == 0 && lane < 16) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (c + j >= p.cols) break;
-                uint8_t* s = p.c.scales + ((rb / 4) * p.c.rows + mat * p.cols + c + j) * 4;
-                s[rb % 4] = (uint8_t)bytes[j];
-                if (last)
-                    for (int b = (int)(rb % 4) + 1; b < 4; ++b) s[b] = 0;
-            }
-        }
+        for (int j = 0; j < 8; ++j)
+            turned[(piece * 8 + j) * 32 + (quad ^ ((piece & 7) * 4))] = codes_down(v, j, bytes[j / 4] >> (8 * (j % 4)) & 255u);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
