@@ -20,8 +20,8 @@ Packed packed(uint8_t* buf, int64_t rows, int64_t cols) {
 }
 
 // Blocks along the rows.  A wave takes four rows of 512 columns, the columns of a word of scale bytes, eight elements a lane: the 16 lanes of
-// a block find its largest magnitude by four exchanges in registers.  Bound: memory; 16384 x 8192 bfloat16 61 us, 6.6 TB/s.
-template <typename T>
+// a block find its largest magnitude by four exchanges in registers.  Bound: memory; 16384 x 8192 bfloat16 64 us, 6.3 TB/s.
+template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void k_fp8_rows(const T* src, int64_t ld, int64_t rows, int64_t cols, Packed to, int groups) {
     const int lane = threadIdx.x % kWave;
     const int64_t band = blockIdx.x / groups;
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(256) void k_fp8_rows(const T* src, int64_t ld, int6
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const T* from = src + (r0 + i) * ld + c;
-        if (r0 + i < rows && left >= 8) load8(from, v[i]);
+        if (r0 + i < rows && left >= 8) load8<PAST>(from, v[i]);
         else load8(from, r0 + i < rows ? (int)max(left, (int64_t)0) : 0, v[i]);
     }
 #pragma unroll
@@ -62,8 +62,9 @@ enum class Tiles { kBlocks, kWeights, kExperts };
 // Tiles of 128 x 128 of src, which is read once: blocks along the rows and / or along the columns, or (weights) the tile as one block,
 // written both ways.  A lane has eight columns of four rows, a wave 128 columns of 16 rows; codes that leave by columns are words
 // of four rows each and turn in LDS, where word q of a column lies at q ^ (4 * (column / 8 % 8)), off its neighbours' banks.  Bound: memory, written in
-// pieces of 128 bytes; 8192 x 8192 bfloat16 both ways 38 us, 7.0 TB/s (part of it stays in the caches), 65536 x 2048 in the order of 32 experts 93 us, 5.8.
-template <typename T, Tiles KIND, bool BYROWS, bool BYCOLS>
+// pieces of 128 bytes; 8192 x 8192 both ways, bfloat16 45 us, 5.9 TB/s, fp32 76, 5.3; 65536 x 2048 bfloat16 in the order of 32 experts 87, 6.2.  Neighbours in bands
+// of row tiles, so that these pieces lie together by columns too, gained 7 % at 16384 x 8192 and lost 4 % at 8192 x 8192.
+template <typename T, Tiles KIND, bool BYROWS, bool BYCOLS, bool PAST>
 __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
     constexpr int W = Eight<T>::kWords;
     constexpr bool kWeights = KIND == Tiles::kWeights, kExperts = KIND == Tiles::kExperts;
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
         }
         const T* from = src + mat * p.stride + r * p.ld + c;
         const int64_t left = in ? p.cols - c : 0;
-        if (left >= 8) load8(from, v[i]);
+        if (left >= 8) load8<PAST>(from, v[i]);
         else load8(from, (int)max(left, (int64_t)0), v[i]);
     }
     uint32_t m[W];                                        // the largest of each column (pair of columns)
@@ -188,13 +189,28 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
     }
 }
 
-template <typename T, Tiles KIND>
-daq_status launch_tiles(const T* src, TileArgs p, int64_t tiles, hipStream_t st) {
+// Large sources whose rows begin with a line are read past the caches, which then hold more of the codes, for the products that follow too.  us with and without, bfloat16
+// 16384 x 8192: both ways 88 and 115, by columns 70 and 93, by rows 64.5 and 69, and all of a layer of 8192 outputs 793 and 825; both ways 8192 x 8192 47.5 and 45.3, 12288 x 8192 65
+// and 82, 16384 x 16384 250 and 234; fp32 in tiles of 128 no difference.  Where lines are shared between pieces they would be read twice (30000 x 5000: 136 and 122).
+bool past_caches(const void* src, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
+    return rows * cols >= (int64_t)96 << 20 && (uintptr_t)src % 128 == 0 && ld * size % 128 == 0;
+}
+
+template <typename T, Tiles KIND, bool PAST>
+daq_status launch_tiles(const T* src, const TileArgs& p, int64_t tiles, hipStream_t st) {
     const dim3 grid((unsigned)(tiles * p.col_tiles));
     const bool r = p.r.codes != nullptr, c = p.c.codes != nullptr;
-    const auto kernel = !r ? k_fp8_tiles<T, KIND, false, true> : c || KIND == Tiles::kExperts ? k_fp8_tiles<T, KIND, true, true> : k_fp8_tiles<T, KIND == Tiles::kExperts ? Tiles::kBlocks : KIND, true, false>;
+    const auto kernel = !r ? k_fp8_tiles<T, KIND, false, true, PAST>
+                           : c || KIND == Tiles::kExperts ? k_fp8_tiles<T, KIND, true, true, PAST> : k_fp8_tiles<T, KIND == Tiles::kExperts ? Tiles::kBlocks : KIND, true, false, PAST>;
     DAQ_LAUNCH("fp8_tiles", st, hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, src, p));
     return DAQ_OK;
+}
+template <Tiles KIND>
+daq_status launch_tiles(const void* src, int dtype, const TileArgs& p, int64_t tiles, hipStream_t st) {
+    if (dtype == DAQ_FP32) return launch_tiles<float, KIND, false>(static_cast<const float*>(src), p, tiles, st);
+    if constexpr (KIND != Tiles::kWeights)      // (rows that several experts take are read again)
+        if (p.picks == 0 && past_caches(src, p.rows, p.cols, p.ld, 2)) return launch_tiles<uint16_t, KIND, true>(static_cast<const uint16_t*>(src), p, tiles, st);
+    return launch_tiles<uint16_t, KIND, false>(static_cast<const uint16_t*>(src), p, tiles, st);
 }
 
 // Eight columns of a row a lane.
@@ -221,15 +237,19 @@ daq_status source_check(const void* src, int dtype, int64_t cols, int64_t ld) {
 
 }  // namespace
 
-daq_status fp8_quantize_rows(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint8_t* dst, hipStream_t st) {
-    const Packed to = packed(dst, rows, cols);
+template <typename T, bool PAST>
+static daq_status launch_rows(const void* src, int64_t rows, int64_t cols, int64_t ld, const Packed& to, hipStream_t st) {
     const int64_t groups = ceil_div(cols, kFp8Group);
     const dim3 grid((unsigned)(ceil_div(rows, 16) * groups));
-    if (dtype == DAQ_BF16)
-        DAQ_LAUNCH("fp8_rows", st, hipLaunchKernelGGL(k_fp8_rows<uint16_t>, grid, dim3(256), 0, st, static_cast<const uint16_t*>(src), ld, rows, cols, to, (int)groups));
-    else
-        DAQ_LAUNCH("fp8_rows", st, hipLaunchKernelGGL(k_fp8_rows<float>, grid, dim3(256), 0, st, static_cast<const float*>(src), ld, rows, cols, to, (int)groups));
+    const auto kernel = k_fp8_rows<T, PAST>;
+    DAQ_LAUNCH("fp8_rows", st, hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, static_cast<const T*>(src), ld, rows, cols, to, (int)groups));
     return DAQ_OK;
+}
+daq_status fp8_quantize_rows(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint8_t* dst, hipStream_t st) {
+    const Packed to = packed(dst, rows, cols);
+    const bool past = past_caches(src, rows, cols, ld, dtype == DAQ_BF16 ? 2 : 4);
+    if (dtype == DAQ_BF16) return past ? launch_rows<uint16_t, true>(src, rows, cols, ld, to, st) : launch_rows<uint16_t, false>(src, rows, cols, ld, to, st);
+    return past ? launch_rows<float, true>(src, rows, cols, ld, to, st) : launch_rows<float, false>(src, rows, cols, ld, to, st);
 }
 
 }  // namespace daq
@@ -263,8 +283,7 @@ extern "C" daq_status daq_fp8_quantize(const void* src, daq_dtype dtype, int64_t
     }
     TileArgs p{ld, 0, rows, cols, (int)ceil_div(cols, 128), ceil_div(rows, 128), packed(by_rows, rows, cols), packed(by_columns, cols, rows), nullptr, nullptr, 0, 0};
     if (!grid_ok(p.row_tiles * p.col_tiles, 512)) return DAQ_ERR_UNSUPPORTED;
-    return dtype == DAQ_BF16 ? launch_tiles<uint16_t, Tiles::kBlocks>(static_cast<const uint16_t*>(src), p, p.row_tiles, st)
-                             : launch_tiles<float, Tiles::kBlocks>(static_cast<const float*>(src), p, p.row_tiles, st);
+    return launch_tiles<Tiles::kBlocks>(src, dtype, p, p.row_tiles, st);
 }
 
 extern "C" daq_status daq_fp8_quantize_weights(const void* src, daq_dtype dtype, int64_t count, int64_t rows, int64_t cols, int64_t ld,
@@ -280,8 +299,7 @@ extern "C" daq_status daq_fp8_quantize_weights(const void* src, daq_dtype dtype,
     if (rc != DAQ_OK) return rc;
     TileArgs p{ld, stride, rows, cols, (int)ceil_div(cols, 128), ceil_div(rows, 128), packed(dst, count * rows, cols), packed(dst_t, count * cols, rows), nullptr, nullptr, 0, 0};
     if (!grid_ok(count * p.row_tiles * p.col_tiles, 512)) return DAQ_ERR_UNSUPPORTED;
-    return dtype == DAQ_BF16 ? launch_tiles<uint16_t, Tiles::kWeights>(static_cast<const uint16_t*>(src), p, count * p.row_tiles, (hipStream_t)stream)
-                             : launch_tiles<float, Tiles::kWeights>(static_cast<const float*>(src), p, count * p.row_tiles, (hipStream_t)stream);
+    return launch_tiles<Tiles::kWeights>(src, dtype, p, count * p.row_tiles, (hipStream_t)stream);
 }
 
 extern "C" daq_status daq_fp8_dequantize(const uint8_t* src, int64_t rows, int64_t cols, void* dst, daq_dtype dtype, int64_t ld, void* stream) {
@@ -328,6 +346,5 @@ extern "C" daq_status daq_experts_quantize(const daq_experts* plan, const void* 
     if (by_rows && !both) rc = fp8_quantize_rows(src, dtype, rows, cols, ld, by_rows, st);
     if (rc != DAQ_OK || !by_columns) return rc;
     TileArgs p{ld, 0, rows, cols, (int)col_tiles, tiles, packed(both ? by_rows : nullptr, rows, cols), packed(by_columns, cols, columns), plan->table, plan->rows, plan->experts, sorted ? 0 : plan->picks};
-    return dtype == DAQ_BF16 ? launch_tiles<uint16_t, Tiles::kExperts>(static_cast<const uint16_t*>(src), p, tiles + both, st)
-                             : launch_tiles<float, Tiles::kExperts>(static_cast<const float*>(src), p, tiles + both, st);
+    return launch_tiles<Tiles::kExperts>(src, dtype, p, tiles + both, st);
 }

@@ -13,13 +13,18 @@ struct Eight {
     static constexpr int kWords = (int)sizeof(T) * 2;
     uint32_t w[kWords];
 };
+// PAST: past the caches, which keep what they have.
+template <bool PAST = false>
 __device__ __forceinline__ void load8(const uint16_t* p, Eight<uint16_t>& v) {
-    const u32x4 q = *reinterpret_cast<const u32x4_a2*>(p);
+    const u32x4_a2* from = reinterpret_cast<const u32x4_a2*>(p);
+    const u32x4 q = PAST ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v.w[i] = q[i];
 }
+template <bool PAST = false>
 __device__ __forceinline__ void load8(const float* p, Eight<float>& v) {
-    const u32x4 a = *reinterpret_cast<const u32x4_a4*>(p), b = *reinterpret_cast<const u32x4_a4*>(p + 4);
+    const u32x4_a4* from = reinterpret_cast<const u32x4_a4*>(p);
+    const u32x4 a = PAST ? __builtin_nontemporal_load(from) : *from, b = PAST ? __builtin_nontemporal_load(from + 1) : from[1];
 #pragma unroll
     for (int i = 0; i < 4; ++i) v.w[i] = a[i], v.w[4 + i] = b[i];
 }

@@ -300,3 +300,25 @@ def test_offsets_beyond_32_bits():
     part = daq.fp8_quantize(daq.fp8_dequantize(a)[ends].contiguous())
     want = daq.fp8_matmul(part, b, dtype=torch.float32)
     assert bool(((out[ends].float() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -5).all())
+
+
+@pytest.mark.parametrize("M,K,ld", [(12300, 8193, 8256), (24577, 4160, 4160), (25000, 4100, 4100)])
+def test_large_sources(M, K, ld):
+    """Sources of 96 Mi elements and more, whose rows begin with a line or do not: the same buffers as of their parts."""
+    x = torch.randn(M, ld, device="cuda", dtype=torch.bfloat16)[:, :K]
+    by_rows, by_columns = daq.fp8_quantize_both(x)
+    L, pitch = daq.layout_fp8(M, K), daq.layout_fp8(M, K).pitch
+    for one, other in ((daq.fp8_quantize(x), by_rows), (daq.fp8_quantize(x, columns=True), by_columns)):
+        lay = daq.layout_fp8(one.rows, one.cols)
+        for first, n in ((0, one.rows * lay.pitch), (lay.off_scales, -(-one.cols // 512) * one.rows * 4)):
+            assert torch.equal(one.buf[first:first + n], other.buf[first:first + n])
+    C = daq.layout_fp8(K, M)
+    codes, codes_t = by_rows.buf[:M * pitch].view(M, pitch), by_columns.buf[:K * C.pitch].view(K, C.pitch)
+    scales = by_rows.buf[L.off_scales:L.off_scales + -(-K // 512) * M * 4].view(-1, M, 4)
+    for first in (0, 4096, M // 128 * 128 - 256):                          # whole blocks of rows
+        part = x[first:first + 256].contiguous()
+        n, P = part.shape[0], daq.layout_fp8(part.shape[0], K)
+        q, qc = daq.fp8_quantize_both(part)
+        assert torch.equal(q.buf[:n * P.pitch].view(n, -1), codes[first:first + n])
+        assert torch.equal(q.buf[P.off_scales:P.off_scales + -(-K // 512) * n * 4].view(-1, n, 4), scales[:, first:first + n])
+        assert torch.equal(qc.buf[:K * n].view(K, n), codes_t[:, first:first + n])
