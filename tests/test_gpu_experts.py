@@ -445,3 +445,28 @@ def test_large_products_of_experts(sorted_rows):
         for to in DT:
             assert np.all(np.abs(grads[to][e] - vd @ vx.T) <= _bound(int(counts[e]), np.abs(vd) @ np.abs(vx).T, vd @ vx.T, to))
     assert bool((out[total:] == 7).all())
+
+
+@pytest.mark.parametrize("D,ld", [(4096, 4096), (4090, 4096), (4100, 4100)])
+def test_sums_of_many_rows(D, ld):
+    """256 MiB and more of experts' rows, some of them behind the last one, the rows' ends inside a lane's eight columns too."""
+    T, k, E = 8400, 4, 8
+    plan = daq.experts_plan(_chosen(T, k, E, 5).cuda(), E)
+    y, dout = torch.randn(T * k, ld, device="cuda", dtype=torch.bfloat16)[:, :D], torch.randn(T, D, device="cuda", dtype=torch.bfloat16)
+    w = torch.rand(T, k, device="cuda")
+    dy = torch.full((T * k, ld), 7.0, device="cuda", dtype=torch.bfloat16)
+    out = daq.experts_combine(y, plan, w)
+    _, dw = daq.experts_combine_backward(dout, y, plan, w, out=dy[:, :D])
+    n = int(plan.counts.sum())
+    assert bool((dy[n:] == 7).all()) and bool((dy[:, D:] == 7).all())
+    for first in range(0, T, 1050):                                        # in parts: 64 bits take memory
+        part = slice(first, first + 1050)
+        place, there = plan.place[part].long(), plan.place[part] >= 0
+        rows = torch.where(there[..., None], y[place.clamp(min=0)].double(), 0.0)
+        terms = w[part].double()[..., None] * rows
+        want, size = terms.sum(1), terms.abs().sum(1)
+        assert bool(((out[part].double() - want).abs() <= 2.0 ** -8 * want.abs() + (k + 1) * 2.0 ** -24 * size * (1 + 2.0 ** -8)).all())
+        d = dout[part].double()[:, None]
+        assert bool((((rows * d).sum(2) - dw[part].double()).abs() <= (-(-D // 512) * 8 + 7) * 2.0 ** -24 * (rows * d).abs().sum(2)).all())
+        g = w[part].double()[..., None] * d
+        assert bool(((dy[place.clamp(min=0)][:, :, :D].double() - g).abs() <= (2.0 ** -8 + 2.0 ** -23) * g.abs())[there].all())
