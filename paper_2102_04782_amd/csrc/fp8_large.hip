@@ -18,7 +18,8 @@ constexpr int kPlaces = kB * kB;                            // products of a ste
 // a product 64.  A stage is read out in the first half of its first step, then the stage after the next is asked for in its place, while
 // the next one has until the second step to land.  Behind a tile's last stage the first two of the next tile are asked for before its results leave.
 // Bound: the matrix cores at the card's power limit.  16384 x 8192 x 8192 700 to 780 us (2.8 to 3.1 PFLOP/s; a loop of these instructions on registers
-// reaches 4.5), 8192 x 8192 x 4096 190 to 200 when others run before it; busy 79 to 85 % of the cycles, at 1.75 to 2.2 GHz.  Four waves of 128 x 128 read a third less from LDS than
+// reaches 4.5), 8192 x 8192 x 4096 190 to 200 when others run before it; busy 78 to 85 % of the cycles, at 1.75 to 2.2 GHz.  Where sums are short a tile's start and results count:
+// 65536 x 2048 x 2048 215 us, and 285 as the rows of 32 experts (2176 tiles instead of 2048; the cores are busy 45 %).  Four waves of 128 x 128 read a third less from LDS than
 // eight of 128 x 64, which reached 2.7 PFLOP/s.
 
 // The lane, as a value that the compiler works on where it stands: places of lanes that it kept from tile to tile would cost the registers that
