@@ -281,9 +281,11 @@ def test_offsets_beyond_32_bits():
     x[ends] = torch.randn(80, K, device="cuda").bfloat16()
     w, _ = daq.fp8_quantize_weights(torch.randn(72, K, device="cuda"))
     q, small = daq.fp8_quantize(x), daq.fp8_quantize(x[ends].contiguous())
+    va, vb = _np(daq.fp8_dequantize(small)), _np(daq.fp8_dequantize(w))
+    exact, absolute = va @ vb.T, np.abs(va) @ np.abs(vb).T
     for to in DT:
-        got, want = daq.fp8_matmul(q, w, dtype=to)[ends].double(), daq.fp8_matmul(small, w, dtype=torch.float32).double()
-        assert bool(((got - want).abs() <= 2.0 ** -6 * want.abs() + 1e-2).all())
+        got = daq.fp8_matmul(q, w, dtype=to)[ends].double()
+        assert np.all(np.abs(_np(got) - exact) <= _bound(K, absolute, exact, to))
         assert torch.equal(got, daq.fp8_linear(x, w, dtype=to)[ends].double())
     assert torch.equal(daq.fp8_dequantize(q, dtype=torch.bfloat16)[ends], daq.fp8_dequantize(small, dtype=torch.bfloat16))
     c = daq.fp8_quantize(x, columns=True)
@@ -297,9 +299,9 @@ def test_offsets_beyond_32_bits():
     a, b = daq.fp8_quantize(torch.randn(70000, 128, device="cuda")), daq.fp8_quantize(torch.randn(36000, 128, device="cuda"))
     out = daq.fp8_matmul(a, b)
     ends = torch.cat((torch.arange(40), torch.arange(70000 - 40, 70000))).cuda()
-    part = daq.fp8_quantize(daq.fp8_dequantize(a)[ends].contiguous())
-    want = daq.fp8_matmul(part, b, dtype=torch.float32)
-    assert bool(((out[ends].float() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -5).all())
+    va, vb = _np(daq.fp8_dequantize(a)[ends]), _np(daq.fp8_dequantize(b))
+    exact, absolute = va @ vb.T, np.abs(va) @ np.abs(vb).T
+    assert np.all(np.abs(_np(out[ends]) - exact) <= _bound(128, absolute, exact, torch.bfloat16))
 
 
 @pytest.mark.parametrize("M,K,ld", [(12300, 8193, 8256), (24577, 4160, 4160), (25000, 4100, 4100)])
@@ -322,3 +324,23 @@ def test_large_sources(M, K, ld):
         assert torch.equal(q.buf[:n * P.pitch].view(n, -1), codes[first:first + n])
         assert torch.equal(q.buf[P.off_scales:P.off_scales + -(-K // 512) * n * 4].view(-1, n, 4), scales[:, first:first + n])
         assert torch.equal(qc.buf[:K * n].view(K, n), codes_t[:, first:first + n])
+
+
+@pytest.mark.parametrize("M,N", [(2, 5), (70, 40), (300, 270)])
+def test_the_longest_sums(M, N):
+    """K = 2^23 - 128.  Products are multiples of 1/2, equal ones side by side, and their sums below 2^23 (of the first row: multiples of 64 below 2^24): fp32 holds
+    every sum on the way, in any order, so results in fp32 are exact and those in bfloat16 are off by their rounding.  The last row's cancel."""
+    K = (1 << 23) - 128
+    a = torch.full((M, K), 0.5, device="cuda", dtype=torch.bfloat16)
+    a[0] = 0
+    a[0, -128:] = 448.0
+    a[-1, 1::2] = -0.5
+    b = torch.ones(N, K, device="cuda", dtype=torch.bfloat16)
+    b[:, -128:] = torch.arange(1, N + 1, device="cuda")[:, None].to(torch.bfloat16)
+    last = daq.fp8_dequantize(daq.fp8_quantize(b[:, -128:].contiguous()))[:, 0].double() * 128
+    want = (0.5 * (K - 128) + 0.5 * last).expand(M, N).clone()
+    want[0] = 448 * last
+    want[-1] = 0
+    qa, qb = daq.fp8_quantize(a), daq.fp8_quantize(b)
+    assert torch.equal(daq.fp8_matmul(qa, qb, dtype=torch.float32).double(), want)
+    assert bool(((daq.fp8_matmul(qa, qb).double() - want).abs() <= 2.0 ** -8 * want).all())

@@ -194,3 +194,33 @@ def test_two_calls_at_once_on_two_streams():
             got[i].append(daq.fp8_linear(a[i], w[i], stream=streams[i]))
     torch.cuda.synchronize()
     assert all(torch.equal(o, want[i]) for i in range(2) for o in got[i])
+
+
+def test_two_graphs_in_turn():
+    """Sums in parts and plans of many workgroups, whose workspaces are each graph's own: replayed in turn on other inputs, with eager calls between."""
+    def step(a, b, chosen):
+        qa, qb = daq.fp8_quantize(a), daq.fp8_quantize(b)
+        plan = daq.experts_plan(chosen, 24)
+        return daq.fp8_matmul(qa, qb), daq.fp8_matmul(qa, qb, dtype=torch.float32), plan.counts, plan.table, plan.rows, plan.place
+
+    graphs = []
+    for _ in range(2):
+        ins = (torch.randn(130, 5000, device="cuda"), torch.randn(70, 5000, device="cuda"), torch.zeros(9000, 4, dtype=torch.int32, device="cuda"))
+        step(*ins)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = step(*ins)
+        graphs.append((ins, graph, outs))
+    for n in range(3):
+        for seed, (ins, _, _) in enumerate(graphs):
+            g = torch.Generator(device="cuda").manual_seed(10 * n + seed)
+            ins[0].normal_(generator=g)
+            ins[1].normal_(generator=g)
+            ins[2].random_(-1, 24, generator=g)
+        for _, graph, _ in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        kept = [[t.clone() for t in outs] for _, _, outs in graphs]
+        for (ins, _, _), got in zip(graphs, kept):
+            assert all(torch.equal(a, b) for a, b in zip(got, step(*ins)))
