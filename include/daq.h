@@ -712,7 +712,8 @@ daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void* X, daq_dt
  *   weights  out  fp32 [tokens][picks];  chosen  out  int32 [tokens][picks]
  * daq_route_backward -- the gradient of the logits from that of the weights, the choice being what it was; in fp32, rounded once to the
  * type of the logits.  Places of expert -1 count for nothing, and dweights is not read there.
- * Limits: experts <= 1024, picks <= 32, groups <= 64, tokens < 2^28.
+ * Limits: experts <= 1024, picks <= 32, groups <= 64; tokens, as a launch takes fewer than 2^32 threads: of daq_route up to 2^26 - 4, of
+ * daq_route_backward up to 2^28 - 16 (of more than 16 picks 2^27 - 8).
  * ------------------------------------------------------------------------------------------- */
 typedef enum { DAQ_SCORES_SOFTMAX = 0, DAQ_SCORES_SIGMOID = 1 } daq_scores;
 typedef struct {

@@ -706,6 +706,7 @@ extern "C" daq_status daq_route(int64_t tokens, int32_t experts, const void* log
     const daq_status rc = route_check(tokens, experts, logits, dtype, ld, opts);
     if (rc != DAQ_OK || tokens == 0) return rc;
     if (!a4(bias) || !weights || !a4(weights) || !chosen || !a4(chosen)) return DAQ_ERR_INVALID_ARG;
+    if (!grid_ok(ceil_div(tokens, 4), 256)) return DAQ_ERR_UNSUPPORTED;
     const RouteArgs p{tokens, ld, experts, opts->picks, opts->groups, opts->top_groups, experts / opts->groups, opts->scores == DAQ_SCORES_SIGMOID,
                       opts->renormalize != 0, (double)opts->scale, bias, weights, chosen};
     return dtype == DAQ_BF16 ? launch_route(static_cast<const uint16_t*>(logits), p, (hipStream_t)stream)
@@ -720,6 +721,7 @@ extern "C" daq_status daq_route_backward(int64_t tokens, int32_t experts, const 
     // what is computed in 64 bits takes a wave as long for one token's places as for several's: four tokens a wave, once there are enough of them (16384 x 256,
     // 8 places, 7.5 us instead of 12)
     const int slot = opts->picks <= 8 ? 3 : opts->picks <= 16 ? 4 : 5, each = tokens >= 8192 ? std::min(4, kWave >> slot) : 1;
+    if (!grid_ok(ceil_div(tokens, 4 * each), 256)) return DAQ_ERR_UNSUPPORTED;
     const RouteBackArgs p{tokens, ld, ldd, experts, opts->picks, opts->scores == DAQ_SCORES_SIGMOID, opts->renormalize != 0, each, slot, opts->scale, dweights, chosen};
     return dtype == DAQ_BF16 ? launch_back(static_cast<const uint16_t*>(logits), static_cast<uint16_t*>(dlogits), p, (hipStream_t)stream)
                              : launch_back(static_cast<const float*>(logits), static_cast<float*>(dlogits), p, (hipStream_t)stream);
