@@ -254,18 +254,18 @@ __global__ __launch_bounds__(256) void k_fp8_sum(const float* parts, int splits,
     }
 }
 
-// Tiles are counted, and eight more of them and four bands, within 31 bits.
-bool tiles_ok(int64_t tm, int64_t tn, int64_t experts) { return tm <= (0x7FFFFFFF - 64) / (4 * tn) && tm * tn + kXcd <= (0x7FFFFFFF - 64) / experts; }
+int form_edge(Fp8Form form) { return form == Fp8Form::k256 ? 256 : form == Fp8Form::k128 ? 128 : 64; }
+// Tiles are counted, and eight more of them and four bands, within 31 bits, and a launch has fewer than 2^32 threads (`experts` times so many tiles).
+bool tiles_fit(Fp8Form form, int64_t tm, int64_t N, int64_t experts) {
+    const int64_t tn = ceil_div(N, form_edge(form));
+    return tm <= (0x7FFFFFFF - 64) / (4 * tn) && tm * tn + kXcd <= (0x7FFFFFFF - 64) / experts &&
+           grid_ok(round_up(tm * tn, kXcd) * experts, form == Fp8Form::k64 ? 128 : 256);
+}
 
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
-daq_status launch_product(ProductArgs p, hipStream_t st) {
+daq_status launch_product(const ProductArgs& p, hipStream_t st) {
     using Product = Fp8Product<WR, WC, RB, CB, SLOTS, EXACT>;
-    const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, Product::kRows), tn = ceil_div(p.N, Product::kCols);
-    if (!tiles_ok(tm, tn, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
-    p.tiles_m = (int)tm;
-    p.tiles_n = (int)tn;
     const int64_t tiles = tile_groups<OF>(p);
-    if (!grid_ok(tiles, Product::kWaves * 64)) return DAQ_ERR_UNSUPPORTED;
     const auto kernel = k_fp8_product<WR, WC, RB, CB, SLOTS, EXACT, OF>;
     if (!allow_lds((const void*)kernel, Product::kLdsBytes)) return DAQ_ERR_HIP;
     DAQ_LAUNCH("fp8_product", st, hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)p.splits), dim3(64 * WR * WC), Product::kLdsBytes, st, p));
@@ -273,18 +273,17 @@ daq_status launch_product(ProductArgs p, hipStream_t st) {
 }
 template <Of OF>
 daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) {
+    const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, form_edge(form));
+    if (!tiles_fit(form, tm, p.N, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
+    p.tiles_m = (int)tm;
+    p.tiles_n = (int)ceil_div(p.N, form_edge(form));
     if (exact) return form == Fp8Form::k64 ? launch_product<2, 1, 1, 2, 4, true, OF>(p, st) : launch_product<2, 2, 2, 2, 2, true, OF>(p, st);
     if (form == Fp8Form::k64) return launch_product<2, 1, 1, 2, 4, false, OF>(p, st);
     if (form == Fp8Form::k128) {
         // a workgroup to a CU: four stages in LDS (512 x 8192 x 8192 39.4 us instead of 48); two to a CU: two each (2048 x 4096 x 4096 32.8 instead of 38)
-        const int64_t tiles = (OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, 128)) * ceil_div(p.N, 128) * (OF == Of::kExpertWeights ? p.experts : 1);
+        const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * (OF == Of::kExpertWeights ? p.experts : 1);
         return tiles <= 256 ? launch_product<2, 2, 2, 2, 4, false, OF>(p, st) : launch_product<2, 2, 2, 2, 2, false, OF>(p, st);
     }
-    const int64_t tm = OF == Of::kExpertRows ? p.tiles_m : ceil_div(p.M, 256), tn = ceil_div(p.N, 256);
-    if (!tiles_ok(tm, tn, OF == Of::kExpertWeights ? p.experts : 1)) return DAQ_ERR_UNSUPPORTED;
-    p.tiles_m = (int)tm;
-    p.tiles_n = (int)tn;
-    if (!grid_ok(tile_groups<OF>(p), 256)) return DAQ_ERR_UNSUPPORTED;
     return fp8_large(OF, p, st);
 }
 
@@ -320,11 +319,10 @@ Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
     pl.per_split = (int)stages;
     if (pl.form == Fp8Form::kFew) return pl;
     // parts of the summed axis, of four stages or more, for what they and the launch that adds them up (at 3 TB/s) take less
-    const int64_t edge = pl.form == Fp8Form::k256 ? 256 : pl.form == Fp8Form::k128 ? 128 : 64;
-    double least = fp8_cost(pl.form, tiles(edge), (double)stages, exact);
+    double least = fp8_cost(pl.form, tiles(form_edge(pl.form)), (double)stages, exact);
     for (const Fp8Form form : {Fp8Form::k64, Fp8Form::k128})
         for (int s = 2; s <= 16 && stages >= 4 * s; s *= 2) {
-            const double cost = fp8_cost(form, tiles(form == Fp8Form::k64 ? 64 : 128) * s, std::ceil((double)stages / s), exact) + 3.5 + s * (double)M * (double)N * 8 / 3e6;
+            const double cost = fp8_cost(form, tiles(form_edge(form)) * s, std::ceil((double)stages / s), exact) + 3.5 + s * (double)M * (double)N * 8 / 3e6;
             if (cost >= least) continue;
             least = cost;
             pl.form = form;
@@ -338,6 +336,12 @@ static bool one_launch(int64_t M, int64_t N, int64_t K, int y_dtype) {
     return fp8_raw_rows(M, K) && fp8_plan(M, N, K, y_dtype == DAQ_FP32).form == Fp8Form::kFew;
 }
 
+// Workgroups of the launch that adds up a product's parts.
+static int64_t sum_groups(int64_t M, int64_t N) { return ceil_div(M * ceil_div(N, 4), 256); }
+// Whether the launches of a product can be made.
+static bool product_fits(const Fp8Plan& pl, int64_t M, int64_t N) {
+    return pl.form == Fp8Form::kFew || (tiles_fit(pl.form, ceil_div(M, form_edge(pl.form)), N, 1) && (pl.splits == 1 || grid_ok(sum_groups(M, N), 256)));
+}
 static daq_status product_sizes(int64_t M, int64_t N, int64_t K) {
     if (M < 0 || N <= 0 || K < 0) return DAQ_ERR_INVALID_ARG;
     daq_status rc = matrix_size(M, K > 0 ? K : 1);
@@ -373,11 +377,9 @@ static daq_status fp8_matmul(int64_t M, int64_t N, int64_t K, const uint8_t* A, 
     }
     p.d = ws;
     p.ldd = round_up(N, 4);
-    const int64_t blocks = ceil_div(M * ceil_div(N, 4), 256);
-    if (!grid_ok(blocks, 256)) return DAQ_ERR_UNSUPPORTED;
     const daq_status rc = launch_form<Of::kWhole>(pl.form, exact, p, st);
     if (rc != DAQ_OK) return rc;
-    DAQ_LAUNCH("fp8_sum", st, hipLaunchKernelGGL(k_fp8_sum, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const float*>(ws), pl.splits, M, N, D, ldd, dtype == DAQ_BF16, accumulate));
+    DAQ_LAUNCH("fp8_sum", st, hipLaunchKernelGGL(k_fp8_sum, dim3((unsigned)sum_groups(M, N)), dim3(256), 0, st, static_cast<const float*>(ws), pl.splits, M, N, D, ldd, dtype == DAQ_BF16, accumulate));
     return DAQ_OK;
 }
 
@@ -389,8 +391,9 @@ extern "C" daq_status daq_fp8_matmul_workspace(int64_t M, int64_t N, int64_t K, 
     if (!bytes || !dtype_ok(dtype)) return DAQ_ERR_INVALID_ARG;
     *bytes = 0;
     const daq_status rc = product_sizes(M, N, K);
-    if (rc != DAQ_OK || M == 0 || K == 0) return rc;
+    if (rc != DAQ_OK || M == 0) return rc;
     const Fp8Plan pl = fp8_plan(M, N, K, dtype == DAQ_FP32);
+    if (!product_fits(pl, M, N)) return DAQ_ERR_UNSUPPORTED;
     if (pl.splits > 1) *bytes = (size_t)round_up(pl.splits * M * round_up(N, 4) * 4, 256);
     return DAQ_OK;
 }
@@ -416,6 +419,7 @@ extern "C" daq_status daq_fp8_linear_workspace(int64_t M, int64_t N, int64_t K, 
     if (!bytes) return DAQ_ERR_INVALID_ARG;
     *bytes = 0;
     if (rc != DAQ_OK || M == 0 || one_launch(M, N, K, y_dtype)) return rc;
+    if (!fp8_rows_grid_ok(M, K)) return DAQ_ERR_UNSUPPORTED;
     daq_fp8_layout L;
     daq_layout_fp8(M, K, &L);
     *bytes = (size_t)L.bytes + product;
@@ -432,7 +436,6 @@ extern "C" daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void
     if (rc != DAQ_OK) return rc;
     if (!X || !elem_aligned(X, x_dtype) || ldx < K || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
     if (one_launch(M, N, K, y_dtype)) return fp8_matmul(M, N, K, nullptr, X, x_dtype, ldx, W, Y, y_dtype, ldy, 0, nullptr, (hipStream_t)stream);
-    if (!fp8_rows_grid_ok(M, K)) return DAQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < need || !aligned256(workspace)) return DAQ_ERR_WORKSPACE;
     uint8_t* xq = static_cast<uint8_t*>(workspace);
     daq_fp8_layout L;
@@ -456,6 +459,12 @@ static bool experts_one_launch(const daq_experts& plan, int64_t N, int64_t K, in
     return experts_form(plan, N, K, y_dtype == DAQ_FP32) == Fp8Form::kFew && fp8_raw_rows(most_rows(plan), K);
 }
 
+static int64_t experts_tiles(const daq_experts& plan, Fp8Form form) { return most_tiles(plan, form_edge(form)); }
+static bool experts_fit(const daq_experts& plan, int64_t N, int64_t K, bool exact) {
+    const Fp8Form form = experts_form(plan, N, K, exact);
+    return form == Fp8Form::kFew || tiles_fit(form, experts_tiles(plan, form), N, 1);
+}
+
 // X not NULL: A from X, in the call.
 static daq_status experts_product(const daq_experts& plan, int64_t N, int64_t K, const uint8_t* A, const void* X, int x_dtype, int64_t ldx, int sorted,
                                   const uint8_t* W, void* Y, int dtype, int64_t ldy, hipStream_t st) {
@@ -477,7 +486,7 @@ static daq_status experts_product(const daq_experts& plan, int64_t N, int64_t K,
     const bool exact = dtype == DAQ_FP32;
     const Fp8Form form = experts_form(plan, N, K, exact);
     if (form == Fp8Form::kFew) return fp8_few(Of::kExpertRows, p, most_tiles(plan, 64), std::min<int64_t>(most_rows(plan), 64), X, x_dtype, ldx, K, st);
-    p.tiles_m = (int)most_tiles(plan, form == Fp8Form::k256 ? 256 : form == Fp8Form::k128 ? 128 : 64);
+    p.tiles_m = (int)experts_tiles(plan, form);
     return launch_form<Of::kExpertRows>(form, exact, p, st);
 }
 
@@ -529,7 +538,7 @@ extern "C" daq_status daq_experts_linear(const daq_experts* plan, int64_t N, int
     if (!X || !elem_aligned(X, x_dtype) || ldx < K || !W || !aligned256(W)) return DAQ_ERR_INVALID_ARG;
     const int64_t rows = sorted ? plan_slots(*plan) : plan->tokens;
     if (experts_one_launch(*plan, N, K, y_dtype)) return experts_product(*plan, N, K, nullptr, X, x_dtype, ldx, sorted, W, Y, y_dtype, ldy, (hipStream_t)stream);
-    if (!fp8_rows_grid_ok(rows, K)) return DAQ_ERR_UNSUPPORTED;
+    if (!fp8_rows_grid_ok(rows, K) || !experts_fit(*plan, N, K, y_dtype == DAQ_FP32)) return DAQ_ERR_UNSUPPORTED;
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned256(workspace))) return DAQ_ERR_WORKSPACE;
     rc = fp8_quantize_rows(X, x_dtype, rows, K, ldx, static_cast<uint8_t*>(workspace), (hipStream_t)stream);
     if (rc != DAQ_OK) return rc;
