@@ -35,6 +35,12 @@ __device__ __forceinline__ void best_of_wave(double& c, int& at) {
     }
 }
 
+// A sigmoid in 64 bits, by the smaller exponential: e^-l they do not hold where l < -709, the sigmoid down to -745.
+__device__ __forceinline__ double sigmoid_of(double l) {
+    const double ex = exp(-fabs(l));
+    return (l >= 0 ? 1.0 : ex) / (1.0 + ex);
+}
+
 // Values as whole numbers of the same order, for one instruction a comparison; kNoKey is below all of them (it is a NaN's).
 constexpr int kNoKey = (int)0x80000000;
 __device__ __forceinline__ int key_of(float v) {
@@ -105,7 +111,7 @@ __device__ __forceinline__ int choose_exactly(const RouteArgs& p, const float (&
     double c[PER];
     if (p.sigmoid) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) c[i] = 1.0 / (1.0 + exp(-(double)l[i]));
+        for (int i = 0; i < PER; ++i) c[i] = sigmoid_of((double)l[i]);
     } else {
         double sum = 0;
 #pragma unroll
@@ -339,7 +345,7 @@ __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
     const double x = there ? (double)logit_at(row + expert) : 0.0;
     double s = 0, total = 1;
     if (p.sigmoid) {
-        s = 1.0 / (1.0 + exp(-x));
+        s = sigmoid_of(x);
     } else {
         s = exp(x - (there ? (double)most : 0.0));
         if (!p.renormalize) {

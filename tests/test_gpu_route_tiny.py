@@ -1,0 +1,39 @@
+"""The router where the scores of the chosen experts are next to nothing: sums of them that 64 bits hold with few bits, or not at all."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import fp8 as ref
+from paper_2102_04782_amd import binding as daq
+
+pytestmark = pytest.mark.gpu
+
+DT = [torch.float32, torch.bfloat16]
+
+
+def _np(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _tiny(T, dtype):
+    """Logits of -708 to -722: sigmoids down to 2^-1042, which 64 bits hold within 2^-33 of themselves; e^715 they do not hold, nor 1 over such a sigmoid.  The chosen
+    ones' shares are their softmax (a sigmoid is its exponential there, to 2^-1000)."""
+    E, k = 12, 4
+    gen = torch.Generator().manual_seed(T)
+    logits = (-715 + 7 * (2 * torch.rand(T, E, generator=gen) - 1)).to(dtype)
+    chosen = np.argsort(-_np(logits), axis=1, kind="stable")[:, :k]
+    x = np.take_along_axis(_np(logits), chosen, 1)
+    share = np.exp(x - x[:, :1])
+    return logits, chosen, share / share.sum(1, keepdims=True), gen
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("T", [5, 8200])
+def test_sigmoids_of_logits_below_minus_709(T, dtype):
+    """The order is that of the scores, and the weights are off by their rounding and 2^-32 (a score and the sum, 2^-33 each)."""
+    logits, chosen, share, _ = _tiny(T, dtype)
+    for bias in (None, torch.full((12,), 0.0).cuda()):
+        w, e = daq.route(logits.cuda(), 4, daq.SCORES_SIGMOID, bias)
+        assert np.array_equal(_np(e), chosen)
+        assert np.all(np.abs(_np(w) - share) <= (2.0 ** -24 + 2.0 ** -32) * share)
+    assert np.array_equal(ref.route(_np(logits[:5]), 4, "sigmoid")[1], chosen[:5])
