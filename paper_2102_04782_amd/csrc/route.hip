@@ -445,9 +445,9 @@ __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits,
                 total += __shfl_xor(total, k);
                 mean += __shfl_xor(mean, k);
             }
-            const double over = total > 0 ? 1.0 / total : 0.0;
-            s *= over;
-            v -= mean * over;
+            if (!(total > 0)) total = 1.0;      // (all scores are zero)
+            s /= total;                         // (1 over a sum of sigmoids may be beyond 64 bits)
+            v -= mean / total;
         }
         d = (float)(p.scale * v * s * rest);
     }

@@ -37,3 +37,18 @@ def test_sigmoids_of_logits_below_minus_709(T, dtype):
         assert np.array_equal(_np(e), chosen)
         assert np.all(np.abs(_np(w) - share) <= (2.0 ** -24 + 2.0 ** -32) * share)
     assert np.array_equal(ref.route(_np(logits[:5]), 4, "sigmoid")[1], chosen[:5])
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("T", [5, 8200])
+def test_gradients_of_sigmoids_whose_sum_has_no_reciprocal(T, dtype):
+    """share * (g - mean of g): off by its rounding and, shares being off by 2^-32, by that part of the share times what is subtracted."""
+    logits, chosen, share, gen = _tiny(T, dtype)
+    g = torch.randn(T, 4, generator=gen)
+    want, off = np.zeros((T, 12)), np.zeros((T, 12))
+    mean, size = (share * _np(g)).sum(1, keepdims=True), (share * np.abs(_np(g))).sum(1, keepdims=True)
+    np.put_along_axis(want, chosen, share * (_np(g) - mean), 1)
+    np.put_along_axis(off, chosen, share * (np.abs(_np(g)) + 2 * size), 1)
+    got = _np(daq.route_backward(g.cuda(), logits.cuda(), torch.from_numpy(chosen).int().cuda(), daq.SCORES_SIGMOID))
+    step = 2.0 ** -24 + (2.0 ** -8 if dtype == torch.bfloat16 else 0)
+    assert np.all(np.abs(got - want) <= step * np.abs(want) + 2.0 ** -31 * off + 1e-38)
