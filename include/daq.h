@@ -704,7 +704,8 @@ daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void* X, daq_dt
  *   groups > 1: the experts are `groups` runs of neighbours; a group counts the sum of its two best c (its best one where it has no
  *   more); the `top_groups` best groups stay
  *   the `picks` best c of those, in descending order, ties to the lowest index (of groups too)
- *   weight = scale * s / (renormalize ? sum of s over the chosen : 1), 0 where that sum is 0
+ *   weight = scale * s / (renormalize ? sum of s over the chosen : 1), 0 where that sum is 0 (sigmoids below e^-745; of a softmax, renormalised, the weights
+ *   are the softmax of the chosen logits, which has a sum wherever there is one)
  * An expert whose logit or bias is -infinity is never chosen: such places hold the expert -1 and the weight 0, as all of a token
  * do whose logits are all -infinity (a padded one).  A token with a NaN, or with an infinity that makes one (softmax), has the expert -1 and the
  * weight NaN in all its places.

@@ -114,6 +114,14 @@ def scores(logits, kind):
         return np.where(total == 0, 0.0, e / np.where(total == 0, 1.0, total))
 
 
+def _shares(x, s, e, kind):
+    """The scores of a token's experts `e` for their renormalised weights, which depend on these alone: of a softmax those of the row without the others,
+    which 64 bits hold however far below them they are."""
+    if kind == "sigmoid":
+        return s
+    return scores(np.where(np.isin(np.arange(len(x)), e), x, -np.inf)[None], kind)[0]
+
+
 def _best(c, n):
     """The indices of the n largest, in descending order, the lowest of equals first; -infinity is never taken."""
     order = sorted((i for i in range(len(c)) if c[i] > -np.inf), key=lambda i: (-c[i], i))[:n]
@@ -140,6 +148,7 @@ def route(logits, picks, kind, bias=None, groups=1, top_groups=1, renormalize=Tr
         chosen[t, :len(best)] = best
         weights[t, :len(best)] = s[t, best]
         if renormalize:
+            weights[t, :len(best)] = _shares(x[t], s[t], best, kind)[best]
             total = weights[t].sum()
             weights[t] = weights[t] / total if total > 0 else 0
         weights[t] *= scale
@@ -158,6 +167,7 @@ def route_backward(dweights, logits, chosen, kind, renormalize=True, scale=1.0):
         e = chosen[t, at]
         ds = np.zeros(E)
         if renormalize:
+            s[t] = _shares(x[t], s[t], e, kind)
             total = s[t, e].sum()
             if total > 0:
                 for j, k in zip(at, e):

@@ -347,6 +347,8 @@ __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
     if (p.sigmoid) {
         s = sigmoid_of(x);
     } else {
+        // renormalised, they are the chosen ones' own softmax, also where 64 bits hold none of their scores
+        if (p.renormalize) most = of_key(top_of_wave(key_of(there ? (float)x : kNone)));
         s = exp(x - (there ? (double)most : 0.0));
         if (!p.renormalize) {
             total = 0;

@@ -52,3 +52,37 @@ def test_gradients_of_sigmoids_whose_sum_has_no_reciprocal(T, dtype):
     got = _np(daq.route_backward(g.cuda(), logits.cuda(), torch.from_numpy(chosen).int().cuda(), daq.SCORES_SIGMOID))
     step = 2.0 ** -24 + (2.0 ** -8 if dtype == torch.bfloat16 else 0)
     assert np.all(np.abs(got - want) <= step * np.abs(want) + 2.0 ** -31 * off + 1e-38)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("T,E,k", [(5, 12, 3), (8199, 40, 9), (70, 300, 17), (33, 1024, 32)])
+def test_chosen_experts_far_below_the_others(T, E, k, kind, dtype):
+    """A bias that chooses experts 1000 below the others; every third token is an ordinary one.  64 bits hold none of their scores.  A softmax's renormalised weights are the chosen
+    logits' own softmax all the same, and their gradient is its gradient; sigmoids of -1000 sum to zero: no weights, no gradient."""
+    gen = torch.Generator().manual_seed(E)
+    logits = torch.randn(T, E, generator=gen)
+    far = torch.arange(E) % (E // k) == 0
+    far &= torch.cumsum(far, 0) <= k
+    low = torch.arange(T) % 3 != 0
+    logits[low[:, None] & far[None, :]] -= 1000
+    logits = logits.to(dtype)
+    bias = torch.where(far, 2.0, 0.0)
+    g = torch.randn(T, k, generator=gen)
+    weights, chosen = ref.route(_np(logits), k, kind, _np(bias))
+    assert np.all(np.sort(chosen, 1) == np.flatnonzero(far.numpy()))
+    w, e = daq.route(logits.cuda(), k, daq.SCORES_SOFTMAX if kind == "softmax" else daq.SCORES_SIGMOID, bias.cuda())
+    assert np.array_equal(_np(e), chosen) and np.all(np.abs(_np(w) - weights) <= (2.0 ** -24 + 2.0 ** -48) * weights)
+    got = _np(daq.route_backward(g.cuda(), logits.cuda(), e, daq.SCORES_SOFTMAX if kind == "softmax" else daq.SCORES_SIGMOID))
+    if kind == "softmax":
+        x = np.take_along_axis(_np(logits), chosen, 1)
+        share = np.exp(x - x.max(1, keepdims=True))
+        share /= share.sum(1, keepdims=True)
+        assert np.all(np.abs(weights - share) <= 2.0 ** -48 * share)
+        want = np.zeros((T, E))
+        np.put_along_axis(want, chosen, share * (_np(g) - (share * _np(g)).sum(1, keepdims=True)), 1)
+        # rounded once, of terms of 64 bits
+        step = 2.0 ** -24 + (2.0 ** -8 if dtype == torch.bfloat16 else 0)
+        assert np.all(np.abs(got - want) <= step * np.abs(want) + 2.0 ** -44 * np.abs(_np(g)).sum(1, keepdims=True))
+    else:
+        assert np.all(weights[low.numpy()] == 0) and np.all(got[low.numpy()] == 0) and np.all(weights[~low.numpy()] > 0)
