@@ -1,4 +1,5 @@
 // Matrices in 8-bit floating point: layout, quantization along rows, along columns and by tiles, and back.
+#include <limits>
 #include <type_traits>
 
 #include "fp8_block.h"
@@ -189,11 +190,16 @@ __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
     }
 }
 
-// Large sources whose rows begin with a line are read past the caches, which then hold more of the codes, for the products that follow too.  us with and without, bfloat16
-// 16384 x 8192: both ways 88 and 115, by columns 70 and 93, by rows 64.5 and 69, and all of a layer of 8192 outputs 793 and 825; both ways 8192 x 8192 47.5 and 45.3, 12288 x 8192 65
-// and 82, 16384 x 16384 250 and 234; fp32 in tiles of 128 no difference.  Where lines are shared between pieces they would be read twice (30000 x 5000: 136 and 122).
-bool past_caches(const void* src, int64_t rows, int64_t cols, int64_t ld, int64_t size) {
-    return rows * cols >= (int64_t)96 << 20 && (uintptr_t)src % 128 == 0 && ld * size % 128 == 0;
+// Large sources whose rows begin with a line are read past the caches, which then hold more of the codes, for the products that follow too (all of a layer of 8192 outputs at
+// 16384 x 8192 793 us instead of 825), until the codes themselves are more than the caches hold.  us without and with it, bfloat16:
+//   both ways   8192 x 8192 44 and 46, 12288 x 8192 80 and 65, 16384 x 8192 115 and 88, 18432 x 8192 119 and 109, 20480 x 8192 134 and 132, 22528 x 8192 146 and 146, 24576 x 8192 158
+//               and 158, 16384 x 16384 233 and 254, 65536 x 8192 428 and 445; in the order of 32 experts 65536 x 2048 114 and 86, 40960 x 4096 134 and 135, 65536 x 4096 214 and 218
+//   by columns  8192 x 8192 31 and 36, 16384 x 8192 96 and 69, 16384 x 16384 196 and 145, 24576 x 16384 244 and 241, 57344 x 8192 274 and 275, 65536 x 8192 326 and 353
+//   by rows     8192 x 8192 32 and 34, 16384 x 8192 69 and 64, 16384 x 16384 134 and 118, 65536 x 8192 263 and 257
+// fp32 in tiles no difference, by rows 12288 x 8192 91 and 88, 65536 x 8192 493 and 490.  Where lines are shared between pieces they would be read twice (30000 x 5000: 136 and 122).
+constexpr int64_t kMi = (int64_t)1 << 20, kPastFrom = 96 * kMi, kPastBoth = 160 * kMi, kPastColumns = 384 * kMi;
+bool past_caches(const void* src, int64_t rows, int64_t cols, int64_t ld, int64_t size, int64_t end) {
+    return rows * cols >= kPastFrom && rows * cols < end && (uintptr_t)src % 128 == 0 && ld * size % 128 == 0;
 }
 
 template <typename T, Tiles KIND, bool PAST>
@@ -209,7 +215,7 @@ template <Tiles KIND>
 daq_status launch_tiles(const void* src, int dtype, const TileArgs& p, int64_t tiles, hipStream_t st) {
     if (dtype == DAQ_FP32) return launch_tiles<float, KIND, false>(static_cast<const float*>(src), p, tiles, st);
     if constexpr (KIND != Tiles::kWeights)      // (rows that several experts take are read again)
-        if (p.picks == 0 && past_caches(src, p.rows, p.cols, p.ld, 2)) return launch_tiles<uint16_t, KIND, true>(static_cast<const uint16_t*>(src), p, tiles, st);
+        if (p.picks == 0 && past_caches(src, p.rows, p.cols, p.ld, 2, p.r.codes ? kPastBoth : kPastColumns)) return launch_tiles<uint16_t, KIND, true>(static_cast<const uint16_t*>(src), p, tiles, st);
     return launch_tiles<uint16_t, KIND, false>(static_cast<const uint16_t*>(src), p, tiles, st);
 }
 
@@ -247,7 +253,7 @@ static daq_status launch_rows(const void* src, int64_t rows, int64_t cols, int64
 }
 daq_status fp8_quantize_rows(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint8_t* dst, hipStream_t st) {
     const Packed to = packed(dst, rows, cols);
-    const bool past = past_caches(src, rows, cols, ld, dtype == DAQ_BF16 ? 2 : 4);
+    const bool past = past_caches(src, rows, cols, ld, dtype == DAQ_BF16 ? 2 : 4, std::numeric_limits<int64_t>::max());
     if (dtype == DAQ_BF16) return past ? launch_rows<uint16_t, true>(src, rows, cols, ld, to, st) : launch_rows<uint16_t, false>(src, rows, cols, ld, to, st);
     return past ? launch_rows<float, true>(src, rows, cols, ld, to, st) : launch_rows<float, false>(src, rows, cols, ld, to, st);
 }
