@@ -28,17 +28,6 @@ inline int64_t most_tiles(const daq_experts& p, int64_t n) {
 daq_status fp8_quantize_rows(const void* src, int dtype, int64_t rows, int64_t cols, int64_t ld, uint8_t* dst, hipStream_t st);
 inline bool fp8_rows_grid_ok(int64_t rows, int64_t cols) { return grid_ok(ceil_div(rows, 16) * ceil_div(cols, kFp8Group), 256); }
 
-// fp8_matmul.hip: form of a product: edge of a workgroup's tile, and parts of the summed axis
-enum class Fp8Form { kFew, k64, k128, k256 };
-struct Fp8Plan {
-    Fp8Form form;
-    int splits, per_split;   // stages of 128 of a part
-};
-// exact: products in bfloat16 (see fp8_matmul.hip)
-Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact);
-bool fp8_raw_rows(int64_t rows, int64_t K);
-Fp8Form experts_form(const daq_experts& plan, int64_t N, int64_t K, bool exact);
-
 #if defined(__HIPCC__)
 // The scale byte of a block from the bits of its largest magnitude: the smallest power of two of which that is at most 448 = 1.75 * 2^8.
 __device__ __forceinline__ uint32_t fp8_scale_byte(uint32_t top) {

@@ -205,9 +205,9 @@ bool past_caches(const void* src, int64_t rows, int64_t cols, int64_t ld, int64_
 template <typename T, Tiles KIND, bool PAST>
 daq_status launch_tiles(const T* src, const TileArgs& p, int64_t tiles, hipStream_t st) {
     const dim3 grid((unsigned)(tiles * p.col_tiles));
-    const bool r = p.r.codes != nullptr, c = p.c.codes != nullptr;
-    const auto kernel = !r ? k_fp8_tiles<T, KIND, false, true, PAST>
-                           : c || KIND == Tiles::kExperts ? k_fp8_tiles<T, KIND, true, true, PAST> : k_fp8_tiles<T, KIND == Tiles::kExperts ? Tiles::kBlocks : KIND, true, false, PAST>;
+    auto kernel = p.r.codes ? k_fp8_tiles<T, KIND, true, true, PAST> : k_fp8_tiles<T, KIND, false, true, PAST>;
+    if constexpr (KIND == Tiles::kWeights)      // (the others by rows alone: k_fp8_rows)
+        if (!p.c.codes) kernel = k_fp8_tiles<T, KIND, true, false, PAST>;
     DAQ_LAUNCH("fp8_tiles", st, hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, src, p));
     return DAQ_OK;
 }

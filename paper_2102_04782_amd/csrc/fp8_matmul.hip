@@ -17,6 +17,13 @@ namespace daq {
 
 namespace {
 
+// Form of a product: edge of a workgroup's tile, and parts of the summed axis.
+enum class Fp8Form { kFew, k64, k128, k256 };
+struct Fp8Plan {
+    Fp8Form form;
+    int splits, per_split;   // stages of 128 of a part
+};
+
 Fp8Operand operand(const uint8_t* buf, int64_t rows, int64_t cols) {
     daq_fp8_layout L;
     daq_layout_fp8(rows, cols, &L);
@@ -292,7 +299,7 @@ daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) 
 static bool few_fits(int64_t tiles, int64_t N) { return tiles <= 65535 && grid_ok(ceil_div(N, 16), 512); }
 // Whether the workgroups of a product of few rows quantize these themselves: 16384 elements are 4 a thread.  us with it and in two launches: 1 x 8192 x 4096
 // 7.7 and 10.7, 4 x 8192 x 8192 18.3 and 18.5, 8 x 8192 x 8192 24 and 19.3.
-bool fp8_raw_rows(int64_t rows, int64_t K) { return rows <= 64 && rows * round_up(K, kFp8Block) <= 16384; }
+static bool fp8_raw_rows(int64_t rows, int64_t K) { return rows <= 64 && rows * round_up(K, kFp8Block) <= 16384; }
 
 // us that a product of so many tiles of a form takes, by what was measured of each: a fixed time, and one for a stage, longer where more workgroups than one are
 // on a CU.  E.g., bfloat16, 64, 128 and 256: 1111 x 1500 x 2030 9.7, 12.7, -; 1777 x 2080 x 4096 28.5, 21.1, 36.5; 2048 x 4096 x 4096 -, 32.8, 38.7;
@@ -310,7 +317,7 @@ static Fp8Form least_cost(double t64, double t128, double t256, double stages, b
 }
 
 // Few rows: up to 32, while their tiles of 64 would not fill the CUs.  8192 columns of K = 8192, 1 to 16 rows 16.6 us, 32 rows 26.8, 64 rows 42.5; tiles 18.
-Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
+static Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
     Fp8Plan pl{};
     const int64_t stages = ceil_div(K, kFp8Block);
     auto tiles = [&](int64_t n) { return (double)ceil_div(M, n) * (double)ceil_div(N, n); };
@@ -448,7 +455,7 @@ extern "C" daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void
 // An expert has at most so many rows: a token may name one several times.
 static int64_t most_rows(const daq_experts& plan) { return plan_slots(plan); }
 
-Fp8Form daq::experts_form(const daq_experts& plan, int64_t N, int64_t K, bool exact) {
+static Fp8Form experts_form(const daq_experts& plan, int64_t N, int64_t K, bool exact) {
     const int64_t slots = plan_slots(plan), each = slots / std::min<int64_t>(slots, plan.experts);
     if (each <= 32 && ceil_div(N, 64) * std::min<int64_t>(slots, plan.experts) < 256 && most_tiles(plan, 64) <= 65535) return Fp8Form::kFew;
     const double active = (double)std::min<int64_t>(slots, plan.experts);
