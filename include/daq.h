@@ -652,8 +652,8 @@ daq_status daq_ckpt8_weight_grad(int64_t M, int64_t N, int64_t K, const void* dY
  * eight neighbouring products (of a block: 8 i .. 8 i + 7) with 2^-13 of the largest of them cut off of each other one, these sums in fp32;
  * on bell-shaped values 2^-16 of the result, against the 2^-9 of its rounding.  A result in fp32 comes from their bfloat16, in which
  * the values are exact (those within its range: scales of 2^-117 .. 2^119 at least), with fp32 sums of exact products, at half the rate.
- * Conventions as of the layers above.  Sizes: as above, and fewer than 2^23
- * columns K of a product; launches of 2^32 threads or more are DAQ_ERR_UNSUPPORTED.
+ * Conventions as of the layers above.  Sizes: as above, and K of a product up to 2^23 - 128; launches of 2^32 threads or more, and products of more tiles than
+ * 31 bits count, are DAQ_ERR_UNSUPPORTED.  Calls that are refused have launched nothing.
  *
  * Matrix: codes of element (r, c) at byte r * pitch + c, pitch = columns rounded up to 128; the scale byte of block (r, c / 128) at
  * off_scales + ((c/512) * rows + r) * 4 + (c/128) % 4.  Padding is quantized as zeros: codes of zero (in a block of byte 255 of NaN, as all
@@ -762,6 +762,8 @@ daq_status daq_experts_plan(int64_t tokens, int32_t picks, int32_t experts, cons
  * daq_experts_weight_grad -- dW[e][n][k] = sum over the rows p of e of dY[p][n] * X[a(p)][k], both by_columns of the same plan;
  *   [experts][N][K], row stride ldw, experts `stride` elements apart; accumulate != 0 (fp32 only) adds.  An expert without rows has
  *   the gradient zero.
+ * Sizes: K up to 2^23 - 128, and daq_experts_columns(...) of a weight gradient the same.  Rows that a product takes by their tokens (sorted == 0) are reached
+ * through one descriptor: tokens * (K rounded up to 128) up to 2^32 - 256; sorted ones are not bounded by it.  Others are DAQ_ERR_UNSUPPORTED.
  * ------------------------------------------------------------------------------------------- */
 daq_status daq_experts_columns(int64_t tokens, int32_t picks, int32_t experts, int64_t* columns);
 daq_status daq_experts_quantize(const daq_experts* plan, const void* src, daq_dtype dtype, int64_t cols, int64_t ld, int32_t sorted,
