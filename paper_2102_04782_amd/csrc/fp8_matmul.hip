@@ -316,12 +316,21 @@ static Fp8Form least_cost(double t64, double t128, double t256, double stages, b
     return a <= b && a <= c ? Fp8Form::k64 : b <= c ? Fp8Form::k128 : Fp8Form::k256;
 }
 
-// Few rows: up to 32, while their tiles of 64 would not fill the CUs.  8192 columns of K = 8192, 1 to 16 rows 16.6 us, 32 rows 26.8, 64 rows 42.5; tiles 18.
+// Up to 32 rows, while their tiles of 64 would not fill the CUs, the few-rows form, as long as the weights are no more elements than this: it takes longer with every row, tiles (parts of the
+// summed axis among them) do not.  us of both, weights from memory:
+//   bfloat16   8 rows 8192 x 8192 19.1 and 18.5, 12288 x 4096 15.5 and 13.9, 4096 x 14336 17.7 and 18.2;   16 rows 8192 x 4096 12.6 and 12.8, 4096 x 8192 12.8 and 12.6, 8192 x 8192 21.7
+//              and 18.7, 12288 x 4096 17.3 and 14.1;   24 rows 4096 x 4096 9.6 and 10.7, 3000 x 5000 10.6 and 10.9, 5120 x 4096 14.9 and 12.5, 8192 x 8192 26.0 and 19.2
+//   fp32       16 rows 8192 x 8192 22.0 and 22.9, 16000 x 4096 21.7 and 21.1;   24 rows 4096 x 4096 9.8 and 12.5, 8192 x 4096 15.9 and 16.7, 12288 x 4096 21.7 and 20.4, 8192 x 8192
+//              26.7 and 23.3
+static int64_t few_weights(int64_t M, bool exact) {
+    constexpr int64_t mi = (int64_t)1 << 20;
+    return M <= 8 ? kMaxElems : M <= 16 ? (exact ? kMaxElems : 32 * mi) : M <= 32 ? (exact ? 32 : 16) * mi : 0;
+}
 static Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
     Fp8Plan pl{};
     const int64_t stages = ceil_div(K, kFp8Block);
     auto tiles = [&](int64_t n) { return (double)ceil_div(M, n) * (double)ceil_div(N, n); };
-    pl.form = M <= 32 && few_fits(1, N) && ceil_div(N, 64) < 256 ? Fp8Form::kFew : least_cost(tiles(64), tiles(128), tiles(256), (double)stages, exact);
+    pl.form = N * K <= few_weights(M, exact) && few_fits(1, N) && ceil_div(N, 64) < 256 ? Fp8Form::kFew : least_cost(tiles(64), tiles(128), tiles(256), (double)stages, exact);
     pl.splits = 1;
     pl.per_split = (int)stages;
     if (pl.form == Fp8Form::kFew) return pl;
