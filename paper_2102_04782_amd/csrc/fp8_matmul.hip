@@ -464,10 +464,18 @@ extern "C" daq_status daq_fp8_linear(int64_t M, int64_t N, int64_t K, const void
 // An expert has at most so many rows: a token may name one several times.
 static int64_t most_rows(const daq_experts& plan) { return plan_slots(plan); }
 
+// Experts of up to 32 rows take the few-rows form, by the tiles of 64 that they would be.  us of both, weights from memory, `each` rows of every expert:
+//   64 tiles    4 of 1024 x 4096, bfloat16 each 1, 16, 32: 8.3 and 13.4, 9.8 and 13.7, 12.2 and 14.2
+//   128 tiles   4 of 2048 x 4096, bfloat16 each 8, 16, 32: 13.0 and 14.4, 14.9 and 14.6, 19.2 and 15.2;  fp32 14.4 and 20.8, 15.5 and 21.0, 19.5 and 21.4
+//   192 tiles   6 of 2048 x 2048, bfloat16 each 1, 4, 16: 10.7 and 10.1, 11.4 and 10.2, 13.4 and 10.5;  fp32 12.7 and 13.7, 13.2 and 13.9, 14.8 and 14.1
+//   228 tiles   4 of 3600 x 4096, bfloat16 each 1, 4, 16: 20.5 and 17.4, 21.5 and 17.4, 25.1 and 17.7;  fp32 21.7 and 21.6, 22.5 and 21.7, 25.9 and 22.1
+// Rows that its workgroups quantize themselves save a launch, which makes up for more than 128 tiles: 6 of 2048 x 2048, each 1, bfloat16 10.1 and 12.9, fp32 10.9 and 16.4, 4 of 4000 x 4096
+// 19.3 and 20.9, 21.0 and 25.0.
 static Fp8Form experts_form(const daq_experts& plan, int64_t N, int64_t K, bool exact) {
-    const int64_t slots = plan_slots(plan), each = slots / std::min<int64_t>(slots, plan.experts);
-    if (each <= 32 && ceil_div(N, 64) * std::min<int64_t>(slots, plan.experts) < 256 && most_tiles(plan, 64) <= 65535) return Fp8Form::kFew;
-    const double active = (double)std::min<int64_t>(slots, plan.experts);
+    const int64_t slots = plan_slots(plan), experts = std::min<int64_t>(slots, plan.experts), each = slots / experts, few_tiles = ceil_div(N, 64) * experts;
+    const int64_t most = fp8_raw_rows(most_rows(plan), K) || (exact && each <= 4) ? 255 : exact || each <= 16 ? 128 : 64;
+    if (each <= 32 && few_tiles <= most && most_tiles(plan, 64) <= 65535) return Fp8Form::kFew;
+    const double active = (double)experts;
     auto tiles = [&](int64_t n) { return active * (double)ceil_div(each, n) * (double)ceil_div(N, n); };
     return least_cost(tiles(64), tiles(128), tiles(256), (double)ceil_div(K, kFp8Block), exact);
 }

@@ -22,3 +22,22 @@ def test_few_rows_of_wide_layers(N, K):
             first = daq.fp8_matmul(q, w, dtype=to)
             assert np.all(np.abs(_np(first) - exact) <= _bound(K, absolute, exact, to)), (M, to)
             assert torch.equal(first, daq.fp8_linear(x, w, dtype=to))
+
+
+@pytest.mark.parametrize("E,N,K", [(4, 1024, 700), (4, 2048, 700), (6, 2048, 520), (4, 3600, 300), (4, 4200, 300)])
+def test_few_rows_of_experts(E, N, K):
+    """64 to 264 tiles of 64 x 64, one row of every expert to 33."""
+    w = daq.fp8_quantize_weights(_x(E * N, K, torch.bfloat16, N).view(E, N, K).cuda(), transposed=False)[0]
+    vw = daq.fp8_dequantize(w).double().view(E, N, K)
+    for each in (1, 4, 5, 16, 17, 32, 33):
+        chosen = (torch.arange(E * each) * 5 % E).int().view(-1, 1).cuda()
+        plan = daq.experts_plan(chosen, E)
+        x = _x(E * each, K, torch.bfloat16, each + K).cuda()
+        q = daq.fp8_quantize(x)
+        v = daq.fp8_dequantize(q).double()[plan.rows.long()]
+        e = chosen.view(-1).long()[plan.rows.long()].tolist()
+        exact, absolute = (np.stack([_np(f(vw[i]) @ f(v[p])) for p, i in enumerate(e)]) for f in (lambda t: t, torch.abs))
+        for to in DT:
+            first = daq.experts_matmul(q, w, plan, dtype=to)
+            assert np.all(np.abs(_np(first) - exact) <= _bound(K, absolute, exact, to)), (each, to)
+            assert torch.equal(first, daq.experts_linear(x, w, plan, dtype=to))
