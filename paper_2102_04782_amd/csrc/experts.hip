@@ -22,7 +22,8 @@ __device__ __forceinline__ void load_some(const T* p, int64_t left, Eight<T>& v)
 }
 
 // Eight columns of a token a lane; the rows of four places are asked for before the first is added.  Bound: memory; 16384 x 4096 bfloat16, 4 places,
-// 671 MB in 108 to 114 us, 6 TB/s.
+// 671 MB in 108 us, 6.2 TB/s; rows of 1024 26 us, 6.5, of 512 14, 5.9, of 128 10.2, 2.1 (16 of a
+// workgroup's 256 threads have columns then).
 template <typename T, bool PAST>
 __global__ __launch_bounds__(256) void k_combine(const T* y, T* out, CombineArgs p) {
     const int64_t t = blockIdx.x / p.chunks, c = (int64_t)(blockIdx.x - t * p.chunks) * 2048 + threadIdx.x * 8, left = p.cols - c;
@@ -47,8 +48,8 @@ __global__ __launch_bounds__(256) void k_combine(const T* y, T* out, CombineArgs
     store8(out + t * p.ldo + c, (int)min(left, (int64_t)8), sum);
 }
 
-// A wave a place of a token: the row's gradient, and the dot product that is its weight's.  Bound: memory; 16384 x 4096 bfloat16, 4 places, 1.21 GB in 202 to 237 us,
-// 5.1 to 6 TB/s (a token's gradient is read once from memory, its other places find it in L2).
+// A wave a place of a token: the row's gradient, and the dot product that is its weight's.  Bound: memory; 16384 x 4096 bfloat16, 4 places, 1.21 GB in 202 us,
+// 6 TB/s; rows of 512 26 us, 5.9, of 128 19, 2.0 (a token's gradient is read once from memory, its other places find it in L2).
 // PAST: bfloat16 (past_caches).
 template <typename T, bool DW, bool PAST>
 __global__ __launch_bounds__(256) void k_combine_back(const T* dout, const T* y, T* dy, CombineArgs p) {

@@ -63,7 +63,8 @@ enum class Tiles { kBlocks, kWeights, kExperts };
 // Tiles of 128 x 128 of src, which is read once: blocks along the rows and / or along the columns, or (weights) the tile as one block,
 // written both ways.  A lane has eight columns of four rows, a wave 128 columns of 16 rows; codes that leave by columns are words
 // of four rows each and turn in LDS, where word q of a column lies at q ^ (4 * (column / 8 % 8)), off its neighbours' banks.  Bound: memory, written in
-// pieces of 128 bytes; 8192 x 8192 both ways, bfloat16 45 us, 5.9 TB/s, fp32 76, 5.3; 65536 x 2048 bfloat16 in the order of 32 experts 87, 6.2.  Neighbours in bands
+// pieces of 128 bytes; 8192 x 8192 both ways, bfloat16 45 us, 6.0 TB/s (62 between the products of a training step), fp32 78, 5.2; as weights 44 and 82; 32 weights of 2048 x 2048
+// 103, 5.2 TB/s, and 151, 5.3; 65536 x 2048 bfloat16 in the order of 32 experts 87, 6.2, taken by their tokens 65.  Neighbours in bands
 // of row tiles, so that these pieces lie together by columns too, gained 7 % at 16384 x 8192 and lost 4 % at 8192 x 8192.
 template <typename T, Tiles KIND, bool BYROWS, bool BYCOLS, bool PAST>
 __global__ __launch_bounds__(512) void k_fp8_tiles(const T* src, TileArgs p) {
@@ -219,7 +220,7 @@ daq_status launch_tiles(const void* src, int dtype, const TileArgs& p, int64_t t
     return launch_tiles<uint16_t, KIND, false>(static_cast<const uint16_t*>(src), p, tiles, st);
 }
 
-// Eight columns of a row a lane.
+// Eight columns of a row a lane.  Bound: memory; 8192 x 8192 to bfloat16 38 us, 5.3 TB/s, to fp32 63, 5.4.
 template <typename T>
 __global__ __launch_bounds__(256) void k_fp8_values(const uint8_t* codes, const uint8_t* scales, int64_t pitch, int64_t rows, int64_t cols, T* dst, int64_t ld) {
     const int64_t strips = (cols + 2047) / 2048, r = blockIdx.x / strips, c = (blockIdx.x - r * strips) * 2048 + threadIdx.x * 8;

@@ -5,8 +5,8 @@
 // The matrix instruction is that of 16 x 16 x 128 (a block), in bfloat16 four of 16 x 16 x 32: lane l has row l % 16 and the 16-byte pieces l / 16 and
 // l / 16 + 4 of a block, so that a load takes 64 bytes in a row of every row.  Where the rows are few they are quantized by every workgroup itself, into
 // LDS, while its first weights are on their way: a launch less.
-// Bound: memory, and at this size the wait for the first of it.  1 x 8192 x 4096 (33.8 MB) 8.4 us, 4.0 TB/s, quantized on the way (10.7 in two launches);
-// 21 x 2300 x 5130, fp32, 10.4 us behind 3.9 for the rows.
+// Bound: memory, and at this size the wait for the first of it.  1 x 8192 x 4096 (33.8 MB) 8.4 us, 4.0 TB/s, quantized on the way, 10.1 with the weights from memory
+// (in two launches 10.9 and 13.0); 21 x 2300 x 5130, fp32, 10.2 us behind 3.5 for the rows.
 #include "fp8_product.h"
 
 namespace daq {

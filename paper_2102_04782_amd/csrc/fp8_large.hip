@@ -17,9 +17,9 @@ constexpr int kPlaces = kB * kB;                            // products of a ste
 // every place between two products is given what it can take: two reads, or a request, as the way into LDS takes 16 cycles of each of the four waves' and
 // a product 64.  A stage is read out in the first half of its first step, then the stage after the next is asked for in its place, while
 // the next one has until the second step to land.  Behind a tile's last stage the first two of the next tile are asked for before its results leave.
-// Bound: the matrix cores at the card's power limit.  16384 x 8192 x 8192 700 to 780 us (2.8 to 3.1 PFLOP/s; a loop of these instructions on registers
-// reaches 4.5), 8192 x 8192 x 4096 190 to 200 when others run before it; busy 78 to 85 % of the cycles, at 1.75 to 2.2 GHz.  Where sums are short a tile's start and results count:
-// 65536 x 2048 x 2048 215 us, and 285 as the rows of 32 experts (2176 tiles instead of 2048; the cores are busy 45 %).  Four waves of 128 x 128 read a third less from LDS than
+// Bound: the matrix cores at the card's power limit.  16384 x 8192 x 8192 741 us (3.0 PFLOP/s; a loop of these instructions on registers
+// reaches 4.5), 8192 x 8192 x 4096 204 in a training step, 187 alone; busy 78 to 85 % of the cycles, at 1.75 to 2.2 GHz.  Where sums are short a tile's start and results count:
+// 65536 x 2048 x 2048 221 us alone, and 264 as the rows of 32 experts, 256 where they lie in order (2176 tiles instead of 2048; the cores are busy 45 %), 297 in a training step.  Four waves of 128 x 128 read a third less from LDS than
 // eight of 128 x 64, which reached 2.7 PFLOP/s.
 
 // The lane, as a value that the compiler works on where it stands: places of lanes that it kept from tile to tile would cost the registers that
@@ -249,7 +249,7 @@ daq_status launch(const ProductArgs& p, hipStream_t st) {
 
 }  // namespace
 
-// Results of more than the caches behind L2 keep (256 MiB) pass them by: 65536 x 2048 x 2048 (256 MiB of results) 215 us instead of 251, 16384 x 8192 x 8192 721
+// Results of more than the caches behind L2 keep (256 MiB) pass them by: 65536 x 2048 x 2048 (256 MiB of results) 215 us instead of 251 (both of one run), 16384 x 8192 x 8192 721
 // instead of 737; of half as much they stay, 8192 x 8192 x 4096 193 instead of 196.
 constexpr int64_t kStreamProduct = (int64_t)192 << 20;
 

@@ -208,7 +208,7 @@ struct Fp8Product {
 };
 
 // Tiles of kRows x kCols results, a workgroup each.  Workgroup b runs on XCD b % 8; an XCD takes an eighth of the tiles, in bands of four row
-// tiles, whose panels its L2 holds.  Bound: too few tiles for the CUs (1111 x 1500 x 2030, fp32: 432 of 64 x 64, 19.7 us, where the bytes take 2 and the
+// tiles, whose panels its L2 holds.  Bound: too few tiles for the CUs (1111 x 1500 x 2030, fp32: 432 of 64 x 64, 19.1 us, where the bytes take 2 and the
 // matrix cores 4), and LDS reads: a wave of a tile of 128 makes 32 products of a byte, of 64 21, of 256 64 (2048 x 4096 x 4096, bfloat16, 32.8 us, 2.1 PFLOP/s).
 template <int WR, int WC, int RB, int CB, int SLOTS, bool EXACT, Of OF>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_fp8_product(ProductArgs p) {
@@ -298,7 +298,7 @@ daq_status launch_form(Fp8Form form, bool exact, ProductArgs p, hipStream_t st) 
 
 static bool few_fits(int64_t tiles, int64_t N) { return tiles <= 65535 && grid_ok(ceil_div(N, 16), 512); }
 // Whether the workgroups of a product of few rows quantize these themselves: 16384 elements are 4 a thread.  us with it and in two launches: 1 x 8192 x 4096
-// 7.7 and 10.7, 4 x 8192 x 8192 18.3 and 18.5, 8 x 8192 x 8192 24 and 19.3.
+// 10.1 and 13.0 with the weights from memory, 8.5 and 10.9 from the caches; 4 x 8192 x 8192 18.3 and 18.5, 8 x 8192 x 8192 24 and 19.3.
 static bool fp8_raw_rows(int64_t rows, int64_t K) { return rows <= 64 && rows * round_up(K, kFp8Block) <= 16384; }
 
 // us that a product of so many tiles of a form takes, by what was measured of each: a fixed time, and one for a stage, longer where more workgroups than one are

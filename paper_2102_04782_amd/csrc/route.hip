@@ -182,8 +182,9 @@ __device__ __forceinline__ int choose_exactly(const RouteArgs& p, const float (&
 
 // A wave a token; lane l has the experts l * PER .. of it.  The choice is made in 32 bits, by the logits themselves where no bias counts (the scores rise with
 // them), otherwise by scores that are off by less than 2^-19 (of 1, or of the largest c).  Wherever two c that decide are nearer to one another than that, or logits
-// than 64 bits keep their scores apart, the wave chooses again in 64 bits.  What bounds it are vector instructions, some 730 a token, 25 of them for a place:
-// 16384 x 256 fp32, sigmoid, bias, 4 of 8 groups, 8 places 35 us, where its bytes take 4.  Four tokens a wave took 40 (registers).
+// than 64 bits keep their scores apart, the wave chooses again in 64 bits.  16384 x 256 fp32, sigmoid, bias, 4 of 8 groups, 8 places 34.5 us, where its bytes take 4.  Bound: some 730 vector
+// instructions a token, 25 of them for a place: 20 us at one every four cycles of a SIMD, and those in 64 bits take longer; its waves wait a third of their cycles, one
+// exchange behind the other.  Four tokens a wave took 40 us (registers).
 template <typename T, int PER>
 __global__ __launch_bounds__(256) void k_route(const T* logits, RouteArgs p) {
     constexpr float kNone = -__builtin_inff();
@@ -410,8 +411,8 @@ __device__ __forceinline__ void lds_in_order() {
 }
 
 // Lane n << slot + j has place j of the wave's token n.  The chosen ones' part goes to its place of the row by way of LDS; the others' is zero or, where the softmax is not
-// renormalised, needs the row.  Bound: memory and the 64-bit exponentials; 16384 x 256 fp32, 8 places, 6.6 us (17 MB written, 2.5 TB/s; the
-// logits' lines of the chosen ones are most of them read).
+// renormalised, needs the row.  Bound: memory and the 64-bit exponentials; 16384 x 256 fp32, 8 places, 7.6 us (17 MB written; the
+// logits' lines of the chosen ones are most of them read), softmax without renormalisation 11.7, bfloat16 10.8 (rows read and written, 34 and 17 MB; exponentials in 32 bits).
 template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits, RouteBackArgs p) {
     __shared__ __attribute__((aligned(16))) float rows[4][PARTS * 256];
@@ -514,7 +515,7 @@ __global__ __launch_bounds__(256) void k_route_back(const T* logits, T* dlogits,
 // ---- the order of the rows --------------------------------------------------------------------
 // A workgroup takes a run of slots, 1024 at a time.  counts[block][expert] by a first launch; the second adds up what stands before its own
 // run and places it.  Within a wave a slot's rank among those of its expert comes from ten votes, one a bit of the expert's number; no atomics decide an order.
-// Bound: launches and the waits of a dozen steps one behind the other; 131072 slots, 256 experts 4.9 + 12 us, up to 4096 slots one launch of 5.
+// Bound: launches and the waits of a dozen steps one behind the other; 131072 slots, 256 experts 4.2 + 12 us, up to 4096 slots one launch of 5.
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;
 
 struct PlanArgs {
@@ -727,7 +728,7 @@ extern "C" daq_status daq_route_backward(int64_t tokens, int32_t experts, const 
     if (rc != DAQ_OK || tokens == 0) return rc;
     if (!dweights || !a4(dweights) || !chosen || !a4(chosen) || !dlogits || !elem_aligned(dlogits, dtype) || ldd < experts) return DAQ_ERR_INVALID_ARG;
     // what is computed in 64 bits takes a wave as long for one token's places as for several's: four tokens a wave, once there are enough of them (16384 x 256,
-    // 8 places, 7.5 us instead of 12)
+    // 8 places, 7.6 us instead of 12)
     const int slot = opts->picks <= 8 ? 3 : opts->picks <= 16 ? 4 : 5, each = tokens >= 8192 ? std::min(4, kWave >> slot) : 1;
     if (!grid_ok(ceil_div(tokens, 4 * each), 256)) return DAQ_ERR_UNSUPPORTED;
     const RouteBackArgs p{tokens, ld, ldd, experts, opts->picks, opts->scores == DAQ_SCORES_SIGMOID, opts->renormalize != 0, each, slot, opts->scale, dweights, chosen};
