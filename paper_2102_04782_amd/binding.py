@@ -1106,8 +1106,13 @@ def fp8_linear(x: torch.Tensor, w: Fp8, dtype=None, out: Optional[torch.Tensor] 
 
 
 @functools.lru_cache(maxsize=256)
-def _route_opts(*fields):      # (read only)
+def _kept_opts(*fields):      # (read only)
     return RouteOpts(*fields)
+
+
+def _route_opts(scores, picks, groups, top_groups, renormalize, scale) -> RouteOpts:
+    """Kept by value: a scale that is held in a tensor may be another one at the next call."""
+    return _kept_opts(scores, picks, groups, top_groups, bool(renormalize), float(scale))
 
 
 def route(logits: torch.Tensor, picks: int, scores=SCORES_SOFTMAX, bias: Optional[torch.Tensor] = None, groups: int = 1, top_groups: int = 1,
@@ -1118,7 +1123,7 @@ def route(logits: torch.Tensor, picks: int, scores=SCORES_SOFTMAX, bias: Optiona
     if out is None:
         out = _new(stream, (tokens, picks), torch.float32, logits), _new(stream, (tokens, picks), torch.int32, logits)
     weights, chosen = out
-    opts = _route_opts(scores, picks, groups, top_groups, bool(renormalize), scale)
+    opts = _route_opts(scores, picks, groups, top_groups, renormalize, scale)
     _check(lib().daq_route(tokens, experts, logits.data_ptr(), code, ld, pb, C.byref(opts), _dense(weights, torch.float32, tokens, picks),
                            _dense(chosen, torch.int32, tokens, picks), _stream(stream)), "daq_route")
     return out
@@ -1132,7 +1137,7 @@ def route_backward(dweights: torch.Tensor, logits: torch.Tensor, chosen: torch.T
     picks = chosen.shape[1]
     out, ldd, _ = _result(out, tokens, experts, logits.dtype, logits, stream)
     _here(out)
-    opts = _route_opts(scores, picks, 1, 1, bool(renormalize), scale)
+    opts = _route_opts(scores, picks, 1, 1, renormalize, scale)
     _check(lib().daq_route_backward(tokens, experts, _dense(dweights, torch.float32, tokens, picks), logits.data_ptr(), code, ld,
                                     _dense(chosen, torch.int32, tokens, picks), C.byref(opts), out.data_ptr(), ldd, _stream(stream)),
            "daq_route_backward")
